@@ -273,6 +273,94 @@ stepq_status stepq_intb_decode_step(const stepq_config *cfg, int bits, int layer
                                     const float *k, const float *v, const float *beta,
                                     const float *gate, float *y, stepq_stream_t stream);
 
+/* --------------------------------------------------- decayed linear attention
+ * The layers of hybrid models whose state is written without the Delta rule's
+ * correction: with S as above (one 128 x 128 fp32 state per slot, layer and value
+ * head) and a decay g_t in [0, 1] per token and value head,
+ *   S_t = g_t S_{t-1} + k_t v_t^T,   y_t = S_t^T q_t.
+ * The state pool is the one of stepq_fp32_decode_step: device fp32
+ * [pool_slots][L][Hv][128][128]. A decay of exactly 0 forgets everything before its
+ * token (the first token of another document in the same sequence). Only dk, dv,
+ * n_layers, heads and gate_kind (STEPQ_GATE_SCALAR, else STEPQ_ERR_UNSUPPORTED) of
+ * cfg are read. The paper has no counterpart of these calls. */
+
+/* Element types of vectors. States, decays and norm parameters are always fp32. */
+#define STEPQ_F32 0
+#define STEPQ_BF16 1
+#define STEPQ_F16 2
+
+/* Activations of stepq_norm. */
+#define STEPQ_ACT_NONE 0
+#define STEPQ_ACT_SILU 1
+#define STEPQ_ACT_SIGMOID 2
+
+/* Normalisation of a row's channels in groups of n, then an activation:
+ *   m = mean(x) if center, else 0;   u = (x - m) / sqrt(mean((x - m)^2) + eps) * weight + bias;
+ *   out = u * act(z) if z is given, else act(u).
+ * center = 1 is group norm, center = 0 is RMS norm of each group. */
+typedef struct {
+    int act;                 /* STEPQ_ACT_* */
+    int center;              /* 0 or 1 */
+    int shared;              /* weight, bias: 0 = [channels of a row], 1 = [n], the same for every group */
+    float eps;               /* >= 0 */
+    const float *weight;     /* device fp32 or NULL (1) */
+    const float *bias;       /* device fp32 or NULL (0) */
+    const void *z;           /* device, rows of all channels in the rows' own type, or NULL */
+    int64_t z_stride;        /* elements from one row of z to the next */
+} stepq_norm;
+
+/* The vectors of a call: one row per token, a head's 128 channels contiguous and the heads
+ * of a row next to each other; strides in elements from one token's row to the next, so
+ * that q, k, v (and z) may be columns of one projection's rows. q, k, v, y and z: 16-byte
+ * aligned, strides a multiple of 16 bytes and >= 0 (y_stride >= 128 Hv); y overlaps no input. */
+typedef struct {
+    int dtype;               /* STEPQ_F32, STEPQ_BF16 or STEPQ_F16: q, k, v, y and norm z */
+    const void *q, *k;       /* device [tokens][Hk][128] */
+    const void *v;           /* device [tokens][Hv][128] */
+    const float *gate;       /* device fp32 [tokens][Hv], each in [0, 1] */
+    void *y;                 /* device [tokens][Hv][128] out */
+    int64_t q_stride, k_stride, v_stride;
+    int64_t gate_stride;     /* 0: one decay per head for every token */
+    int64_t y_stride;
+} stepq_linattn_io;
+
+/* One token of one layer for B slots (row b of io belongs to slots[b]): the states are
+ * updated in place, y is the readout after the update. norm (or NULL) normalises each
+ * head's 128 readouts (weight and bias [128 Hv], or [128] if shared) before y is rounded
+ * to its type. Slots out of range raise STEPQ_ERR_SLOT_RANGE and are skipped, repeated ones
+ * raise STEPQ_ERR_DUP_SLOT (device errors). pool: 16-byte aligned. */
+stepq_status stepq_linattn_decode_step(const stepq_config *cfg, int layer, float *pool,
+                                       int pool_slots, const int32_t *slots, int B,
+                                       const stepq_linattn_io *io, const stepq_norm *norm,
+                                       stepq_stream_t stream);
+
+/* Prompts of B sequences, packed: sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1] - 1
+ * of io's `tokens` rows (device int32 [B+1], ascending within [0, tokens]; NULL: B
+ * sequences of tokens / B each, tokens a multiple of B). Its state starts as slots[b]'s
+ * where resume[b] != 0 (device uint8 [B]; NULL: all), else as zero, whatever the slot holds;
+ * the state after its last token is written to the slot. A sequence without tokens leaves
+ * its slot as it is. y and norm as in stepq_linattn_decode_step.
+ * max_len: the longest sequence's length, which only chooses how the work is split (0: not
+ * known). workspace: device, 256-byte aligned, at least
+ * stepq_linattn_workspace_bytes(cfg, B, tokens, max_len) bytes (0: NULL is fine), clobbered.
+ * A sequence whose bounds are not ascending within [0, tokens] raises STEPQ_ERR_ARG and
+ * one whose slot is out of range STEPQ_ERR_SLOT_RANGE (device errors); either is skipped.
+ * A value that is not finite may reach any output of its own sequence from the 64 tokens
+ * it lies in (multiples of 64 from the start) on, and no other sequence. */
+size_t stepq_linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int max_len);
+stepq_status stepq_linattn_prefill(const stepq_config *cfg, int layer, float *pool, int pool_slots,
+                                   const int32_t *slots, const uint8_t *resume,
+                                   const int32_t *cu_seqlens, int B, int tokens, int max_len,
+                                   const stepq_linattn_io *io, const stepq_norm *norm,
+                                   void *workspace, size_t workspace_bytes, stepq_stream_t stream);
+
+/* The normalisation on its own: x [rows][groups * width] in dtype (rows x_stride elements
+ * apart, channels contiguous) to out (the same, out_stride apart; out may be x). Any width
+ * from 1 on and any alignment of x, out and z that their type has; statistics in fp32. */
+stepq_status stepq_group_norm(int dtype, int64_t rows, int groups, int width, const void *x,
+                              int64_t x_stride, void *out, int64_t out_stride,
+                              const stepq_norm *norm, stepq_stream_t stream);
+
 /* ------------------------------------------------------------- calibration (App. A.3)
  * Accumulate sum_t g_{t,i}^2 with g_t = A_t^T q_t (Sec. 4.1, Eq.
  * kda_sensitivity) and sum_t log r_{t,u} for n calibration tokens of one layer.

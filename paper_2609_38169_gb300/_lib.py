@@ -31,7 +31,19 @@ class StepqPlanInfo(C.Structure):
                 ("w", P), ("lifetime", P), ("head_offset", P), ("head_bytes", P)]
 
 
+class StepqNorm(C.Structure):
+    _fields_ = [("act", I), ("center", I), ("shared", I), ("eps", C.c_float), ("weight", P), ("bias", P), ("z", P),
+                ("z_stride", C.c_int64)]
+
+
+class StepqLinattnIo(C.Structure):
+    _fields_ = [("dtype", I), ("q", P), ("k", P), ("v", P), ("gate", P), ("y", P), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("gate_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
 CFG = C.POINTER(StepqConfig)
+IO = C.POINTER(StepqLinattnIo)
+NORM = C.POINTER(StepqNorm)
 
 # name -> (restype, argtypes); the exported symbol set of include/stepq.h
 SIGNATURES = {
@@ -62,6 +74,10 @@ SIGNATURES = {
     "stepq_calib_workspace_bytes": (SZ, [CFG, I]),
     "stepq_debug_stall": (I, [C.c_longlong, I]),
     "stepq_calibrate_from_trace": (I, [CFG, I, I, I, P, P, P, P, P, P, SZ, C.POINTER(StepqCalibResult), P]),
+    "stepq_linattn_decode_step": (I, [CFG, I, P, I, P, I, IO, NORM, P]),
+    "stepq_linattn_workspace_bytes": (SZ, [CFG, I, I, I]),
+    "stepq_linattn_prefill": (I, [CFG, I, P, I, P, P, P, I, I, I, IO, NORM, P, SZ, P]),
+    "stepq_group_norm": (I, [I, C.c_int64, I, I, P, C.c_int64, P, C.c_int64, NORM, P]),
     "stepq_validate_slots": (I, [P, I, I, P, P, P]),
     "stepq_validate_slots_noalloc": (I, [P, I, I, P, P]),
     "stepq_device_error": (I, [P]),

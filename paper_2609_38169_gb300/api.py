@@ -18,6 +18,7 @@ D = 128
 GATE_SCALAR = 0
 GATE_CHANNEL = 1
 PIVOT_BITS = 16
+ACT_NONE, ACT_SILU, ACT_SIGMOID = 0, 1, 2
 
 
 @dataclass
@@ -425,6 +426,142 @@ def stepq_device_error(stream=None) -> int:
 
 def stepq_stream_status(stream=None) -> int:
     return int(_lib.lib().stepq_stream_status(_stream(stream)))
+
+
+# ------------------------------------------------------------------ decayed linear attention
+@dataclass
+class Norm:
+    """stepq_norm: group norm (center) or RMS norm of groups of channels, an affine map
+    (fp32 weight and bias per channel, or per channel of a group where `shared`), and an
+    activation of the result, or of the gate z that multiplies it."""
+    weight: object = None
+    bias: object = None
+    z: object = None
+    act: int = ACT_SILU
+    center: bool = True
+    shared: bool = False
+    eps: float = 1e-5
+
+
+_DTYPES: dict = {}
+
+
+def _dtype_code(dtype) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    if dtype not in _DTYPES:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
+    return _DTYPES[dtype]
+
+
+def _rows_ptr(t, dtype, rows, channels, what):
+    """Pointer and row stride of a CUDA tensor [rows][channels] or [rows][heads][128] whose
+    rows are contiguous, `stride` elements apart."""
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"expected {dtype}, got {t.dtype}")
+    shape, st = t.shape, t.stride()
+    if len(shape) == 3:
+        ok = shape[1] * shape[2] == channels and shape[2] == D and st[2] == 1 and (shape[1] == 1 or st[1] == D)
+    else:
+        ok = len(shape) == 2 and shape[1] == channels and (channels == 1 or st[1] == 1)
+    if not ok or shape[0] != rows:
+        raise ValueError(f"{what}: expected {rows} contiguous rows of {channels} channels, got shape {tuple(shape)}, "
+                         f"strides {tuple(st)}")
+    # the stride of a single row is never used, and torch leaves it arbitrary
+    return t.data_ptr(), st[0] if rows > 1 else channels
+
+
+def _param_ptr(t, n, what):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{what}: expected {n} values, got {t.numel()}")
+    return _dev_ptr(t, _f32())
+
+
+def _c_norm(norm, dtype, rows, channels, width):
+    if norm is None:
+        return None
+    n = width if norm.shared else channels
+    z, zs = (None, 0) if norm.z is None else _rows_ptr(norm.z, dtype, rows, channels, "z")
+    return C.byref(_lib.StepqNorm(norm.act, int(norm.center), int(norm.shared), norm.eps,
+                                  _param_ptr(norm.weight, n, "weight"), _param_ptr(norm.bias, n, "bias"), z, zs))
+
+
+def _linattn_io(cfg, q, k, v, gate, y):
+    dt, n, Hv = q.dtype, q.shape[0], cfg.n_value_heads
+    qp, qs = _rows_ptr(q, dt, n, cfg.n_key_heads * D, "q")
+    kp, ks = _rows_ptr(k, dt, n, cfg.n_key_heads * D, "k")
+    vp, vs = _rows_ptr(v, dt, n, Hv * D, "v")
+    yp, ys = _rows_ptr(y, dt, n, Hv * D, "y")
+    if gate.dim() == 1:
+        gp, gs = _param_ptr(gate, Hv, "gate"), 0
+    else:
+        gp, gs = _rows_ptr(gate, _f32(), n, Hv, "gate")
+    return _lib.StepqLinattnIo(_dtype_code(dt), qp, kp, vp, gp, yp, qs, ks, vs, gs, ys)
+
+
+def stepq_linattn_decode_step(cfg: Config, layer: int, pool, slots, q, k, v, gate, y, norm: Norm | None = None,
+                              pool_slots=None, stream=None):
+    """One token of decayed linear attention for the batch's slots: q, k [B][Hk][128],
+    v, y [B][Hv][128] (rows may be strided), gate [B][Hv] or [Hv]; pool as for
+    stepq_fp32_decode_step."""
+    f, B = _f32(), slots.numel()
+    if q.shape[0] != B:
+        raise ValueError(f"q: expected {B} rows, got {q.shape[0]}")
+    c = cfg.c()
+    io = _linattn_io(cfg, q, k, v, gate, y)
+    Hv = cfg.n_value_heads
+    check(_lib.lib().stepq_linattn_decode_step(C.byref(c), layer, _dev_ptr(pool, f),
+                                               int(pool.shape[0] if pool_slots is None else pool_slots),
+                                               _dev_ptr(slots, _Torch.i32), B, C.byref(io),
+                                               _c_norm(norm, q.dtype, B, Hv * D, D), _stream(stream)),
+          "stepq_linattn_decode_step")
+
+
+def stepq_linattn_workspace_bytes(cfg: Config, B: int, tokens: int, max_len: int = 0) -> int:
+    c = cfg.c()
+    return int(_lib.lib().stepq_linattn_workspace_bytes(C.byref(c), int(B), int(tokens), int(max_len)))
+
+
+def stepq_linattn_prefill(cfg: Config, layer: int, pool, slots, q, k, v, gate, y, cu_seqlens=None, max_len: int = 0,
+                          resume=None, norm: Norm | None = None, workspace=None, pool_slots=None, stream=None):
+    """Prompts of decayed linear attention: q, k [tokens][Hk][128], v, y [tokens][Hv][128],
+    gate [tokens][Hv] or [Hv]; cu_seqlens int32 [B+1] (None: equal lengths), resume uint8 [B].
+    A workspace that is needed and not given (uint8) comes from torch."""
+    f, B, n = _f32(), slots.numel(), q.shape[0]
+    for t, m, what in ((cu_seqlens, B + 1, "cu_seqlens"), (resume, B, "resume")):
+        if t is not None and t.numel() != m:
+            raise ValueError(f"{what}: expected {m} values, got {t.numel()}")
+    c = cfg.c()
+    lib = _lib.lib()
+    io = _linattn_io(cfg, q, k, v, gate, y)
+    nbytes = lib.stepq_linattn_workspace_bytes(C.byref(c), B, n, int(max_len)) if workspace is None else 0
+    if nbytes:
+        import torch
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        if stream is not None:                       # the block is not reused before this stream's work is done
+            workspace.record_stream(stream)
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    check(lib.stepq_linattn_prefill(C.byref(c), layer, _dev_ptr(pool, f),
+                                    int(pool.shape[0] if pool_slots is None else pool_slots),
+                                    _dev_ptr(slots, _Torch.i32), _dev_ptr(resume, _Torch.u8),
+                                    _dev_ptr(cu_seqlens, _Torch.i32), B, n, int(max_len), C.byref(io),
+                                    _c_norm(norm, q.dtype, n, cfg.n_value_heads * D, D), _dev_ptr(workspace), have,
+                                    _stream(stream)), "stepq_linattn_prefill")
+
+
+def stepq_group_norm(x, groups: int, out, norm: Norm, stream=None):
+    """Group norm of x [rows][channels] into out (which may be x), see Norm."""
+    rows, channels = x.shape
+    if groups < 1 or channels % groups:
+        raise ValueError(f"{channels} channels do not make {groups} groups")
+    xp, xs = _rows_ptr(x, x.dtype, rows, channels, "x")
+    op, os_ = _rows_ptr(out, x.dtype, rows, channels, "out")
+    check(_lib.lib().stepq_group_norm(_dtype_code(x.dtype), rows, int(groups), channels // groups, xp, xs, op, os_,
+                                      _c_norm(norm, x.dtype, rows, channels, channels // groups),
+                                      _stream(stream)), "stepq_group_norm")
 
 
 # ------------------------------------------------------------------ calibration driver

@@ -135,6 +135,18 @@ stepq_status launch_intb_decode(const stepq_config *cfg, int bits, int layer, ui
                                 int pool_slots, const int32_t *slots, int B, const float *q,
                                 const float *k, const float *v, const float *beta,
                                 const float *gate, float *y, cudaStream_t s);
+// linattn_decode.cu, linattn_prefill.cu: decayed linear attention (arguments checked)
+stepq_status launch_linattn_decode(const stepq_config *cfg, int layer, float *pool, int pool_slots,
+                                   const int32_t *slots, int B, const stepq_linattn_io *io,
+                                   const stepq_norm *norm, cudaStream_t s);
+stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *pool, int pool_slots,
+                                    const int32_t *slots, const uint8_t *resume, const int32_t *cu, int B,
+                                    int tokens, int max_len, const stepq_linattn_io *io, const stepq_norm *norm,
+                                    void *workspace, cudaStream_t s);
+size_t linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int max_len);
+// groupnorm.cu
+stepq_status launch_group_norm(int dtype, int64_t rows, int groups, int width, const void *x, int64_t x_stride,
+                               void *out, int64_t out_stride, const stepq_norm *norm, cudaStream_t s);
 // calib.cu
 stepq_status launch_calib_observe(const stepq_config *cfg, int layers, const float *q, const float *k,
                                   const float *beta, const float *gate, int n, double *omega_sum,

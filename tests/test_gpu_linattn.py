@@ -1,0 +1,328 @@
+"""Decayed linear attention against the 64-bit recurrence (tolerances: linattn_ref)."""
+import pytest
+
+from paper_2609_38169_gb300 import api as A
+
+import linattn_ref as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+D = 128
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+NAMES = ["f32", "bf16", "f16"]
+
+
+@pytest.fixture(autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    yield
+    assert A.stepq_device_error() == 0
+
+
+def rows(g, n, heads, dt, wide):
+    """[n][heads][128]: rows of their own, or a slice of wider rows."""
+    x = torch.randn((n, heads + (3 if wide else 0), D), generator=g, device="cuda").to(dt)
+    return x[:, 1:1 + heads] if wide else x
+
+
+def inputs(g, n, hk, hv, dt, wide=False):
+    q, k, v, z = (rows(g, n, h, dt, wide) for h in (hk, hk, hv, hv))
+    k.mul_(0.09)
+    u = torch.rand((n, hv), generator=g, device="cuda")
+    long_lived = torch.arange(hv, device="cuda") % 3 == 0
+    return q, k, v, z, torch.where(long_lived, 0.99 + 0.0099 * u, 0.7 + 0.29 * u)
+
+
+def norm_of(kind, hv, z, g):
+    """The library's norm and the reference's arguments."""
+    if kind is None:
+        return None, None
+    w, b = 1 + 0.2 * torch.randn((2, hv * D), generator=g, device="cuda")
+    args = {"group": dict(w=w, b=b - 1, z=z, kind=1, center=True),
+            "rms": dict(w=w[:D].contiguous(), z=z, kind=2, center=False, shared=True),
+            "silu": dict(kind=1, center=True), "plain": dict(b=b, z=z, kind=0, center=False)}[kind]
+    return A.Norm(weight=args.get("w"), bias=args.get("b"), z=args.get("z"), act=args["kind"],
+                  center=args["center"], shared=args.get("shared", False)), args
+
+
+def check_y(got, y, ya, dt, args, rows_):
+    """One sequence's outputs [T][hv][128] against y, with the norm's arguments if any."""
+    hv = y.shape[1]
+    e = R.y_bound(y, ya, dt)
+    if args is None:
+        want, tol = y, e
+    else:
+        args = dict(args)
+        if args.get("z") is not None:
+            args["z"] = args["z"][rows_].flatten(1)
+        want, gain, part = R.norm(y.flatten(1), hv, **args)
+        tol = R.norm_bound(e.flatten(1), gain, part, hv)
+        want, tol = want.view_as(y), tol.view_as(y)
+    R.assert_within(got, want, R.rounded(tol, want, dt), "y")
+
+
+def run_prefill(lens, hk, hv, dt, norm=None, wide=False, resume=None, layers=1, seed=0, edit=None, extra=0,
+                max_len=None, per_head=False, stream=None):
+    """A packed batch through the library and the reference; checks every output."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    B, n = len(lens), sum(lens)
+    q, k, v, z, gate = inputs(g, n + extra, hk, hv, dt, wide)
+    if per_head:
+        gate = gate[0].contiguous()
+    if edit:
+        edit(q, k, v, gate)
+    pool = torch.randn((B + 2, layers, hv, D, D), generator=g, device="cuda")
+    slots = torch.randperm(B + 2, generator=g, device="cuda")[:B].to(torch.int32)
+    flags = None if resume is None else torch.tensor([resume(b) for b in range(B)], dtype=torch.uint8, device="cuda")
+    before = pool.clone()
+    if flags is not None:                                    # a new sequence's slot may hold anything
+        for b in range(B):
+            if not flags[b] and lens[b]:
+                pool[slots[b].long()] = torch.nan
+        kept = pool.clone()
+    cfg = A.Config(n_layers=layers, n_key_heads=hk, n_value_heads=hv)
+    lib_norm, args = norm_of(norm, hv, z, g)
+    y = torch.full((n + extra, hv, D), 7.0, dtype=dt, device="cuda")
+    cu = torch.tensor([sum(lens[:b]) for b in range(B + 1)], dtype=torch.int32, device="cuda")
+    layer = layers - 1
+    torch.cuda.synchronize()
+    A.stepq_linattn_prefill(cfg, layer, pool, slots, q, k, v, gate, y, cu_seqlens=cu,
+                            max_len=max(lens, default=0) if max_len is None else max_len, resume=flags, norm=lib_norm,
+                            stream=stream)
+    torch.cuda.synchronize()
+    at = 0
+    for b, T in enumerate(lens):
+        s, r = int(slots[b]), slice(at, at + T)
+        if T:
+            S = before[s, layer].double() if flags is None or flags[b] else torch.zeros((hv, D, D), dtype=torch.float64, device="cuda")
+            yr, ya, Sa = R.linattn(S, q[r], k[r], v[r], gate if per_head else gate[r])
+            check_y(y[r], yr, ya, dt, args, r)
+            R.assert_within(pool[s, layer], S, 64 * R.U * Sa + 1e-37, f"state of sequence {b}")
+            before[s, layer] = pool[s, layer]
+            if flags is not None and not flags[b] and layers > 1:
+                assert bool(pool[s, :layer].isnan().all())
+                before[s, :layer] = 0
+                pool[s, :layer] = 0
+        at += T
+    assert torch.equal(pool, before)                         # nothing else in the pool moved
+    assert bool((y[n:] == 7.0).all())
+    return y, pool
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("lens", [[1], [2], [7], [31], [63], [64], [65], [127], [128], [129], [200], [515]], ids=str)
+def test_lengths(lens, dt):
+    run_prefill(lens, 2, 4, dt, seed=lens[0])
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("hk,hv", [(1, 1), (1, 4), (3, 3), (7, 14)])
+def test_ragged_batches_and_heads(hk, hv, dt):
+    run_prefill([5, 0, 130, 64, 1, 0, 77, 193, 0], hk, hv, dt, resume=lambda b: b % 2, layers=2, seed=hv, extra=9)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("norm", ["group", "rms", "silu", "plain"])
+def test_norm_of_readouts_and_strided_rows(norm, dt):
+    run_prefill([70, 3, 129], 2, 4, dt, norm=norm, wide=True, seed=5, resume=lambda b: b != 1)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("kind", ["resets", "reset runs", "tiny", "ones", "zeros", "small", "per head"])
+def test_decays(kind, dt):
+    """Zeros (alone, in runs, at a chunk's ends, everywhere), decays whose products leave
+    fp32's range, no decay at all, and one decay per head for all tokens."""
+    def edit(q, k, v, gate):
+        if kind == "resets":
+            gate[[0, 13, 63, 64, 100, 127, 128, 255]] = 0.0
+        elif kind == "reset runs":
+            gate[60:70] = 0.0
+            gate[190:, 0] = 0.0
+        elif kind == "tiny":
+            gate[::3] = 1e-20
+            gate[1::3] = 1e-30
+        elif kind == "ones":
+            gate.fill_(1.0)
+        elif kind == "zeros":
+            gate.zero_()
+        elif kind == "small":
+            gate.mul_(0.05)
+    run_prefill([260], 1, 3, dt, edit=edit, per_head=kind == "per head", seed=11)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("lens", [[4096], [3000, 40, 5, 2049], [900] * 3], ids=str)
+def test_long_sequences_on_few_heads(lens, dt):
+    run_prefill(lens, 1, 2, dt, seed=3, resume=lambda b: b % 2 == 0, norm="group")
+
+
+@pytest.mark.parametrize("max_len", [0, 1, 10 ** 6])
+def test_the_longest_length_is_only_a_hint(max_len):
+    run_prefill([1500, 3, 700], 1, 2, torch.bfloat16, max_len=max_len, seed=4)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+def test_values_over_a_wide_range(dt):
+    """Keys and values over the type's exponents (states far above fp16's range)."""
+    def edit(q, k, v, gate):
+        s = torch.exp2(torch.randint(-10, 11, (v.shape[0], 1, 1), device="cuda").float())
+        v.mul_(s.to(dt))
+        k.mul_(torch.exp2(torch.randint(-4, 11, (k.shape[0], 1, 1), device="cuda").float()).to(dt))
+        q.mul_(1e-4)
+    run_prefill([150, 90], 2, 2, dt, edit=edit, seed=8)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_sequence_with_bad_values_leaves_the_others_alone(dt, bad):
+    """Non-finite q, k, v and decays right beside a sequence's rows, in a full and a ragged
+    chunk: its outputs and state are the ones it has without them."""
+    lens, hk, hv = [70, 65, 64, 3], 1, 2
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n = sum(lens)
+    q, k, v, z, gate = inputs(g, n, hk, hv, dt)
+    cfg = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv)
+    slots = torch.arange(4, dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 70, 135, 199, 202], dtype=torch.int32, device="cuda")
+    got = []
+    for spoil in (False, True):
+        if spoil:
+            for x in (q, k, v):
+                x[70:135] = bad
+            gate[70:135] = bad
+        pool = torch.zeros((4, 1, hv, D, D), device="cuda")
+        y = torch.zeros((n, hv, D), dtype=dt, device="cuda")
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, cu_seqlens=cu, max_len=70)
+        got.append((torch.cat([y[:70], y[135:]]), pool[[0, 2, 3]]))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_equal_lengths_without_offsets():
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v, z, gate = inputs(g, 3 * 50, 2, 4, torch.bfloat16)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=2, n_value_heads=4), torch.arange(3, dtype=torch.int32, device="cuda")
+    out = []
+    for cu in (None, torch.tensor([0, 50, 100, 150], dtype=torch.int32, device="cuda")):
+        pool = torch.ones((3, 1, 4, D, D), device="cuda")
+        y = torch.zeros((150, 4, D), dtype=torch.bfloat16, device="cuda")
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, cu_seqlens=cu, max_len=50)
+        out.append((y, pool))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+# ------------------------------------------------------------------ single tokens
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("norm", [None, "group", "rms", "silu"])
+@pytest.mark.parametrize("B,hk,hv", [(1, 1, 1), (1, 4, 4), (3, 2, 4), (41, 16, 32), (130, 7, 7)])
+def test_decode(B, hk, hv, norm, dt):
+    g = torch.Generator(device="cuda").manual_seed(B + hv)
+    q, k, v, z, gate = inputs(g, B, hk, hv, dt, wide=B % 2 == 1)
+    gate[0, 0] = 0.0
+    layers, layer = 2, 1
+    pool = torch.randn((B + 3, layers, hv, D, D), generator=g, device="cuda")
+    slots = torch.randperm(B + 3, generator=g, device="cuda")[:B].to(torch.int32)
+    before = pool.clone()
+    lib_norm, args = norm_of(norm, hv, z, g)
+    y = torch.zeros((B, hv, D), dtype=dt, device="cuda")
+    A.stepq_linattn_decode_step(A.Config(n_layers=layers, n_key_heads=hk, n_value_heads=hv), layer, pool, slots, q, k, v,
+                                gate, y, norm=lib_norm)
+    for b in range(B):
+        s, r = int(slots[b]), slice(b, b + 1)
+        S = before[s, layer].double()
+        yr, ya, Sa = R.linattn(S, q[r], k[r], v[r], gate[r])
+        check_y(y[r], yr, ya, dt, args, r)
+        R.assert_within(pool[s, layer], S, 4 * R.U * Sa, "state")     # two roundings
+        before[s, layer] = pool[s, layer]
+    assert torch.equal(pool, before)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+def test_decode_continues_a_prompt(dt):
+    """A prompt, then tokens one by one: the recurrence over all of them."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    hk, hv, T, more = 2, 4, 133, 5
+    q, k, v, z, gate = inputs(g, T + more, hk, hv, dt)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pool = torch.full((1, 1, hv, D, D), torch.nan, device="cuda")
+    y = torch.empty((T + more, hv, D), dtype=dt, device="cuda")
+    fresh = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    A.stepq_linattn_prefill(cfg, 0, pool, slots, q[:T], k[:T], v[:T], gate[:T], y[:T], max_len=T, resume=fresh)
+    for t in range(T, T + more):
+        r = slice(t, t + 1)
+        A.stepq_linattn_decode_step(cfg, 0, pool, slots, q[r], k[r], v[r], gate[r], y[r])
+    S = torch.zeros((hv, D, D), dtype=torch.float64, device="cuda")
+    yr, ya, Sa = R.linattn(S, q, k, v, gate)
+    check_y(y, yr, ya, dt, None, None)
+    R.assert_within(pool[0, 0], S, 64 * R.U * Sa, "state")
+
+
+# ------------------------------------------------------------------ streams, graphs, errors
+def test_side_stream_and_graph():
+    """Captured on a side stream, a prompt and two tokens replay to the bytes of the calls
+    made one by one."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    hk, hv, lens = 2, 4, [300, 40]
+    n, B = sum(lens), 2
+    q, k, v, z, gate = inputs(g, n, hk, hv, torch.bfloat16)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv), torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 300, 340], dtype=torch.int32, device="cuda")
+    pool, y = torch.empty((2, 1, hv, D, D), device="cuda"), torch.empty((n, hv, D), dtype=torch.bfloat16, device="cuda")
+    yd = torch.empty((B, hv, D), dtype=torch.bfloat16, device="cuda")
+    work = torch.empty(max(256, A.stepq_linattn_workspace_bytes(cfg, B, n, 300)), dtype=torch.uint8, device="cuda")
+    norm = A.Norm(z=z, act=A.ACT_SILU)
+
+    def chain(between=lambda: None):
+        pool.fill_(0.5); between()
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, cu_seqlens=cu, max_len=300, norm=norm, workspace=work)
+        between()
+        for _ in range(2):
+            A.stepq_linattn_decode_step(cfg, 0, pool, slots, q[:B], k[:B], y[:B], gate[:B], yd); between()
+            A.stepq_group_norm(yd.flatten(1), hv, yd.flatten(1), A.Norm(act=A.ACT_SILU)); between()
+
+    chain(torch.cuda.synchronize)
+    want = [t.clone() for t in (pool, y, yd)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (pool, y, yd)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for _ in range(3):
+        for t in (pool, y, yd):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (pool, y, yd)))
+
+
+def test_device_errors():
+    """Slots and bounds out of range are skipped and reported; the others are served."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    hk, hv = 1, 2
+    q, k, v, z, gate = inputs(g, 90, hk, hv, torch.bfloat16)
+    cfg = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def prefill(slots, cu):
+        pool, y = torch.ones((3, 1, hv, D, D), device="cuda"), torch.zeros((90, hv, D), dtype=torch.bfloat16, device="cuda")
+        A.stepq_linattn_prefill(cfg, 0, pool, i32(*slots), q, k, v, gate, y, cu_seqlens=i32(*cu), max_len=90)
+        return pool, y, A.stepq_device_error()
+
+    want, wy, err = prefill((0, 1, 2), (0, 30, 60, 90))
+    assert err == 0
+    for bad in (3, -1):
+        pool, y, err = prefill((0, bad, 2), (0, 30, 60, 90))
+        assert err == 2 and torch.equal(pool[[0, 2]], want[[0, 2]]) and bool((pool[1] == 1).all())
+        assert torch.equal(y[:30], wy[:30]) and bool((y[30:60] == 0).all()) and torch.equal(y[60:], wy[60:])
+    for cu in ((0, 30, 20, 90), (-1, 30, 60, 90), (0, 30, 60, 91), (0, 2 ** 31 - 1, 60, 90)):
+        pool, y, err = prefill((0, 1, 2), cu)
+        assert err == 1
+    pool = torch.ones((3, 1, hv, D, D), device="cuda")
+    y = torch.zeros((3, hv, D), dtype=torch.bfloat16, device="cuda")
+    for slots, code in (((0, 5, 1), 2), ((2, 0, 2), 3)):
+        A.stepq_linattn_decode_step(cfg, 0, pool, i32(*slots), q[:3], k[:3], v[:3], gate[:3], y)
+        assert A.stepq_device_error() == code

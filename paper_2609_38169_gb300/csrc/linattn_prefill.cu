@@ -6,46 +6,12 @@
 // threads as shared-memory broadcasts. 3 x 128^2 FMA-pipe operations a token and head bound it.
 #include "async.cuh"
 #include "device.cuh"
-#include "linattn.cuh"
+#include "linattn_prefill.cuh"
 
 namespace stepq {
 namespace la {
 
 constexpr int kBlockTokens = 16;       // tokens staged at a time
-
-struct PrefillArgs {
-    float *pool;
-    uint64_t slot_floats, layer_off;
-    int pool_slots, B, tokens, Hk, Hv;
-    const int32_t *slots, *cu;
-    const uint8_t *resume;
-    const void *q, *k, *v;
-    const float *gate;
-    void *y;
-    int64_t qs, ks, vs, gs, ys;
-    NormArgs norm;
-    unsigned int *err;
-};
-
-// First row and length of sequence b, and its slot; false (and the device error) if either
-// is out of range. lead: the thread that raises it.
-__device__ __forceinline__ bool sequence(const PrefillArgs &a, int b, bool lead, int &start, int &len, int &slot) {
-    const int each = a.tokens / a.B;
-    start = a.cu ? a.cu[b] : b * each;
-    const int end = a.cu ? a.cu[b + 1] : start + each;
-    slot = a.slots[b];
-    len = end - start;
-    const bool bounds = start >= 0 && end >= start && end <= a.tokens;
-    if (!bounds) {
-        if (lead) raise_error(a.err, STEPQ_ERR_ARG);
-        return false;
-    }
-    if (slot < 0 || slot >= a.pool_slots) {
-        if (lead) raise_error(a.err, STEPQ_ERR_SLOT_RANGE);
-        return false;
-    }
-    return true;
-}
 
 template <class T>
 __global__ void __launch_bounds__(kD) linattn_prefill_tokens_kernel(PrefillArgs a) {
@@ -126,6 +92,9 @@ stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *p
     a.qs = io->q_stride; a.ks = io->k_stride; a.vs = io->v_stride; a.gs = io->gate_stride; a.ys = io->y_stride;
     a.norm = la::norm_args(norm);
     a.err = device_error_word();
+    a.stall = stall_knob();
+    a.items = B * a.Hv;
+    if (la::linattn_chunks_takes(cfg, io)) return la::launch_linattn_chunks(a, a.items, true, s);
     return la::by_type(io->dtype, [&](auto t) {
         return launch_overlapped(la::linattn_prefill_tokens_kernel<decltype(t)>, B * a.Hv, kD, 0, s, a);
     });

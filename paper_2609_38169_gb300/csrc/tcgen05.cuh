@@ -48,6 +48,21 @@ __device__ __forceinline__ uint64_t sdesc(const void *smem, uint32_t lbo, uint32
            ((uint64_t)((sbo & 0x3FFFFu) >> 4) << 32) | (1ull << 46);
 }
 
+// kind::f16 with bf16 operands and an fp32 accumulator: D format F32, A and B format BF16
+// (bits 7-9 and 10-12 = 1), bit 15 / 16: A / B is MN-major (else K-major).
+__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn, int b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+           ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Shared-memory descriptor of an operand in the 128-byte swizzle (rows of 128 bytes, 16-byte
+// piece p of row r at p ^ (r & 7); 1024-byte aligned blocks of 8 rows). K-major: a row is 64
+// elements of K, `sbo` the distance of 8-row blocks along M/N, lbo unused. MN-major: a row
+// is 64 elements of M/N, `sbo` the distance of 8-row blocks along K, `lbo` that of the next
+// 64 elements of M/N. Bits 61-63 hold the layout, 2.
+__device__ __forceinline__ uint64_t sdesc_sw128(const void *smem, uint32_t lbo, uint32_t sbo) {
+    return sdesc(smem, lbo, sbo) | (2ull << 61);
+}
+
 // The calls below are made by a whole warp with the same arguments, and take effect for
 // the lane with `lead` set (elect()): arguments that are uniform over a converged warp
 // stay in uniform registers, from which the instructions take them (a single thread had
@@ -73,6 +88,24 @@ __device__ __forceinline__ void mma_tf32_ss(uint32_t lead, uint32_t d_tmem, uint
     asm volatile(
         "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
         "@e tcgen05.mma.cta_group::1.kind::tf32 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc), "r"(lead)
+        : "memory");
+}
+// The same for kind::f16 (16 elements of K): A in tensor memory holds two elements of K a
+// column, the first in the low half.
+__device__ __forceinline__ void mma_f16_ts(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
+                                           uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16_ss(uint32_t lead, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                           uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
         "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc), "r"(lead)
         : "memory");
 }
@@ -166,6 +199,11 @@ __device__ __forceinline__ void st64(uint32_t taddr, const float (&v)[64]) {
                                                           "r"(__float_as_uint(v[61])), "r"(__float_as_uint(v[62])),
                                                             "r"(__float_as_uint(v[63]))
         : "memory");
+}
+__device__ __forceinline__ void st8(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]),
+                 "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 

@@ -326,3 +326,27 @@ def test_device_errors():
     for slots, code in (((0, 5, 1), 2), ((2, 0, 2), 3)):
         A.stepq_linattn_decode_step(cfg, 0, pool, i32(*slots), q[:3], k[:3], v[:3], gate[:3], y)
         assert A.stepq_device_error() == code
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_a_stalled_prompt_reports_a_timeout(norm):
+    """Copies that never start: every wait gives up within its bound, the launch ends and
+    reports it, and the next one is whole."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, z, gate = inputs(g, 4 * 200, 1, 2, torch.bfloat16)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=2), torch.arange(4, dtype=torch.int32, device="cuda")
+
+    def call():
+        pool, y = torch.ones((4, 1, 2, D, D), device="cuda"), torch.zeros((800, 2, D), dtype=torch.bfloat16, device="cuda")
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, max_len=200, norm=A.Norm(z=z) if norm else None)
+        return pool, y, A.stepq_device_error()
+
+    want = call()
+    assert want[2] == 0
+    try:
+        A.stepq_debug_stall(2_000_000, 3)
+        assert call()[2] == 8
+    finally:
+        A.stepq_debug_stall()
+    got = call()
+    assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

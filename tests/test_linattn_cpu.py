@@ -141,7 +141,7 @@ def run(tmp_path_factory):
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(build_ext.nvcc())))
     fake = str(tmp_path_factory.mktemp("fake") / "libfake.so")
     subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-Wall", "-I", os.path.join(cuda, "include"),
-                    os.path.join(HERE, "fake_cudart.c"), "-o", fake], check=True)
+                    os.path.join(HERE, "fake_cudart.c"), os.path.join(HERE, "fake_tensormap.c"), "-o", fake], check=True)
 
     def child(code):
         r = subprocess.run([sys.executable, "-c", CALLS + code], cwd=os.path.dirname(HERE), capture_output=True,

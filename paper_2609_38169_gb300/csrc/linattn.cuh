@@ -51,54 +51,76 @@ inline NormArgs norm_args(const stepq_norm *n) {
     return {n->weight, n->bias, n->z, n->z_stride, n->eps, n->act, n->center, n->shared, 1};
 }
 
-// Vectors of 16 bits leave a result 8 or 11 bits: the fast exponential and quotient (a few
-// units in 2^-23, and 2^-24 |x| from the exponent's product) are far below that. fp32
-// results take expf and the rounded quotient.
+// act(x), without branches. Vectors of 16 bits leave a result 8 or 11 bits: the fast exponential
+// and quotient (a few units in 2^-23, and 2^-24 |x| from the exponent's product) are far below
+// that. fp32 results take expf and the rounded quotient.
 template <class T>
 __device__ __forceinline__ float activation(int act, float x) {
-    if (act == STEPQ_ACT_NONE) return x;
-    const float num = act == STEPQ_ACT_SILU ? x : 1.f;
-    if (sizeof(T) == 2) return __fdividef(num, 1.f + __expf(-x));
-    return num / (1.f + expf(-x));
+    const float e = sizeof(T) == 2 ? __expf(-x) : expf(-x);
+    const float num = act == STEPQ_ACT_SIGMOID ? 1.f : x, den = act == STEPQ_ACT_NONE ? 1.f : 1.f + e;
+    return sizeof(T) == 2 ? __fdividef(num, den) : num / den;
 }
 
 // out = u act(z) or act(u) of one channel, u = xc * rstd * w + b with xc = x - mean.
 template <class T>
 __device__ __forceinline__ float norm_out(const NormArgs &n, float xc, float rstd, float w, float b, float z) {
     const float u = fmaf(xc * rstd, w, b);
-    return n.z ? u * activation<T>(n.act, z) : activation<T>(n.act, u);
+    return (n.z ? u : 1.f) * activation<T>(n.act, n.z ? z : u);
 }
 
 __device__ __forceinline__ float rstd_of(float var, float eps) { return rsqrtf(var + eps); }
 
-// One head's readouts of a token in a warp, lane l holding channels N l .. N l + N - 1 of N * 32.
-// h: the head; row: the token's row (of z).
-template <class T, int N>
-__device__ __forceinline__ void norm_head(const NormArgs &n, int h, int64_t row, int lane, float (&y)[N]) {
-    constexpr int W = 32 * N;
-    float m = 0.f;
-    if (n.center) {
+// The affine parameters of lane l's channels 4 l .. 4 l + 3 of head h.
+struct HeadAffine {
+    float w[4], b[4];
+    __device__ __forceinline__ HeadAffine(const NormArgs &n, int h, int lane) {
+        const int c = 4 * lane + (n.shared ? 0 : h * kD);
 #pragma unroll
-        for (int i = 0; i < N; i++) m += y[i];
-#pragma unroll
-        for (int o = 16; o; o >>= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
-        m *= 1.f / W;
+        for (int i = 0; i < 4; i++) {
+            w[i] = n.w ? n.w[c + i] : 1.f;
+            b[i] = n.b ? n.b[c + i] : 0.f;
+        }
     }
-    float ss = 0.f;
+};
+
+// One head's readouts of N tokens in a warp, lane l holding channels 4 l .. 4 l + 3: their
+// sums cross the warp together. z(i) is lane l's place in token i's row of the gate.
+template <class T, int N, class Z>
+__device__ __forceinline__ void norm_head(const NormArgs &n, const HeadAffine &p, Z &&z, float (&y)[N][4]) {
+    float g[N][4], s[N], m[N];
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        y[i] -= m;
-        ss = fmaf(y[i], y[i], ss);
+        if (n.z) load_vec<T, 4>(z(i), g[i]);
+        m[i] = 0.f;
+        s[i] = (y[i][0] + y[i][1]) + (y[i][2] + y[i][3]);
+    }
+    if (n.center) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; i++) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+#pragma unroll
+        for (int i = 0; i < N; i++) m[i] = s[i] * (1.f / kD);
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float r = rstd_of(ss * (1.f / W), n.eps);
-    const int c = N * lane, pc = c + (n.shared ? 0 : h * W);
-    float z[N] = {};
-    if (n.z) load_vec<T, N>((const T *)n.z + row * n.z_stride + (int64_t)h * W + c, z);
+    for (int i = 0; i < N; i++) {
+        s[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; i++)
-        y[i] = norm_out<T>(n, y[i], r, n.w ? n.w[pc + i] : 1.f, n.b ? n.b[pc + i] : 0.f, z[i]);
+        for (int e = 0; e < 4; e++) {
+            y[i][e] -= m[i];
+            s[i] = fmaf(y[i][e], y[i][e], s[i]);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; i++) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float r = rstd_of(s[i] * (1.f / kD), n.eps);
+#pragma unroll
+        for (int e = 0; e < 4; e++) y[i][e] = norm_out<T>(n, y[i][e], r, p.w[e], p.b[e], g[i][e]);
+    }
 }
 
 // Runs f(T{}) for the element type of a call.

@@ -7,24 +7,26 @@
 //   Y^T = (S_0^T Q^T) diag(c_t) + V^T P^T,   P_ts = w_ts (q_t . k_s), zero for s > t
 //   S_C = c_C S_0 + U,   U^T = V^T K',   K'_s = w_Cs k_s
 // Four products a chunk, all with M = 128 (lane = value channel, or token):
-//   scores  Q K^T            A = Q, B = K in smem        N = 64, K = 128   (rows 64.. unused)
-//   QS      S_0^T Q^T        A = S^T in tmem, B = Q      N = 64, K = 128   x 2 (head, rest)
-//   PV      V^T P^T          A = V^T, B = P in smem      N = 64, K = 64    x 2 (head, rest)
-//   KV      V^T K'           A = V^T, B = K' in smem     N = 128, K = 64   x 3
+//   scores  Q K^T            A = Q, B = K in smem         N = 64, K = 128   (rows 64.. unused)
+//   QS      S_0^T Q^T        A = S^T in tmem, B = Q       N = 64, K = 128   x 2 (head, rest of S)
+//   PV      V^T P^T          A = V^T, B = P in smem       N = 128, K = 64   (head and rest of P side by side)
+//   KV      V^T K'           A = V^T, B = K' in smem      N = 128, K = 64   x 3
 // q, k and v are bf16 and enter as they are, from where TMA put them. What is fp32 enters as
-// a sum of bf16: K' as three truncated terms, exactly; S and P as a truncated head and a
-// rounded rest (2^-17 of each value; the result is rounded to 2^-9). The state itself stays
-// in fp32 registers of the chain's warps and U is formed apart from it, so what is added from
-// chunk to chunk is rounded to nearest (the tensor core's own sums truncate).
+// a sum of bf16: K' as three truncated terms, exactly, since states are kept in fp32; S and P
+// as a truncated head and a rounded rest (2^-17 of each value; the result is rounded to
+// 2^-9). The state itself stays in fp32 registers and U is formed apart from it, so what is
+// added from chunk to chunk is rounded to nearest (the tensor core's own sums truncate).
 //
-// One persistent CTA of 19 warps per SM:
-//   warps 0-7    the chain: S <- c_C S + U, its split into tensor memory, and Y (lane = value
-//                channel j, warps w and w + 4 sharing lanes 32 (w % 4) ..)
-//   warps 8-15   quadrants 0, 1 (lanes = tokens): P; quadrants 2, 3: K'
-//   warp 16      issues the MMAs
-//   warp 17      loads q, k and v (TMA, two places each)
-//   warp 18      decays: their products over the chunk
-// Hand-over by mbarriers, every wait bounded.
+// One persistent CTA of 28 warps per SM:
+//   warps 0-7    the state: S <- c_C S + U, its split into tensor memory (lane = value channel,
+//                warps w and w + 4 sharing lanes 32 (w % 4) ..)
+//   warps 8-15   the outputs (lanes likewise)
+//   warps 16, 17, 21   P (lanes = tokens), a 32 x 32 block each
+//   warp 18      loads q, k and v (TMA, two places each); decays and their products
+//   warps 19, 20 issue the MMAs: scores and PV; KV and QS
+//   warps 22-27  K'
+// Hand-over by mbarriers, every wait bounded. Loops keep few unrolled steps: unrolled, the
+// warps' code did not fit the instruction caches (a third of the stalls of issuing warps).
 #include <cuda.h>
 
 #include "async.cuh"
@@ -37,101 +39,121 @@ namespace la {
 namespace ch {
 
 constexpr int C = kChunk;
-constexpr int kPlaces = 2;                              // of q, k and v
-constexpr int kGateRing = 4;
-constexpr int kBlock = 19 * 32 + 32;                    // registers are shared out by warpgroups
-constexpr int kRegs = 96, kRegsChain = 136, kRegsOperand = 80, kRegsIssue = 48;
-static_assert(256 * (kRegsChain + kRegsOperand) + 128 * kRegsIssue <= kBlock * kRegs, "register shares");
+constexpr int kPlaces = 2;                              // of q, k, v and P
+constexpr int kBlock = 28 * 32;                         // registers are shared out by warpgroups
+constexpr int kRegs = 72, kRegsState = 112, kRegsOut = 64, kRegsOperand = 48;
+static_assert(256 * (kRegsState + kRegsOut) + 384 * kRegsOperand <= kBlock * kRegs, "register shares");
+constexpr int kScaleWarps = 6;
 constexpr uint32_t kColU = 0, kColSh = 128, kColSl = 192, kColP = 256, kColY1 = 320, kColY2 = 384, kCols = 512;
 
 constexpr int kTile = C * 128;                          // 64 rows of 128 bytes: 64 channels of a chunk
-constexpr int kOffQ = 0;                                // [place][2 tiles]
-constexpr int kOffK = kOffQ + kPlaces * 2 * kTile;
-constexpr int kOffV = kOffK + kPlaces * 2 * kTile;
-constexpr int kOffKp = kOffV + kPlaces * 2 * kTile;     // K': 3 terms x 2 tiles
-constexpr int kOffP = kOffKp + 3 * 2 * kTile;           // P: head, rest
-constexpr int kOffY = kOffP + 2 * kTile;                // float [C][kYRow] readouts to normalise
-constexpr int kYRow = 132;
-struct Gates {
-    float g[C], c[C], wk[C];                            // decays, c_t, w_Cs (0 past the last token)
+constexpr int kOffK = 0, kOffQ = kOffK + kPlaces * 2 * kTile, kOffV = kOffQ + kPlaces * 2 * kTile;   // [place][2 tiles]
+constexpr int kOffKp = kOffV + kPlaces * 2 * kTile;     // K': [term][2 tiles]
+constexpr int kOffP = kOffKp + 3 * 2 * kTile;           // P: [place][head, rest]
+constexpr int kOffY = kOffP + kPlaces * 2 * kTile;      // [C][128] readouts: bf16, or float to normalise
+struct alignas(16) Gates {
+    float next[C], c[C], wk[C];                         // g_{t+1}, c_t, w_Cs (0 past the last token)
     float suf[32], pre[32];                             // w_{31,s} of the first half, c_t / c_31 of the second
     float total, pad[3];                                // c_C
 };
-constexpr int kOffG = kOffY + C * kYRow * 4;
-constexpr int kOffBar = kOffG + kGateRing * (int)sizeof(Gates);
+// Two places for the decays where the readouts take twice the room.
+template <bool NORM> constexpr int kRing = NORM ? 2 : 4;
+template <bool NORM> constexpr int kOffG = kOffY + C * kD * (NORM ? 4 : 2);
+template <bool NORM> constexpr int kOffBar = kOffG<NORM> + kRing<NORM> * (int)sizeof(Gates);
 enum {
-    kFullQ, kFullK = kFullQ + kPlaces, kFullV = kFullK + kPlaces, kFreeQ = kFullV + kPlaces, kFreeK = kFreeQ + kPlaces,
-    kFreeV = kFreeK + kPlaces, kFullG = kFreeV + kPlaces, kFreeG = kFullG + kGateRing, kScores = kFreeG + kGateRing,
-    kScoresFree, kPReady, kKpReady, kSReady, kUFree, kYFree, kQs, kKv, kPv, kDrain, kBars
+    kFullK, kFullQ = kFullK + kPlaces, kFullV = kFullQ + kPlaces, kFreeK = kFullV + kPlaces, kFreeQ = kFreeK + kPlaces,
+    kFreeV = kFreeQ + kPlaces, kPReady = kFreeV + kPlaces, kKpReady = kPReady + kPlaces, kKpFree = kKpReady + 2,
+    kFullG = kKpFree + 2, kFreeG = kFullG + 4, kScores = kFreeG + 4, kSReady, kUFree, kYFree, kQs, kKv, kPv, kDrainA, kDrainB, kBars
 };
-constexpr int kOffTmem = kOffBar + kBars * 8;
-constexpr int kSmem = kOffTmem + 16;
-static_assert(kSmem <= kSmemMax, "one CTA's shared memory");
-static_assert(kOffBar % 8 == 0 && kOffG % 16 == 0, "alignment");
+template <bool NORM> constexpr int kOffTmem = kOffBar<NORM> + kBars * 8;
+template <bool NORM> constexpr int kSmem = kOffTmem<NORM> + 16;      // the tensor memory's base
+static_assert(kSmem<true> <= kSmemMax && kSmem<false> <= kSmemMax, "one CTA's shared memory");
 
 constexpr uint32_t kIdescScores = tc::idesc_bf16(128, 64, 0, 0);
 constexpr uint32_t kIdescQs = tc::idesc_bf16(128, 64, 0, 0);
-constexpr uint32_t kIdescPv = tc::idesc_bf16(128, 64, 1, 0);
+constexpr uint32_t kIdescPv = tc::idesc_bf16(128, 128, 1, 0);
 constexpr uint32_t kIdescKv = tc::idesc_bf16(128, 128, 1, 1);
 
 struct Maps {
-    CUtensorMap q, k, v;
+    CUtensorMap of[3];                                  // k, q, v
 };
 
+template <bool NORM>
 struct Ctx {
     const PrefillArgs &a;
     uint8_t *smem;
     uint64_t *bars;
-    // warp-uniform: true once the phase of the given parity has completed
-    __device__ __forceinline__ bool wait(int bar, uint32_t parity) const {
-        return __all_sync(0xffffffffu, mbar_wait(&bars[bar], parity, a.stall.wait_cycles));
+    mutable uint32_t limit;                                 // of a wait, in cycles; 0: one has run out
+    static constexpr int R = kRing<NORM>;
+    // Waits for the phase of the given parity. Once a wait has run out no other of this warp
+    // holds: the warps reach their ends without early exits, and the outputs are undefined.
+    __device__ __forceinline__ void wait(int bar, uint32_t parity) const {
+        const uint32_t t0 = (uint32_t)clock();
+        while (!mbar_test(&bars[bar], parity))
+            if ((uint32_t)clock() - t0 > limit) {
+                limit = 0;
+                break;
+            }
+        __syncwarp();
     }
-    // The phase of use n of a ring of R places; `again`: that it was given back before.
-    template <int R> __device__ __forceinline__ bool wait_full(int bar, uint32_t n) const {
-        return wait(bar + n % R, (n / R) & 1u);
+    // Use n of a ring of N places: filled; given back after use n - N.
+    template <int N> __device__ __forceinline__ void wait_full(int bar, uint32_t n) const { wait(bar + n % N, (n / N) & 1u); }
+    template <int N> __device__ __forceinline__ void wait_free(int bar, uint32_t n) const {
+        wait(bar + n % N, ((n / N) & 1u) ^ 1u);             // before a barrier's first phase its parity is 1
     }
-    template <int R> __device__ __forceinline__ bool wait_free(int bar, uint32_t n) const {
-        return n < R || wait(bar + n % R, (n / R - 1) & 1u);
+    // Use n of a single place: the one before has ended.
+    __device__ __forceinline__ void wait_last(int bar, uint32_t n) const {
+        wait(bar, (n & 1u) ^ 1u);
     }
     // One arrival for the warp, after what its lanes did.
     __device__ __forceinline__ void arrive(int bar) const {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(&bars[bar]);
     }
-    __device__ __forceinline__ const Gates &gates(uint32_t n) const {
-        return ((const Gates *)(smem + kOffG))[n % kGateRing];
-    }
+    __device__ __forceinline__ Gates &gates(uint32_t n) const { return ((Gates *)(smem + kOffG<NORM>))[n % R]; }
 };
 
-__device__ __forceinline__ uint32_t high_halves(float a, float b) {      // truncated to bf16, a low
-    return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+// The pieces of a pair of fp32 values: both truncated to bf16 (the first in the low half),
+// what remains of them (exact), and both rounded to bf16.
+__device__ __forceinline__ uint32_t heads(uint64_t p) {
+    return __byte_perm((uint32_t)p, (uint32_t)(p >> 32), 0x7632);
 }
-__device__ __forceinline__ float head_of(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
-__device__ __forceinline__ uint32_t rounded_halves(float a, float b) {
+__device__ __forceinline__ uint64_t rests(uint64_t p) {
+    return fsub2(p, u2pair((uint32_t)p & 0xFFFF0000u, (uint32_t)(p >> 32) & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint32_t rounded(uint64_t p) {
     uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(f2hi(p)), "f"(f2lo(p)));
     return d;
 }
-// Two fp32 values as a truncated bf16 head and a rounded rest each.
-__device__ __forceinline__ void split2(float a, float b, uint32_t &head, uint32_t &rest) {
-    head = high_halves(a, b);
-    rest = rounded_halves(a - head_of(a), b - head_of(b));
+__device__ __forceinline__ uint64_t pair_at(const float *p) {           // 8-byte aligned
+    return *(const uint64_t *)p;
 }
 
-// Warp 18: the decays of every chunk and their products, a block of 32 tokens per half.
-__device__ __forceinline__ bool decays(const Ctx &x) {
+// Warp 18: the decays of every chunk and their products, a block of 32 tokens per half, and
+// k, q and v.
+template <bool OUT, bool NORM>
+__device__ __forceinline__ void load(const Ctx<NORM> &x, const Maps &maps) {
     const PrefillArgs &a = x.a;
-    const int l = threadIdx.x & 31;
-    uint32_t n = 0;
-    for (Items it(a); it.next();) {
+    const int grp = a.Hv / a.Hk, l = threadIdx.x & 31;
+    const uint32_t lead = tc::elect();
+    uint32_t n = 0, started = 0;                            // chunks; copies, three a chunk
+    for (Items it(a); it.next(l == 0);) {
+        if (it.item == a.stall.withhold_item) break;        // test switch: these copies never start
+        const int hk = it.h / grp;
+        const float *gate = a.gate + (int64_t)it.row * a.gs + it.h;
+        const auto decay = [&](int t) { return t < it.len ? gate[(int64_t)t * a.gs] : 1.f; };
+        float g0 = decay(l), g1 = decay(32 + l);
+#pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const int m = it.len - t0;                      // tokens from here on
-            const float *g = a.gate + ((int64_t)it.row + t0) * a.gs + it.h;
-            const float g0 = l < m ? g[(int64_t)l * a.gs] : 1.f, g1 = l + 32 < m ? g[(int64_t)(l + 32) * a.gs] : 1.f;
+            const int m = it.len - t0;
             float p0 = g0, p1 = g1;                         // inclusive from the block's start
-            float s0 = __shfl_down_sync(0xffffffffu, g0, 1), s1 = __shfl_down_sync(0xffffffffu, g1, 1);
-            if (l == 31) s0 = s1 = 1.f;                     // exclusive to the block's end
-#pragma unroll
+            float n0 = __shfl_down_sync(0xffffffffu, g0, 1), n1 = __shfl_down_sync(0xffffffffu, g1, 1);
+            if (l == 31) n0 = n1 = 1.f;
+            float s0 = n0, s1 = n1;                         // exclusive to the block's end
+            g0 = decay(t0 + C + l);                         // the next chunk's
+            g1 = decay(t0 + C + 32 + l);
+#pragma unroll 1
             for (int o = 1; o < 32; o *= 2) {
                 const float u0 = __shfl_up_sync(0xffffffffu, p0, o), u1 = __shfl_up_sync(0xffffffffu, p1, o);
                 const float d0 = __shfl_down_sync(0xffffffffu, s0, o), d1 = __shfl_down_sync(0xffffffffu, s1, o);
@@ -139,10 +161,10 @@ __device__ __forceinline__ bool decays(const Ctx &x) {
                 if (l + o < 32) s0 *= d0, s1 *= d1;
             }
             const float all0 = __shfl_sync(0xffffffffu, p0, 31), all1 = __shfl_sync(0xffffffffu, p1, 31);
-            if (!x.wait_free<kGateRing>(kFreeG, n)) return false;
-            Gates &o = ((Gates *)(x.smem + kOffG))[n % kGateRing];
-            o.g[l] = g0;
-            o.g[32 + l] = g1;
+            x.template wait_free<x.R>(kFreeG, n);
+            Gates &o = x.gates(n);
+            o.next[l] = n0;
+            o.next[32 + l] = n1;
             o.c[l] = p0;
             o.c[32 + l] = all0 * p1;
             o.wk[l] = l < m ? s0 * all1 : 0.f;
@@ -150,372 +172,420 @@ __device__ __forceinline__ bool decays(const Ctx &x) {
             o.suf[l] = s0;
             o.pre[l] = p1;
             if (l == 0) o.total = all0 * all1;
-            x.arrive(kFullG + n % kGateRing);
+            x.arrive(kFullG + n % x.R);
+#pragma unroll 1
+            for (int i = 0; i < 3; i++) {                   // k, q, v
+                if (!OUT && i == 1) {
+                    started++;
+                    continue;
+                }
+                x.template wait_free<kPlaces>(kFreeK + i * kPlaces, n);
+                if (x.limit == 0) goto drain;               // nothing more is started
+                started++;
+                uint64_t *full = &x.bars[kFullK + i * kPlaces + n % kPlaces];
+                uint8_t *dst = x.smem + (i * kPlaces + n % kPlaces) * 2 * kTile;
+                const int ch = (i == 2 ? it.h : hk) * kD;
+                if (lead) {
+                    mbar_arrive_tx(full, 2 * kTile);
+                    tma_load_2d(dst, &maps.of[i], ch, it.row + t0, full);
+                    tma_load_2d(dst + kTile, &maps.of[i], ch + 64, it.row + t0, full);
+                }
+                __syncwarp();
+            }
         }
     }
-    return true;
+drain:                                                      // no copy is in flight when the CTA ends
+#pragma unroll 1
+    for (uint32_t u = started < 3 * kPlaces ? 0 : started - 3 * kPlaces; u < started; u++)
+        if (OUT || u % 3 != 1) mbar_wait(&x.bars[kFullK + (u % 3) * kPlaces + u / 3 % kPlaces], (u / 3 / kPlaces) & 1u, x.a.stall.wait_cycles);
 }
 
-// Warp 17: q, k and v of every chunk.
-template <bool OUT>
-__device__ __forceinline__ bool load(const Ctx &x, const Maps &maps) {
-    const PrefillArgs &a = x.a;
-    const int grp = a.Hv / a.Hk;
-    const uint32_t lead = tc::elect();
-    uint32_t count[3] = {0, 0, 0};                          // chunks of k, q and v started
-    bool ok = true;
-    const auto fetch = [&](int which, const CUtensorMap *map, int full, int free, int off, int ch, int row) {
-        const uint32_t n = count[which];
-        if (!x.wait_free<kPlaces>(free, n)) return false;
-        uint8_t *dst = x.smem + off + (n % kPlaces) * 2 * kTile;
-        if (lead) {
-            mbar_arrive_tx(&x.bars[full + n % kPlaces], 2 * kTile);
-            tma_load_2d(dst, map, ch, row, &x.bars[full + n % kPlaces]);
-            tma_load_2d(dst + kTile, map, ch + 64, row, &x.bars[full + n % kPlaces]);
-        }
-        __syncwarp();
-        count[which]++;
-        return true;
-    };
-    for (Items it(a); ok && it.next();) {
-        const int hk = it.h / grp;
-        if (it.item == a.stall.withhold_item) ok = false;   // test switch: these copies never start
-        for (int t0 = 0; ok && t0 < it.len; t0 += C) {
-            const int row = it.row + t0;
-            ok = fetch(0, &maps.k, kFullK, kFreeK, kOffK, hk * kD, row) &&
-                 (!OUT || fetch(1, &maps.q, kFullQ, kFreeQ, kOffQ, hk * kD, row)) &&
-                 fetch(2, &maps.v, kFullV, kFreeV, kOffV, it.h * kD, row);
-        }
-    }
-    // no copy is in flight when the CTA ends
-    const int full[3] = {kFullK, kFullQ, kFullV};
-#pragma unroll
-    for (int i = 0; i < 3; i++)
-        for (uint32_t m = count[i] < kPlaces ? 0 : count[i] - kPlaces; m < count[i]; m++)
-            ok = x.wait_full<kPlaces>(full[i], m) && ok;
-    return ok;
+__device__ __forceinline__ uint32_t chunks_of(const PrefillArgs &a) {
+    uint32_t n = 0;
+    for (Items it(a); it.next();) n += (uint32_t)(it.len + C - 1) / C;
+    return n;
+}
+// Descriptor of the two tiles of chunk n in one of the loaded operands' places.
+template <bool NORM>
+__device__ __forceinline__ uint64_t operand(const Ctx<NORM> &x, int off, uint32_t n, uint32_t lbo) {
+    return tc::sdesc_sw128(x.smem + off + (n % kPlaces) * 2 * kTile, lbo, 1024);
 }
 
-// Warp 16: the MMAs.
-template <bool OUT>
-__device__ __forceinline__ bool issue(const Ctx &x, uint32_t tm) {
-    const uint32_t lead = tc::elect();
-    uint32_t chunks = 0;
-    for (Items it(x.a); it.next();) chunks += (uint32_t)(it.len + C - 1) / C;
-    const auto at = [&](int off, uint32_t n) { return x.smem + off + (n % kPlaces) * 2 * kTile; };
-    const auto scores = [&](uint32_t n) {
-        if (!x.wait_full<kPlaces>(kFullQ, n) || !x.wait_full<kPlaces>(kFullK, n) || (n > 0 && !x.wait(kScoresFree, (n - 1) & 1u)))
-            return false;
-        tc::fence_after();
-        const uint64_t q = tc::sdesc_sw128(at(kOffQ, n), 16, 1024), k = tc::sdesc_sw128(at(kOffK, n), 16, 1024);
+// Warp 19: scores and PV. The scores of a chunk are formed ahead of its PV.
+template <bool NORM>
+__device__ __forceinline__ void issue_scores(const Ctx<NORM> &x, uint32_t tm) {
+    const uint32_t lead = tc::elect(), chunks = chunks_of(x.a);
+#pragma unroll 1
+    for (uint32_t n = 0; n <= chunks; n++) {
+        const uint32_t m = n - 1;
+        if (n > 0) x.template wait_full<kPlaces>(kPReady, m);       // the scores of chunk m have been read
+        if (n < chunks) {
+            x.template wait_full<kPlaces>(kFullK, n);
+            x.template wait_full<kPlaces>(kFullQ, n);
+            tc::fence_after();
+            const uint64_t q = operand(x, kOffQ, n, 16), k = operand(x, kOffK, n, 16);
+#pragma unroll 1
+            for (int i = 0; i < 2; i++)
 #pragma unroll
-        for (int s = 0; s < 8; s++) {
-            const uint64_t step = (s >> 2) * (kTile / 16) + (s & 3) * 2;
-            tc::mma_f16_ss(lead, tm + kColP, q + step, k + step, kIdescScores, s > 0);
+                for (int s = 0; s < 4; s++)
+                    tc::mma_f16_ss(lead, tm + kColP, q + i * (kTile / 16) + s * 2, k + i * (kTile / 16) + s * 2, kIdescScores,
+                                   i > 0 || s > 0);
+            tc::commit(lead, &x.bars[kScores]);
+            tc::commit(lead, &x.bars[kFreeK + n % kPlaces]);
+            tc::commit(lead, &x.bars[kFreeQ + n % kPlaces]);
         }
-        tc::commit(lead, &x.bars[kScores]);
-        tc::commit(lead, &x.bars[kFreeK + n % kPlaces]);
-        return true;
-    };
-    const uint64_t kp = tc::sdesc_sw128(x.smem + kOffKp, kTile, 1024), p = tc::sdesc_sw128(x.smem + kOffP, 16, 1024);
-    bool ok = true;
-    if (OUT && chunks > 0) ok = scores(0);
-    for (uint32_t n = 0; ok && n < chunks; n++) {
-        const uint32_t ph = n & 1u;
-        if (!(ok = x.wait(kKpReady, ph) && x.wait_full<kPlaces>(kFullV, n) && (n == 0 || x.wait(kUFree, ph ^ 1u)))) break;
+        if (n == 0) continue;
+        x.template wait_full<kPlaces>(kFullV, m);
+        x.wait_last(kYFree, m);
         tc::fence_after();
-        const uint64_t v = tc::sdesc_sw128(at(kOffV, n), kTile, 1024);
+        const uint64_t v = operand(x, kOffV, m, kTile), p = operand(x, kOffP, m, 16);
 #pragma unroll
-        for (int s = 0; s < 12; s++)                      // the smallest terms first
-            tc::mma_f16_ss(lead, tm + kColU, v + (s & 3) * 128, kp + (2 - s / 4) * (2 * kTile / 16) + (s & 3) * 128, kIdescKv,
-                           s > 0);
-        tc::commit(lead, &x.bars[kKv]);
-        if (!OUT) {
-            tc::commit(lead, &x.bars[kFreeV + n % kPlaces]);
-            continue;
-        }
-        if (!(ok = x.wait(kSReady, ph) && (n == 0 || x.wait(kYFree, ph ^ 1u)))) break;
-        tc::fence_after();
-        const uint64_t q = tc::sdesc_sw128(at(kOffQ, n), 16, 1024);
-#pragma unroll
-        for (int s = 0; s < 16; s++) {
-            const int e = s & 7;
-            tc::mma_f16_ts(lead, tm + kColY1, tm + (s < 8 ? kColSl : kColSh) + 8 * e, q + (e >> 2) * (kTile / 16) + (e & 3) * 2,
-                           kIdescQs, s > 0);
-        }
-        tc::commit(lead, &x.bars[kQs]);
-        tc::commit(lead, &x.bars[kFreeQ + n % kPlaces]);
-        if (n + 1 < chunks && !(ok = scores(n + 1))) break;
-        if (!(ok = x.wait(kPReady, ph))) break;
-        tc::fence_after();
-#pragma unroll
-        for (int s = 0; s < 8; s++)
-            tc::mma_f16_ss(lead, tm + kColY2, v + (s & 3) * 128, p + (s < 4 ? kTile / 16 : 0) + (s & 3) * 2, kIdescPv, s > 0);
+        for (int s = 0; s < 4; s++) tc::mma_f16_ss(lead, tm + kColY2, v + s * 128, p + s * 2, kIdescPv, s > 0);
         tc::commit(lead, &x.bars[kPv]);
-        tc::commit(lead, &x.bars[kFreeV + n % kPlaces]);
+        tc::commit(lead, &x.bars[kFreeV + m % kPlaces]);
     }
     // every MMA has ended before the tensor memory is given back
-    tc::commit(lead, &x.bars[kDrain]);
-    return x.wait(kDrain, 0) && ok;
+    tc::commit(lead, &x.bars[kDrainA]);
+    if (!mbar_wait(&x.bars[kDrainA], 0, x.a.stall.wait_cycles)) x.limit = 0;
 }
 
-// Warps 8-15, quadrants 2 and 3: K' = w_Cs k_s as three truncated bf16 terms. A warp takes
-// 32 tokens (lane = token) of one tile of 64 channels, so that 8 lanes' 16-byte pieces of a
-// swizzled tile lie in different banks. In a chunk with fewer tokens the rows past the last
-// belong to other sequences: zeros take their place here and in V.
-template <bool OUT>
-__device__ __forceinline__ bool scale_keys(const Ctx &x, int w) {
+// Warp 20: KV and QS.
+template <bool OUT, bool NORM>
+__device__ __forceinline__ void issue_state(const Ctx<NORM> &x, uint32_t tm) {
+    const uint32_t lead = tc::elect(), chunks = chunks_of(x.a);
+    const uint64_t kp = tc::sdesc_sw128(x.smem + kOffKp, kTile, 1024);
+#pragma unroll 1
+    for (uint32_t n = 0; n < chunks; n++) {
+        x.template wait_full<kPlaces>(kFullV, n);
+        x.wait_last(kUFree, n);
+        const uint64_t v = operand(x, kOffV, n, kTile);
+#pragma unroll 1
+        for (uint32_t h = 0; h < 2; h++) {                // the chunk's halves, so that one is scaled under the other
+            x.wait(kKpReady + h, n & 1u);
+            tc::fence_after();
+#pragma unroll 1
+            for (int i = 2; i >= 0; i--)                  // the smallest terms first
+#pragma unroll
+                for (int s = 0; s < 2; s++)
+                    tc::mma_f16_ss(lead, tm + kColU, v + (2 * h + s) * 128, kp + i * (2 * kTile / 16) + (2 * h + s) * 128, kIdescKv,
+                                   h > 0 || i < 2 || s > 0);
+            tc::commit(lead, &x.bars[kKpFree + h]);
+        }
+        tc::commit(lead, &x.bars[kKv]);
+        tc::commit(lead, &x.bars[kFreeV + n % kPlaces]);
+        if (!OUT) continue;
+        x.template wait_full<kPlaces>(kFullQ, n);
+        x.wait_last(kYFree, n);
+        x.wait(kSReady, n & 1u);
+        tc::fence_after();
+        const uint64_t q = operand(x, kOffQ, n, 16);
+#pragma unroll 1
+        for (int i = 0; i < 4; i++)                       // rest, head; each its two halves of K
+#pragma unroll
+            for (int s = 0; s < 4; s++)
+                tc::mma_f16_ts(lead, tm + kColY1, tm + (i < 2 ? kColSl : kColSh) + 32 * (i & 1) + 8 * s,
+                               q + (i & 1) * (kTile / 16) + s * 2, kIdescQs, i > 0 || s > 0);
+        tc::commit(lead, &x.bars[kQs]);
+        tc::commit(lead, &x.bars[kFreeQ + n % kPlaces]);
+    }
+    tc::commit(lead, &x.bars[kDrainB]);
+    if (!mbar_wait(&x.bars[kDrainB], 0, x.a.stall.wait_cycles)) x.limit = 0;
+}
+
+// Warps 22-27: K' = w_Cs k_s as three truncated bf16 terms. A unit is a 16-byte piece of 32
+// tokens (lane = token) of a tile, so that 8 lanes' pieces of the swizzled rows lie in
+// different banks. In a chunk with fewer tokens the rows past the last belong to other
+// sequences: zeros take their place here and in V.
+template <bool OUT, bool NORM>
+__device__ __forceinline__ void scale(const Ctx<NORM> &x, int w) {
     const PrefillArgs &a = x.a;
-    const int l = threadIdx.x & 31, s = 32 * (w & 1) + l, tile = w >> 1;       // w 0..3
+    const int l = threadIdx.x & 31;
     uint32_t n = 0;
     for (Items it(a); it.next();) {
+#pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const int m = it.len - t0;
-            if (!x.wait_full<kGateRing>(kFullG, n) || !x.wait_full<kPlaces>(kFullK, n)) return false;
-            const float f = x.gates(n).wk[s];
-            if (n > 0 && !x.wait(kKv, (n - 1) & 1u)) return false;
-            const uint8_t *k = x.smem + kOffK + ((n % kPlaces) * 2 + tile) * kTile + s * 128;
-            uint8_t *kp = x.smem + kOffKp + tile * kTile + s * 128;
-            const bool valid = s < m;
+            const int m = it.len - t0, place = (n % kPlaces) * 2 * kTile;
+            x.template wait_full<x.R>(kFullG, n);
+            x.template wait_full<kPlaces>(kFullK, n);
+            if (m < C) x.template wait_full<kPlaces>(kFullV, n);
+            const Gates &g = x.gates(n);
+#pragma unroll 1
+            for (int h = 0; h < 2; h++) {
+                x.wait_last(kKpFree + h, n);
+                const int s = 32 * h + l;
+                const uint64_t f = f2s(g.wk[s]);
+#pragma unroll 1
+                for (int u = (w + 4 * h) % kScaleWarps; u < 16; u += kScaleWarps) {
+                    uint8_t *at = x.smem + (u >> 3) * kTile + s * 128 + ((u & 7) ^ (l & 7)) * 16;
+                    uint4 r = *(const uint4 *)(at + kOffK + place);
+                    if (s >= m) {
+                        r = make_uint4(0, 0, 0, 0);
+                        *(uint4 *)(at + kOffV + place) = r;
+                    }
+                    const uint32_t in[4] = {r.x, r.y, r.z, r.w};
+                    uint32_t t[3][4];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int o = (i ^ (s & 7)) * 16;
-                const uint4 r = *(const uint4 *)(k + o);
-                const uint32_t in[4] = {r.x, r.y, r.z, r.w};
-                uint32_t t[3][4];
+                    for (int e = 0; e < 4; e++) {
+                        uint64_t p = fmul2(u2pair(in[e] << 16, in[e] & 0xFFFF0000u), f);
+                        t[0][e] = heads(p);
+                        p = rests(p);
+                        t[1][e] = heads(p);
+                        t[2][e] = heads(rests(p));
+                    }
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    float lo = valid ? __uint_as_float(in[e] << 16) * f : 0.f;
-                    float hi = valid ? __uint_as_float(in[e] & 0xFFFF0000u) * f : 0.f;
-                    t[0][e] = high_halves(lo, hi);
-                    lo -= head_of(lo);
-                    hi -= head_of(hi);
-                    t[1][e] = high_halves(lo, hi);
-                    lo -= head_of(lo);
-                    hi -= head_of(hi);
-                    t[2][e] = high_halves(lo, hi);
+                    for (int i = 0; i < 3; i++)
+                        *(uint4 *)(at + kOffKp + i * 2 * kTile) = make_uint4(t[i][0], t[i][1], t[i][2], t[i][3]);
                 }
-#pragma unroll
-                for (int u = 0; u < 3; u++) *(uint4 *)(kp + u * 2 * kTile + o) = make_uint4(t[u][0], t[u][1], t[u][2], t[u][3]);
+                fence_async_smem();
+                x.arrive(kKpReady + h);
             }
-            if (m < C) {
-                if (!x.wait_full<kPlaces>(kFullV, n)) return false;
-                if (!valid)
-#pragma unroll
-                    for (int i = 0; i < 8; i++)
-                        *(uint4 *)(x.smem + kOffV + ((n % kPlaces) * 2 + tile) * kTile + s * 128 + i * 16) = make_uint4(0, 0, 0, 0);
-            }
-            fence_async_smem();
-            x.arrive(kKpReady);
             x.arrive(kFreeK + n % kPlaces);
+            x.arrive(kFreeG + n % x.R);
         }
     }
-    return true;
 }
 
-// Warps 8-15, quadrants 0 and 1: P of tokens t = 32 quad + lane over keys 32 half .. + 31, for
-// the three of the four blocks that are not all zero. Diagonal blocks: w_ts by a running
-// product down the row; the block below them: the product of its two parts.
-__device__ __forceinline__ bool weigh_scores(const Ctx &x, uint32_t tm, int quad, int half) {
+// Warps 16, 17, 21: P of tokens t = 32 quad + lane over keys 32 half .. + 31, 16 keys at a time;
+// the block above the diagonal stays zero. Diagonal blocks: w_ts by a running product down
+// the row (zero above the diagonal); the block below them: the product of its two parts.
+template <bool NORM>
+__device__ __forceinline__ void weigh_scores(const Ctx<NORM> &x, uint32_t tm, int quad, int half) {
     const int l = threadIdx.x & 31, t = 32 * quad + l;
-    const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + kColP + 32 * half;
-    uint8_t *row = x.smem + kOffP + t * 128;
+    const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + kColP;
     uint32_t n = 0;
     for (Items it(x.a); it.next();) {
+#pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const uint32_t ph = n & 1u;
-            if (!x.wait_full<kGateRing>(kFullG, n)) return false;
-            const Gates &g = x.gates(n);
-            const float pre = g.pre[l];
-            if (!x.wait(kScores, ph)) return false;
+            x.template wait_full<x.R>(kFullG, n);
+            x.template wait_free<kPlaces>(kFreeV, n);       // PV of two chunks ago has read the place
+            x.wait(kScores, n & 1u);
             tc::fence_after();
-            float p[32], w = 0.f;
-            {
-                float u[16];
-                tc::ld16(tl, u);
+            const Gates &g = x.gates(n);
+            uint8_t *row = x.smem + kOffP + (n % kPlaces) * 2 * kTile + t * 128;
+            const uint64_t pre = f2s(g.pre[l]);
+            const int m = it.len - t0;                      // keys past the last: other sequences' rows
+            float w = 0.f;
+#pragma unroll 1
+            for (int b = 2 * half + 1; b >= 2 * half; b--) { // keys 16 b .. + 15
+                uint32_t u[16];
+                tc::ld16_start(tl + 16 * b, u);
+                tc::wait_ld(u);
+                uint64_t f[8];                              // the weights
+                if (half < quad) {
 #pragma unroll
-                for (int e = 0; e < 16; e++) p[e] = u[e];
-                tc::ld16(tl + 16, u);
+                    for (int i = 0; i < 8; i++) f[i] = fmul2(pair_at(&g.suf[16 * b + 2 * i]), pre);
+                } else {
+                    const int d = t - 16 * b;
+                    const float4 *nx = (const float4 *)&g.next[16 * b];
 #pragma unroll
-                for (int e = 0; e < 16; e++) p[16 + e] = u[e];
+                    for (int i = 7; i >= 0; i -= 2) {
+                        const float4 v = nx[i >> 1];
+                        const float w3 = d == 2 * i + 1 ? 1.f : w * v.w, w2 = d == 2 * i ? 1.f : w3 * v.z;
+                        const float w1 = d == 2 * i - 1 ? 1.f : w2 * v.y;
+                        w = d == 2 * i - 2 ? 1.f : w1 * v.x;
+                        f[i] = f2(w2, w3);
+                        f[i - 1] = f2(w, w1);
+                    }
+                }
+                if (m < 16 * b + 16)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) u[i] = 16 * b + i < m ? u[i] : 0u;
+                uint32_t h[8], r[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint64_t p = fmul2(u2pair(u[2 * i], u[2 * i + 1]), f[i]);
+                    h[i] = heads(p);
+                    r[i] = rounded(rests(p));
+                }
+                const int o0 = ((2 * b) ^ (t & 7)) * 16, o1 = ((2 * b + 1) ^ (t & 7)) * 16;
+                *(uint4 *)(row + o0) = make_uint4(h[0], h[1], h[2], h[3]);
+                *(uint4 *)(row + o1) = make_uint4(h[4], h[5], h[6], h[7]);
+                *(uint4 *)(row + kTile + o0) = make_uint4(r[0], r[1], r[2], r[3]);
+                *(uint4 *)(row + kTile + o1) = make_uint4(r[4], r[5], r[6], r[7]);
             }
             tc::fence_before();
-            x.arrive(kScoresFree);
-            if (quad != half) {
-#pragma unroll
-                for (int e = 0; e < 32; e++) p[e] *= g.suf[e] * pre;
-            } else {
-#pragma unroll
-                for (int e = 31; e >= 0; e--) {
-                    w = l == e ? 1.f : w * g.g[32 * half + (e + 1 & 31)];
-                    p[e] = l >= e ? p[e] * w : 0.f;
-                }
-            }
-            if (n > 0 && !x.wait(kPv, ph ^ 1u)) return false;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                uint32_t h[4], r[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) split2(p[8 * i + 2 * e], p[8 * i + 2 * e + 1], h[e], r[e]);
-                const int o = ((4 * half + i) ^ (t & 7)) * 16;
-                *(uint4 *)(row + o) = make_uint4(h[0], h[1], h[2], h[3]);
-                *(uint4 *)(row + kTile + o) = make_uint4(r[0], r[1], r[2], r[3]);
-            }
             fence_async_smem();
-            x.arrive(kPReady);
+            x.arrive(kPReady + n % kPlaces);
+            x.arrive(kFreeG + n % x.R);
         }
     }
-    return true;
 }
 
-// Barrier over the 256 threads of warps 0-7; returns the OR of their predicates.
-__device__ __forceinline__ bool chain_any(bool p) {
-    uint32_t r;
-    asm volatile(
-        "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 1, 256, p; selp.u32 %0, 1, 0, q; }"
-        : "=r"(r)
-        : "r"((uint32_t)p)
-        : "memory");
-    return r != 0;
-}
-
-// Warps 0-7: the state and the outputs. This thread: value channel j, key channels
-// 64 half .. + 63 of the state, tokens 32 half .. + 31 of the outputs.
+// Warps 0-7: the state. This thread: value channel j, key channels 64 half .. + 63, in pairs.
 template <bool OUT, bool NORM>
-__device__ __forceinline__ bool chain(const Ctx &x, uint32_t tm) {
+__device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
     const PrefillArgs &a = x.a;
     const int w = threadIdx.x >> 5, l = threadIdx.x & 31, quad = w & 3, half = w >> 2, j = 32 * quad + l;
     const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16);
-    float *ys = (float *)(x.smem + kOffY);
     uint32_t n = 0;
-    float s[64];
-    const auto publish = [&]() {                            // S^T's head and rest as an operand
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            uint32_t h[8], r[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) split2(s[16 * i + 2 * e], s[16 * i + 2 * e + 1], h[e], r[e]);
-            tc::st8(tl + kColSh + 32 * half + 8 * i, h);
-            tc::st8(tl + kColSl + 32 * half + 8 * i, r);
-        }
-        tc::wait_st();
-        tc::fence_before();
-        x.arrive(kSReady);
-    };
-    // A wait ran out: the other warps meet this one at the chunk's next barrier.
-    const auto give_up = [&]() {
-        if (NORM) chain_any(true);
-        return false;
-    };
+    uint64_t s[32];
     for (Items it(a); it.next();) {
         const float *in = it.state_in();
 #pragma unroll
-        for (int e = 0; e < 64; e++) s[e] = in ? in[(64 * half + e) * kD + j] : 0.f;
-        if (OUT) publish();
+        for (int e = 0; e < 32; e++)
+            s[e] = in ? f2(in[(64 * half + 2 * e) * kD + j], in[(64 * half + 2 * e + 1) * kD + j]) : 0;
         float total = 1.f;                                  // the segment's decay
+#pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const uint32_t ph = n & 1u;
-            const bool last = t0 + C >= it.len;
-            if (!x.wait_full<kGateRing>(kFullG, n) || !x.wait(kKv, ph)) return give_up();
+            if (OUT) {                                      // S^T's head and rest as an operand
+                x.wait_last(kQs, n);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    uint32_t h[8], r[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        h[e] = heads(s[8 * i + e]);
+                        r[e] = rounded(rests(s[8 * i + e]));
+                    }
+                    tc::st8(tl + kColSh + 32 * half + 8 * i, h);
+                    tc::st8(tl + kColSl + 32 * half + 8 * i, r);
+                }
+                tc::wait_st();
+                tc::fence_before();
+                x.arrive(kSReady);
+            }
+            x.template wait_full<x.R>(kFullG, n);
+            x.wait(kKv, n & 1u);
             tc::fence_after();
-            const Gates &g = x.gates(n);
-            const float gc = g.total;
+            const float gc = x.gates(n).total;
+            const uint64_t g2 = f2s(gc);
             total *= gc;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                float u[16];
-                tc::ld16(tl + kColU + 64 * half + 16 * i, u);
+            for (int i = 0; i < 2; i++) {
+                uint64_t u[16];
+                tc::ld32_pairs(tl + kColU + 64 * half + 32 * i, u);
 #pragma unroll
-                for (int e = 0; e < 16; e++) s[16 * i + e] = fmaf(gc, s[16 * i + e], u[e]);
+                for (int e = 0; e < 16; e++) s[16 * i + e] = ffma2(g2, s[16 * i + e], u[e]);
             }
             tc::fence_before();
             x.arrive(kUFree);
-            if (!OUT) {
-                x.arrive(kFreeG + n % kGateRing);
-                continue;
-            }
-            if (!x.wait(kQs, ph)) return give_up();
-            tc::fence_after();
-            if (!last) publish();
-            if (!x.wait(kPv, ph)) return give_up();
-            tc::fence_after();
-            const int64_t row = (int64_t)it.row + t0;
-            const int m = min(C, it.len - t0);
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int c0 = 32 * half + 16 * i;
-                float y1[16], y2[16];
-                tc::ld16(tl + kColY1 + c0, y1);
-                tc::ld16(tl + kColY2 + c0, y2);
-                bf16 *y = (bf16 *)a.y + (row + c0) * a.ys + it.h * kD + j;
-#pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const float r = fmaf(g.c[c0 + e], y1[e], y2[e]);
-                    if (NORM) ys[(c0 + e) * kYRow + j] = r;
-                    else if (c0 + e < m) y[e * a.ys] = __float2bfloat16_rn(r);
-                }
-            }
-            tc::fence_before();
-            x.arrive(kYFree);
-            x.arrive(kFreeG + n % kGateRing);
-            if (NORM) {
-                if (chain_any(false)) return false;
-                for (int t = w; t < m; t += 8) {
-                    const float4 r = *(const float4 *)&ys[t * kYRow + 4 * l];
-                    float y[4] = {r.x, r.y, r.z, r.w};
-                    norm_head<bf16, 4>(a.norm, it.h, row + t, l, y);
-                    store_vec<bf16, 4>((bf16 *)a.y + (row + t) * a.ys + it.h * kD + 4 * l, y);
-                }
-                chain_any(false);
-            }
+            x.arrive(kFreeG + n % x.R);
         }
         float *out = it.state_out();
         if (out)
 #pragma unroll
-            for (int e = 0; e < 64; e++) out[(64 * half + e) * kD + j] = s[e];
+            for (int e = 0; e < 32; e++) {
+                out[(64 * half + 2 * e) * kD + j] = f2lo(s[e]);
+                out[(64 * half + 2 * e + 1) * kD + j] = f2hi(s[e]);
+            }
         if (!OUT && threadIdx.x == 0) *it.total_out() = total;
     }
-    return true;
+}
+
+// Barrier over the 256 threads of warps 8-15.
+__device__ __forceinline__ void out_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
+
+// Warps 8-15: the outputs. This thread: value channel j of tokens 32 half .. + 31; through
+// shared memory a token's 128 channels come together, to leave in 16-byte pieces or to be
+// normalised by a warp.
+template <bool NORM>
+__device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
+    const PrefillArgs &a = x.a;
+    const int w = (threadIdx.x >> 5) - 8, l = threadIdx.x & 31, quad = w & 3, half = w >> 2, j = 32 * quad + l;
+    const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + 32 * half;
+    float *yf = (float *)(x.smem + kOffY) + 32 * half * kD + j;
+    uint16_t *yb = (uint16_t *)(x.smem + kOffY) + 32 * half * kD + j;
+    uint32_t n = 0;
+    for (Items it(a); it.next();) {
+        bf16 *y = (bf16 *)a.y + (int64_t)it.row * a.ys + it.h * kD;
+        const bf16 *z = (const bf16 *)a.norm.z + (int64_t)it.row * a.norm.z_stride + it.h * kD;
+#pragma unroll 1
+        for (int t0 = 0; t0 < it.len; t0 += C, n++) {
+            const int m = min(C, it.len - t0);
+            if (NORM && a.norm.z) {                         // on its way before it is needed
+                const int t = w + 8 * (l >> 1);
+                if (l < 16 && t < m) asm volatile("prefetch.global.L1 [%0];" ::"l"(z + t * a.norm.z_stride + 64 * (l & 1)));
+            }
+            x.template wait_full<x.R>(kFullG, n);
+            x.wait(kPv, n & 1u);
+            x.wait(kQs, n & 1u);
+            out_sync();                                     // the chunk before's readouts have left the place
+            tc::fence_after();
+            const float *c = x.gates(n).c + 32 * half;
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 8) {
+                uint32_t y1[8], y2[8], y3[8];
+                tc::ld8_start(tl + kColY1 + i, y1);
+                tc::ld8_start(tl + kColY2 + i, y2);
+                tc::ld8_start(tl + kColY2 + C + i, y3);
+                tc::wait_ld(y1);
+                tc::wait_ld(y2);
+                tc::wait_ld(y3);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint64_t v = ffma2(pair_at(&c[i + e]), u2pair(y1[e], y1[e + 1]),
+                                             fadd2(u2pair(y2[e], y2[e + 1]), u2pair(y3[e], y3[e + 1])));
+                    if (NORM) {
+                        yf[(i + e) * kD] = f2lo(v);
+                        yf[(i + e + 1) * kD] = f2hi(v);
+                    } else {
+                        const uint32_t b = rounded(v);
+                        yb[(i + e) * kD] = (uint16_t)b;
+                        yb[(i + e + 1) * kD] = (uint16_t)(b >> 16);
+                    }
+                }
+            }
+            tc::fence_before();
+            x.arrive(kYFree);
+            x.arrive(kFreeG + n % x.R);
+            out_sync();
+            if (NORM) {
+                constexpr int N = 2;                        // tokens w, w + 8 of 16 at a time
+                const float *ys = (const float *)(x.smem + kOffY) + 4 * l;
+                const HeadAffine p(a.norm, it.h, l);
+#pragma unroll 1
+                for (int b = w; b < m; b += 8 * N) {
+                    float v[N][4];
+#pragma unroll
+                    for (int i = 0; i < N; i++) {
+                        const float4 u = *(const float4 *)&ys[(b + 8 * i) * kD];
+                        v[i][0] = u.x;
+                        v[i][1] = u.y;
+                        v[i][2] = u.z;
+                        v[i][3] = u.w;
+                    }
+                    norm_head<bf16, N>(a.norm, p, [&](int i) { return z + min(b + 8 * i, m - 1) * a.norm.z_stride + 4 * l; }, v);
+#pragma unroll
+                    for (int i = 0; i < N; i++)
+                        if (b + 8 * i < m) store_vec<bf16, 4>(y + (b + 8 * i) * a.ys + 4 * l, v[i]);
+                }
+                z += C * a.norm.z_stride;
+            } else {
+                const int t1 = 2 * w + (l >> 4);
+                const bf16 *ys = (const bf16 *)(x.smem + kOffY) + 8 * (l & 15);
+                bf16 *yt = y + t1 * a.ys + 8 * (l & 15);
+#pragma unroll
+                for (int t = 0; t < C; t += 16, yt += 16 * a.ys)
+                    if (t1 + t < m) *(uint4 *)yt = *(const uint4 *)(ys + (t1 + t) * kD);
+            }
+            y += C * a.ys;
+        }
+    }
 }
 
 template <bool OUT, bool NORM>
 __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a, const __grid_constant__ Maps maps) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint64_t *bars = (uint64_t *)(smem + kOffBar);
-    uint32_t *tbase = (uint32_t *)(smem + kOffTmem);
+    uint64_t *bars = (uint64_t *)(smem + kOffBar<NORM>);
+    uint32_t *tbase = (uint32_t *)(smem + kOffTmem<NORM>);
     const int tid = threadIdx.x, w = __shfl_sync(0xffffffffu, tid >> 5, 0);
     if (w == 0) {
         tc::tmem_alloc(tbase, kCols);
         tc::tmem_relinquish();
     }
-    if (tid == 0) {
-        for (int i = 0; i < kPlaces; i++) {
-            mbar_init(&bars[kFullQ + i], 1);
-            mbar_init(&bars[kFullK + i], 1);
-            mbar_init(&bars[kFullV + i], 1);
-            mbar_init(&bars[kFreeQ + i], 1);
-            mbar_init(&bars[kFreeK + i], OUT ? 5 : 4);      // the scores, four warps of K'
-            mbar_init(&bars[kFreeV + i], 1);
-        }
-        for (int i = 0; i < kGateRing; i++) {
-            mbar_init(&bars[kFullG + i], 1);
-            mbar_init(&bars[kFreeG + i], 8);
-        }
-        mbar_init(&bars[kScores], 1);
-        mbar_init(&bars[kScoresFree], 3);
-        mbar_init(&bars[kPReady], 3);
-        mbar_init(&bars[kKpReady], 4);
-        mbar_init(&bars[kSReady], 8);
-        mbar_init(&bars[kUFree], 8);
-        mbar_init(&bars[kYFree], 8);
-        mbar_init(&bars[kQs], 1);
-        mbar_init(&bars[kKv], 1);
-        mbar_init(&bars[kPv], 1);
-        mbar_init(&bars[kDrain], 1);
+    if (tid < kBars) {
+        int count = 1;                                      // TMA, the end of MMAs, the decays
+        if (tid >= kFreeK && tid < kFreeQ) count = kScaleWarps + (OUT ? 1 : 0);            // K', the scores
+        if (tid >= kFreeQ && tid < kPReady) count = OUT ? 2 : 1;                           // scores, QS; KV, PV
+        if (tid >= kPReady && tid < kKpReady) count = 3;
+        if (tid >= kFreeG && tid < kScores) count = 8 + kScaleWarps + (OUT ? 11 : 0);      // state, K', P, outputs
+        if (tid >= kKpReady && tid < kKpFree) count = kScaleWarps;
+        if (tid >= kSReady && tid <= kYFree) count = 8;
+        mbar_init(&bars[tid], count);
         mbar_init_fence();
     }
     if (OUT && w >= 8 && w < 10) {                          // P's block above the diagonal stays zero
-        for (int i = tid - 256; i < 2 * 32 * 4; i += 64) {
+        for (int i = tid - 256; i < kPlaces * 2 * 32 * 4; i += 64) {
             const int t = (i >> 2) & 31, o = ((4 + (i & 3)) ^ (t & 7)) * 16;
             *(uint4 *)(smem + kOffP + (i >> 7) * kTile + t * 128 + o) = make_uint4(0, 0, 0, 0);
         }
@@ -527,23 +597,24 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
     griddep_wait();
     griddep_launch();
     const uint32_t tm = *tbase;
-    const Ctx x{a, smem, bars};
-    bool ok = true;
+    const Ctx<NORM> x{a, smem, bars, (uint32_t)min(a.stall.wait_cycles, 0xFFFFFFF0ll)};
     if (w < 8) {
-        tc::regs_inc<kRegsChain>();
-        ok = chain<OUT, NORM>(x, tm);
+        tc::regs_inc<kRegsState>();
+        states<OUT>(x, tm);
     } else if (w < 16) {
-        tc::regs_dec<kRegsOperand>();
-        const int quad = w & 3, half = (w - 8) >> 2;
-        if (quad >= 2) ok = scale_keys<OUT>(x, 2 * half + quad - 2);
-        else if (OUT && quad >= half) ok = weigh_scores(x, tm, quad, half);
+        tc::regs_dec<kRegsOut>();
+        if (OUT) outputs(x, tm);
     } else {
-        tc::regs_dec<kRegsIssue>();
-        if (w == 16) ok = issue<OUT>(x, tm);
-        else if (w == 17) ok = load<OUT>(x, maps);
-        else if (w == 18) ok = decays(x);
+        tc::regs_dec<kRegsOperand>();
+        if (w == 18) load<OUT>(x, maps);
+        else if (w == 20) issue_state<OUT>(x, tm);
+        else if (w >= 22) scale<OUT>(x, w - 22);
+        else if (OUT) {
+            if (w == 19) issue_scores(x, tm);
+            else weigh_scores(x, tm, w & 3, w == 17);
+        }
     }
-    if (!ok) raise_error(a.err, STEPQ_ERR_TIMEOUT);
+    if (x.limit == 0) raise_error(a.err, STEPQ_ERR_TIMEOUT);
     __syncwarp();
     tc::fence_before();
     __syncthreads();
@@ -583,7 +654,7 @@ template <bool OUT, bool NORM>
 static stepq_status launch(const PrefillArgs &a, const Maps &maps, int items, cudaStream_t s) {
     const auto kernel = linattn_chunks_kernel<OUT, NORM>;
     static SmemOptIn opt;
-    const stepq_status st = opt((const void *)kernel, kSmem);
+    const stepq_status st = opt((const void *)kernel, kSmem<NORM>);
     if (st != STEPQ_OK) return st;
     // the register shares are taken from what the kernel is launched with
     static std::atomic<int> regs{0};
@@ -595,7 +666,7 @@ static stepq_status launch(const PrefillArgs &a, const Maps &maps, int items, cu
     }
     if (regs.load(std::memory_order_relaxed) < kRegs) return STEPQ_ERR_CUDA;
     const int grid = sm_count();
-    return launch_overlapped(kernel, grid < items ? grid : items, kBlock, kSmem, s, a, maps);
+    return launch_overlapped(kernel, grid < items ? grid : items, kBlock, kSmem<NORM>, s, a, maps);
 }
 
 }  // namespace ch
@@ -612,8 +683,8 @@ bool linattn_chunks_takes(const stepq_config *cfg, const stepq_linattn_io *io) {
 stepq_status launch_linattn_chunks(const PrefillArgs &a, int items, bool out, cudaStream_t s) {
     const ch::Encode f = ch::encoder();
     ch::Maps maps;
-    if (!f || !ch::encode(f, &maps.q, a.q, kD * a.Hk, a.tokens, a.qs) || !ch::encode(f, &maps.k, a.k, kD * a.Hk, a.tokens, a.ks) ||
-        !ch::encode(f, &maps.v, a.v, kD * a.Hv, a.tokens, a.vs))
+    if (!f || !ch::encode(f, &maps.of[0], a.k, kD * a.Hk, a.tokens, a.ks) ||
+        !ch::encode(f, &maps.of[1], a.q, kD * a.Hk, a.tokens, a.qs) || !ch::encode(f, &maps.of[2], a.v, kD * a.Hv, a.tokens, a.vs))
         return STEPQ_ERR_CUDA;
     if (!out) return ch::launch<false, false>(a, maps, items, s);
     return a.norm.on ? ch::launch<true, true>(a, maps, items, s) : ch::launch<true, false>(a, maps, items, s);

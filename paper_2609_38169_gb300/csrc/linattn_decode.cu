@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads) linattn_decode_kernel(DecodeArgs a) 
     float v[4];
     load_vec<T, 4>((const T *)a.v + b * a.vs + h * kD + 4 * l, v);
     __syncthreads();
-    float y[4] = {};
+    float y[1][4] = {};
 #pragma unroll
     for (int p = 0; p < 16; p++) {
         const int i = 8 * p + w;
@@ -61,24 +61,26 @@ __global__ void __launch_bounds__(kThreads) linattn_decode_kernel(DecodeArgs a) 
         s[p] = make_float4(fmaf(ki, v[0], g * s[p].x), fmaf(ki, v[1], g * s[p].y), fmaf(ki, v[2], g * s[p].z),
                            fmaf(ki, v[3], g * s[p].w));
         S[i * 32 + l] = s[p];
-        y[0] = fmaf(qi, s[p].x, y[0]);
-        y[1] = fmaf(qi, s[p].y, y[1]);
-        y[2] = fmaf(qi, s[p].z, y[2]);
-        y[3] = fmaf(qi, s[p].w, y[3]);
+        y[0][0] = fmaf(qi, s[p].x, y[0][0]);
+        y[0][1] = fmaf(qi, s[p].y, y[0][1]);
+        y[0][2] = fmaf(qi, s[p].z, y[0][2]);
+        y[0][3] = fmaf(qi, s[p].w, y[0][3]);
     }
-    *(float4 *)&red[w][4 * l] = make_float4(y[0], y[1], y[2], y[3]);
+    *(float4 *)&red[w][4 * l] = make_float4(y[0][0], y[0][1], y[0][2], y[0][3]);
     __syncthreads();
     if (w > 0) return;
 #pragma unroll
     for (int o = 1; o < 8; o++) {
         const float4 r = *(const float4 *)&red[o][4 * l];
-        y[0] += r.x;
-        y[1] += r.y;
-        y[2] += r.z;
-        y[3] += r.w;
+        y[0][0] += r.x;
+        y[0][1] += r.y;
+        y[0][2] += r.z;
+        y[0][3] += r.w;
     }
-    if (a.norm.on) norm_head<T, 4>(a.norm, h, b, l, y);
-    store_vec<T, 4>((T *)a.y + b * a.ys + h * kD + 4 * l, y);
+    if (a.norm.on)
+        norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l),
+                        [&](int) { return (const T *)a.norm.z + b * a.norm.z_stride + h * kD + 4 * l; }, y);
+    store_vec<T, 4>((T *)a.y + b * a.ys + h * kD + 4 * l, y[0]);
 }
 
 }  // namespace la

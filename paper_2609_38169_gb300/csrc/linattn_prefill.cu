@@ -56,9 +56,11 @@ __global__ void __launch_bounds__(kD) linattn_prefill_tokens_kernel(PrefillArgs 
         __syncthreads();
         for (int t = w; t < n; t += 4) {
             const float4 r = *(const float4 *)&vy[t][4 * l];
-            float y[4] = {r.x, r.y, r.z, r.w};
-            if (a.norm.on) norm_head<T, 4>(a.norm, h, row + t, l, y);
-            store_vec<T, 4>((T *)a.y + (row + t) * a.ys + h * kD + 4 * l, y);
+            float y[1][4] = {{r.x, r.y, r.z, r.w}};
+            if (a.norm.on)
+                norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l),
+                                [&](int) { return (const T *)a.norm.z + (row + t) * a.norm.z_stride + h * kD + 4 * l; }, y);
+            store_vec<T, 4>((T *)a.y + (row + t) * a.ys + h * kD + 4 * l, y[0]);
         }
         __syncthreads();
     }

@@ -51,11 +51,13 @@ struct Items {
     const PrefillArgs &a;
     int item, h, row, len;
     __device__ __forceinline__ explicit Items(const PrefillArgs &args) : a(args), item((int)blockIdx.x - (int)gridDim.x) {}
-    __device__ __forceinline__ bool next() {
+    // lead: the thread that raises what is wrong with a sequence (one of a CTA's warps)
+    __device__ __forceinline__ bool next(bool lead = false) {
+#pragma unroll 1
         for (item += gridDim.x; item < a.items; item += gridDim.x) {
             b = item / a.Hv;
             h = item - b * a.Hv;
-            if (sequence(a, b, threadIdx.x == 0, row, len, slot) && len > 0) return true;
+            if (sequence(a, b, lead, row, len, slot) && len > 0) return true;
         }
         return false;
     }

@@ -83,14 +83,13 @@ struct HeadAffine {
     }
 };
 
-// One head's readouts of N tokens in a warp, lane l holding channels 4 l .. 4 l + 3: their
-// sums cross the warp together. z(i) is lane l's place in token i's row of the gate.
-template <class T, int N, class Z>
-__device__ __forceinline__ void norm_head(const NormArgs &n, const HeadAffine &p, Z &&z, float (&y)[N][4]) {
-    float g[N][4], s[N], m[N];
+// One head's readouts of N tokens in a warp, lane l holding channels 4 l .. 4 l + 3 (z: of the
+// gate, if there is one): their sums cross the warp together.
+template <class T, int N>
+__device__ __forceinline__ void norm_head(const NormArgs &n, const HeadAffine &p, const Vec<T, 4> *z, float (&y)[N][4]) {
+    float s[N], m[N];
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        if (n.z) load_vec<T, 4>(z(i), g[i]);
         m[i] = 0.f;
         s[i] = (y[i][0] + y[i][1]) + (y[i][2] + y[i][3]);
     }
@@ -119,7 +118,7 @@ __device__ __forceinline__ void norm_head(const NormArgs &n, const HeadAffine &p
     for (int i = 0; i < N; i++) {
         const float r = rstd_of(s[i] * (1.f / kD), n.eps);
 #pragma unroll
-        for (int e = 0; e < 4; e++) y[i][e] = norm_out<T>(n, y[i][e], r, p.w[e], p.b[e], g[i][e]);
+        for (int e = 0; e < 4; e++) y[i][e] = norm_out<T>(n, y[i][e], r, p.w[e], p.b[e], to_f32(z[i].e[e]));
     }
 }
 

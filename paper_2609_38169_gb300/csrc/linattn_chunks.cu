@@ -9,9 +9,12 @@
 // Four products a chunk, all with M = 128 (lane = value channel, or token):
 //   scores  Q K^T            A = Q, B = K in smem         N = 64, K = 128   (rows 64.. unused)
 //   QS      S_0^T Q^T        A = S^T in tmem, B = Q       N = 64, K = 128   x 2 (head, rest of S)
-//   PV      V^T P^T          A = V^T, B = P in smem       N = 128, K = 64   (head and rest of P side by side)
-//   KV      V^T K'           A = V^T, B = K' in smem      N = 128, K = 64   x 3
-// q, k and v are bf16 and enter as they are, from where TMA put them. What is fp32 enters as
+//   PV      V^T P^T          A = V^T in tmem, B = P       N = 64, K = 64    x 2 (head, rest of P)
+//   KV      V^T K'           A = V^T in tmem, B = K'      N = 128, K = 64   x 3
+// Shared-memory bandwidth is what they and the warps compete for (128 bytes a cycle: with V
+// read from there by PV and KV and the readouts passing through it, its use added up to the
+// chunk's whole time, 4100 cycles), so V is transposed once into tensor memory.
+// q, k and v are bf16 and enter as they are. What is fp32 enters as
 // a sum of bf16: K' as three truncated terms, exactly, since states are kept in fp32; S and P
 // as a truncated head and a rounded rest (2^-17 of each value; the result is rounded to
 // 2^-9). The state itself stays in fp32 registers and U is formed apart from it, so what is
@@ -20,15 +23,13 @@
 // One persistent CTA of 28 warps per SM:
 //   warps 0-7    the state: S <- c_C S + U, its split into tensor memory (lane = value channel,
 //                warps w and w + 4 sharing lanes 32 (w % 4) ..)
-//   warps 8-15   the outputs (lanes likewise)
-//   warps 16, 17, 21   P (lanes = tokens), a 32 x 32 block each
-//   warp 18      loads q, k and v (TMA, two places each); decays and their products
-//   warps 19, 20 issue the MMAs: scores and PV; KV and QS
-//   warps 22-27  K'
+//   warps 8-15   V^T, and the outputs (lanes likewise)
+//   3 warps      P (lanes = tokens), a 32 x 32 block each
+//   1 warp       loads q, k and v (TMA, two places each); decays and their products
+//   2 warps      issue the MMAs: scores and PV; KV and QS
+//   6 warps      K'
 // Hand-over by mbarriers, every wait bounded. Loops keep few unrolled steps: unrolled, the
 // warps' code did not fit the instruction caches (a third of the stalls of issuing warps).
-#include <cuda.h>
-
 #include "async.cuh"
 #include "device.cuh"
 #include "linattn_prefill.cuh"
@@ -41,42 +42,48 @@ namespace ch {
 constexpr int C = kChunk;
 constexpr int kPlaces = 2;                              // of q, k, v and P
 constexpr int kBlock = 28 * 32;                         // registers are shared out by warpgroups
+constexpr int kOutWarps = 8, kFirst = 8 + kOutWarps;    // P, P, loads, MMAs, MMAs, P, then K'
+constexpr int kScaleWarps = 28 - kFirst - 6;
 constexpr int kRegs = 72, kRegsState = 112, kRegsOut = 64, kRegsOperand = 48;
 static_assert(256 * (kRegsState + kRegsOut) + 384 * kRegsOperand <= kBlock * kRegs, "register shares");
-constexpr int kScaleWarps = 6;
-constexpr uint32_t kColU = 0, kColSh = 128, kColSl = 192, kColP = 256, kColY1 = 320, kColY2 = 384, kCols = 512;
+constexpr uint32_t kColU = 0, kColSh = 128, kColSl = 192, kColP = 256, kColY1 = 320, kColY2 = 384, kColV = 448,
+                   kCols = 512;                         // V^T: two places of 32
 
 constexpr int kTile = C * 128;                          // 64 rows of 128 bytes: 64 channels of a chunk
 constexpr int kOffK = 0, kOffQ = kOffK + kPlaces * 2 * kTile, kOffV = kOffQ + kPlaces * 2 * kTile;   // [place][2 tiles]
 constexpr int kOffKp = kOffV + kPlaces * 2 * kTile;     // K': [term][2 tiles]
 constexpr int kOffP = kOffKp + 3 * 2 * kTile;           // P: [place][head, rest]
-constexpr int kOffY = kOffP + kPlaces * 2 * kTile;      // [C][128] readouts: bf16, or float to normalise
+constexpr int kOffY = kOffP + kPlaces * 2 * kTile;      // float [C][128] readouts to normalise
 struct alignas(16) Gates {
     float next[C], c[C], wk[C];                         // g_{t+1}, c_t, w_Cs (0 past the last token)
     float suf[32], pre[32];                             // w_{31,s} of the first half, c_t / c_31 of the second
     float total, pad[3];                                // c_C
 };
-// Two places for the decays where the readouts take twice the room.
-template <bool NORM> constexpr int kRing = NORM ? 2 : 4;
-template <bool NORM> constexpr int kOffG = kOffY + C * kD * (NORM ? 4 : 2);
-template <bool NORM> constexpr int kOffBar = kOffG<NORM> + kRing<NORM> * (int)sizeof(Gates);
+constexpr int kRing = 4;                                // places of decays and of items
+struct alignas(16) Item {
+    const float *in;                                    // the state before the segment, or null: zero
+    float *out, *total;                                 // the state after it, its decays' product, or null
+    int row, len, h, pad;                               // len 0: no more items
+};
+template <bool NORM> constexpr int kOffG = kOffY + (NORM ? C * kD * 4 : 0);
+template <bool NORM> constexpr int kOffItem = kOffG<NORM> + kRing * (int)sizeof(Gates);
+template <bool NORM> constexpr int kOffBar = kOffItem<NORM> + kRing * (int)sizeof(Item);
 enum {
     kFullK, kFullQ = kFullK + kPlaces, kFullV = kFullQ + kPlaces, kFreeK = kFullV + kPlaces, kFreeQ = kFreeK + kPlaces,
-    kFreeV = kFreeQ + kPlaces, kPReady = kFreeV + kPlaces, kKpReady = kPReady + kPlaces, kKpFree = kKpReady + 2,
-    kFullG = kKpFree + 2, kFreeG = kFullG + 4, kScores = kFreeG + 4, kSReady, kUFree, kYFree, kQs, kKv, kPv, kDrainA, kDrainB, kBars
+    kFreeV = kFreeQ + kPlaces, kVtReady = kFreeV + kPlaces, kVtFree = kVtReady + kPlaces, kPReady = kVtFree + kPlaces,
+    kKpReady = kPReady + kPlaces, kKpFree = kKpReady + 2,
+    kFullG = kKpFree + 2, kFreeG = kFullG + kRing, kFullItem = kFreeG + kRing,
+    kFreeItem = kFullItem + kRing, kScores = kFreeItem + kRing, kSReady, kUFree, kYFree, kQs, kKv, kPv, kDrainA, kDrainB, kBars
 };
 template <bool NORM> constexpr int kOffTmem = kOffBar<NORM> + kBars * 8;
-template <bool NORM> constexpr int kSmem = kOffTmem<NORM> + 16;      // the tensor memory's base
+template <bool NORM> constexpr int kOffStop = kOffTmem<NORM> + 8;      // uint32 of each group of warps
+template <bool NORM> constexpr int kSmem = kOffStop<NORM> + 32;
 static_assert(kSmem<true> <= kSmemMax && kSmem<false> <= kSmemMax, "one CTA's shared memory");
 
 constexpr uint32_t kIdescScores = tc::idesc_bf16(128, 64, 0, 0);
 constexpr uint32_t kIdescQs = tc::idesc_bf16(128, 64, 0, 0);
-constexpr uint32_t kIdescPv = tc::idesc_bf16(128, 128, 1, 0);
-constexpr uint32_t kIdescKv = tc::idesc_bf16(128, 128, 1, 1);
-
-struct Maps {
-    CUtensorMap of[3];                                  // k, q, v
-};
+constexpr uint32_t kIdescPv = tc::idesc_bf16(128, 64, 0, 0);
+constexpr uint32_t kIdescKv = tc::idesc_bf16(128, 128, 0, 1);
 
 template <bool NORM>
 struct Ctx {
@@ -84,7 +91,7 @@ struct Ctx {
     uint8_t *smem;
     uint64_t *bars;
     mutable uint32_t limit;                                 // of a wait, in cycles; 0: one has run out
-    static constexpr int R = kRing<NORM>;
+    static constexpr int R = kRing;
     // Waits for the phase of the given parity. Once a wait has run out no other of this warp
     // holds: the warps reach their ends without early exits, and the outputs are undefined.
     __device__ __forceinline__ void wait(int bar, uint32_t parity) const {
@@ -111,6 +118,49 @@ struct Ctx {
         if ((threadIdx.x & 31) == 0) mbar_arrive(&bars[bar]);
     }
     __device__ __forceinline__ Gates &gates(uint32_t n) const { return ((Gates *)(smem + kOffG<NORM>))[n % R]; }
+    __device__ __forceinline__ volatile uint32_t *stopped() const { return (volatile uint32_t *)(smem + kOffStop<NORM>); }
+    __device__ __forceinline__ Item &item(uint32_t n) const { return ((Item *)(smem + kOffItem<NORM>))[n % R]; }
+};
+
+// Barriers of the groups of warps. Within a group one warp waits for the phases and the
+// others for it: a waiting warp tests every 140 cycles or so, and 28 of them took half of
+// the SM's issue slots.
+enum { kSyncNone, kSyncState, kSyncOut, kSyncKeys, kSyncScores, kSyncs };
+template <int ID, int WARPS>
+__device__ __forceinline__ void group_sync() {
+    asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(32 * WARPS) : "memory");
+}
+
+// A warp's walk over the items that the loads' warp hands out. The warps of a group walk it
+// in step: they end where their first one (`leader`) ends, after which none of them is left
+// at one of the group's barriers.
+template <bool NORM, int ID = kSyncNone, int WARPS = 1>
+struct Items {
+    const Ctx<NORM> &x;
+    bool leader;
+    uint32_t n = 0;
+    const float *in;
+    float *out, *total;
+    int row, len, h;
+    __device__ __forceinline__ explicit Items(const Ctx<NORM> &c, bool first = true) : x(c), leader(first) {}
+    __device__ __forceinline__ bool next() {
+        if (leader) x.template wait_full<kRing>(kFullItem, n);
+        bool stop = x.limit == 0;                           // a wait ran out: nothing more
+        if (WARPS > 1) {
+            if (leader) x.stopped()[ID] = stop;
+            group_sync<ID, WARPS>();
+            stop = x.stopped()[ID];
+        }
+        const Item &i = x.item(n);
+        in = i.in;
+        out = i.out;
+        total = i.total;
+        row = i.row;
+        len = stop ? 0 : i.len;
+        h = i.h;
+        x.arrive(kFreeItem + n++ % kRing);
+        return len > 0;
+    }
 };
 
 // The pieces of a pair of fp32 values: both truncated to bf16 (the first in the low half),
@@ -130,23 +180,53 @@ __device__ __forceinline__ uint64_t pair_at(const float *p) {           // 8-byt
     return *(const uint64_t *)p;
 }
 
-// Warp 18: the decays of every chunk and their products, a block of 32 tokens per half, and
+// The decays of every chunk and their products, a block of 32 tokens per half, and
 // k, q and v.
 template <bool OUT, bool NORM>
-__device__ __forceinline__ void load(const Ctx<NORM> &x, const Maps &maps) {
+__device__ __forceinline__ void load(const Ctx<NORM> &x, const ChunkMaps &maps) {
     const PrefillArgs &a = x.a;
     const int grp = a.Hv / a.Hk, l = threadIdx.x & 31;
     const uint32_t lead = tc::elect();
     uint32_t n = 0, started = 0;                            // chunks; copies, three a chunk
-    for (Items it(a); it.next(l == 0);) {
-        if (it.item == a.stall.withhold_item) break;        // test switch: these copies never start
-        const int hk = it.h / grp;
-        const float *gate = a.gate + (int64_t)it.row * a.gs + it.h;
-        const auto decay = [&](int t) { return t < it.len ? gate[(int64_t)t * a.gs] : 1.f; };
+    const int segments = a.plan->segments;
+    int i = 0;                                              // segment * Hv + head
+    Segment it;
+    // The longest segment and head left; a sequence's last segment has no part to hand on.
+    const auto take = [&]() {
+        do {
+            if (lead) i = atomicAdd(&a.plan->next[OUT], 1);
+            i = __reduce_max_sync(0xffffffffu, i);
+            it.len = 0;
+            if (i / a.Hv < segments) it = a.table[i / a.Hv];
+        } while (!OUT && it.len > 0 && it.out == kStatePool);
+    };
+    take();
+    for (uint32_t k = 0;; k++) {
+        x.template wait_free<kRing>(kFreeItem, k);
+        const int h = i % a.Hv, row = it.row, len = it.len;
+        if (lead) {
+            Item &o = x.item(k);
+            float *work = a.states + ((uint64_t)it.id * a.Hv + h) * kN, *page = pool_page(a, it.slot, h);
+            o.row = row;
+            o.len = len;
+            o.h = h;
+            o.in = !OUT || it.in == kStateZero ? nullptr : it.in == kStatePool ? page : work;
+            o.out = !OUT ? work + (uint64_t)a.Hv * kN : it.out == kStatePool ? page : nullptr;
+            o.total = OUT ? nullptr : a.totals + (uint64_t)it.id * a.Hv + h;
+        }
+        x.arrive(kFullItem + k % kRing);
+        if (len == 0 || x.limit == 0) break;
+        if (i == a.stall.withhold_item) {                   // test switch: these copies never start
+            x.limit = 0;
+            break;
+        }
+        const int hk = h / grp;
+        const float *gate = a.gate + (int64_t)row * a.gs + h;
+        const auto decay = [&](int t) { return t < len ? gate[(int64_t)t * a.gs] : 1.f; };
         float g0 = decay(l), g1 = decay(32 + l);
 #pragma unroll 1
-        for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const int m = it.len - t0;
+        for (int t0 = 0; t0 < len; t0 += C, n++) {
+            const int m = len - t0;
             float p0 = g0, p1 = g1;                         // inclusive from the block's start
             float n0 = __shfl_down_sync(0xffffffffu, g0, 1), n1 = __shfl_down_sync(0xffffffffu, g1, 1);
             if (l == 31) n0 = n1 = 1.f;
@@ -174,24 +254,25 @@ __device__ __forceinline__ void load(const Ctx<NORM> &x, const Maps &maps) {
             if (l == 0) o.total = all0 * all1;
             x.arrive(kFullG + n % x.R);
 #pragma unroll 1
-            for (int i = 0; i < 3; i++) {                   // k, q, v
-                if (!OUT && i == 1) {
+            for (int e = 0; e < 3; e++) {                   // k, q, v
+                if (!OUT && e == 1) {
                     started++;
                     continue;
                 }
-                x.template wait_free<kPlaces>(kFreeK + i * kPlaces, n);
+                x.template wait_free<kPlaces>(kFreeK + e * kPlaces, n);
                 if (x.limit == 0) goto drain;               // nothing more is started
                 started++;
-                uint64_t *full = &x.bars[kFullK + i * kPlaces + n % kPlaces];
-                uint8_t *dst = x.smem + (i * kPlaces + n % kPlaces) * 2 * kTile;
-                const int ch = (i == 2 ? it.h : hk) * kD;
+                uint64_t *full = &x.bars[kFullK + e * kPlaces + n % kPlaces];
+                uint8_t *dst = x.smem + (e * kPlaces + n % kPlaces) * 2 * kTile;
+                const int ch = (e == 2 ? h : hk) * kD;
                 if (lead) {
                     mbar_arrive_tx(full, 2 * kTile);
-                    tma_load_2d(dst, &maps.of[i], ch, it.row + t0, full);
-                    tma_load_2d(dst + kTile, &maps.of[i], ch + 64, it.row + t0, full);
+                    tma_load_2d(dst, &maps.of[e], ch, row + t0, full);
+                    tma_load_2d(dst + kTile, &maps.of[e], ch + 64, row + t0, full);
                 }
                 __syncwarp();
             }
+            if (t0 == 0) take();                            // the next one, known long before it is due
         }
     }
 drain:                                                      // no copy is in flight when the CTA ends
@@ -200,26 +281,29 @@ drain:                                                      // no copy is in fli
         if (OUT || u % 3 != 1) mbar_wait(&x.bars[kFullK + (u % 3) * kPlaces + u / 3 % kPlaces], (u / 3 / kPlaces) & 1u, x.a.stall.wait_cycles);
 }
 
-__device__ __forceinline__ uint32_t chunks_of(const PrefillArgs &a) {
-    uint32_t n = 0;
-    for (Items it(a); it.next();) n += (uint32_t)(it.len + C - 1) / C;
-    return n;
-}
 // Descriptor of the two tiles of chunk n in one of the loaded operands' places.
 template <bool NORM>
 __device__ __forceinline__ uint64_t operand(const Ctx<NORM> &x, int off, uint32_t n, uint32_t lbo) {
     return tc::sdesc_sw128(x.smem + off + (n % kPlaces) * 2 * kTile, lbo, 1024);
 }
 
-// Warp 19: scores and PV. The scores of a chunk are formed ahead of its PV.
+// Scores and PV. The scores of a chunk are formed ahead of the PV of the one before.
 template <bool NORM>
 __device__ __forceinline__ void issue_scores(const Ctx<NORM> &x, uint32_t tm) {
-    const uint32_t lead = tc::elect(), chunks = chunks_of(x.a);
+    const uint32_t lead = tc::elect();
+    Items<NORM> it(x);
+    int left = 0;                                           // tokens of the item
+    bool more = true;
 #pragma unroll 1
-    for (uint32_t n = 0; n <= chunks; n++) {
+    for (uint32_t n = 0; more; n++) {
         const uint32_t m = n - 1;
+        left -= C;
+        if (left <= 0) {
+            more = it.next();
+            left = it.len;
+        }
         if (n > 0) x.template wait_full<kPlaces>(kPReady, m);       // the scores of chunk m have been read
-        if (n < chunks) {
+        if (more) {
             x.template wait_full<kPlaces>(kFullK, n);
             x.template wait_full<kPlaces>(kFullQ, n);
             tc::fence_after();
@@ -235,30 +319,40 @@ __device__ __forceinline__ void issue_scores(const Ctx<NORM> &x, uint32_t tm) {
             tc::commit(lead, &x.bars[kFreeQ + n % kPlaces]);
         }
         if (n == 0) continue;
-        x.template wait_full<kPlaces>(kFullV, m);
+        x.template wait_full<kPlaces>(kVtReady, m);
         x.wait_last(kYFree, m);
         tc::fence_after();
-        const uint64_t v = operand(x, kOffV, m, kTile), p = operand(x, kOffP, m, 16);
+        const uint64_t p = operand(x, kOffP, m, 16);
+#pragma unroll 1
+        for (int i = 1; i >= 0; i--)                        // rest, head
 #pragma unroll
-        for (int s = 0; s < 4; s++) tc::mma_f16_ss(lead, tm + kColY2, v + s * 128, p + s * 2, kIdescPv, s > 0);
+            for (int s = 0; s < 4; s++)
+                tc::mma_f16_ts(lead, tm + kColY2, tm + kColV + 32 * (m % kPlaces) + 8 * s, p + i * (kTile / 16) + s * 2, kIdescPv,
+                               i < 1 || s > 0);
         tc::commit(lead, &x.bars[kPv]);
-        tc::commit(lead, &x.bars[kFreeV + m % kPlaces]);
+        tc::commit(lead, &x.bars[kVtFree + m % kPlaces]);
     }
     // every MMA has ended before the tensor memory is given back
     tc::commit(lead, &x.bars[kDrainA]);
     if (!mbar_wait(&x.bars[kDrainA], 0, x.a.stall.wait_cycles)) x.limit = 0;
 }
 
-// Warp 20: KV and QS.
+// KV and QS.
 template <bool OUT, bool NORM>
 __device__ __forceinline__ void issue_state(const Ctx<NORM> &x, uint32_t tm) {
-    const uint32_t lead = tc::elect(), chunks = chunks_of(x.a);
+    const uint32_t lead = tc::elect();
     const uint64_t kp = tc::sdesc_sw128(x.smem + kOffKp, kTile, 1024);
+    Items<NORM> it(x);
+    int left = 0;
 #pragma unroll 1
-    for (uint32_t n = 0; n < chunks; n++) {
-        x.template wait_full<kPlaces>(kFullV, n);
+    for (uint32_t n = 0;; n++) {
+        left -= C;
+        if (left <= 0) {
+            if (!it.next()) break;
+            left = it.len;
+        }
+        x.template wait_full<kPlaces>(kVtReady, n);
         x.wait_last(kUFree, n);
-        const uint64_t v = operand(x, kOffV, n, kTile);
 #pragma unroll 1
         for (uint32_t h = 0; h < 2; h++) {                // the chunk's halves, so that one is scaled under the other
             x.wait(kKpReady + h, n & 1u);
@@ -267,12 +361,12 @@ __device__ __forceinline__ void issue_state(const Ctx<NORM> &x, uint32_t tm) {
             for (int i = 2; i >= 0; i--)                  // the smallest terms first
 #pragma unroll
                 for (int s = 0; s < 2; s++)
-                    tc::mma_f16_ss(lead, tm + kColU, v + (2 * h + s) * 128, kp + i * (2 * kTile / 16) + (2 * h + s) * 128, kIdescKv,
-                                   h > 0 || i < 2 || s > 0);
+                    tc::mma_f16_ts(lead, tm + kColU, tm + kColV + 32 * (n % kPlaces) + 8 * (2 * h + s),
+                                   kp + i * (2 * kTile / 16) + (2 * h + s) * 128, kIdescKv, h > 0 || i < 2 || s > 0);
             tc::commit(lead, &x.bars[kKpFree + h]);
         }
         tc::commit(lead, &x.bars[kKv]);
-        tc::commit(lead, &x.bars[kFreeV + n % kPlaces]);
+        tc::commit(lead, &x.bars[kVtFree + n % kPlaces]);
         if (!OUT) continue;
         x.template wait_full<kPlaces>(kFullQ, n);
         x.wait_last(kYFree, n);
@@ -292,36 +386,36 @@ __device__ __forceinline__ void issue_state(const Ctx<NORM> &x, uint32_t tm) {
     if (!mbar_wait(&x.bars[kDrainB], 0, x.a.stall.wait_cycles)) x.limit = 0;
 }
 
-// Warps 22-27: K' = w_Cs k_s as three truncated bf16 terms. A unit is a 16-byte piece of 32
-// tokens (lane = token) of a tile, so that 8 lanes' pieces of the swizzled rows lie in
-// different banks. In a chunk with fewer tokens the rows past the last belong to other
-// sequences: zeros take their place here and in V.
+// K' = w_Cs k_s as three truncated bf16 terms. A unit is a 16-byte piece of 32 tokens (lane =
+// token) of a tile, so that 8 lanes' pieces of the swizzled rows lie in different banks. In a
+// chunk with fewer tokens the rows past the last belong to other sequences: zeros take
+// their place.
 template <bool OUT, bool NORM>
 __device__ __forceinline__ void scale(const Ctx<NORM> &x, int w) {
+    constexpr int W = kScaleWarps;
     const PrefillArgs &a = x.a;
     const int l = threadIdx.x & 31;
     uint32_t n = 0;
-    for (Items it(a); it.next();) {
+    for (Items<NORM, kSyncKeys, kScaleWarps> it(x, w == 0); it.next();) {
 #pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
             const int m = it.len - t0, place = (n % kPlaces) * 2 * kTile;
-            x.template wait_full<x.R>(kFullG, n);
-            x.template wait_full<kPlaces>(kFullK, n);
-            if (m < C) x.template wait_full<kPlaces>(kFullV, n);
+            if (w == 0) {
+                x.template wait_full<x.R>(kFullG, n);
+                x.template wait_full<kPlaces>(kFullK, n);
+            }
             const Gates &g = x.gates(n);
 #pragma unroll 1
             for (int h = 0; h < 2; h++) {
-                x.wait_last(kKpFree + h, n);
+                if (w == 0) x.wait_last(kKpFree + h, n);
+                group_sync<kSyncKeys, W>();
                 const int s = 32 * h + l;
                 const uint64_t f = f2s(g.wk[s]);
 #pragma unroll 1
-                for (int u = (w + 4 * h) % kScaleWarps; u < 16; u += kScaleWarps) {
+                for (int u = (w + 4 * h) % W; u < 16; u += W) {
                     uint8_t *at = x.smem + (u >> 3) * kTile + s * 128 + ((u & 7) ^ (l & 7)) * 16;
                     uint4 r = *(const uint4 *)(at + kOffK + place);
-                    if (s >= m) {
-                        r = make_uint4(0, 0, 0, 0);
-                        *(uint4 *)(at + kOffV + place) = r;
-                    }
+                    if (s >= m) r = make_uint4(0, 0, 0, 0);
                     const uint32_t in[4] = {r.x, r.y, r.z, r.w};
                     uint32_t t[3][4];
 #pragma unroll
@@ -345,7 +439,35 @@ __device__ __forceinline__ void scale(const Ctx<NORM> &x, int w) {
     }
 }
 
-// Warps 16, 17, 21: P of tokens t = 32 quad + lane over keys 32 half .. + 31, 16 keys at a time;
+// V^T of chunk n, m tokens, into tensor memory: 16 channels of this warp's quadrant. Rows past the last token belong to other sequences:
+// zeros take their place.
+template <bool NORM>
+__device__ __forceinline__ void transpose_v(const Ctx<NORM> &x, uint32_t tm, uint32_t n, int m, int h) {
+    const int l = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3;
+    // ldmatrix: this lane's row of the four 8 x 8 matrices (tokens 0-7 | 8-15) x (channels 0-7 | 8-15)
+    const int row = (l & 7) + 8 * (l >> 4), piece = 4 * (quad & 1) + ((l >> 3) & 1);
+    x.template wait_full<kPlaces>(kFullV, n);
+    x.template wait_free<kPlaces>(kVtFree, n);
+    tc::fence_after();
+    const uint8_t *v = x.smem + kOffV + (n % kPlaces) * 2 * kTile + (quad >> 1) * kTile + row * 128;
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 4; i++)                             // 16 tokens
+        tc::load_transposed(v + i * 16 * 128 + ((piece + 2 * h) ^ (l & 7)) * 16, r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+    if (m < C)
+#pragma unroll
+        for (int i = 0; i < 16; i++) {                      // tokens 2 (l & 3) and + 1 of the 8 at 8 (i >> 1)
+            const int t = 8 * (i >> 1) + 2 * (l & 3);
+            r[i] = t + 1 < m ? r[i] : t < m ? r[i] & 0xFFFFu : 0u;
+        }
+    tc::st_16x32(tm + ((uint32_t)(32 * quad + 16 * h) << 16) + kColV + 32 * (n % kPlaces), r);
+    tc::wait_st();
+    tc::fence_before();
+    x.arrive(kVtReady + n % kPlaces);
+    x.arrive(kFreeV + n % kPlaces);
+}
+
+// P of tokens t = 32 quad + lane over keys 32 half .. + 31, 16 keys at a time;
 // the block above the diagonal stays zero. Diagonal blocks: w_ts by a running product down
 // the row (zero above the diagonal); the block below them: the product of its two parts.
 template <bool NORM>
@@ -353,12 +475,15 @@ __device__ __forceinline__ void weigh_scores(const Ctx<NORM> &x, uint32_t tm, in
     const int l = threadIdx.x & 31, t = 32 * quad + l;
     const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + kColP;
     uint32_t n = 0;
-    for (Items it(x.a); it.next();) {
+    for (Items<NORM, kSyncScores, 3> it(x, quad == 0); it.next();) {
 #pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            x.template wait_full<x.R>(kFullG, n);
-            x.template wait_free<kPlaces>(kFreeV, n);       // PV of two chunks ago has read the place
-            x.wait(kScores, n & 1u);
+            if (quad == 0) {
+                x.template wait_full<x.R>(kFullG, n);
+                x.template wait_free<kPlaces>(kVtFree, n);  // PV of two chunks ago has read the place
+                x.wait(kScores, n & 1u);
+            }
+            group_sync<kSyncScores, 3>();
             tc::fence_after();
             const Gates &g = x.gates(n);
             uint8_t *row = x.smem + kOffP + (n % kPlaces) * 2 * kTile + t * 128;
@@ -411,7 +536,7 @@ __device__ __forceinline__ void weigh_scores(const Ctx<NORM> &x, uint32_t tm, in
     }
 }
 
-// Warps 0-7: the state. This thread: value channel j, key channels 64 half .. + 63, in pairs.
+// The state. This thread: value channel j, key channels 64 half .. + 63, in pairs.
 template <bool OUT, bool NORM>
 __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
     const PrefillArgs &a = x.a;
@@ -419,8 +544,8 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
     const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16);
     uint32_t n = 0;
     uint64_t s[32];
-    for (Items it(a); it.next();) {
-        const float *in = it.state_in();
+    for (Items<NORM, kSyncState, 8> it(x, w == 0); it.next();) {
+        const float *in = it.in;
 #pragma unroll
         for (int e = 0; e < 32; e++)
             s[e] = in ? f2(in[(64 * half + 2 * e) * kD + j], in[(64 * half + 2 * e + 1) * kD + j]) : 0;
@@ -428,7 +553,8 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
 #pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
             if (OUT) {                                      // S^T's head and rest as an operand
-                x.wait_last(kQs, n);
+                if (w == 0) x.wait_last(kQs, n);
+                group_sync<kSyncState, 8>();
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     uint32_t h[8], r[8];
@@ -444,8 +570,11 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
                 tc::fence_before();
                 x.arrive(kSReady);
             }
-            x.template wait_full<x.R>(kFullG, n);
-            x.wait(kKv, n & 1u);
+            if (w == 0) {
+                x.template wait_full<x.R>(kFullG, n);
+                x.wait(kKv, n & 1u);
+            }
+            group_sync<kSyncState, 8>();
             tc::fence_after();
             const float gc = x.gates(n).total;
             const uint64_t g2 = f2s(gc);
@@ -461,102 +590,106 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
             x.arrive(kUFree);
             x.arrive(kFreeG + n % x.R);
         }
-        float *out = it.state_out();
+        float *out = it.out;
         if (out)
 #pragma unroll
             for (int e = 0; e < 32; e++) {
                 out[(64 * half + 2 * e) * kD + j] = f2lo(s[e]);
                 out[(64 * half + 2 * e + 1) * kD + j] = f2hi(s[e]);
             }
-        if (!OUT && threadIdx.x == 0) *it.total_out() = total;
+        if (!OUT && threadIdx.x == 0) *it.total = total;
     }
 }
 
-// Barrier over the 256 threads of warps 8-15.
-__device__ __forceinline__ void out_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
-
-// Warps 8-15: the outputs. This thread: value channel j of tokens 32 half .. + 31; through
-// shared memory a token's 128 channels come together, to leave in 16-byte pieces or to be
-// normalised by a warp.
-template <bool NORM>
+// V^T of the next chunk, and the outputs. This thread: value channel j of tokens 32 half .. + 31,
+// a warp's 64 bytes of a token straight from registers (16-byte pieces by way of stmatrix and
+// shared memory: a tenth fewer instructions, but 5% slower for the shared memory they take);
+// or, to be normalised, through shared memory, where a token's 128 channels come together in
+// a warp.
+template <bool OUT, bool NORM>
 __device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
+    constexpr int W = kOutWarps;
     const PrefillArgs &a = x.a;
     const int w = (threadIdx.x >> 5) - 8, l = threadIdx.x & 31, quad = w & 3, half = w >> 2, j = 32 * quad + l;
     const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + 32 * half;
-    float *yf = (float *)(x.smem + kOffY) + 32 * half * kD + j;
-    uint16_t *yb = (uint16_t *)(x.smem + kOffY) + 32 * half * kD + j;
+    float *ys = (float *)(x.smem + kOffY);
     uint32_t n = 0;
-    for (Items it(a); it.next();) {
-        bf16 *y = (bf16 *)a.y + (int64_t)it.row * a.ys + it.h * kD;
-        const bf16 *z = (const bf16 *)a.norm.z + (int64_t)it.row * a.norm.z_stride + it.h * kD;
+    // V^T runs a chunk ahead, into the next item's first: that item is known by then
+    Items<NORM, kSyncOut, W> ahead(x, w == 0);
+    bool more = ahead.next();
+    if (more) transpose_v(x, tm, 0, ahead.len, half);
+    while (more) {
+        const int row = ahead.row, len = ahead.len, h = ahead.h;
+        bf16 *y = (bf16 *)a.y + (int64_t)row * a.ys + h * kD;
+        const bf16 *z = (const bf16 *)a.norm.z + (int64_t)row * a.norm.z_stride + h * kD;
 #pragma unroll 1
-        for (int t0 = 0; t0 < it.len; t0 += C, n++) {
-            const int m = min(C, it.len - t0);
-            if (NORM && a.norm.z) {                         // on its way before it is needed
-                const int t = w + 8 * (l >> 1);
-                if (l < 16 && t < m) asm volatile("prefetch.global.L1 [%0];" ::"l"(z + t * a.norm.z_stride + 64 * (l & 1)));
+        for (int t0 = 0; t0 < len; t0 += C, n++) {
+            int next = len - t0 - C;                        // tokens of the next chunk and on
+            if (next <= 0) {
+                more = ahead.next();
+                next = ahead.len;
             }
-            x.template wait_full<x.R>(kFullG, n);
-            x.wait(kPv, n & 1u);
-            x.wait(kQs, n & 1u);
-            out_sync();                                     // the chunk before's readouts have left the place
+            if (more) transpose_v(x, tm, n + 1, next, half);
+            if (!OUT) continue;
+            const int m = min(C, len - t0);
+            Vec<bf16, 4> g[NORM ? 8 : 1];                   // the gate of tokens w, w + 8, ..., on its way before it is needed
+            if (NORM && a.norm.z)
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    g[i] = *(const Vec<bf16, 4> *)(z + min(w + 8 * i, m - 1) * a.norm.z_stride + 4 * l);
+            if (w == 0) {
+                x.template wait_full<x.R>(kFullG, n);
+                x.wait(kPv, n & 1u);
+                x.wait(kQs, n & 1u);
+            }
+            group_sync<kSyncOut, W>();                      // and the chunk before's readouts have left the place
             tc::fence_after();
             const float *c = x.gates(n).c + 32 * half;
+            bf16 *yt = y + 32 * half * a.ys + j;
 #pragma unroll 1
-            for (int i = 0; i < 32; i += 8) {
-                uint32_t y1[8], y2[8], y3[8];
-                tc::ld8_start(tl + kColY1 + i, y1);
-                tc::ld8_start(tl + kColY2 + i, y2);
-                tc::ld8_start(tl + kColY2 + C + i, y3);
+            for (int i = 0; i < 32; i += 16) {
+                uint32_t y1[16], y2[16];
+                tc::ld16_start(tl + kColY1 + i, y1);
+                tc::ld16_start(tl + kColY2 + i, y2);
                 tc::wait_ld(y1);
                 tc::wait_ld(y2);
-                tc::wait_ld(y3);
+                if (i == 16) {
+                    tc::fence_before();
+                    x.arrive(kYFree);
+                }
+                float *p = ys + (32 * half + i) * kD + j;
+                const int left = m - 32 * half - i;
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const uint64_t v = ffma2(pair_at(&c[i + e]), u2pair(y1[e], y1[e + 1]),
-                                             fadd2(u2pair(y2[e], y2[e + 1]), u2pair(y3[e], y3[e + 1])));
+                for (int e = 0; e < 16; e += 2) {
+                    const uint64_t v = ffma2(pair_at(&c[i + e]), u2pair(y1[e], y1[e + 1]), u2pair(y2[e], y2[e + 1]));
                     if (NORM) {
-                        yf[(i + e) * kD] = f2lo(v);
-                        yf[(i + e + 1) * kD] = f2hi(v);
+                        p[e * kD] = f2lo(v);
+                        p[(e + 1) * kD] = f2hi(v);
                     } else {
                         const uint32_t b = rounded(v);
-                        yb[(i + e) * kD] = (uint16_t)b;
-                        yb[(i + e + 1) * kD] = (uint16_t)(b >> 16);
+                        if (e < left) *(uint16_t *)yt = (uint16_t)b;
+                        yt += a.ys;
+                        if (e + 1 < left) *(uint16_t *)yt = (uint16_t)(b >> 16);
+                        yt += a.ys;
                     }
                 }
             }
-            tc::fence_before();
-            x.arrive(kYFree);
             x.arrive(kFreeG + n % x.R);
-            out_sync();
             if (NORM) {
-                constexpr int N = 2;                        // tokens w, w + 8 of 16 at a time
-                const float *ys = (const float *)(x.smem + kOffY) + 4 * l;
-                const HeadAffine p(a.norm, it.h, l);
-#pragma unroll 1
-                for (int b = w; b < m; b += 8 * N) {
+                group_sync<kSyncOut, W>();
+                const HeadAffine p(a.norm, h, l);
+                constexpr int N = 4;                        // tokens at a time
+#pragma unroll
+                for (int k = 0; k < 8; k += N) {
                     float v[N][4];
 #pragma unroll
-                    for (int i = 0; i < N; i++) {
-                        const float4 u = *(const float4 *)&ys[(b + 8 * i) * kD];
-                        v[i][0] = u.x;
-                        v[i][1] = u.y;
-                        v[i][2] = u.z;
-                        v[i][3] = u.w;
-                    }
-                    norm_head<bf16, N>(a.norm, p, [&](int i) { return z + min(b + 8 * i, m - 1) * a.norm.z_stride + 4 * l; }, v);
+                    for (int i = 0; i < N; i++) load_vec<float, 4>(&ys[(w + 8 * (k + i)) * kD + 4 * l], v[i]);
+                    norm_head<bf16, N>(a.norm, p, &g[k], v);
 #pragma unroll
                     for (int i = 0; i < N; i++)
-                        if (b + 8 * i < m) store_vec<bf16, 4>(y + (b + 8 * i) * a.ys + 4 * l, v[i]);
+                        if (w + 8 * (k + i) < m) store_vec<bf16, 4>(y + (w + 8 * (k + i)) * a.ys + 4 * l, v[i]);
                 }
                 z += C * a.norm.z_stride;
-            } else {
-                const int t1 = 2 * w + (l >> 4);
-                const bf16 *ys = (const bf16 *)(x.smem + kOffY) + 8 * (l & 15);
-                bf16 *yt = y + t1 * a.ys + 8 * (l & 15);
-#pragma unroll
-                for (int t = 0; t < C; t += 16, yt += 16 * a.ys)
-                    if (t1 + t < m) *(uint4 *)yt = *(const uint4 *)(ys + (t1 + t) * kD);
             }
             y += C * a.ys;
         }
@@ -564,7 +697,7 @@ __device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
 }
 
 template <bool OUT, bool NORM>
-__global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a, const __grid_constant__ ChunkMaps maps) {
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t *bars = (uint64_t *)(smem + kOffBar<NORM>);
     uint32_t *tbase = (uint32_t *)(smem + kOffTmem<NORM>);
@@ -576,11 +709,15 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
     if (tid < kBars) {
         int count = 1;                                      // TMA, the end of MMAs, the decays
         if (tid >= kFreeK && tid < kFreeQ) count = kScaleWarps + (OUT ? 1 : 0);            // K', the scores
-        if (tid >= kFreeQ && tid < kPReady) count = OUT ? 2 : 1;                           // scores, QS; KV, PV
+        if (tid >= kFreeQ && tid < kFreeV) count = OUT ? 2 : 1;                            // scores, QS
+        if (tid >= kFreeV && tid < kVtFree) count = kOutWarps;                       // the warps of V^T
+        if (tid >= kVtFree && tid < kPReady) count = OUT ? 2 : 1;                          // KV, PV
         if (tid >= kPReady && tid < kKpReady) count = 3;
-        if (tid >= kFreeG && tid < kScores) count = 8 + kScaleWarps + (OUT ? 11 : 0);      // state, K', P, outputs
+        if (tid >= kFreeItem && tid < kScores) count = 9 + kScaleWarps + kOutWarps + (OUT ? 4 : 0);     // state, MMAs, K', V^T; P, scores
+        if (tid >= kFreeG && tid < kFullItem) count = 8 + kScaleWarps + (OUT ? 3 + kOutWarps : 0);      // state, K', P, outputs
         if (tid >= kKpReady && tid < kKpFree) count = kScaleWarps;
-        if (tid >= kSReady && tid <= kYFree) count = 8;
+        if (tid >= kSReady && tid < kYFree) count = 8;
+        if (tid == kYFree) count = kOutWarps;
         mbar_init(&bars[tid], count);
         mbar_init_fence();
     }
@@ -601,17 +738,18 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
     if (w < 8) {
         tc::regs_inc<kRegsState>();
         states<OUT>(x, tm);
-    } else if (w < 16) {
+    } else if (w < kFirst) {
         tc::regs_dec<kRegsOut>();
-        if (OUT) outputs(x, tm);
+        outputs<OUT>(x, tm);
     } else {
         tc::regs_dec<kRegsOperand>();
-        if (w == 18) load<OUT>(x, maps);
-        else if (w == 20) issue_state<OUT>(x, tm);
-        else if (w >= 22) scale<OUT>(x, w - 22);
+        const int i = w - kFirst;
+        if (i == 2) load<OUT>(x, maps);
+        else if (i == 4) issue_state<OUT>(x, tm);
+        else if (i >= 6) scale<OUT>(x, i - 6);
         else if (OUT) {
-            if (w == 19) issue_scores(x, tm);
-            else weigh_scores(x, tm, w & 3, w == 17);
+            if (i == 3) issue_scores(x, tm);
+            else weigh_scores(x, tm, w & 3, i == 1);
         }
     }
     if (x.limit == 0) raise_error(a.err, STEPQ_ERR_TIMEOUT);
@@ -650,23 +788,21 @@ static bool encode(Encode f, CUtensorMap *map, const void *p, int channels, int 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The shared memory a launch takes, and the registers that its warps share out.
 template <bool OUT, bool NORM>
-static stepq_status launch(const PrefillArgs &a, const Maps &maps, int items, cudaStream_t s) {
-    const auto kernel = linattn_chunks_kernel<OUT, NORM>;
+static stepq_status prepare() {
+    const auto kernel = (const void *)linattn_chunks_kernel<OUT, NORM>;
     static SmemOptIn opt;
-    const stepq_status st = opt((const void *)kernel, kSmem<NORM>);
+    const stepq_status st = opt(kernel, kSmem<NORM>);
     if (st != STEPQ_OK) return st;
-    // the register shares are taken from what the kernel is launched with
-    static std::atomic<int> regs{0};
+    static std::atomic<int> regs{0};                    // kept once known
     if (regs.load(std::memory_order_relaxed) == 0) {
         cudaFuncAttributes f{};
-        const stepq_status e = cuda_status(cudaFuncGetAttributes(&f, (const void *)kernel));
+        const stepq_status e = cuda_status(cudaFuncGetAttributes(&f, kernel));
         if (e != STEPQ_OK) return e;
         regs.store(f.numRegs, std::memory_order_relaxed);
     }
-    if (regs.load(std::memory_order_relaxed) < kRegs) return STEPQ_ERR_CUDA;
-    const int grid = sm_count();
-    return launch_overlapped(kernel, grid < items ? grid : items, kBlock, kSmem<NORM>, s, a, maps);
+    return regs.load(std::memory_order_relaxed) < kRegs ? STEPQ_ERR_CUDA : STEPQ_OK;
 }
 
 }  // namespace ch
@@ -680,14 +816,21 @@ bool linattn_chunks_takes(const stepq_config *cfg, const stepq_linattn_io *io) {
            io->q_stride < most && io->k_stride < most && io->v_stride < most;
 }
 
-stepq_status launch_linattn_chunks(const PrefillArgs &a, int items, bool out, cudaStream_t s) {
+stepq_status prepare_linattn_chunks(const PrefillArgs &a, bool parts, ChunkMaps &maps) {
     const ch::Encode f = ch::encoder();
-    ch::Maps maps;
     if (!f || !ch::encode(f, &maps.of[0], a.k, kD * a.Hk, a.tokens, a.ks) ||
         !ch::encode(f, &maps.of[1], a.q, kD * a.Hk, a.tokens, a.qs) || !ch::encode(f, &maps.of[2], a.v, kD * a.Hv, a.tokens, a.vs))
         return STEPQ_ERR_CUDA;
-    if (!out) return ch::launch<false, false>(a, maps, items, s);
-    return a.norm.on ? ch::launch<true, true>(a, maps, items, s) : ch::launch<true, false>(a, maps, items, s);
+    const stepq_status st = parts ? ch::prepare<false, false>() : STEPQ_OK;
+    if (st != STEPQ_OK) return st;
+    return a.norm.on ? ch::prepare<true, true>() : ch::prepare<true, false>();
+}
+
+stepq_status launch_linattn_chunks(const PrefillArgs &a, const ChunkMaps &maps, int grid, bool out, cudaStream_t s) {
+    using namespace ch;
+    if (!out) return launch_overlapped(linattn_chunks_kernel<false, false>, grid, kBlock, kSmem<false>, s, a, maps);
+    if (a.norm.on) return launch_overlapped(linattn_chunks_kernel<true, true>, grid, kBlock, kSmem<true>, s, a, maps);
+    return launch_overlapped(linattn_chunks_kernel<true, false>, grid, kBlock, kSmem<false>, s, a, maps);
 }
 
 }  // namespace la

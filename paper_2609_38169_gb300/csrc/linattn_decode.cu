@@ -77,9 +77,11 @@ __global__ void __launch_bounds__(kThreads) linattn_decode_kernel(DecodeArgs a) 
         y[0][2] += r.z;
         y[0][3] += r.w;
     }
-    if (a.norm.on)
-        norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l),
-                        [&](int) { return (const T *)a.norm.z + b * a.norm.z_stride + h * kD + 4 * l; }, y);
+    if (a.norm.on) {
+        Vec<T, 4> z{};
+        if (a.norm.z) z = *(const Vec<T, 4> *)((const T *)a.norm.z + b * a.norm.z_stride + h * kD + 4 * l);
+        norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l), &z, y);
+    }
     store_vec<T, 4>((T *)a.y + b * a.ys + h * kD + 4 * l, y[0]);
 }
 

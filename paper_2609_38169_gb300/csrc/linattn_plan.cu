@@ -1,0 +1,131 @@
+// The work of a prompt call laid out on the device, where the sequences' lengths are: segments
+// in the order of falling length, which the CTAs of the tensor-core kernel take one after
+// another; and the states before the segments of split sequences.
+#include "async.cuh"
+#include "device.cuh"
+#include "linattn_prefill.cuh"
+
+namespace stepq {
+namespace la {
+
+constexpr int kSms = 152;                               // a GB300's multiprocessors
+
+// One CTA per SM takes a segment and head at a time, longest first, so the time of a call is
+// about its share W = tokens x Hv / 152 tokens a CTA, or the longest item's length L. Splitting
+// a sequence lets its segments run side by side, but the state before each has to be there:
+// a pass over k and v alone for the segments' own parts (about 0.55 of the full pass) and a
+// scan. It pays where L > 1.6 W. A segment is W / 4 tokens, so that the last round of items is
+// short, but not less than 256, whose 128 KiB of state traffic are half of its vectors'.
+Split split_of(int Hv, int B, int tokens, int max_len) {
+    const int longest = max_len > 0 && max_len < tokens ? max_len : max_len > 0 ? tokens : (tokens + B - 1) / B;
+    const double share = (double)tokens * Hv / kSms;
+    Split s{tokens, B, false};
+    if (longest > 512 && longest > 1.6 * share) {
+        const int q = (int)(share / 4);
+        s.segment = q < 256 ? 256 : (q + kChunk - 1) / kChunk * kChunk;
+        s.most = B + tokens / s.segment;
+        s.on = true;
+    }
+    return s;
+}
+
+// Buckets of lengths in chunks: exponent and three bits of mantissa.
+constexpr int kBuckets = 256;
+__device__ __forceinline__ int bucket_of(int len) {
+    const int chunks = (len + kChunk - 1) / kChunk;
+    return min(kBuckets - 1, (int)(__float_as_uint((float)chunks) >> 20) - (127 << 3));
+}
+
+// One CTA. Counting sort of the segments by bucket; within one the order is arbitrary, which
+// changes no result. Sequences out of range raise the error and make no segment.
+__global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
+    __shared__ int count[kBuckets], total;
+    const int tid = threadIdx.x;
+    if (tid < kBuckets) count[tid] = 0;
+    if (tid == 0) total = 0;
+    __syncthreads();
+    griddep_wait();
+    griddep_launch();
+    for (int b = tid; b < a.B; b += 1024) {
+        int row, len, slot;
+        if (!sequence(a, b, true, row, len, slot)) len = 0;
+        const int n = (len + a.segment - 1) / a.segment;
+        a.sequences[b] = {n ? atomicAdd(&total, n) : 0, n};
+        if (n > 1) atomicAdd(&count[bucket_of(a.segment)], n - 1);
+        if (n > 0) atomicAdd(&count[bucket_of(len - (n - 1) * a.segment)], 1);
+    }
+    __syncthreads();
+    // first place of each bucket, the longest first
+    if (tid < 32) {
+        int run = 0;
+        for (int c = kBuckets - 32; c >= 0; c -= 32) {
+            const int mine = count[c + 31 - tid];
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int up = __shfl_up_sync(0xffffffffu, sum, o);
+                if (tid >= o) sum += up;
+            }
+            count[c + 31 - tid] = run + sum - mine;
+            run += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (tid == 0) *a.plan = PlanHeader{run, {0, 0}, {}};
+    }
+    __syncthreads();
+    for (int b = tid; b < a.B; b += 1024) {
+        int row, len, slot;
+        if (!sequence(a, b, false, row, len, slot)) continue;
+        const Sequence q = a.sequences[b];
+        for (int i = 0; i < q.segments; i++) {
+            Segment s{row + i * a.segment, min(a.segment, len - i * a.segment), slot, q.id + i, 0, 0, {}};
+            s.in = q.segments > 1 ? kStateWork : !a.resume || a.resume[b] ? kStatePool : kStateZero;
+            s.out = i == q.segments - 1 ? kStatePool : kStateZero;
+            a.table[atomicAdd(&count[bucket_of(s.len)], 1)] = s;
+        }
+    }
+}
+
+// States before the segments of a split sequence: S_0 from the slot or zero, and
+// S_{i+1} = (product of segment i's decays) S_i + U_i, where U_i lies in S_{i+1}'s place. A
+// CTA takes 1024 elements of one sequence and head; two states a segment through L2.
+__global__ void __launch_bounds__(256) linattn_join_kernel(PrefillArgs a) {
+    griddep_wait();
+    griddep_launch();
+    const int part = blockIdx.x & 15, item = blockIdx.x >> 4, b = item / a.Hv, h = item - b * a.Hv;
+    const Sequence q = a.sequences[b];
+    if (q.segments < 2) return;
+    const int e = part * 1024 + 4 * threadIdx.x;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!a.resume || a.resume[b]) s = *(const float4 *)(pool_page(a, a.slots[b], h) + e);
+    float *at = a.states + ((uint64_t)q.id * a.Hv + h) * kN + e;
+    const float *total = a.totals + (uint64_t)q.id * a.Hv + h;
+    const uint64_t step = (uint64_t)a.Hv * kN;
+    *(float4 *)at = s;
+    constexpr int N = 4;                                // segments read ahead
+    for (int i = 1; i < q.segments; i += N) {
+        float4 u[N];
+        float g[N];
+#pragma unroll
+        for (int n = 0; n < N; n++)
+            if (i + n < q.segments) {
+                u[n] = *(const float4 *)(at + (i + n) * step);
+                g[n] = total[(i + n - 1) * a.Hv];
+            }
+#pragma unroll
+        for (int n = 0; n < N; n++)
+            if (i + n < q.segments) {
+                s = make_float4(fmaf(g[n], s.x, u[n].x), fmaf(g[n], s.y, u[n].y), fmaf(g[n], s.z, u[n].z), fmaf(g[n], s.w, u[n].w));
+                *(float4 *)(at + (i + n) * step) = s;
+            }
+    }
+}
+
+stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s) {
+    return launch_overlapped(linattn_plan_kernel, 1, 1024, 0, s, a);
+}
+stepq_status launch_linattn_join(const PrefillArgs &a, cudaStream_t s) {
+    return launch_overlapped(linattn_join_kernel, a.B * a.Hv * 16, 256, 0, s, a);
+}
+
+}  // namespace la
+}  // namespace stepq

@@ -57,9 +57,11 @@ __global__ void __launch_bounds__(kD) linattn_prefill_tokens_kernel(PrefillArgs 
         for (int t = w; t < n; t += 4) {
             const float4 r = *(const float4 *)&vy[t][4 * l];
             float y[1][4] = {{r.x, r.y, r.z, r.w}};
-            if (a.norm.on)
-                norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l),
-                                [&](int) { return (const T *)a.norm.z + (row + t) * a.norm.z_stride + h * kD + 4 * l; }, y);
+            if (a.norm.on) {
+                Vec<T, 4> z{};
+                if (a.norm.z) z = *(const Vec<T, 4> *)((const T *)a.norm.z + (row + t) * a.norm.z_stride + h * kD + 4 * l);
+                norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l), &z, y);
+            }
             store_vec<T, 4>((T *)a.y + (row + t) * a.ys + h * kD + 4 * l, y[0]);
         }
         __syncthreads();
@@ -73,12 +75,40 @@ __global__ void __launch_bounds__(kD) linattn_prefill_tokens_kernel(PrefillArgs 
 
 }  // namespace la
 
-size_t linattn_workspace_bytes(const stepq_config *, int, int, int) { return 0; }
+namespace {
+
+// The workspace's parts, each at a multiple of 256 bytes.
+struct Workspace {
+    size_t table, sequences, totals, states, bytes;
+    Workspace(int Hv, int B, const la::Split &split) {
+        const auto part = [&](size_t n) {
+            const size_t at = bytes;
+            bytes += (n + 255) / 256 * 256;
+            return at;
+        };
+        bytes = 0;
+        part(sizeof(la::PlanHeader));
+        table = part((size_t)split.most * sizeof(la::Segment));
+        sequences = part((size_t)B * sizeof(la::Sequence));
+        totals = part(split.on ? (size_t)split.most * Hv * 4 : 0);
+        states = part(split.on ? (size_t)split.most * Hv * kN * 4 : 0);
+    }
+};
+
+// The tensor-core kernel takes 64 tokens at a time with its operands in flight; for a few tokens
+// the walk token by token is done sooner: (measured rule below).
+constexpr int kFewTokens = 16;
+
+}  // namespace
+
+size_t linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int max_len) {
+    return Workspace(cfg->n_value_heads, B, la::split_of(cfg->n_value_heads, B, tokens, max_len)).bytes;
+}
 
 stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *pool, int pool_slots,
                                     const int32_t *slots, const uint8_t *resume, const int32_t *cu, int B,
-                                    int tokens, int, const stepq_linattn_io *io, const stepq_norm *norm, void *,
-                                    cudaStream_t s) {
+                                    int tokens, int max_len, const stepq_linattn_io *io, const stepq_norm *norm,
+                                    void *workspace, cudaStream_t s) {
     la::PrefillArgs a{};
     const uint64_t per_layer = (uint64_t)kN * cfg->n_value_heads;
     a.pool = pool;
@@ -95,11 +125,28 @@ stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *p
     a.norm = la::norm_args(norm);
     a.err = device_error_word();
     a.stall = stall_knob();
-    a.items = B * a.Hv;
-    if (la::linattn_chunks_takes(cfg, io)) return la::launch_linattn_chunks(a, a.items, true, s);
-    return la::by_type(io->dtype, [&](auto t) {
-        return launch_overlapped(la::linattn_prefill_tokens_kernel<decltype(t)>, B * a.Hv, kD, 0, s, a);
-    });
+    const bool few = (max_len > 0 ? max_len : tokens) <= kFewTokens;
+    if (few || !la::linattn_chunks_takes(cfg, io))
+        return la::by_type(io->dtype, [&](auto t) {
+            return launch_overlapped(la::linattn_prefill_tokens_kernel<decltype(t)>, B * a.Hv, kD, 0, s, a);
+        });
+    const la::Split split = la::split_of(a.Hv, B, tokens, max_len);
+    const Workspace w(a.Hv, B, split);
+    uint8_t *base = (uint8_t *)workspace;
+    a.plan = (la::PlanHeader *)base;
+    a.table = (la::Segment *)(base + w.table);
+    a.sequences = (la::Sequence *)(base + w.sequences);
+    a.totals = (float *)(base + w.totals);
+    a.states = (float *)(base + w.states);
+    a.segment = split.segment;
+    const long long items = (long long)split.most * a.Hv;
+    const int grid = items < sm_count() ? (int)items : sm_count();
+    la::ChunkMaps maps;                                    // what may be refused comes before the first launch
+    stepq_status st = la::prepare_linattn_chunks(a, split.on, maps);
+    if (st == STEPQ_OK) st = la::launch_linattn_plan(a, s);
+    if (st == STEPQ_OK && split.on) st = la::launch_linattn_chunks(a, maps, grid, false, s);
+    if (st == STEPQ_OK && split.on) st = la::launch_linattn_join(a, s);
+    return st == STEPQ_OK ? la::launch_linattn_chunks(a, maps, grid, true, s) : st;
 }
 
 }  // namespace stepq

@@ -1,6 +1,8 @@
-// What the prompt kernels of decayed linear attention share: arguments and the walk over
-// their work.
+// What the prompt kernels of decayed linear attention share: arguments, the plan that
+// linattn_plan.cu lays down in the workspace, and the launches.
 #pragma once
+
+#include <cuda.h>
 
 #include "linattn.cuh"
 
@@ -8,6 +10,25 @@ namespace stepq {
 namespace la {
 
 constexpr int kChunk = 64;             // tokens a chunk of the tensor-core kernel
+
+// Consecutive tokens of one sequence that a CTA takes with one head: a whole sequence, or, of
+// one that is split, kSegment tokens or what is left.
+struct alignas(16) Segment {
+    int row, len;                      // first row, tokens
+    int slot;
+    int id;                            // place of its state in the workspace
+    int in, out;                       // kState*: where the state before it comes from, where the one after it goes
+    int pad[2];
+};
+enum { kStateZero, kStatePool, kStateWork };           // in; out: kStateZero is none
+struct PlanHeader {
+    int segments;
+    int next[2];                       // the items taken so far by the two passes
+    int pad[5];
+};
+struct Sequence {
+    int id, segments;                  // of its first segment; 0 or 1: not split
+};
 
 struct PrefillArgs {
     float *pool;
@@ -22,7 +43,12 @@ struct PrefillArgs {
     NormArgs norm;
     unsigned int *err;
     StallKnob stall;
-    int items;                         // (sequence, head) pairs
+    // the plan (tensor-core kernel)
+    PlanHeader *plan;
+    Segment *table;                    // by falling length
+    Sequence *sequences;
+    float *totals, *states;            // [segments][Hv]: products of a segment's decays; states before the segments
+    int segment;                       // tokens
 };
 
 // First row and length of sequence b, and its slot; false (and the device error) if either
@@ -44,37 +70,29 @@ __device__ __forceinline__ bool sequence(const PrefillArgs &a, int b, bool lead,
     }
     return true;
 }
+__device__ __forceinline__ float *pool_page(const PrefillArgs &a, int slot, int h) {
+    return a.pool + (uint64_t)slot * a.slot_floats + a.layer_off + (uint64_t)h * kN;
+}
 
-// The work of one CTA of a persistent grid: items blockIdx.x, + gridDim.x, ... that have
-// tokens. Every warp walks it alike.
-struct Items {
-    const PrefillArgs &a;
-    int item, h, row, len;
-    __device__ __forceinline__ explicit Items(const PrefillArgs &args) : a(args), item((int)blockIdx.x - (int)gridDim.x) {}
-    // lead: the thread that raises what is wrong with a sequence (one of a CTA's warps)
-    __device__ __forceinline__ bool next(bool lead = false) {
-#pragma unroll 1
-        for (item += gridDim.x; item < a.items; item += gridDim.x) {
-            b = item / a.Hv;
-            h = item - b * a.Hv;
-            if (sequence(a, b, lead, row, len, slot) && len > 0) return true;
-        }
-        return false;
-    }
-    __device__ __forceinline__ float *page() const {
-        return a.pool + (uint64_t)slot * a.slot_floats + a.layer_off + (uint64_t)h * kN;
-    }
-    __device__ __forceinline__ const float *state_in() const { return !a.resume || a.resume[b] ? page() : nullptr; }
-    __device__ __forceinline__ float *state_out() const { return page(); }
-    __device__ __forceinline__ float *total_out() const { return nullptr; }
-
-  private:
-    int b, slot;
+// Tokens of a segment for a call, and the most segments it can make.
+struct Split {
+    int segment, most;
+    bool on;                           // whether a sequence may be split
 };
+Split split_of(int Hv, int B, int tokens, int max_len);
 
-// linattn_chunks.cu
+// linattn_plan.cu: the segments; the states before the segments of split sequences from the
+// segments' own parts
+stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s);
+stepq_status launch_linattn_join(const PrefillArgs &a, cudaStream_t s);
+// linattn_chunks.cu. prepare: what a launch needs of the runtime and the driver; parts: also the
+// pass with out = false, which forms only the segments' own parts of the state
+struct ChunkMaps {
+    CUtensorMap of[3];                 // k, q, v
+};
 bool linattn_chunks_takes(const stepq_config *cfg, const stepq_linattn_io *io);
-stepq_status launch_linattn_chunks(const PrefillArgs &a, int items, bool out, cudaStream_t s);
+stepq_status prepare_linattn_chunks(const PrefillArgs &a, bool parts, ChunkMaps &maps);
+stepq_status launch_linattn_chunks(const PrefillArgs &a, const ChunkMaps &maps, int grid, bool out, cudaStream_t s);
 
 }  // namespace la
 }  // namespace stepq

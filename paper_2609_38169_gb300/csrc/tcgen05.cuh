@@ -251,6 +251,24 @@ __device__ __forceinline__ void st8(uint32_t taddr, const uint32_t (&v)[8]) {
                  "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                  : "memory");
 }
+// 16 lanes (from the lane in taddr) x 32 columns, as 8 x 8 matrices of 16-bit pairs: thread t
+// holds, of lanes t / 4 (v[2 i]) and t / 4 + 8 (v[2 i + 1]), column 4 i + t % 4.
+__device__ __forceinline__ void st_16x32(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+            taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+// Four 8 x 8 matrices of 16-bit values, transposed: lane l gives the address of row l % 8 of
+// matrix l / 8; thread t receives of each matrix column t / 4 its rows 2 (t % 4) and + 1.
+__device__ __forceinline__ void load_transposed(const void *row, uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(a), "=r"(b), "=r"(c), "=r"(d)
+                 : "r"(smem_addr(row))
+                 : "memory");
+}
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // What x has beyond its TF32 head, exact: kind::tf32 reads an fp32 operand, from

@@ -52,20 +52,24 @@ inline NormArgs norm_args(const stepq_norm *n) {
 }
 
 // act(x), without branches. Vectors of 16 bits leave a result 8 or 11 bits: the fast exponential
-// and quotient (a few units in 2^-23, and 2^-24 |x| from the exponent's product) are far below
-// that. fp32 results take expf and the rounded quotient.
+// and reciprocal (a few units in 2^-23, and 2^-24 |x| from the exponent's product) are far
+// below that. fp32 results take expf and the rounded quotient.
 template <class T>
 __device__ __forceinline__ float activation(int act, float x) {
-    const float e = sizeof(T) == 2 ? __expf(-x) : expf(-x);
-    const float num = act == STEPQ_ACT_SIGMOID ? 1.f : x, den = act == STEPQ_ACT_NONE ? 1.f : 1.f + e;
-    return sizeof(T) == 2 ? __fdividef(num, den) : num / den;
+    const float num = act == STEPQ_ACT_SIGMOID ? 1.f : x;
+    if (sizeof(T) == 2) {
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
+        return act == STEPQ_ACT_NONE ? x : num * r;
+    }
+    return act == STEPQ_ACT_NONE ? x : num / (1.f + expf(-x));
 }
 
 // out = u act(z) or act(u) of one channel, u = xc * rstd * w + b with xc = x - mean.
 template <class T>
 __device__ __forceinline__ float norm_out(const NormArgs &n, float xc, float rstd, float w, float b, float z) {
-    const float u = fmaf(xc * rstd, w, b);
-    return (n.z ? u : 1.f) * activation<T>(n.act, n.z ? z : u);
+    const float u = fmaf(xc * rstd, w, b), a = activation<T>(n.act, n.z ? z : u);
+    return n.z ? u * a : a;
 }
 
 __device__ __forceinline__ float rstd_of(float var, float eps) { return rsqrtf(var + eps); }
@@ -84,41 +88,35 @@ struct HeadAffine {
 };
 
 // One head's readouts of N tokens in a warp, lane l holding channels 4 l .. 4 l + 3 (z: of the
-// gate, if there is one): their sums cross the warp together.
+// gate, if there is one). Mean m and centred sum of squares q of ever larger parts in one
+// butterfly: of two parts of n values each, m = (m1 + m2) / 2 and q = q1 + q2 + (m1 - m2)^2 n / 2,
+// which cancels nothing; the sum of squares about zero is q + 128 m^2.
 template <class T, int N>
 __device__ __forceinline__ void norm_head(const NormArgs &n, const HeadAffine &p, const Vec<T, 4> *z, float (&y)[N][4]) {
-    float s[N], m[N];
+    float m[N], q[N];
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        m[i] = 0.f;
-        s[i] = (y[i][0] + y[i][1]) + (y[i][2] + y[i][3]);
+        m[i] = 0.25f * ((y[i][0] + y[i][1]) + (y[i][2] + y[i][3]));
+        q[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) q[i] = fmaf(y[i][e] - m[i], y[i][e] - m[i], q[i]);
     }
-    if (n.center) {
+    float half = 2.f;                                       // of the values in a part
 #pragma unroll
-        for (int o = 16; o; o >>= 1)
+    for (int o = 1; o < 32; o *= 2, half *= 2.f)
 #pragma unroll
-            for (int i = 0; i < N; i++) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
-#pragma unroll
-        for (int i = 0; i < N; i++) m[i] = s[i] * (1.f / kD);
-    }
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        s[i] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            y[i][e] -= m[i];
-            s[i] = fmaf(y[i][e], y[i][e], s[i]);
+        for (int i = 0; i < N; i++) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m[i], o), d = m[i] - m2;
+            q[i] += __shfl_xor_sync(0xffffffffu, q[i], o);
+            q[i] = fmaf(d * half, d, q[i]);
+            m[i] = 0.5f * (m[i] + m2);
         }
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; i++) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        const float r = rstd_of(s[i] * (1.f / kD), n.eps);
+        const float c = n.center ? m[i] : 0.f;
+        const float r = rstd_of(fmaf(m[i] - c, m[i], q[i] * (1.f / kD)), n.eps);
 #pragma unroll
-        for (int e = 0; e < 4; e++) y[i][e] = norm_out<T>(n, y[i][e], r, p.w[e], p.b[e], to_f32(z[i].e[e]));
+        for (int e = 0; e < 4; e++) y[i][e] = norm_out<T>(n, y[i][e] - c, r, p.w[e], p.b[e], to_f32(z[i].e[e]));
     }
 }
 

@@ -23,7 +23,7 @@
 // One persistent CTA of 28 warps per SM:
 //   warps 0-7    the state: S <- c_C S + U, its split into tensor memory (lane = value channel,
 //                warps w and w + 4 sharing lanes 32 (w % 4) ..)
-//   warps 8-15   V^T, and the outputs (lanes likewise)
+//   8 warps      V^T, and the outputs (lanes likewise)
 //   3 warps      P (lanes = tokens), a 32 x 32 block each
 //   1 warp       loads q, k and v (TMA, two places each); decays and their products
 //   2 warps      issue the MMAs: scores and PV; KV and QS
@@ -53,7 +53,12 @@ constexpr int kTile = C * 128;                          // 64 rows of 128 bytes:
 constexpr int kOffK = 0, kOffQ = kOffK + kPlaces * 2 * kTile, kOffV = kOffQ + kPlaces * 2 * kTile;   // [place][2 tiles]
 constexpr int kOffKp = kOffV + kPlaces * 2 * kTile;     // K': [term][2 tiles]
 constexpr int kOffP = kOffKp + 3 * 2 * kTile;           // P: [place][head, rest]
-constexpr int kOffY = kOffP + kPlaces * 2 * kTile;      // float [C][128] readouts to normalise
+// Where readouts are normalised, P has one place, to make room for them, the gate and the
+// affine map: float [C][128], bf16 [C][128], float [2][128].
+template <bool NORM> constexpr int kPlacesP = NORM ? 1 : kPlaces;
+template <bool NORM> constexpr int kOffY = kOffP + kPlacesP<NORM> * 2 * kTile;
+template <bool NORM> constexpr int kOffZ = kOffY<NORM> + (NORM ? C * kD * 4 : 0);
+template <bool NORM> constexpr int kOffAffine = kOffZ<NORM> + (NORM ? C * kD * 2 : 0);
 struct alignas(16) Gates {
     float next[C], c[C], wk[C];                         // g_{t+1}, c_t, w_Cs (0 past the last token)
     float suf[32], pre[32];                             // w_{31,s} of the first half, c_t / c_31 of the second
@@ -65,7 +70,7 @@ struct alignas(16) Item {
     float *out, *total;                                 // the state after it, its decays' product, or null
     int row, len, h, pad;                               // len 0: no more items
 };
-template <bool NORM> constexpr int kOffG = kOffY + (NORM ? C * kD * 4 : 0);
+template <bool NORM> constexpr int kOffG = kOffAffine<NORM> + (NORM ? 2 * kD * 4 : 0);
 template <bool NORM> constexpr int kOffItem = kOffG<NORM> + kRing * (int)sizeof(Gates);
 template <bool NORM> constexpr int kOffBar = kOffItem<NORM> + kRing * (int)sizeof(Item);
 enum {
@@ -125,7 +130,7 @@ struct Ctx {
 // Barriers of the groups of warps. Within a group one warp waits for the phases and the
 // others for it: a waiting warp tests every 140 cycles or so, and 28 of them took half of
 // the SM's issue slots.
-enum { kSyncNone, kSyncState, kSyncOut, kSyncKeys, kSyncScores, kSyncs };
+enum { kSyncNone, kSyncState, kSyncOut, kSyncKeys, kSyncScores };
 template <int ID, int WARPS>
 __device__ __forceinline__ void group_sync() {
     asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(32 * WARPS) : "memory");
@@ -322,7 +327,7 @@ __device__ __forceinline__ void issue_scores(const Ctx<NORM> &x, uint32_t tm) {
         x.template wait_full<kPlaces>(kVtReady, m);
         x.wait_last(kYFree, m);
         tc::fence_after();
-        const uint64_t p = operand(x, kOffP, m, 16);
+        const uint64_t p = operand(x, kOffP, kPlacesP<NORM> > 1 ? m : 0, 16);
 #pragma unroll 1
         for (int i = 1; i >= 0; i--)                        // rest, head
 #pragma unroll
@@ -439,8 +444,8 @@ __device__ __forceinline__ void scale(const Ctx<NORM> &x, int w) {
     }
 }
 
-// V^T of chunk n, m tokens, into tensor memory: 16 channels of this warp's quadrant. Rows past the last token belong to other sequences:
-// zeros take their place.
+// V^T of chunk n, m tokens, into tensor memory: 16 channels (half h) of this warp's
+// quadrant. Rows past the last token belong to other sequences: zeros take their place.
 template <bool NORM>
 __device__ __forceinline__ void transpose_v(const Ctx<NORM> &x, uint32_t tm, uint32_t n, int m, int h) {
     const int l = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3;
@@ -480,21 +485,21 @@ __device__ __forceinline__ void weigh_scores(const Ctx<NORM> &x, uint32_t tm, in
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
             if (quad == 0) {
                 x.template wait_full<x.R>(kFullG, n);
-                x.template wait_free<kPlaces>(kVtFree, n);  // PV of two chunks ago has read the place
+                if (kPlacesP<NORM> > 1) x.template wait_free<kPlaces>(kVtFree, n);     // PV has read the place
+                else x.wait_last(kPv, n);
                 x.wait(kScores, n & 1u);
             }
             group_sync<kSyncScores, 3>();
             tc::fence_after();
             const Gates &g = x.gates(n);
-            uint8_t *row = x.smem + kOffP + (n % kPlaces) * 2 * kTile + t * 128;
+            uint8_t *row = x.smem + kOffP + (n % kPlacesP<NORM>) * 2 * kTile + t * 128;
             const uint64_t pre = f2s(g.pre[l]);
             const int m = it.len - t0;                      // keys past the last: other sequences' rows
             float w = 0.f;
 #pragma unroll 1
             for (int b = 2 * half + 1; b >= 2 * half; b--) { // keys 16 b .. + 15
                 uint32_t u[16];
-                tc::ld16_start(tl + 16 * b, u);
-                tc::wait_ld(u);
+                tc::ld16(tl + 16 * b, u);
                 uint64_t f[8];                              // the weights
                 if (half < quad) {
 #pragma unroll
@@ -601,58 +606,134 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
     }
 }
 
+// u act(z) or act(u) for a pair of channels (stepq_norm), u = y A + B.
+struct GateForm {
+    float zu, uz1, uz0, num1, num0;                         // t = z + zu u, out = act(t) (uz1 u + uz0), act's numerator num1 t + num0
+    bool none;
+    __device__ __forceinline__ explicit GateForm(const NormArgs &n)
+        : zu(n.z ? 0.f : 1.f), uz1(n.z ? 1.f : 0.f), uz0(n.z ? 0.f : 1.f), num1(n.act == STEPQ_ACT_SIGMOID ? 0.f : 1.f),
+          num0(n.act == STEPQ_ACT_SIGMOID ? 1.f : 0.f), none(n.act == STEPQ_ACT_NONE) {}
+    __device__ __forceinline__ uint64_t operator()(uint64_t y, uint64_t A, uint64_t B, uint64_t z) const {
+        const uint64_t u = ffma2(y, A, B), t = ffma2(f2s(zu), u, z);
+        const uint64_t x = fmul2(t, f2s(-1.44269504f));     // exp(-t) = 2^x
+        float e0, e1;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(f2lo(x)));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(f2hi(x)));
+        const uint64_t d = fadd2(f2(e0, e1), f2s(1.f));
+        float r0, r1;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(f2lo(d)));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(f2hi(d)));
+        const uint64_t r = none ? f2s(1.f) : f2(r0, r1);
+        return fmul2(fmul2(ffma2(t, f2s(num1), f2s(num0)), r), ffma2(u, f2s(uz1), f2s(uz0)));
+    }
+};
+
+// Normalises the chunk's readouts ys [C][128], its first m tokens, into y. Eight lanes a token,
+// lane k of them channels 32 i + 4 k .. + 3: with 32 lanes a token the sums' five steps took as
+// long as the rest. Means and centred sums of squares of ever larger parts: see norm_head.
+__device__ __forceinline__ void norm_chunk(const PrefillArgs &a, const float *ys, const bf16 *zs, const float *affine, bf16 *y,
+                                           int m, int w, int l) {
+    const int k = l & 7;
+    const GateForm gate(a.norm);
+#pragma unroll 1
+    for (int t = 4 * w + (l >> 3); t < C; t += 32) {
+        uint64_t v[8];
+        float mean = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float4 u = *(const float4 *)&ys[t * kD + 32 * i + 4 * k];
+            v[2 * i] = f2(u.x, u.y);
+            v[2 * i + 1] = f2(u.z, u.w);
+            mean += (u.x + u.y) + (u.z + u.w);
+        }
+        mean *= 1.f / 16;
+        uint64_t q2 = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint64_t d = fsub2(v[i], f2s(mean));
+            q2 = ffma2(d, d, q2);
+        }
+        float q = f2lo(q2) + f2hi(q2);
+#pragma unroll
+        for (int o = 1; o < 8; o *= 2) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, mean, o), d = mean - m2;
+            q += __shfl_xor_sync(0xffffffffu, q, o);
+            q = fmaf(d * (8.f * o), d, q);
+            mean = 0.5f * (mean + m2);
+        }
+        const float c = a.norm.center ? mean : 0.f, r = rstd_of(fmaf(mean - c, mean, q * (1.f / kD)), a.norm.eps);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int ch = 32 * i + 4 * k;
+            const ulonglong2 w4 = *(const ulonglong2 *)&affine[ch], b4 = *(const ulonglong2 *)&affine[kD + ch];
+            uint2 z = *(const uint2 *)&zs[t * kD + ch];
+            if (!a.norm.z) z = make_uint2(0, 0);
+            const uint64_t o0 = gate(fsub2(v[2 * i], f2s(c)), fmul2(w4.x, f2s(r)), b4.x, u2pair(z.x << 16, z.x & 0xFFFF0000u));
+            const uint64_t o1 = gate(fsub2(v[2 * i + 1], f2s(c)), fmul2(w4.y, f2s(r)), b4.y, u2pair(z.y << 16, z.y & 0xFFFF0000u));
+            if (t < m) *(uint2 *)(y + t * a.ys + ch) = make_uint2(rounded(o0), rounded(o1));
+        }
+    }
+}
+
 // V^T of the next chunk, and the outputs. This thread: value channel j of tokens 32 half .. + 31,
 // a warp's 64 bytes of a token straight from registers (16-byte pieces by way of stmatrix and
 // shared memory: a tenth fewer instructions, but 5% slower for the shared memory they take);
-// or, to be normalised, through shared memory, where a token's 128 channels come together in
-// a warp.
+// or, to be normalised, through shared memory, where a token's 128 channels come together.
 template <bool OUT, bool NORM>
 __device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
     constexpr int W = kOutWarps;
     const PrefillArgs &a = x.a;
     const int w = (threadIdx.x >> 5) - 8, l = threadIdx.x & 31, quad = w & 3, half = w >> 2, j = 32 * quad + l;
     const uint32_t tl = tm + ((uint32_t)(32 * quad) << 16) + 32 * half;
-    float *ys = (float *)(x.smem + kOffY);
+    float *ys = (float *)(x.smem + kOffY<NORM>), *affine = (float *)(x.smem + kOffAffine<NORM>);
+    bf16 *zs = (bf16 *)(x.smem + kOffZ<NORM>);
     uint32_t n = 0;
     // V^T runs a chunk ahead, into the next item's first: that item is known by then
     Items<NORM, kSyncOut, W> ahead(x, w == 0);
     bool more = ahead.next();
-    if (more) transpose_v(x, tm, 0, ahead.len, half);
+    int next = ahead.len;                                   // tokens of its item from chunk v on
+    uint32_t v = 0;
     while (more) {
         const int row = ahead.row, len = ahead.len, h = ahead.h;
         bf16 *y = (bf16 *)a.y + (int64_t)row * a.ys + h * kD;
         const bf16 *z = (const bf16 *)a.norm.z + (int64_t)row * a.norm.z_stride + h * kD;
+        if (NORM) {                                         // (no warp reads the last item's any more)
+            const int c = threadIdx.x & (kD - 1), pc = c + (a.norm.shared ? 0 : h * kD);
+            if (threadIdx.x & kD) affine[c] = a.norm.w ? a.norm.w[pc] : 1.f;
+            else affine[kD + c] = a.norm.b ? a.norm.b[pc] : 0.f;
+        }
 #pragma unroll 1
         for (int t0 = 0; t0 < len; t0 += C, n++) {
-            int next = len - t0 - C;                        // tokens of the next chunk and on
-            if (next <= 0) {
-                more = ahead.next();
-                next = ahead.len;
+#pragma unroll 1
+            for (; v <= n + 1; v++, next -= C) {
+                if (next <= 0) {
+                    more = ahead.next();
+                    next = ahead.len;
+                    if (!more) break;
+                }
+                transpose_v(x, tm, v, next, half);
             }
-            if (more) transpose_v(x, tm, n + 1, next, half);
             if (!OUT) continue;
             const int m = min(C, len - t0);
-            Vec<bf16, 4> g[NORM ? 8 : 1];                   // the gate of tokens w, w + 8, ..., on its way before it is needed
-            if (NORM && a.norm.z)
+            if (NORM && a.norm.z)                           // the gate, on its way before it is needed
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    g[i] = *(const Vec<bf16, 4> *)(z + min(w + 8 * i, m - 1) * a.norm.z_stride + 4 * l);
+                for (int i = 0; i < 4; i++) {
+                    const int t = 2 * w + (l >> 4) + 16 * i;
+                    cp_async16_or_zero(zs + t * kD + 8 * (l & 15), z + min(t, m - 1) * a.norm.z_stride + 8 * (l & 15), t < m);
+                }
             if (w == 0) {
                 x.template wait_full<x.R>(kFullG, n);
                 x.wait(kPv, n & 1u);
                 x.wait(kQs, n & 1u);
             }
-            group_sync<kSyncOut, W>();                      // and the chunk before's readouts have left the place
+            group_sync<kSyncOut, W>();
             tc::fence_after();
             const float *c = x.gates(n).c + 32 * half;
             bf16 *yt = y + 32 * half * a.ys + j;
 #pragma unroll 1
             for (int i = 0; i < 32; i += 16) {
                 uint32_t y1[16], y2[16];
-                tc::ld16_start(tl + kColY1 + i, y1);
-                tc::ld16_start(tl + kColY2 + i, y2);
-                tc::wait_ld(y1);
-                tc::wait_ld(y2);
+                tc::ld16_two(tl + kColY1 + i, y1, tl + kColY2 + i, y2);
                 if (i == 16) {
                     tc::fence_before();
                     x.arrive(kYFree);
@@ -661,12 +742,12 @@ __device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
                 const int left = m - 32 * half - i;
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                    const uint64_t v = ffma2(pair_at(&c[i + e]), u2pair(y1[e], y1[e + 1]), u2pair(y2[e], y2[e + 1]));
+                    const uint64_t u = ffma2(pair_at(&c[i + e]), u2pair(y1[e], y1[e + 1]), u2pair(y2[e], y2[e + 1]));
                     if (NORM) {
-                        p[e * kD] = f2lo(v);
-                        p[(e + 1) * kD] = f2hi(v);
+                        p[e * kD] = f2lo(u);
+                        p[(e + 1) * kD] = f2hi(u);
                     } else {
-                        const uint32_t b = rounded(v);
+                        const uint32_t b = rounded(u);
                         if (e < left) *(uint16_t *)yt = (uint16_t)b;
                         yt += a.ys;
                         if (e + 1 < left) *(uint16_t *)yt = (uint16_t)(b >> 16);
@@ -676,19 +757,10 @@ __device__ __forceinline__ void outputs(const Ctx<NORM> &x, uint32_t tm) {
             }
             x.arrive(kFreeG + n % x.R);
             if (NORM) {
+                cp_async_wait_all();
                 group_sync<kSyncOut, W>();
-                const HeadAffine p(a.norm, h, l);
-                constexpr int N = 4;                        // tokens at a time
-#pragma unroll
-                for (int k = 0; k < 8; k += N) {
-                    float v[N][4];
-#pragma unroll
-                    for (int i = 0; i < N; i++) load_vec<float, 4>(&ys[(w + 8 * (k + i)) * kD + 4 * l], v[i]);
-                    norm_head<bf16, N>(a.norm, p, &g[k], v);
-#pragma unroll
-                    for (int i = 0; i < N; i++)
-                        if (w + 8 * (k + i) < m) store_vec<bf16, 4>(y + (w + 8 * (k + i)) * a.ys + 4 * l, v[i]);
-                }
+                norm_chunk(a, ys, zs, affine, y, m, w, l);
+                group_sync<kSyncOut, W>();                  // the readouts' and the gate's places are free again
                 z += C * a.norm.z_stride;
             }
             y += C * a.ys;
@@ -707,22 +779,22 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
         tc::tmem_relinquish();
     }
     if (tid < kBars) {
-        int count = 1;                                      // TMA, the end of MMAs, the decays
+        int count = 1;                                      // TMA, the end of MMAs, the decays, items
         if (tid >= kFreeK && tid < kFreeQ) count = kScaleWarps + (OUT ? 1 : 0);            // K', the scores
         if (tid >= kFreeQ && tid < kFreeV) count = OUT ? 2 : 1;                            // scores, QS
-        if (tid >= kFreeV && tid < kVtFree) count = kOutWarps;                       // the warps of V^T
+        if (tid >= kFreeV && tid < kVtFree) count = kOutWarps;                             // V^T (and kVtReady)
         if (tid >= kVtFree && tid < kPReady) count = OUT ? 2 : 1;                          // KV, PV
         if (tid >= kPReady && tid < kKpReady) count = 3;
-        if (tid >= kFreeItem && tid < kScores) count = 9 + kScaleWarps + kOutWarps + (OUT ? 4 : 0);     // state, MMAs, K', V^T; P, scores
-        if (tid >= kFreeG && tid < kFullItem) count = 8 + kScaleWarps + (OUT ? 3 + kOutWarps : 0);      // state, K', P, outputs
         if (tid >= kKpReady && tid < kKpFree) count = kScaleWarps;
+        if (tid >= kFreeG && tid < kFullItem) count = 8 + kScaleWarps + (OUT ? 3 + kOutWarps : 0);     // state, K', P, outputs
+        if (tid >= kFreeItem && tid < kScores) count = 9 + kScaleWarps + kOutWarps + (OUT ? 4 : 0);    // and the MMAs
         if (tid >= kSReady && tid < kYFree) count = 8;
         if (tid == kYFree) count = kOutWarps;
         mbar_init(&bars[tid], count);
         mbar_init_fence();
     }
     if (OUT && w >= 8 && w < 10) {                          // P's block above the diagonal stays zero
-        for (int i = tid - 256; i < kPlaces * 2 * 32 * 4; i += 64) {
+        for (int i = tid - 256; i < kPlacesP<NORM> * 2 * 32 * 4; i += 64) {
             const int t = (i >> 2) & 31, o = ((4 + (i & 3)) ^ (t & 7)) * 16;
             *(uint4 *)(smem + kOffP + (i >> 7) * kTile + t * 128 + o) = make_uint4(0, 0, 0, 0);
         }

@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "async.cuh"
 #include "internal.h"
 
 namespace stepq {
@@ -51,18 +52,29 @@ inline NormArgs norm_args(const stepq_norm *n) {
     return {n->weight, n->bias, n->z, n->z_stride, n->eps, n->act, n->center, n->shared, 1};
 }
 
-// act(x), without branches. Vectors of 16 bits leave a result 8 or 11 bits: the fast exponential
-// and reciprocal (a few units in 2^-23, and 2^-24 |x| from the exponent's product) are far
-// below that. fp32 results take expf and the rounded quotient.
+// act(x). Vectors of 16 bits leave a result 8 or 11 bits: the fast exponential and reciprocal (a
+// few units in 2^-23, and 2^-24 |x| from the exponent's product) are far below that. fp32 results
+// take expf and the rounded quotient.
+__device__ __forceinline__ float fast_sigmoid(float scaled) {  // of x, scaled = -x / ln 2
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(scaled));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+}
+constexpr float kToExponent = -1.44269504f;
+
 template <class T>
 __device__ __forceinline__ float activation(int act, float x) {
-    const float num = act == STEPQ_ACT_SIGMOID ? 1.f : x;
-    if (sizeof(T) == 2) {
-        float r;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
-        return act == STEPQ_ACT_NONE ? x : num * r;
-    }
-    return act == STEPQ_ACT_NONE ? x : num / (1.f + expf(-x));
+    if (act == STEPQ_ACT_NONE) return x;
+    if (sizeof(T) == 2) return (act == STEPQ_ACT_SIGMOID ? 1.f : x) * fast_sigmoid(x * kToExponent);
+    return (act == STEPQ_ACT_SIGMOID ? 1.f : x) / (1.f + expf(-x));
+}
+
+// A pair of a 16-bit type's.
+__device__ __forceinline__ uint64_t activation2(int act, uint64_t x) {
+    if (act == STEPQ_ACT_NONE) return x;
+    const uint64_t t = fmul2(x, f2s(kToExponent)), r = f2(fast_sigmoid(f2lo(t)), fast_sigmoid(f2hi(t)));
+    return act == STEPQ_ACT_SIGMOID ? r : fmul2(x, r);
 }
 
 // out = u act(z) or act(u) of one channel, u = xc * rstd * w + b with xc = x - mean.

@@ -606,25 +606,16 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
     }
 }
 
-// u act(z) or act(u) for a pair of channels (stepq_norm), u = y A + B.
+// u act(z) or act(u) for a pair of channels (stepq_norm), u = y A + B, by selects alone: branches
+// cost a normalised prompt a tenth of its time.
 struct GateForm {
-    float zu, uz1, uz0, num1, num0;                         // t = z + zu u, out = act(t) (uz1 u + uz0), act's numerator num1 t + num0
-    bool none;
+    bool gated, none, sigmoid;
     __device__ __forceinline__ explicit GateForm(const NormArgs &n)
-        : zu(n.z ? 0.f : 1.f), uz1(n.z ? 1.f : 0.f), uz0(n.z ? 0.f : 1.f), num1(n.act == STEPQ_ACT_SIGMOID ? 0.f : 1.f),
-          num0(n.act == STEPQ_ACT_SIGMOID ? 1.f : 0.f), none(n.act == STEPQ_ACT_NONE) {}
+        : gated(n.z), none(n.act == STEPQ_ACT_NONE), sigmoid(n.act == STEPQ_ACT_SIGMOID) {}
     __device__ __forceinline__ uint64_t operator()(uint64_t y, uint64_t A, uint64_t B, uint64_t z) const {
-        const uint64_t u = ffma2(y, A, B), t = ffma2(f2s(zu), u, z);
-        const uint64_t x = fmul2(t, f2s(-1.44269504f));     // exp(-t) = 2^x
-        float e0, e1;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(f2lo(x)));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(f2hi(x)));
-        const uint64_t d = fadd2(f2(e0, e1), f2s(1.f));
-        float r0, r1;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(f2lo(d)));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(f2hi(d)));
-        const uint64_t r = none ? f2s(1.f) : f2(r0, r1);
-        return fmul2(fmul2(ffma2(t, f2s(num1), f2s(num0)), r), ffma2(u, f2s(uz1), f2s(uz0)));
+        const uint64_t one = f2s(1.f), u = ffma2(y, A, B), t = gated ? z : u, x = fmul2(t, f2s(kToExponent));
+        const uint64_t r = f2(fast_sigmoid(f2lo(x)), fast_sigmoid(f2hi(x)));
+        return fmul2(fmul2(sigmoid ? one : t, none ? one : r), gated ? u : one);
     }
 };
 

@@ -257,6 +257,27 @@ def test_decode_continues_a_prompt(dt):
     R.assert_within(pool[0, 0], S, 64 * R.U * Sa, "state")
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tokens", [0, 9, 100])
+def test_infinite_gates(tokens, dt):
+    """A sigmoid gate of plus infinity passes the normalised readout, of minus infinity stops it
+    (0 tokens: one a sequence, by the decode step)."""
+    hk, hv, n = 2, 4, tokens or 3
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    q, k, v, z, gate = inputs(g, n, hk, hv, dt)
+    cfg, got = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv), []
+    for act, fill in ((A.ACT_NONE, 1.0), (A.ACT_SIGMOID, torch.inf), (A.ACT_SIGMOID, -torch.inf)):
+        pool = torch.ones((n, 1, hv, D, D), device="cuda")
+        y, norm = torch.empty((n, hv, D), dtype=dt, device="cuda"), A.Norm(z=torch.full_like(z, fill), act=act)
+        slots = torch.arange(n if not tokens else 1, dtype=torch.int32, device="cuda")
+        if tokens:
+            A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, max_len=n, norm=norm)
+        else:
+            A.stepq_linattn_decode_step(cfg, 0, pool, slots, q, k, v, gate, y, norm=norm)
+        got.append(y)
+    assert torch.equal(got[1], got[0]) and bool((got[2] == 0).all())
+
+
 # ------------------------------------------------------------------ streams, graphs, errors
 def test_side_stream_and_graph():
     """Captured on a side stream, a prompt and two tokens replay to the bytes of the calls

@@ -104,3 +104,29 @@ def test_gates_that_saturate():
         for dt in TYPES:
             out = torch.empty((2, 128), device="cuda", dtype=dt)
             check(x.to(dt), 1, out, A.Norm(z=z.to(dt), act=act))
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("rows,groups,width", [(5000, 5, 64), (9000, 32, 8), (700, 97, 24), (60, 1009, 16), (9001, 3, 75),
+                                               (1500, 7, 333), (3001, 3, 600), (2000, 1, 2048), (700, 2, 1003)])
+def test_many_rows(rows, groups, width, dt):
+    """More groups than the GPU holds at once: a team's later groups, of one column or another."""
+    g = torch.Generator(device="cuda").manual_seed(width)
+    C = groups * width
+    x, z = torch.randn((2, rows, C), generator=g, device="cuda").to(dt)
+    w, b = torch.randn((2, C), generator=g, device="cuda")
+    check(x, groups, torch.empty_like(x), A.Norm(weight=w, bias=b, z=z, act=A.ACT_SILU))
+    check(x, groups, torch.empty_like(x), A.Norm(weight=w[:width].contiguous(), act=A.ACT_NONE, center=False, shared=True))
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("width", [128, 75])
+def test_infinite_gates(width, dt):
+    """A sigmoid gate of plus infinity passes the value, of minus infinity stops it."""
+    x = torch.randn((5, 2 * width), device="cuda").to(dt)
+    z = torch.zeros_like(x)
+    z[:, ::2], z[:, 1::2] = torch.inf, -torch.inf
+    got, want = torch.empty_like(x), torch.empty_like(x)
+    A.stepq_group_norm(x, 2, got, A.Norm(z=z, act=A.ACT_SIGMOID))
+    A.stepq_group_norm(x, 2, want, A.Norm(act=A.ACT_NONE))
+    assert torch.equal(got[:, ::2], want[:, ::2]) and bool((got[:, 1::2] == 0).all())

@@ -42,8 +42,7 @@ class StepqLinattnIo(C.Structure):
 
 
 CFG = C.POINTER(StepqConfig)
-IO = C.POINTER(StepqLinattnIo)
-NORM = C.POINTER(StepqNorm)
+IO = NORM = P           # a structure by reference, or its bytes (api.py packs them: a tenth of a Structure's time)
 
 # name -> (restype, argtypes); the exported symbol set of include/stepq.h
 SIGNATURES = {

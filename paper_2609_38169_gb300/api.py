@@ -7,6 +7,7 @@ library raises: there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass, field
 
 import numpy as np
@@ -19,6 +20,9 @@ GATE_SCALAR = 0
 GATE_CHANNEL = 1
 PIVOT_BITS = 16
 ACT_NONE, ACT_SILU, ACT_SIGMOID = 0, 1, 2
+
+
+_CONFIGS: dict = {}
 
 
 @dataclass
@@ -40,6 +44,17 @@ class Config:
         return StepqConfig(self.dk, self.dv, self.n_layers, self.n_key_heads, self.n_value_heads,
                            self.gate_kind, self.nominal_bits, len(self.candidates),
                            (C.c_int * 4)(*cs), self.n_pivots, self.horizon, self.fit_iters)
+
+    def c_ref(self):
+        """A reference to the C structure, kept from call to call by the fields' values."""
+        key = (self.dk, self.dv, self.n_layers, self.n_key_heads, self.n_value_heads, self.gate_kind, self.nominal_bits,
+               tuple(self.candidates), self.n_pivots, self.horizon, self.fit_iters)
+        ref = _CONFIGS.get(key)
+        if ref is None:
+            if len(_CONFIGS) >= 64:
+                _CONFIGS.clear()
+            ref = _CONFIGS[key] = C.byref(self.c())
+        return ref
 
     @classmethod
     def from_workload(cls, wl, **kw) -> "Config":
@@ -444,6 +459,8 @@ class Norm:
 
 
 _DTYPES: dict = {}
+_pack_norm = struct.Struct("@iiifPPPq").pack           # the layout of _lib.StepqNorm
+_pack_io = struct.Struct("@i4xPPPPPqqqqq").pack       # of _lib.StepqLinattnIo
 
 
 def _dtype_code(dtype) -> int:
@@ -484,9 +501,9 @@ def _c_norm(norm, dtype, rows, channels, width):
     if norm is None:
         return None
     n = width if norm.shared else channels
-    z, zs = (None, 0) if norm.z is None else _rows_ptr(norm.z, dtype, rows, channels, "z")
-    return C.byref(_lib.StepqNorm(norm.act, int(norm.center), int(norm.shared), norm.eps,
-                                  _param_ptr(norm.weight, n, "weight"), _param_ptr(norm.bias, n, "bias"), z, zs))
+    z, zs = (0, 0) if norm.z is None else _rows_ptr(norm.z, dtype, rows, channels, "z")
+    return _pack_norm(norm.act, norm.center, norm.shared, norm.eps, _param_ptr(norm.weight, n, "weight") or 0,
+                      _param_ptr(norm.bias, n, "bias") or 0, z, zs)
 
 
 def _linattn_io(cfg, q, k, v, gate, y):
@@ -499,7 +516,7 @@ def _linattn_io(cfg, q, k, v, gate, y):
         gp, gs = _param_ptr(gate, Hv, "gate"), 0
     else:
         gp, gs = _rows_ptr(gate, _f32(), n, Hv, "gate")
-    return _lib.StepqLinattnIo(_dtype_code(dt), qp, kp, vp, gp, yp, qs, ks, vs, gs, ys)
+    return _pack_io(_dtype_code(dt), qp, kp, vp, gp, yp, qs, ks, vs, gs, ys)
 
 
 def stepq_linattn_decode_step(cfg: Config, layer: int, pool, slots, q, k, v, gate, y, norm: Norm | None = None,
@@ -510,19 +527,17 @@ def stepq_linattn_decode_step(cfg: Config, layer: int, pool, slots, q, k, v, gat
     f, B = _f32(), slots.numel()
     if q.shape[0] != B:
         raise ValueError(f"q: expected {B} rows, got {q.shape[0]}")
-    c = cfg.c()
     io = _linattn_io(cfg, q, k, v, gate, y)
     Hv = cfg.n_value_heads
-    check(_lib.lib().stepq_linattn_decode_step(C.byref(c), layer, _dev_ptr(pool, f),
+    check(_lib.lib().stepq_linattn_decode_step(cfg.c_ref(), layer, _dev_ptr(pool, f),
                                                int(pool.shape[0] if pool_slots is None else pool_slots),
-                                               _dev_ptr(slots, _Torch.i32), B, C.byref(io),
+                                               _dev_ptr(slots, _Torch.i32), B, io,
                                                _c_norm(norm, q.dtype, B, Hv * D, D), _stream(stream)),
           "stepq_linattn_decode_step")
 
 
 def stepq_linattn_workspace_bytes(cfg: Config, B: int, tokens: int, max_len: int = 0) -> int:
-    c = cfg.c()
-    return int(_lib.lib().stepq_linattn_workspace_bytes(C.byref(c), int(B), int(tokens), int(max_len)))
+    return int(_lib.lib().stepq_linattn_workspace_bytes(cfg.c_ref(), int(B), int(tokens), int(max_len)))
 
 
 def stepq_linattn_prefill(cfg: Config, layer: int, pool, slots, q, k, v, gate, y, cu_seqlens=None, max_len: int = 0,
@@ -534,20 +549,20 @@ def stepq_linattn_prefill(cfg: Config, layer: int, pool, slots, q, k, v, gate, y
     for t, m, what in ((cu_seqlens, B + 1, "cu_seqlens"), (resume, B, "resume")):
         if t is not None and t.numel() != m:
             raise ValueError(f"{what}: expected {m} values, got {t.numel()}")
-    c = cfg.c()
+    c = cfg.c_ref()
     lib = _lib.lib()
     io = _linattn_io(cfg, q, k, v, gate, y)
-    nbytes = lib.stepq_linattn_workspace_bytes(C.byref(c), B, n, int(max_len)) if workspace is None else 0
+    nbytes = lib.stepq_linattn_workspace_bytes(c, B, n, int(max_len)) if workspace is None else 0
     if nbytes:
         import torch
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
         if stream is not None:                       # the block is not reused before this stream's work is done
             workspace.record_stream(stream)
     have = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    check(lib.stepq_linattn_prefill(C.byref(c), layer, _dev_ptr(pool, f),
+    check(lib.stepq_linattn_prefill(c, layer, _dev_ptr(pool, f),
                                     int(pool.shape[0] if pool_slots is None else pool_slots),
                                     _dev_ptr(slots, _Torch.i32), _dev_ptr(resume, _Torch.u8),
-                                    _dev_ptr(cu_seqlens, _Torch.i32), B, n, int(max_len), C.byref(io),
+                                    _dev_ptr(cu_seqlens, _Torch.i32), B, n, int(max_len), io,
                                     _c_norm(norm, q.dtype, n, cfg.n_value_heads * D, D), _dev_ptr(workspace), have,
                                     _stream(stream)), "stepq_linattn_prefill")
 
@@ -584,7 +599,7 @@ def stepq_calibrate_from_trace(cfg: Config, q, k, v, beta, gate, every: int, str
     import torch
     f = _f32()
     L, T, n = q.shape[0], q.shape[1], q.shape[2]
-    c = cfg.c()
+    c = cfg.c_ref()
     lib = _lib.lib()
     nbytes = lib.stepq_calib_workspace_bytes(C.byref(c), n)
     if nbytes == 0:

@@ -185,3 +185,22 @@ for name, call in calls.items():
     assert fake.fake_pending_error() == 0, name
     assert call() == 0 and fake.fake_launches() > before, name
 """)
+
+
+def test_packed_structures_are_the_declared_ones():
+    """The binding's packed arguments, byte for byte the ctypes structures'."""
+    io = _lib.StepqLinattnIo(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11)
+    assert bytes(io) == A._pack_io(1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11)
+    norm = _lib.StepqNorm(2, 1, 0, 0.5, 4, 5, 6, 7)
+    assert bytes(norm) == A._pack_norm(2, True, False, 0.5, 4, 5, 6, 7)
+
+
+def test_kept_configurations_follow_the_fields():
+    """A changed field reaches the library although the structure is kept."""
+    cfg = A.Config(n_layers=1, n_key_heads=2, n_value_heads=4)
+    before = A.stepq_linattn_workspace_bytes(cfg, 2, 4096, 4000)
+    cfg.n_value_heads = 8
+    after = A.stepq_linattn_workspace_bytes(cfg, 2, 4096, 4000)
+    assert before and after and before != after
+    cfg.n_value_heads = 4
+    assert A.stepq_linattn_workspace_bytes(cfg, 2, 4096, 4000) == before

@@ -10,10 +10,11 @@
 // eight row lanes r leave token r's in lane r (28 shuffles for 8 x 4 values), which adds its
 // block's part.
 //
-// The FMA units bound it: 3 x 333 tokens of 32 heads in fp32, 96 CTAs on 152 multiprocessors, take
-// 104 us, with those pipes 65% busy where a CTA runs (token by token: 215 us; the vectors' and
-// states' bytes alone: 12). 16 warps of 8 columns: 112, twice the shared-memory reads. CTAs of 64
-// or 32 columns: 123 and 126, every CTA forming P.
+// The FMA units and the chain of a block bound it: 3 x 333 tokens of 32 heads in fp32, 96 CTAs of
+// two warps a scheduler on 152 multiprocessors, take 96 us (token by token: 215; with P formed in
+// the block that takes it, three barriers: 104; the vectors' and states' bytes alone: 12). 16 warps
+// of 8 columns: 8% more, for twice the shared-memory reads. CTAs of 64 or 32 columns: 18 and 21%
+// more, every CTA forming P.
 #include "async.cuh"
 #include "device.cuh"
 #include "linattn_prefill.cuh"
@@ -31,8 +32,8 @@ template <class T, bool OUT, bool NORM>
 __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
     constexpr int TB = kBlockTokens, J = 4;
     static_assert(TB == 8, "a warp a token");
-    __shared__ __align__(16) BlockStage stage[2];
-    __shared__ __align__(16) float P[TB][TB];
+    __shared__ __align__(16) BlockStage stage[3];            // read, ready, and being filled
+    __shared__ __align__(16) float P[2][TB][TB];
     __shared__ __align__(16) float ys[NORM ? TB : 1][kD];
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, r = l >> 2, c = l & 3;
     griddep_wait();
@@ -91,44 +92,57 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
         *(float4 *)&s.v[t][ch] = f4(nv);
         if (tid < TB) s.g[tid] = ng;
     };
+    // P of token t = w: 4 channels a lane, eight keys' sums reduced together
+    const auto scores = [&](const BlockStage &s, float (*P)[TB]) {
+        float g[TB], p[TB];
+        load_vec<float, 4>(s.g, *(float(*)[4]) & g[0]);
+        load_vec<float, 4>(s.g + 4, *(float(*)[4]) & g[4]);
+        const float4 q = *(const float4 *)&s.q[t][4 * l];
+#pragma unroll
+        for (int i = 0; i < TB; i++) {
+            const float4 k = *(const float4 *)&s.k[i][4 * l];
+            p[i] = fmaf(q.x, k.x, q.y * k.y) + fmaf(q.z, k.z, q.w * k.w);
+        }
+#pragma unroll
+        for (int b = 0; b < 3; b++) {                        // lane bit 4 - b chooses key bit 2 - b
+            const int half = 4 >> b;
+            const bool up = l & (16 >> b);
+#pragma unroll
+            for (int i = 0; i < half; i++) {
+                const float give = up ? p[i] : p[i + half];
+                p[i] = (up ? p[i + half] : p[i]) + __shfl_xor_sync(0xffffffffu, give, 16 >> b);
+            }
+        }
+        p[0] += __shfl_xor_sync(0xffffffffu, p[0], 2);
+        p[0] += __shfl_xor_sync(0xffffffffu, p[0], 1);
+        const int key = l >> 2;
+        float wt = 1.f;
+#pragma unroll
+        for (int j = 1; j < TB; j++) wt *= j > key && j <= t ? g[j] : 1.f;
+        if ((l & 3) == 0) P[t][key] = key <= t ? p[0] * wt : 0.f;
+    };
     fetch(0);
     put(stage[0]);
-    __syncthreads();
+    if (len > TB) {
+        fetch(TB);
+        put(stage[1]);
+    }
+    if (OUT) {
+        __syncthreads();
+        scores(stage[0], P[0]);
+    }
+    int at_stage = 0;                                        // n mod 3
     for (int t0 = 0, n = 0; t0 < len; t0 += TB, n++) {
-        const BlockStage &s = stage[n & 1];
-        const bool more = t0 + TB < len;
-        if (more) fetch(t0 + TB);
+        // One barrier a block: it shows the next block's vectors and this one's P, formed ahead.
+        __syncthreads();
+        const BlockStage &s = stage[at_stage], &next = stage[at_stage == 2 ? 0 : at_stage + 1];
+        BlockStage &last = stage[at_stage == 0 ? 2 : at_stage - 1];
+        at_stage = at_stage == 2 ? 0 : at_stage + 1;
+        if (t0 + 2 * TB < len) fetch(t0 + 2 * TB);
         float g[TB];
         load_vec<float, 4>(s.g, *(float(*)[4]) & g[0]);
         load_vec<float, 4>(s.g + 4, *(float(*)[4]) & g[4]);
         if (OUT) {
-            // P of token t: 4 channels a lane, eight keys' sums reduced together
-            {
-                const float4 q = *(const float4 *)&s.q[t][4 * l];
-                float p[TB];
-#pragma unroll
-                for (int i = 0; i < TB; i++) {
-                    const float4 k = *(const float4 *)&s.k[i][4 * l];
-                    p[i] = fmaf(q.x, k.x, q.y * k.y) + fmaf(q.z, k.z, q.w * k.w);
-                }
-#pragma unroll
-                for (int b = 0; b < 3; b++) {            // lane bit 4 - b chooses key bit 2 - b
-                    const int half = 4 >> b;
-                    const bool up = l & (16 >> b);
-#pragma unroll
-                    for (int i = 0; i < half; i++) {
-                        const float give = up ? p[i] : p[i + half];
-                        p[i] = (up ? p[i + half] : p[i]) + __shfl_xor_sync(0xffffffffu, give, 16 >> b);
-                    }
-                }
-                p[0] += __shfl_xor_sync(0xffffffffu, p[0], 2);
-                p[0] += __shfl_xor_sync(0xffffffffu, p[0], 1);
-                const int key = l >> 2;
-                float wt = 1.f;
-#pragma unroll
-                for (int j = 1; j < TB; j++) wt *= j > key && j <= t ? g[j] : 1.f;
-                if ((l & 3) == 0) P[t][key] = key <= t ? p[0] * wt : 0.f;
-            }
             // S_0^T q_t: this lane's rows, then the sum over the row lanes
             float y[TB][J];
 #pragma unroll
@@ -155,14 +169,13 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
                         y[t][j] = (up ? y[t + half][j] : y[t][j]) + __shfl_xor_sync(0xffffffffu, give, 16 >> b);
                     }
             }
-            __syncthreads();                             // P
             // token r: its part of the state before the block, then the block's own
             float ct = 1.f;
 #pragma unroll
             for (int j = 0; j < TB; j++) ct *= j <= r ? g[j] : 1.f;
             float o[J], pr[TB];
-            load_vec<float, 4>(&P[r][0], *(float(*)[4]) & pr[0]);
-            load_vec<float, 4>(&P[r][4], *(float(*)[4]) & pr[4]);
+            load_vec<float, 4>(&P[n & 1][r][0], *(float(*)[4]) & pr[0]);
+            load_vec<float, 4>(&P[n & 1][r][4], *(float(*)[4]) & pr[4]);
 #pragma unroll
             for (int j = 0; j < J; j++) o[j] = ct * y[0][j];
 #pragma unroll
@@ -221,8 +234,8 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
                 }
             }
         }
-        if (more) put(stage[(n + 1) & 1]);
-        __syncthreads();
+        if (OUT && t0 + TB < len) scores(next, P[~n & 1]);
+        if (t0 + 2 * TB < len) put(last);
     }
     if (!OUT && tid == 0) *total_to = total;
     if (out)
@@ -271,9 +284,9 @@ struct Workspace {
 };
 
 // bf16 sequences of few tokens, where they are no more than fill the GPU's multiprocessors twice:
-// blocks of eight need no plan before them (device time of a call, 16 tokens of 32 heads: 24 us for
-// four sequences or eight, 64 tokens at a time on the tensor cores 27; 16 tokens of 16 sequences 34
-// against 30, of 64 sequences 133 against 81).
+// blocks of eight need no plan before them (calls in a row, 16 tokens of 32 heads: 21 to 24 us for
+// one sequence to eight, 64 tokens at a time on the tensor cores 27; of 16 sequences 34 against 30,
+// of 64 sequences 133 against 81).
 constexpr int kFewTokens = 16;
 
 }  // namespace

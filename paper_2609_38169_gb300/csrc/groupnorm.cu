@@ -25,7 +25,7 @@ struct GroupArgs {
     NormArgs norm;
 };
 
-constexpr int kWarpTeamThreads = 256, kCtaTeamThreads = 512, kScalarCtas = 6;
+constexpr int kWarpTeamThreads = 256, kCtaTeamThreads = 512;
 
 // The elements as fp32 pairs, and back: 16-bit ones a word at a time, half the byte moves of one
 // by one.

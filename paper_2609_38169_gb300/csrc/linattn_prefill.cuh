@@ -85,6 +85,8 @@ Split split_of(int Hv, int B, int tokens, int max_len);
 // segments' own parts
 stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s);
 stepq_status launch_linattn_join(const PrefillArgs &a, cudaStream_t s);
+// linattn_terms.cu. a = nullptr: only what a launch needs of the runtime
+stepq_status launch_linattn_terms(int dtype, const PrefillArgs *a, int items, bool out, bool norm, cudaStream_t s);
 // linattn_chunks.cu. prepare: what a launch needs of the runtime and the driver; parts: also the
 // pass with out = false, which forms only the segments' own parts of the state
 struct ChunkMaps {

@@ -19,11 +19,11 @@
 // no second chunk could be prepared beside it. Vectors are split into their terms once, by the thread that loads them, into swizzled rows of 256 bytes;
 // P is formed a block ahead; two barriers a block.
 //
-// The products' rate and latency bound it (216 of a warp a block in fp32, 140 in fp16, the pipe
-// 69% busy): 16 x 1024 tokens of 32 heads take 0.92 ms in fp32, 0.63 in fp16; 3 x 333 tokens in
-// fp32 80 us. The same in blocks of eight tokens on the FMA units: 1.10 and 1.10 ms, and 95 us; token
-// by token 215 us. 16-bit vectors leave room for two CTAs a multiprocessor (fp16 with one: 0.83 ms); in
-// fp32 two spill (0.99 ms).
+// The products' rate and latency bound it (216 of a warp a block in fp32, 140 in fp16; the pipe 69%
+// busy): 16 x 1024 tokens of 32 heads take 0.88 ms in fp32, 0.63 in fp16; 3 x 333 tokens in fp32
+// 76 us. In blocks of eight tokens on the FMA units the same took 1.10 and 1.10 ms, and 95 us; token by
+// token 215 us. 16-bit vectors leave room for two CTAs a multiprocessor (fp16 with one: 0.83 ms);
+// in fp32 two spill (1.00 ms).
 #include "async.cuh"
 #include "device.cuh"
 #include "linattn_prefill.cuh"
@@ -125,12 +125,19 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
     bf16 *P = (bf16 *)(smem + 2 * kTileBytes<T> + kPartBytes);   // [term][16 t][kPitchP]
     float *ys = (float *)(smem + 2 * kTileBytes<T> + kPartBytes + kPBytes);   // [2][16][128]
 
-    float S[16][4];                                          // tile j: rows (value columns) g, g + 8, key rows 8 j + 2 c, + 1
-    const int vcol = 16 * w + g;
+    // Tile j of S^T: key rows 8 j + 2 c, + 1 of a product's rows g and g + 8, which are value columns
+    // 2 g and 2 g + 1 of the warp's 16: V's tiles hold a group's even columns before its odd ones, so
+    // that a thread's two are one access to states and readouts.
+    float S[16][4];
+    const int vcol = 16 * w + 2 * g;
 #pragma unroll
     for (int j = 0; j < 16; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) S[j][e] = in ? in[(8 * j + 2 * c + (e & 1)) * kD + vcol + 8 * (e >> 1)] : 0.f;
+        for (int e = 0; e < 2; e++) {
+            const float2 x = in ? *(const float2 *)&in[(8 * j + 2 * c + e) * kD + vcol] : make_float2(0.f, 0.f);
+            S[j][e] = x.x;
+            S[j][e + 2] = x.y;
+        }
 
     // A block's vectors on their way: token t of it, channels 8 ch .. + 7; the decay of token l % 16.
     const int t = tid >> 4, ch = tid & 15;
@@ -179,8 +186,16 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
 #pragma unroll
             for (int i = 0; i < 4; i++) split<M>(fmul2(f2(to_f32(x.e[2 * i]), to_f32(x.e[2 * i + 1])), scale), r[i]);
 #pragma unroll
-            for (int m = 0; m < M; m++)
-                *(uint4 *)(tile(stage, which, m) + at(t, ch)) = make_uint4(r[0][m], r[1][m], r[2][m], r[3][m]);
+            for (int m = 0; m < M; m++) {
+                if (which == 2) {                            // even columns, odd columns
+                    bf16 *at0 = tile(stage, 2, m) + 4 * (ch & 1);
+                    const int g16 = ch & ~1;
+                    *(uint2 *)(at0 + at(t, g16)) = make_uint2(__byte_perm(r[0][m], r[1][m], 0x5410), __byte_perm(r[2][m], r[3][m], 0x5410));
+                    *(uint2 *)(at0 + at(t, g16 + 1)) = make_uint2(__byte_perm(r[0][m], r[1][m], 0x7632), __byte_perm(r[2][m], r[3][m], 0x7632));
+                } else {
+                    *(uint4 *)(tile(stage, which, m) + at(t, ch)) = make_uint4(r[0][m], r[1][m], r[2][m], r[3][m]);
+                }
+            }
         };
         if (OUT) {
             terms(nq, 0, f2s(1.f), std::integral_constant<int, N>{});
@@ -290,7 +305,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
             for (int j = 0; j < 8; j++) {
                 uint32_t A[NS][4], B[N][4];
 #pragma unroll
-                for (int e = 0; e < 4; e++) {                // rows g (+ 8), key rows 16 j + 2 c (+ 8)
+                for (int e = 0; e < 4; e++) {                // its rows g (+ 8), key rows 16 j + 2 c (+ 8)
                     uint32_t x[NS];
                     const float *s = &S[2 * j + (e >> 1)][2 * (e & 1)];
                     split<NS>(f2(s[0], s[1]), x);
@@ -324,11 +339,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
                 float o[1][4] = {};
                 product<NS>(o, V, b0, b1);
 #pragma unroll
-                for (int e = 0; e < 4; e++) {                // value column g (+ 8), token 8 i + 2 c (+ 1)
-                    const int tk = 8 * i + 2 * c + (e & 1), col = vcol + 8 * (e >> 1);
-                    const float r = fmaf(__shfl_sync(0xffffffffu, pre, tk), total_of(y[i], e), o[0][e]);
-                    if (NORM) ys[(stage * TB + tk) * kD + col] = r;
-                    else if (t0 + tk < len) ((T *)a.y)[((int64_t)row + t0 + tk) * a.ys + h * kD + col] = from_f32<T>(r);
+                for (int e = 0; e < 2; e++) {                // token 8 i + 2 c (+ 1)
+                    const int tk = 8 * i + 2 * c + e;
+                    const float ct = __shfl_sync(0xffffffffu, pre, tk);
+                    const float r[2] = {fmaf(ct, total_of(y[i], e), o[0][e]), fmaf(ct, total_of(y[i], e + 2), o[0][e + 2])};
+                    if (NORM) store_vec<float, 2>(&ys[(stage * TB + tk) * kD + vcol], r);
+                    else if (t0 + tk < len) store_vec<T, 2>((T *)a.y + ((int64_t)row + t0 + tk) * a.ys + h * kD + vcol, r);
                 }
             }
         }
@@ -368,7 +384,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
 #pragma unroll
         for (int j = 0; j < 16; j++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) out[(8 * j + 2 * c + (e & 1)) * kD + vcol + 8 * (e >> 1)] = S[j][e];
+            for (int e = 0; e < 2; e++) *(float2 *)&out[(8 * j + 2 * c + e) * kD + vcol] = make_float2(S[j][e], S[j][e + 2]);
 }
 
 template <class T, bool OUT, bool NORM>

@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
 #pragma unroll
         for (int m = 0; m < NS; m++) *(uint16_t *)&P[(m * TB + t) * kPitchP + s] = (uint16_t)r[m];
     };
-    // Tokens 2 w and 2 w + 1 of block n, a block late: see the blocks of eight.
+    // Tokens 2 w and 2 w + 1 of block n, a block late: the next products fill the waits of their sums.
     const HeadAffine affine(a.norm, h, l);
     Vec<T, 4> z[2] = {};
     const auto normalise = [&](int n) {

@@ -371,3 +371,20 @@ def test_a_stalled_prompt_reports_a_timeout(norm):
         A.stepq_debug_stall()
     got = call()
     assert got[2] == 0 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T", [5, 40, 1500])
+def test_rows_given_once_for_all_tokens(T, dt):
+    """q and k of one row, broadcast over the tokens by a stride of zero."""
+    hk, hv = 1, 2
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q, k, v, z, gate = inputs(g, T, hk, hv, dt)
+    q, k = q[:1].expand(T, hk, D), k[:1].expand(T, hk, D)
+    cfg = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv)
+    pool, y = torch.randn((1, 1, hv, D, D), generator=g, device="cuda"), torch.empty((T, hv, D), dtype=dt, device="cuda")
+    S = pool[0, 0].double()
+    A.stepq_linattn_prefill(cfg, 0, pool, torch.zeros(1, dtype=torch.int32, device="cuda"), q, k, v, gate, y, max_len=T)
+    yr, ya, Sa = R.linattn(S, q, k, v, gate)
+    check_y(y, yr, ya, dt, None, None)
+    R.assert_within(pool[0, 0], S, 64 * R.U * Sa + 1e-37, "state")

@@ -135,19 +135,20 @@ struct Items {
     __device__ __forceinline__ int affine() const { return a.norm.shared ? 0 : grp * a.width; }
 };
 
-// Vectors of 16 bytes, two a thread, copied ahead of their item. The affine parameters stay in
+// Vectors of 16 bytes, K a thread, copied ahead of their item: two or three a lane of a team in a
+// warp, four where the CTA is the team (rows of 4096 in bf16 171 us, with two 183; 7168 113 and 136). The affine parameters stay in
 // registers where a team's items have the same. Four times the CTAs that fit: the multiprocessors
 // get out of step, and HBM's reads and writes mix (one: 267 us for 241).
-constexpr int kDepth = 3, kK = 2, kWaves = 4;
-constexpr int ring_bytes(int threads) { return kDepth * 2 * kK * 16 * threads; }
+constexpr int kDepth = 3, kWaves = 4, kCtaVectors = 4;
+constexpr int ring_bytes(int K, int threads) { return kDepth * 2 * K * 16 * threads; }
 // CTAs of 256 threads a multiprocessor: what the registers of values and parameters leave (16-bit
 // types at three, registers spilled: 20% slower; fp32 at two: 8%).
 template <class T>
 constexpr int kResident = sizeof(T) == 2 ? 2 : 3;
 
-template <class T, bool CTA>
+template <class T, int K, bool CTA>
 __global__ void __launch_bounds__(CTA ? kCtaTeamThreads : kWarpTeamThreads, CTA ? 1 : kResident<T>) group_norm_kernel(GroupArgs a) {
-    constexpr int V = 16 / sizeof(T), H = V / 2, K = kK;
+    constexpr int V = 16 / sizeof(T), H = V / 2;
     __shared__ float part[2][kCtaTeamThreads / 32];
     extern __shared__ __align__(16) uint8_t ring[];
     int turn = 0;
@@ -334,13 +335,14 @@ static stepq_status launch_groups(void (*kernel)(GroupArgs), GroupArgs &a, int t
     return launch_overlapped(kernel, grid, threads, smem, s, a);
 }
 
-template <class T, bool CTA>
+template <class T, int K, bool CTA>
 static stepq_status launch_vectors(GroupArgs &a, int threads, cudaStream_t s) {
     static SmemOptIn opt_in;
-    const stepq_status st = opt_in((const void *)group_norm_kernel<T, CTA>, ring_bytes(CTA ? kCtaTeamThreads : threads));
-    return st == STEPQ_OK ? launch_groups(group_norm_kernel<T, CTA>, a, CTA ? 1 : threads / a.lanes,
-                                          CTA ? 256 * kResident<T> / threads : kWaves * kResident<T>,
-                                          threads, ring_bytes(threads), s) : st;
+    const auto kernel = group_norm_kernel<T, K, CTA>;
+    const stepq_status st = opt_in((const void *)kernel, ring_bytes(K, CTA ? kCtaTeamThreads : threads));
+    if (st != STEPQ_OK) return st;
+    return launch_groups(kernel, a, CTA ? 1 : threads / a.lanes, CTA ? 256 * kResident<T> / threads : kWaves * kResident<T>,
+                         threads, ring_bytes(K, threads), s);
 }
 
 }  // namespace la
@@ -365,11 +367,13 @@ stepq_status launch_group_norm(int dtype, int64_t rows, int groups, int width, c
         };
         const bool vectors = width % V == 0 && on(x, x_stride) && on(out, out_stride) && on(norm->z, norm->z_stride) &&
                              on(norm->weight, 0) && on(norm->bias, 0);
-        const int vecs = width / V, a_lane = vectors ? la::kK : la::kScalars;
+        const int vecs = width / V, pieces = vectors ? vecs : width, a_lane = vectors ? 2 : la::kScalars;
         a.lanes = 1;
-        while (a.lanes < 32 && a_lane * a.lanes < (vectors ? vecs : width)) a.lanes *= 2;
-        if (vectors && vecs <= la::kK * 32) return la::launch_vectors<T, false>(a, la::kWarpTeamThreads, s);
-        if (vectors && vecs <= la::kK * la::kCtaTeamThreads) return la::launch_vectors<T, true>(a, warps((vecs + 1) / la::kK), s);
+        while (a.lanes < 32 && a_lane * a.lanes < pieces) a.lanes *= 2;
+        if (vectors && vecs <= 2 * 32) return la::launch_vectors<T, 2, false>(a, la::kWarpTeamThreads, s);
+        if (vectors && vecs <= 3 * 32) return la::launch_vectors<T, 3, false>(a, la::kWarpTeamThreads, s);
+        if (vectors && vecs <= la::kCtaVectors * la::kCtaTeamThreads)
+            return la::launch_vectors<T, la::kCtaVectors, true>(a, warps((vecs + la::kCtaVectors - 1) / la::kCtaVectors), s);
         if (!vectors && width <= la::kScalars * 32)
             return la::launch_groups(la::group_norm_scalars_kernel<T>, a, la::kWarpTeamThreads / a.lanes, 4, la::kWarpTeamThreads, 0, s);
         const int threads = vectors ? la::kCtaTeamThreads : warps(width / la::kScalars);

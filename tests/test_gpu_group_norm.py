@@ -108,7 +108,8 @@ def test_gates_that_saturate():
 
 @pytest.mark.parametrize("dt", TYPES, ids=NAMES)
 @pytest.mark.parametrize("rows,groups,width", [(5000, 5, 64), (9000, 32, 8), (700, 97, 24), (60, 1009, 16), (9001, 3, 75),
-                                               (1500, 7, 333), (3001, 3, 600), (2000, 1, 2048), (700, 2, 1003)])
+                                               (1500, 7, 333), (3001, 3, 600), (2000, 1, 2048), (700, 2, 1003),
+                                               (4000, 3, 360), (3000, 1, 7168), (300, 1, 16384)])
 def test_many_rows(rows, groups, width, dt):
     """More groups than the GPU holds at once: a team's later groups, of one column or another."""
     g = torch.Generator(device="cuda").manual_seed(width)

@@ -14,16 +14,17 @@ constexpr int kSms = 152;                               // a GB300's multiproces
 // about its share W = tokens x Hv / 152 tokens a CTA, or the longest item's length L. Splitting
 // a sequence lets its segments run side by side, but the state before each has to be there:
 // a pass over k and v alone for the segments' own parts (about 0.55 of the full pass) and a
-// scan. It pays where L > 1.6 W. A segment is W / 4 tokens, so that the last round of items is
-// short, but not less than 256, whose 128 KiB of state traffic are half of its vectors'.
-// One prompt of 16384 tokens, 32 heads: 207 us split (75 the parts, 12 the scan, 119 the full
-// pass), 470 by 32 CTAs.
+// scan. It pays where L > 1.6 W. A segment is W / 3 tokens, so that the last round of items is
+// short (one prompt of 4096 tokens, 32 heads: 78 us, by W / 4 or W / 6 85; of 16384 209, by W / 2
+// 220, W / 4 212, W / 6 223), but not less than 256, whose 128 KiB of state traffic are half of its
+// vectors'. Of the 16384 tokens' time the parts take 72 us, the scan 11, the full pass 122; 32 CTAs
+// by themselves 470.
 Split split_of(int Hv, int B, int tokens, int max_len) {
     const int longest = max_len > 0 && max_len < tokens ? max_len : max_len > 0 ? tokens : (tokens + B - 1) / B;
     const double share = (double)tokens * Hv / kSms;
     Split s{tokens, B, false};
     if (longest > 512 && longest > 1.6 * share) {
-        const int q = (int)(share / 4);
+        const int q = (int)(share / 3);
         s.segment = q < 256 ? 256 : (q + kChunk - 1) / kChunk * kChunk;
         s.most = B + tokens / s.segment;
         s.on = true;

@@ -27,7 +27,7 @@
 //   3 warps      P (lanes = tokens), a 32 x 32 block each
 //   1 warp       loads q, k and v (TMA, two places each); decays and their products
 //   2 warps      issue the MMAs: scores and PV; KV and QS
-//   6 warps      K'
+//   6 warps      K' (8 where only the segments' parts are formed)
 // Hand-over by mbarriers, every wait bounded. Loops keep few unrolled steps: unrolled, the
 // warps' code did not fit the instruction caches (a third of the stalls of issuing warps).
 //
@@ -47,7 +47,9 @@ constexpr int C = kChunk;
 constexpr int kPlaces = 2;                              // of q, k, v and P
 constexpr int kBlock = 28 * 32;                         // registers are shared out by warpgroups
 constexpr int kOutWarps = 8, kFirst = 8 + kOutWarps;    // P, P, loads, MMAs, MMAs, P, then K'
-constexpr int kScaleWarps = 28 - kFirst - 6;
+// K': the six after those; where no outputs are formed, the first two that would form P as well (the
+// pass for the parts alone of 16384 tokens: 68 us for 72).
+template <bool OUT> constexpr int kScaleWarps = OUT ? 6 : 8;
 constexpr int kRegs = 72, kRegsState = 112, kRegsOut = 64, kRegsOperand = 48;
 static_assert(256 * (kRegsState + kRegsOut) + 384 * kRegsOperand <= kBlock * kRegs, "register shares");
 constexpr uint32_t kColU = 0, kColSh = 128, kColSl = 192, kColP = 256, kColY1 = 320, kColY2 = 384, kColV = 448,
@@ -401,11 +403,11 @@ __device__ __forceinline__ void issue_state(const Ctx<NORM> &x, uint32_t tm) {
 // their place.
 template <bool OUT, bool NORM>
 __device__ __forceinline__ void scale(const Ctx<NORM> &x, int w) {
-    constexpr int W = kScaleWarps;
+    constexpr int W = kScaleWarps<OUT>;
     const PrefillArgs &a = x.a;
     const int l = threadIdx.x & 31;
     uint32_t n = 0;
-    for (Items<NORM, kSyncKeys, kScaleWarps> it(x, w == 0); it.next();) {
+    for (Items<NORM, kSyncKeys, W> it(x, w == 0); it.next();) {
 #pragma unroll 1
         for (int t0 = 0; t0 < it.len; t0 += C, n++) {
             const int m = it.len - t0, place = (n % kPlaces) * 2 * kTile;
@@ -775,14 +777,14 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
     }
     if (tid < kBars) {
         int count = 1;                                      // TMA, the end of MMAs, the decays, items
-        if (tid >= kFreeK && tid < kFreeQ) count = kScaleWarps + (OUT ? 1 : 0);            // K', the scores
+        if (tid >= kFreeK && tid < kFreeQ) count = kScaleWarps<OUT> + (OUT ? 1 : 0);            // K', the scores
         if (tid >= kFreeQ && tid < kFreeV) count = OUT ? 2 : 1;                            // scores, QS
         if (tid >= kFreeV && tid < kVtFree) count = kOutWarps;                             // V^T (and kVtReady)
         if (tid >= kVtFree && tid < kPReady) count = OUT ? 2 : 1;                          // KV, PV
         if (tid >= kPReady && tid < kKpReady) count = 3;
-        if (tid >= kKpReady && tid < kKpFree) count = kScaleWarps;
-        if (tid >= kFreeG && tid < kFullItem) count = 8 + kScaleWarps + (OUT ? 3 + kOutWarps : 0);     // state, K', P, outputs
-        if (tid >= kFreeItem && tid < kScores) count = 9 + kScaleWarps + kOutWarps + (OUT ? 4 : 0);    // and the MMAs
+        if (tid >= kKpReady && tid < kKpFree) count = kScaleWarps<OUT>;
+        if (tid >= kFreeG && tid < kFullItem) count = 8 + kScaleWarps<OUT> + (OUT ? 3 + kOutWarps : 0);     // state, K', P, outputs
+        if (tid >= kFreeItem && tid < kScores) count = 9 + kScaleWarps<OUT> + kOutWarps + (OUT ? 4 : 0);    // and the MMAs
         if (tid >= kSReady && tid < kYFree) count = 8;
         if (tid == kYFree) count = kOutWarps;
         mbar_init(&bars[tid], count);
@@ -814,6 +816,7 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
         if (i == 2) load<OUT>(x, maps);
         else if (i == 4) issue_state<OUT>(x, tm);
         else if (i >= 6) scale<OUT>(x, i - 6);
+        else if (!OUT && i < 2) scale<OUT>(x, i + 6);
         else if (OUT) {
             if (i == 3) issue_scores(x, tm);
             else weigh_scores(x, tm, w & 3, i == 1);

@@ -17,7 +17,7 @@ constexpr int kSms = 152;                               // a GB300's multiproces
 // scan. It pays where L > 1.6 W. A segment is W / 3 tokens, so that the last round of items is
 // short (one prompt of 4096 tokens, 32 heads: 78 us, by W / 4 or W / 6 85; of 16384 209, by W / 2
 // 220, W / 4 212, W / 6 223), but not less than 256, whose 128 KiB of state traffic are half of its
-// vectors'. Of the 16384 tokens' time the parts take 72 us, the scan 11, the full pass 122; 32 CTAs
+// vectors'. Of the 16384 tokens' time the parts take 68 us, the scan 11, the full pass 122; 32 CTAs
 // by themselves 470.
 Split split_of(int Hv, int B, int tokens, int max_len) {
     const int longest = max_len > 0 && max_len < tokens ? max_len : max_len > 0 ? tokens : (tokens + B - 1) / B;

@@ -40,12 +40,19 @@ __device__ __forceinline__ int bucket_of(int len) {
 }
 
 // One CTA. Counting sort of the segments by bucket; within one the order is arbitrary, which
-// changes no result. Sequences out of range raise the error and make no segment.
+// changes no result. Sequences out of range raise the error and make no segment. The workspace is
+// laid out for sequences that share no row. Around a sequence whose bounds descend others may share
+// rows: if those to be split have more rows together than there are, the call raises the error and
+// has no segments at all.
 __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
     __shared__ int count[kBuckets], total;
+    __shared__ unsigned long long rows;                 // of the sequences to be split
     const int tid = threadIdx.x;
     if (tid < kBuckets) count[tid] = 0;
-    if (tid == 0) total = 0;
+    if (tid == 0) {
+        total = 0;
+        rows = 0;
+    }
     __syncthreads();
     griddep_wait();
     griddep_launch();
@@ -54,10 +61,21 @@ __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
         if (!sequence(a, b, true, row, len, slot)) len = 0;
         const int n = (len + a.segment - 1) / a.segment;
         a.sequences[b] = {n ? atomicAdd(&total, n) : 0, n};
-        if (n > 1) atomicAdd(&count[bucket_of(a.segment)], n - 1);
+        if (n > 1) {
+            atomicAdd(&rows, (unsigned long long)len);
+            atomicAdd(&count[bucket_of(a.segment)], n - 1);
+        }
         if (n > 0) atomicAdd(&count[bucket_of(len - (n - 1) * a.segment)], 1);
     }
     __syncthreads();
+    if (rows > (unsigned long long)a.tokens) {
+        for (int b = tid; b < a.B; b += 1024) a.sequences[b] = {0, 0};
+        if (tid == 0) {
+            *a.plan = PlanHeader{};
+            raise_error(a.err, STEPQ_ERR_ARG);
+        }
+        return;
+    }
     // first place of each bucket, the longest first
     if (tid < 32) {
         int run = 0;

@@ -388,3 +388,34 @@ def test_rows_given_once_for_all_tokens(T, dt):
     yr, ya, Sa = R.linattn(S, q, k, v, gate)
     check_y(y, yr, ya, dt, None, None)
     R.assert_within(pool[0, 0], S, 64 * R.U * Sa + 1e-37, "state")
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("hk,hv,tokens", [(1, 2, 4096), (16, 32, 1000)])
+def test_split_sequences_that_share_rows_are_refused(hk, hv, tokens, dt):
+    """Bounds that go back and forth make three sequences of all the rows. Their segments would be
+    more than the workspace has room for: the call is reported and writes nothing, and the next
+    one with the same workspace is whole."""
+    g = torch.Generator(device="cuda").manual_seed(hv)
+    q, k, v, z, gate = inputs(g, tokens, hk, hv, dt)
+    cfg, B = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv), 5
+    need = A.stepq_linattn_workspace_bytes(cfg, B, tokens, tokens)
+    assert need > A.stepq_linattn_workspace_bytes(cfg, B, tokens, 256)      # split
+    work = torch.full((need + (1 << 24),), 0x5A, dtype=torch.uint8, device="cuda")
+    slots = torch.arange(B, dtype=torch.int32, device="cuda")
+
+    def call(*cu):
+        pool, y = torch.ones((B, 1, hv, D, D), device="cuda"), torch.full((tokens, hv, D), 7.0, dtype=dt, device="cuda")
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, max_len=tokens, workspace=work[:need],
+                                cu_seqlens=torch.tensor(cu, dtype=torch.int32, device="cuda"))
+        return pool, y, A.stepq_device_error()
+
+    pool, y, err = call(0, tokens, 0, tokens, 0, tokens)
+    assert err == 1 and bool((pool == 1).all()) and bool((y == 7.0).all()) and bool((work[need:] == 0x5A).all())
+    pool, y, err = call(0, 0, tokens - 7, tokens, tokens, tokens)
+    assert err == 0 and bool((pool[[0, 3, 4]] == 1).all()) and bool((work[need:] == 0x5A).all())
+    S = torch.ones((hv, D, D), dtype=torch.float64, device="cuda")
+    r = slice(0, tokens - 7)
+    yr, ya, Sa = R.linattn(S, q[r], k[r], v[r], gate[r])
+    check_y(y[r], yr, ya, dt, None, r)
+    R.assert_within(pool[1, 0], S, 64 * R.U * Sa + 1e-37, "state")

@@ -133,6 +133,16 @@ def _stream(stream):
     return _Torch.stream() if stream is None else stream.cuda_stream
 
 
+def _scratch(nbytes, device, stream):
+    """Bytes from torch for a call on `stream` (None: the current one). They come from that
+    stream's own blocks: a block of another stream may still be in use there."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def version() -> str:
     return _lib.lib().stepq_version().decode()
 
@@ -554,10 +564,7 @@ def stepq_linattn_prefill(cfg: Config, layer: int, pool, slots, q, k, v, gate, y
     io = _linattn_io(cfg, q, k, v, gate, y)
     nbytes = lib.stepq_linattn_workspace_bytes(c, B, n, int(max_len)) if workspace is None else 0
     if nbytes:
-        import torch
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-        if stream is not None:                       # the block is not reused before this stream's work is done
-            workspace.record_stream(stream)
+        workspace = _scratch(nbytes, q.device, stream)
     have = 0 if workspace is None else workspace.numel() * workspace.element_size()
     check(lib.stepq_linattn_prefill(c, layer, _dev_ptr(pool, f),
                                     int(pool.shape[0] if pool_slots is None else pool_slots),

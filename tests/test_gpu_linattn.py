@@ -419,3 +419,57 @@ def test_split_sequences_that_share_rows_are_refused(hk, hv, tokens, dt):
     yr, ya, Sa = R.linattn(S, q[r], k[r], v[r], gate[r])
     check_y(y[r], yr, ya, dt, None, r)
     R.assert_within(pool[1, 0], S, 64 * R.U * Sa + 1e-37, "state")
+
+
+def test_a_workspace_belongs_to_the_stream_of_its_call(monkeypatch):
+    """Blocks of another stream may still be in use there: what a call on a given stream takes from
+    torch is a block of that stream."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v, z, gate = inputs(g, 1500, 1, 2, torch.bfloat16)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=2), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pool, y = torch.ones((1, 1, 2, D, D), device="cuda"), torch.empty((1500, 2, D), dtype=torch.bfloat16, device="cuda")
+    side, seen, empty = torch.cuda.Stream(), [], torch.empty
+    torch.cuda.synchronize()
+
+    def watched(*a, **kw):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **kw)
+
+    monkeypatch.setattr(torch, "empty", watched)
+    for stream in (side, None, side):
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, max_len=1500, stream=stream)
+        torch.cuda.synchronize()
+    here = torch.cuda.current_stream().cuda_stream
+    assert seen == [side.cuda_stream, here, side.cuda_stream]
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+def test_unrelated_prompts_on_two_streams(dt):
+    """Split prompts on the current and on a given stream, nothing ordering them and each with a
+    workspace of its own from torch, give the bytes of the calls made one by one."""
+    T, n, hk, hv = 3000, 4, 2, 4
+    g = torch.Generator(device="cuda").manual_seed(12)
+    cfg, slots = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv), torch.zeros(1, dtype=torch.int32, device="cuda")
+    calls = [inputs(g, T - 100 * i, hk, hv, dt) for i in range(n)]
+    pools = [torch.empty((1, 1, hv, D, D), device="cuda") for _ in calls]
+    ys = [torch.empty((T - 100 * i, hv, D), dtype=dt, device="cuda") for i in range(n)]
+    side = torch.cuda.Stream()
+
+    def serve(i, stream):
+        q, k, v, z, gate = calls[i]
+        A.stepq_linattn_prefill(cfg, 0, pools[i], slots, q, k, v, gate, ys[i], max_len=T - 100 * i, stream=stream)
+
+    def round_(between, streams):
+        for p in pools:
+            p.fill_(0.5)
+        torch.cuda.synchronize()
+        for i in range(n):
+            serve(i, streams[i % 2])
+            between()
+        torch.cuda.synchronize()
+        return [t.clone() for t in pools + ys]
+
+    want = round_(torch.cuda.synchronize, (None, None))
+    for _ in range(5):
+        got = round_(lambda: None, (None, side))
+        assert all(torch.equal(a, b) for a, b in zip(want, got))

@@ -603,7 +603,6 @@ def stepq_calibrate_from_trace(cfg: Config, q, k, v, beta, gate, every: int, str
     """The calibration protocol of App. A.3 on a device trace (q, k [L][T][n][Hk][128],
     v [L][T][n][Hv][128], beta [L][T][n][Hv], gate [L][T][n][Hv] or [L][T][n][Hv][128]),
     all in the library (stepq_calibrate_from_trace); the workspace comes from torch."""
-    import torch
     f = _f32()
     L, T, n = q.shape[0], q.shape[1], q.shape[2]
     c = cfg.c()
@@ -611,7 +610,7 @@ def stepq_calibrate_from_trace(cfg: Config, q, k, v, beta, gate, every: int, str
     nbytes = lib.stepq_calib_workspace_bytes(C.byref(c), n)
     if nbytes == 0:
         raise ValueError("invalid configuration or sequence count")
-    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=q.device)
+    ws = _scratch(nbytes + 256, q.device, stream)
     base = (ws.data_ptr() + 255) // 256 * 256
     U = stepq_num_units(cfg)
     K1 = len(cfg.candidates) + 1

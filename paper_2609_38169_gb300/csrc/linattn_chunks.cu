@@ -199,17 +199,15 @@ __device__ __forceinline__ void load(const Ctx<NORM> &x, const ChunkMaps &maps) 
     const int grp = a.Hv / a.Hk, l = threadIdx.x & 31;
     const uint32_t lead = tc::elect();
     uint32_t n = 0, started = 0;                            // chunks; copies, three a chunk
-    const int segments = a.plan->segments;
+    const int segments = OUT ? a.plan->segments : a.plan->parts;
     int i = 0;                                              // segment * Hv + head
     Segment it;
-    // The longest segment and head left; a sequence's last segment has no part to hand on.
+    // The longest segment and head left.
     const auto take = [&]() {
-        do {
-            if (lead) i = atomicAdd(&a.plan->next[OUT], 1);
-            i = __reduce_max_sync(0xffffffffu, i);
-            it.len = 0;
-            if (i / a.Hv < segments) it = a.table[i / a.Hv];
-        } while (!OUT && it.len > 0 && it.out == kStatePool);
+        if (lead) i = atomicAdd(&a.plan->next[OUT], 1);
+        i = __reduce_max_sync(0xffffffffu, i);
+        it.len = 0;
+        if (i / a.Hv < segments) it = a.table[i / a.Hv];
     };
     take();
     for (uint32_t k = 0;; k++) {

@@ -22,21 +22,22 @@ constexpr int kSms = 152;                               // a GB300's multiproces
 Split split_of(int Hv, int B, int tokens, int max_len) {
     const int longest = max_len > 0 && max_len < tokens ? max_len : max_len > 0 ? tokens : (tokens + B - 1) / B;
     const double share = (double)tokens * Hv / kSms;
-    Split s{tokens, B, false};
+    Split s{tokens, B, 0};
     if (longest > 512 && longest > 1.6 * share) {
         const int q = (int)(share / 3);
         s.segment = q < 256 ? 256 : (q + kChunk - 1) / kChunk * kChunk;
-        s.most = B + tokens / s.segment;
-        s.on = true;
+        s.parts = tokens / s.segment;
+        s.most = B + s.parts;
     }
     return s;
 }
 
-// Buckets of lengths in chunks: exponent and three bits of mantissa.
-constexpr int kBuckets = 256;
+// Buckets of lengths in chunks: exponent and three bits of mantissa. The last is for the parts: the
+// segments of split sequences but each one's last, all of the greatest length.
+constexpr int kBuckets = 256, kParts = kBuckets - 1;
 __device__ __forceinline__ int bucket_of(int len) {
     const int chunks = (len + kChunk - 1) / kChunk;
-    return min(kBuckets - 1, (int)(__float_as_uint((float)chunks) >> 20) - (127 << 3));
+    return min(kParts - 1, (int)(__float_as_uint((float)chunks) >> 20) - (127 << 3));
 }
 
 // One CTA. Counting sort of the segments by bucket; within one the order is arbitrary, which
@@ -45,12 +46,12 @@ __device__ __forceinline__ int bucket_of(int len) {
 // rows: if those to be split have more rows together than there are, the call raises the error and
 // has no segments at all.
 __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
-    __shared__ int count[kBuckets], total;
+    __shared__ int count[kBuckets], states, splits;     // states: segments of split sequences
     __shared__ unsigned long long rows;                 // of the sequences to be split
     const int tid = threadIdx.x;
     if (tid < kBuckets) count[tid] = 0;
     if (tid == 0) {
-        total = 0;
+        states = splits = 0;
         rows = 0;
     }
     __syncthreads();
@@ -60,10 +61,11 @@ __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
         int row, len, slot;
         if (!sequence(a, b, true, row, len, slot)) len = 0;
         const int n = (len + a.segment - 1) / a.segment;
-        a.sequences[b] = {n ? atomicAdd(&total, n) : 0, n};
+        a.sequences[b] = {n > 1 ? atomicAdd(&states, n) : 0, n};
         if (n > 1) {
             atomicAdd(&rows, (unsigned long long)len);
-            atomicAdd(&count[bucket_of(a.segment)], n - 1);
+            atomicAdd(&splits, 1);
+            atomicAdd(&count[kParts], n - 1);
         }
         if (n > 0) atomicAdd(&count[bucket_of(len - (n - 1) * a.segment)], 1);
     }
@@ -90,18 +92,19 @@ __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
             count[c + 31 - tid] = run + sum - mine;
             run += __shfl_sync(0xffffffffu, sum, 31);
         }
-        if (tid == 0) *a.plan = PlanHeader{run, {0, 0}, {}};
+        if (tid == 0) *a.plan = PlanHeader{run, states - splits, splits, {0, 0}, {}};
     }
     __syncthreads();
     for (int b = tid; b < a.B; b += 1024) {
         int row, len, slot;
         if (!sequence(a, b, false, row, len, slot)) continue;
         const Sequence q = a.sequences[b];
+        if (q.segments > 1) a.split[atomicSub(&splits, 1) - 1] = {b, q.id, q.segments, 0};
         for (int i = 0; i < q.segments; i++) {
             Segment s{row + i * a.segment, min(a.segment, len - i * a.segment), slot, q.id + i, 0, 0, {}};
             s.in = q.segments > 1 ? kStateWork : !a.resume || a.resume[b] ? kStatePool : kStateZero;
             s.out = i == q.segments - 1 ? kStatePool : kStateZero;
-            a.table[atomicAdd(&count[bucket_of(s.len)], 1)] = s;
+            a.table[atomicAdd(&count[i < q.segments - 1 ? kParts : bucket_of(s.len)], 1)] = s;
         }
     }
 }
@@ -109,34 +112,35 @@ __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
 // States before the segments of a split sequence: S_0 from the slot or zero, and
 // S_{i+1} = (product of segment i's decays) S_i + U_i, where U_i lies in S_{i+1}'s place. A
 // CTA takes 1024 elements of one sequence and head; two states a segment through L2.
+// The next kernel starts with this one's end, not under it: its CTAs, placed around this one's, would
+// take multiprocessors in twos while others are free (1500 tokens of 7 heads in fp16: 106 us for 83).
 __global__ void __launch_bounds__(256) linattn_join_kernel(PrefillArgs a) {
     griddep_wait();
-    griddep_launch();
-    const int part = blockIdx.x & 15, item = blockIdx.x >> 4, b = item / a.Hv, h = item - b * a.Hv;
-    const Sequence q = a.sequences[b];
-    if (q.segments < 2) return;
+    const int part = blockIdx.x & 15, item = blockIdx.x >> 4, i = item / a.Hv, h = item - i * a.Hv;
+    const SplitSequence q = a.split[i];                     // (on its way with the number of them)
+    if (i >= a.plan->splits) return;
     const int e = part * 1024 + 4 * threadIdx.x;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!a.resume || a.resume[b]) s = *(const float4 *)(pool_page(a, a.slots[b], h) + e);
+    if (!a.resume || a.resume[q.b]) s = *(const float4 *)(pool_page(a, a.slots[q.b], h) + e);
     float *at = a.states + ((uint64_t)q.id * a.Hv + h) * kN + e;
     const float *total = a.totals + (uint64_t)q.id * a.Hv + h;
     const uint64_t step = (uint64_t)a.Hv * kN;
     *(float4 *)at = s;
     constexpr int N = 4;                                // segments read ahead
-    for (int i = 1; i < q.segments; i += N) {
+    for (int j = 1; j < q.segments; j += N) {
         float4 u[N];
         float g[N];
 #pragma unroll
         for (int n = 0; n < N; n++)
-            if (i + n < q.segments) {
-                u[n] = *(const float4 *)(at + (i + n) * step);
-                g[n] = total[(i + n - 1) * a.Hv];
+            if (j + n < q.segments) {
+                u[n] = *(const float4 *)(at + (j + n) * step);
+                g[n] = total[(j + n - 1) * a.Hv];
             }
 #pragma unroll
         for (int n = 0; n < N; n++)
-            if (i + n < q.segments) {
+            if (j + n < q.segments) {
                 s = make_float4(fmaf(g[n], s.x, u[n].x), fmaf(g[n], s.y, u[n].y), fmaf(g[n], s.z, u[n].z), fmaf(g[n], s.w, u[n].w));
-                *(float4 *)(at + (i + n) * step) = s;
+                *(float4 *)(at + (j + n) * step) = s;
             }
     }
 }
@@ -144,8 +148,8 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(PrefillArgs a) {
 stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s) {
     return launch_overlapped(linattn_plan_kernel, 1, 1024, 0, s, a);
 }
-stepq_status launch_linattn_join(const PrefillArgs &a, cudaStream_t s) {
-    return launch_overlapped(linattn_join_kernel, a.B * a.Hv * 16, 256, 0, s, a);
+stepq_status launch_linattn_join(const PrefillArgs &a, int splits, cudaStream_t s) {
+    return launch_overlapped(linattn_join_kernel, splits * a.Hv * 16, 256, 0, s, a);
 }
 
 }  // namespace la

@@ -8,7 +8,7 @@ namespace {
 
 // The workspace's parts, each at a multiple of 256 bytes.
 struct Workspace {
-    size_t table, sequences, totals, states, bytes;
+    size_t table, sequences, splits, totals, states, bytes;
     Workspace(int Hv, int B, const la::Split &split) {
         const auto part = [&](size_t n) {
             const size_t at = bytes;
@@ -19,8 +19,10 @@ struct Workspace {
         part(sizeof(la::PlanHeader));
         table = part((size_t)split.most * sizeof(la::Segment));
         sequences = part((size_t)B * sizeof(la::Sequence));
-        totals = part(split.on ? (size_t)split.most * Hv * 4 : 0);
-        states = part(split.on ? (size_t)split.most * Hv * kN * 4 : 0);
+        splits = part((size_t)split.parts * sizeof(la::SplitSequence));
+        const size_t held = split.states();
+        totals = part(held * Hv * 4);
+        states = part(held * Hv * kN * 4);
     }
 };
 
@@ -62,16 +64,17 @@ stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *p
     a.plan = (la::PlanHeader *)base;
     a.table = (la::Segment *)(base + w.table);
     a.sequences = (la::Sequence *)(base + w.sequences);
+    a.split = (la::SplitSequence *)(base + w.splits);
     a.totals = (float *)(base + w.totals);
     a.states = (float *)(base + w.states);
     a.segment = split.segment;
-    const long long items = (long long)split.most * a.Hv;
+    const int items = split.most * a.Hv, parts = split.parts * a.Hv, splits = B < split.parts ? B : split.parts;
     const bool few = (max_len > 0 ? max_len : tokens) <= kFewTokens;
     if (few || !la::linattn_chunks_takes(cfg, io)) {
         const auto terms = [&](const la::PrefillArgs *args, bool out) {
-            return la::launch_linattn_terms(io->dtype, args, (int)items, out, norm != nullptr, s);
+            return la::launch_linattn_terms(io->dtype, args, out ? items : parts, out, norm != nullptr, s);
         };
-        if (!split.on) {                                   // a segment is a sequence
+        if (!split.parts) {                                 // a segment is a sequence
             a.plan = nullptr;
             return terms(&a, true);
         }
@@ -79,16 +82,16 @@ stepq_status launch_linattn_prefill(const stepq_config *cfg, int layer, float *p
         if (st == STEPQ_OK) st = terms(nullptr, true);
         if (st == STEPQ_OK) st = la::launch_linattn_plan(a, s);
         if (st == STEPQ_OK) st = terms(&a, false);
-        if (st == STEPQ_OK) st = la::launch_linattn_join(a, s);
+        if (st == STEPQ_OK) st = la::launch_linattn_join(a, splits, s);
         return st == STEPQ_OK ? terms(&a, true) : st;
     }
-    const int grid = items < sm_count() ? (int)items : sm_count();
+    const int sms = sm_count();
     la::ChunkMaps maps;                                    // what may be refused comes before the first launch
-    stepq_status st = la::prepare_linattn_chunks(a, split.on, maps);
+    stepq_status st = la::prepare_linattn_chunks(a, parts > 0, maps);
     if (st == STEPQ_OK) st = la::launch_linattn_plan(a, s);
-    if (st == STEPQ_OK && split.on) st = la::launch_linattn_chunks(a, maps, grid, false, s);
-    if (st == STEPQ_OK && split.on) st = la::launch_linattn_join(a, s);
-    return st == STEPQ_OK ? la::launch_linattn_chunks(a, maps, grid, true, s) : st;
+    if (st == STEPQ_OK && parts) st = la::launch_linattn_chunks(a, maps, parts < sms ? parts : sms, false, s);
+    if (st == STEPQ_OK && parts) st = la::launch_linattn_join(a, splits, s);
+    return st == STEPQ_OK ? la::launch_linattn_chunks(a, maps, items < sms ? items : sms, true, s) : st;
 }
 
 }  // namespace stepq

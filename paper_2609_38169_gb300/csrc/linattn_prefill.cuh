@@ -12,22 +12,26 @@ namespace la {
 constexpr int kChunk = 64;             // tokens a chunk of the tensor-core kernel
 
 // Consecutive tokens of one sequence that a CTA takes with one head: a whole sequence, or, of
-// one that is split, kSegment tokens or what is left.
+// one that is split, Split::segment tokens or what is left.
 struct alignas(16) Segment {
     int row, len;                      // first row, tokens
     int slot;
-    int id;                            // place of its state in the workspace
+    int id;                            // place of its state in the workspace, where its sequence is split
     int in, out;                       // kState*: where the state before it comes from, where the one after it goes
     int pad[2];
 };
 enum { kStateZero, kStatePool, kStateWork };           // in; out: kStateZero is none
 struct PlanHeader {
     int segments;
+    int parts, splits;                 // the first segments of the table, whose own parts come first; split sequences
     int next[2];                       // the items taken so far by the two passes
-    int pad[5];
+    int pad[3];
 };
 struct Sequence {
-    int id, segments;                  // of its first segment; 0 or 1: not split
+    int id, segments;                  // id: its first segment's, where there are several
+};
+struct alignas(16) SplitSequence {
+    int b, id, segments, pad;
 };
 
 struct PrefillArgs {
@@ -43,11 +47,12 @@ struct PrefillArgs {
     NormArgs norm;
     unsigned int *err;
     StallKnob stall;
-    // the plan (tensor-core kernel)
+    // the plan; without one (linattn_terms.cu alone) an item is a sequence
     PlanHeader *plan;
     Segment *table;                    // by falling length
     Sequence *sequences;
-    float *totals, *states;            // [segments][Hv]: products of a segment's decays; states before the segments
+    SplitSequence *split;
+    float *totals, *states;            // [their segments][Hv]: products of a segment's decays; states before the segments
     int segment;                       // tokens
 };
 
@@ -74,17 +79,19 @@ __device__ __forceinline__ float *pool_page(const PrefillArgs &a, int slot, int 
     return a.pool + (uint64_t)slot * a.slot_floats + a.layer_off + (uint64_t)h * kN;
 }
 
-// Tokens of a segment for a call, and the most segments it can make.
+// Tokens of a segment for a call, the most segments it can make, and the most of them that are
+// parts: a split sequence has `segment` tokens for each segment but its last, and one token or more
+// for that, so there are no more split sequences than parts, and no more than 2 x parts segments of theirs.
 struct Split {
-    int segment, most;
-    bool on;                           // whether a sequence may be split
+    int segment, most, parts;          // parts = 0: no sequence is split
+    int states() const { return 2 * parts < most || !parts ? 2 * parts : most; }
 };
 Split split_of(int Hv, int B, int tokens, int max_len);
 
 // linattn_plan.cu: the segments; the states before the segments of split sequences from the
 // segments' own parts
 stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s);
-stepq_status launch_linattn_join(const PrefillArgs &a, cudaStream_t s);
+stepq_status launch_linattn_join(const PrefillArgs &a, int splits, cudaStream_t s);
 // linattn_terms.cu. a = nullptr: only what a launch needs of the runtime
 stepq_status launch_linattn_terms(int dtype, const PrefillArgs *a, int items, bool out, bool norm, cudaStream_t s);
 // linattn_chunks.cu. prepare: what a launch needs of the runtime and the driver; parts: also the

@@ -102,10 +102,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
     const float *in = nullptr;
     float *out, *total_to = nullptr, total = 1.f;            // a part's decay
     if (a.plan) {
-        if (part >= a.plan->segments) return;
+        if (part >= (OUT ? a.plan->segments : a.plan->parts)) return;
         const Segment s = a.table[part];
         float *work = a.states + ((uint64_t)s.id * a.Hv + h) * kN, *page = pool_page(a, s.slot, h);
-        if (!OUT && s.out == kStatePool) return;             // a sequence's last segment has no part to hand on
         row = s.row;
         len = s.len;
         if (OUT) in = s.in == kStateZero ? nullptr : s.in == kStatePool ? page : work;

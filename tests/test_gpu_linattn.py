@@ -473,3 +473,10 @@ def test_unrelated_prompts_on_two_streams(dt):
     for _ in range(5):
         got = round_(lambda: None, (None, side))
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("lens", [[1] * 30 + [1500] + [3] * 20 + [1000, 0, 17], [700, 699, 1, 641, 640, 639]], ids=["one beside many", "close"])
+def test_split_sequences_beside_others(lens, dt):
+    """Sequences that are split, some just, between sequences of a few tokens."""
+    run_prefill(lens, 1, 2, dt, seed=len(lens), resume=lambda b: b % 3 > 0, layers=2)

@@ -86,6 +86,19 @@ def test_workspace():
         assert prefill(**kw, ws=P + 128, nbytes=need) == ALIGN
 
 
+@pytest.mark.parametrize("hv", [1, 2, 7, 16, 32, 64, 90])
+@pytest.mark.parametrize("longest", [600, 8192, 100000, 1 << 22])
+@pytest.mark.parametrize("others", [0, 512, 5000])
+def test_the_workspace_holds_the_states_of_split_sequences_only(hv, longest, others):
+    """One long sequence beside others of one token. Split, it makes segments of a third of a
+    multiprocessor's share of the work (152 of them) at least, so about 456 over all heads that
+    have one after them, and no more than twice as many states of 64 KiB; a sequence adds its
+    places in two tables (40 bytes)."""
+    cfg = A.Config(n_layers=1, n_key_heads=hv, n_value_heads=hv)
+    need = A.stepq_linattn_workspace_bytes(cfg, 1 + others, longest + others, longest)
+    assert need <= 2 * 456 * (65536 + 4) + 40 * others + 32768
+
+
 def group(dtype=1, rows=3, groups=2, width=5, x=P, xs=10, out=P, os_=10, n=None):
     return _lib.lib().stepq_group_norm(dtype, rows, groups, width, x, xs, out, os_, C.byref(n or norm()), None)
 

@@ -345,6 +345,7 @@ stepq_status stepq_linattn_decode_step(const stepq_config *cfg, int layer, float
  * stepq_linattn_workspace_bytes(cfg, B, tokens, max_len) bytes (0: NULL is fine), clobbered.
  * A sequence whose bounds are not ascending within [0, tokens] raises STEPQ_ERR_ARG and
  * one whose slot is out of range STEPQ_ERR_SLOT_RANGE (device errors); either is skipped.
+ * Two sequences with tokens and the same slot raise STEPQ_ERR_DUP_SLOT; theirs is undefined then.
  * Where bounds descend the sequences around may share rows: if those that are split hold more
  * than `tokens` rows together, the call raises STEPQ_ERR_ARG and skips every sequence.
  * A value that is not finite may reach any output of its own sequence from the 64 tokens

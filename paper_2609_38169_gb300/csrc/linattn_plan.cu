@@ -40,11 +40,11 @@ __device__ __forceinline__ int bucket_of(int len) {
     return min(kParts - 1, (int)(__float_as_uint((float)chunks) >> 20) - (127 << 3));
 }
 
-// One CTA. Counting sort of the segments by bucket; within one the order is arbitrary, which
+// CTA 0: counting sort of the segments by bucket; within one the order is arbitrary, which
 // changes no result. Sequences out of range raise the error and make no segment. The workspace is
 // laid out for sequences that share no row. Around a sequence whose bounds descend others may share
 // rows: if those to be split have more rows together than there are, the call raises the error and
-// has no segments at all.
+// has no segments at all. The other CTAs look for slots given twice, a sequence a warp at a time.
 __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
     __shared__ int count[kBuckets], states, splits;     // states: segments of split sequences
     __shared__ unsigned long long rows;                 // of the sequences to be split
@@ -57,6 +57,10 @@ __global__ void __launch_bounds__(1024) linattn_plan_kernel(PrefillArgs a) {
     __syncthreads();
     griddep_wait();
     griddep_launch();
+    if (blockIdx.x) {
+        for (int b = (blockIdx.x - 1) * 32 + (tid >> 5); b < a.B; b += (gridDim.x - 1) * 32) check_slot(a, b, tid & 31, 32);
+        return;
+    }
     for (int b = tid; b < a.B; b += 1024) {
         int row, len, slot;
         if (!sequence(a, b, true, row, len, slot)) len = 0;
@@ -146,7 +150,8 @@ __global__ void __launch_bounds__(256) linattn_join_kernel(PrefillArgs a) {
 }
 
 stepq_status launch_linattn_plan(const PrefillArgs &a, cudaStream_t s) {
-    return launch_overlapped(linattn_plan_kernel, 1, 1024, 0, s, a);
+    const int pairs = a.B < 2 ? 0 : (a.B + 31) / 32;
+    return launch_overlapped(linattn_plan_kernel, 1 + (pairs < kSms ? pairs : kSms), 1024, 0, s, a);
 }
 stepq_status launch_linattn_join(const PrefillArgs &a, int splits, cudaStream_t s) {
     return launch_overlapped(linattn_join_kernel, splits * a.Hv * 16, 256, 0, s, a);

@@ -75,6 +75,17 @@ __device__ __forceinline__ bool sequence(const PrefillArgs &a, int b, bool lead,
     }
     return true;
 }
+// Sequence b against those after it, `threads` of them at a time: two with tokens and one slot raise
+// the device error.
+__device__ __forceinline__ bool has_tokens(const PrefillArgs &a, int b) {
+    return !a.cu || (a.cu[b] >= 0 && a.cu[b + 1] > a.cu[b] && a.cu[b + 1] <= a.tokens);
+}
+__device__ __forceinline__ void check_slot(const PrefillArgs &a, int b, int thread, int threads) {
+    const int slot = a.slots[b];
+    for (int j = b + 1 + thread; j < a.B; j += threads)
+        if (a.slots[j] == slot && slot >= 0 && slot < a.pool_slots && has_tokens(a, b) && has_tokens(a, j))
+            raise_error(a.err, STEPQ_ERR_DUP_SLOT);
+}
 __device__ __forceinline__ float *pool_page(const PrefillArgs &a, int slot, int h) {
     return a.pool + (uint64_t)slot * a.slot_floats + a.layer_off + (uint64_t)h * kN;
 }

@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
     } else {
         int slot;
         if (!sequence(a, part, tid == 0, row, len, slot) || len == 0) return;
+        if (h == 0) check_slot(a, part, tid, 256);
         out = pool_page(a, slot, h);
         in = !a.resume || a.resume[part] ? out : nullptr;
     }

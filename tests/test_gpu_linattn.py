@@ -480,3 +480,31 @@ def test_unrelated_prompts_on_two_streams(dt):
 def test_split_sequences_beside_others(lens, dt):
     """Sequences that are split, some just, between sequences of a few tokens."""
     run_prefill(lens, 1, 2, dt, seed=len(lens), resume=lambda b: b % 3 > 0, layers=2)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("lens,max_len", [([5, 3, 7], 7), ([40, 30, 50], 50), ([70, 700, 90], 700), ([9] * 2500, 9), ([65] * 2500, 65)],
+                         ids=["few", "blocks", "split", "many few", "many"])
+def test_slots_given_twice(lens, max_len, dt):
+    """Two sequences with one slot are reported, wherever they stand; one without tokens shares a slot
+    with nobody."""
+    B, n = len(lens), sum(lens)
+    g = torch.Generator(device="cuda").manual_seed(B)
+    q, k, v, z, gate = inputs(g, n, 1, 1, dt)
+    cfg, pool = A.Config(n_layers=1, n_key_heads=1, n_value_heads=1), torch.zeros((B, 1, 1, D, D), device="cuda")
+    y = torch.empty((n, 1, D), dtype=dt, device="cuda")
+    ends = torch.tensor(lens).cumsum(0)
+
+    def call(twice=None, empty=False):
+        slots, cu = torch.randperm(B, generator=g, device="cuda").to(torch.int32), torch.cat([torch.zeros(1, dtype=torch.int64), ends])
+        if twice:
+            slots[twice[1]] = slots[twice[0]]
+        if empty:                                                # its rows go to the one after it
+            cu[twice[0] + 1] = cu[twice[0]]
+        A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, gate, y, cu_seqlens=cu.to("cuda", torch.int32), max_len=max_len)
+        return A.stepq_device_error()
+
+    assert call() == 0
+    for twice in ((0, B - 1), (0, 1), (B - 2, B - 1), (B // 2, B - 1)):
+        assert call(twice) == 3
+    assert call((0, 2), empty=True) == 0

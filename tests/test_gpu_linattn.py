@@ -508,3 +508,123 @@ def test_slots_given_twice(lens, max_len, dt):
     for twice in ((0, B - 1), (0, 1), (B - 2, B - 1), (B // 2, B - 1)):
         assert call(twice) == 3
     assert call((0, 2), empty=True) == 0
+
+
+# ------------------------------------------------------------------ split sequences: streams, graphs, errors
+def split_batch(lens, hk, hv, dt, norm, seed):
+    """Inputs of a packed batch on a layer with few heads, whose long sequences are split."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n, B = sum(lens), len(lens)
+    q, k, v, z, gate = inputs(g, n, hk, hv, dt)
+    cfg = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv)
+    need = A.stepq_linattn_workspace_bytes(cfg, B, n, max(lens))
+    assert need > A.stepq_linattn_workspace_bytes(cfg, B, n, 64)          # room for states: split
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    cu = torch.tensor([sum(lens[:b]) for b in range(B + 1)], dtype=torch.int32, device="cuda")
+    slots = torch.randperm(B, generator=g, device="cuda").to(torch.int32)
+    pool, y = torch.empty((B, 1, hv, D, D), device="cuda"), torch.empty((n, hv, D), dtype=dt, device="cuda")
+    lib_norm = A.Norm(z=z, act=A.ACT_SILU) if norm else None
+
+    def call(**kw):
+        args = dict(slots=slots, cu_seqlens=cu, max_len=max(lens), norm=lib_norm, workspace=work)
+        args.update(kw)
+        A.stepq_linattn_prefill(cfg, 0, pool, args.pop("slots"), q, k, v, gate, y, **args)
+    return call, pool, y, cu, slots
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("norm", [False, True])
+def test_split_prompts_on_side_streams_and_in_graphs(norm, dt):
+    """The plan, both passes and the scan between them, captured and replayed, and in calls in a row
+    through one workspace: the bytes of a call by itself."""
+    call, pool, y, _, _ = split_batch([2049, 40, 900], 2, 4, dt, norm, 5)
+
+    def chain():
+        pool.fill_(0.5)
+        call()
+        call()
+
+    chain()
+    torch.cuda.synchronize()
+    want = pool.clone(), y.clone()
+    pool.fill_(0.5)
+    for _ in range(2):                                       # the same, each call by itself
+        torch.cuda.synchronize()
+        call()
+    torch.cuda.synchronize()
+    assert torch.equal(want[0], pool) and torch.equal(want[1], y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    pool.zero_(), y.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain()
+    side.synchronize()
+    assert torch.equal(want[0], pool) and torch.equal(want[1], y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for _ in range(3):
+        pool.zero_(), y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want[0], pool) and torch.equal(want[1], y)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+def test_device_errors_between_split_sequences(dt):
+    """Slots and bounds out of range beside sequences that are split: skipped and reported, the others
+    served."""
+    lens = [1500, 700, 1000, 40]
+    call, pool, y, cu, slots = split_batch(lens, 1, 2, dt, False, 6)
+    pool.fill_(1.0), y.fill_(7.0)
+    call()
+    want, wy = pool.clone(), y.clone()
+    assert A.stepq_device_error() == 0
+    at = cu.tolist()
+    for b, value in ((0, -1), (1, len(lens)), (2, 10 ** 6), (3, -5)):
+        bad = slots.clone()
+        bad[b] = value
+        pool.fill_(1.0), y.fill_(7.0)
+        call(slots=bad)
+        assert A.stepq_device_error() == 2
+        for c in range(len(lens)):
+            s, rows_ = int(slots[c]), slice(at[c], at[c + 1])
+            if c == b:
+                assert bool((pool[s] == 1.0).all()) and bool((y[rows_] == 7.0).all())
+            else:
+                assert torch.equal(pool[s], want[s]) and torch.equal(y[rows_], wy[rows_])
+    for edge, value in ((0, -1), (4, at[4] + 1), (4, at[3] - 1)):             # the first's, the last's
+        bad = cu.clone()
+        bad[edge] = value
+        pool.fill_(1.0), y.fill_(7.0)
+        call(cu_seqlens=bad)
+        assert A.stepq_device_error() == 1
+        for c in range(len(lens)):
+            s, rows_ = int(slots[c]), slice(at[c], at[c + 1])
+            if c == min(edge, 3):
+                assert bool((pool[s] == 1.0).all()) and bool((y[rows_] == 7.0).all())
+            else:
+                assert torch.equal(pool[s], want[s]) and torch.equal(y[rows_], wy[rows_])
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("item", [0, 3, 8, 13])
+def test_a_stalled_split_prompt_reports_a_timeout(item, norm):
+    """Copies that never start in the pass for the segments' parts, or in the one for the outputs: every
+    wait gives up within its bound, both passes end, and the next call is whole."""
+    call, pool, y, _, _ = split_batch([1500, 40, 900], 1, 2, torch.bfloat16, norm, 7)
+    pool.fill_(0.5)
+    call()
+    assert A.stepq_device_error() == 0
+    want = pool.clone(), y.clone()
+    try:
+        A.stepq_debug_stall(2_000_000, item)
+        pool.fill_(0.5)
+        call()
+        assert A.stepq_device_error() == 8
+    finally:
+        A.stepq_debug_stall()
+    pool.fill_(0.5)
+    call()
+    assert A.stepq_device_error() == 0 and torch.equal(want[0], pool) and torch.equal(want[1], y)

@@ -453,8 +453,9 @@ stepq_status stepq_stream_status(stepq_stream_t stream);
 /* Test support for the bounded waits (not for production use). Every wait of
  * the pipelined kernels (stepq_decode_step, the split halves, the FP32 and INT-b
  * decode steps, stepq_prefill_fp32, stepq_linattn_prefill in bf16) gives up after
- * `wait_cycles` SM clock cycles (default 2e9, about one second; at least 1000),
- * raises STEPQ_ERR_TIMEOUT and lets its CTA return. withhold_item >= 0 makes every
+ * `wait_cycles` SM clock cycles (default 2e9, about one second; at least 1000;
+ * stepq_linattn_prefill waits 2^31 at most), raises STEPQ_ERR_TIMEOUT and lets its
+ * CTA return. withhold_item >= 0 makes every
  * later launch skip the copies of that item (head * B + batch entry;
  * stepq_prefill_fp32: the first copies of batch entry * Hv + head;
  * stepq_linattn_prefill: of segment * Hv + head, the segments longest first), so

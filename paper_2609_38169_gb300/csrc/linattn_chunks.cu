@@ -71,6 +71,8 @@ struct alignas(16) Gates {
     float total, pad[3];                                // c_C
 };
 constexpr int kRing = 4;                                // places of decays and of items
+// Cycles: waits are measured with a 32-bit clock, which has to be seen past the limit before it wraps.
+constexpr long long kLongestWait = 1ll << 31;
 struct alignas(16) Item {
     const float *in;                                    // the state before the segment, or null: zero
     float *out, *total;                                 // the state after it, its decays' product, or null
@@ -801,7 +803,7 @@ __global__ void __launch_bounds__(kBlock, 1) linattn_chunks_kernel(PrefillArgs a
     griddep_wait();
     griddep_launch();
     const uint32_t tm = *tbase;
-    const Ctx<NORM> x{a, smem, bars, (uint32_t)min(a.stall.wait_cycles, 0xFFFFFFF0ll)};
+    const Ctx<NORM> x{a, smem, bars, (uint32_t)min(a.stall.wait_cycles, kLongestWait)};
     if (w < 8) {
         tc::regs_inc<kRegsState>();
         states<OUT>(x, tm);

@@ -628,3 +628,23 @@ def test_a_stalled_split_prompt_reports_a_timeout(item, norm):
     pool.fill_(0.5)
     call()
     assert A.stepq_device_error() == 0 and torch.equal(want[0], pool) and torch.equal(want[1], y)
+
+
+def test_a_wait_bound_beyond_the_clock_still_holds():
+    """A bound above what the kernel's 32-bit clock counts is cut to what it can see: the stalled call
+    ends after about a second."""
+    call, pool, y, _, _ = split_batch([1500, 40, 900], 1, 2, torch.bfloat16, False, 8)
+    pool.fill_(0.5)
+    call()
+    assert A.stepq_device_error() == 0
+    want = pool.clone(), y.clone()
+    try:
+        A.stepq_debug_stall(5_000_000_000, 3)
+        pool.fill_(0.5)
+        call()
+        assert A.stepq_device_error() == 8
+    finally:
+        A.stepq_debug_stall()
+    pool.fill_(0.5)
+    call()
+    assert A.stepq_device_error() == 0 and torch.equal(want[0], pool) and torch.equal(want[1], y)

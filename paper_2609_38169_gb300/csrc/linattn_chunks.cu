@@ -89,8 +89,8 @@ enum {
     kFreeItem = kFullItem + kRing, kScores = kFreeItem + kRing, kSReady, kUFree, kYFree, kQs, kKv, kPv, kDrainA, kDrainB, kBars
 };
 template <bool NORM> constexpr int kOffTmem = kOffBar<NORM> + kBars * 8;
-template <bool NORM> constexpr int kOffStop = kOffTmem<NORM> + 8;      // uint32 of each group of warps
-template <bool NORM> constexpr int kSmem = kOffStop<NORM> + 32;
+template <bool NORM> constexpr int kOffStop = kOffTmem<NORM> + 8;      // uint32 [2] of each group of warps
+template <bool NORM> constexpr int kSmem = kOffStop<NORM> + 40;
 static_assert(kSmem<true> <= kSmemMax && kSmem<false> <= kSmemMax, "one CTA's shared memory");
 
 constexpr uint32_t kIdescScores = tc::idesc_bf16(128, 64, 0, 0);
@@ -160,9 +160,12 @@ struct Items {
         if (leader) x.template wait_full<kRing>(kFullItem, n);
         bool stop = x.limit == 0;                           // a wait ran out: nothing more
         if (WARPS > 1) {
-            if (leader) x.stopped()[ID] = stop;
+            // Two words in turn: the leader may come to the next item before another warp has read this
+            // one's, but not to the one after that, since they meet in between.
+            volatile uint32_t *word = x.stopped() + 2 * ID + n % 2;
+            if (leader) *word = stop;
             group_sync<ID, WARPS>();
-            stop = x.stopped()[ID];
+            stop = *word;
         }
         const Item &i = x.item(n);
         in = i.in;

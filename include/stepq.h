@@ -358,7 +358,8 @@ stepq_status stepq_linattn_prefill(const stepq_config *cfg, int layer, float *po
                                    void *workspace, size_t workspace_bytes, stepq_stream_t stream);
 
 /* The normalisation on its own: x [rows][groups * width] in dtype (rows x_stride elements
- * apart, channels contiguous) to out (the same, out_stride apart; out may be x). Any width
+ * apart, channels contiguous) to out (the same, out_stride apart; out may be x or z with the
+ * same stride, else it overlaps neither). Any width
  * from 1 on and any alignment of x, out and z that their type has; statistics in fp32. */
 stepq_status stepq_group_norm(int dtype, int64_t rows, int groups, int width, const void *x,
                               int64_t x_stride, void *out, int64_t out_stride,

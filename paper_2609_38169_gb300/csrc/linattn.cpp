@@ -93,6 +93,9 @@ extern "C" stepq_status stepq_group_norm(int dtype, int64_t rows, int groups, in
     if (rows == 0) return STEPQ_OK;
     if (!x || !out || x_stride < 0 || (rows > 1 && out_stride < channels) || (norm->z && norm->z_stride < 0))
         return STEPQ_ERR_ARG;
+    // in place only row by row: else a row would be written before another one is read there
+    if (rows > 1 && ((out == x && out_stride != x_stride) || (out == norm->z && out_stride != norm->z_stride)))
+        return STEPQ_ERR_ARG;
     const uintptr_t e = (uintptr_t)type_bytes(dtype);
     if (!aligned(x, e) || !aligned(out, e) || !aligned(norm->z, e)) return STEPQ_ERR_ALIGN;
     return launch_group_norm(dtype, rows, groups, width, x, x_stride, out, out_stride, norm, (cudaStream_t)stream);

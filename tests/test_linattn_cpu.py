@@ -114,6 +114,14 @@ def test_group_norm_refusals():
     assert group(rows=0) == OK
 
 
+def test_group_norm_in_place_keeps_the_rows():
+    """out may be x or z only where their rows lie alike."""
+    far = P << 10
+    assert group(x=P, xs=12, out=P, os_=10) == ARG and group(x=P, xs=0, out=P, os_=10) == ARG
+    assert group(x=P, xs=10, out=far, os_=12, n=norm(z=far, z_stride=10)) == ARG
+    assert group(rows=0, x=P, xs=12, out=P, os_=10) == OK
+
+
 def test_binding_refuses_shapes_and_types():
     torch = pytest.importorskip("torch")
     x = torch.zeros(2, 4, 128)

@@ -340,8 +340,8 @@ stepq_status stepq_linattn_decode_step(const stepq_config *cfg, int layer, float
  * where resume[b] != 0 (device uint8 [B]; NULL: all), else as zero, whatever the slot holds;
  * the state after its last token is written to the slot. A sequence without tokens leaves
  * its slot as it is. y and norm as in stepq_linattn_decode_step.
- * max_len: the longest sequence's length, which only chooses how the work is split (0: not
- * known). workspace: device, 256-byte aligned, at least
+ * max_len: the longest sequence's length (0: not known), which only chooses how the work is
+ * split and by which kernel it is done, hence the last bits of the results. workspace: device, 256-byte aligned, at least
  * stepq_linattn_workspace_bytes(cfg, B, tokens, max_len) bytes (0: NULL is fine), clobbered.
  * A sequence whose bounds are not ascending within [0, tokens] raises STEPQ_ERR_ARG and
  * one whose slot is out of range STEPQ_ERR_SLOT_RANGE (device errors); either is skipped.
@@ -349,7 +349,10 @@ stepq_status stepq_linattn_decode_step(const stepq_config *cfg, int layer, float
  * Where bounds descend the sequences around may share rows: if those that are split hold more
  * than `tokens` rows together, the call raises STEPQ_ERR_ARG and skips every sequence.
  * A value that is not finite may reach any output of its own sequence from the 64 tokens
- * it lies in (multiples of 64 from the start) on, and no other sequence. */
+ * it lies in (multiples of 64 from the start) on, and no other sequence.
+ * States, and fp32 readouts, are as exact as fp32 sums. In 16 bits a readout is within 2^-15 of
+ * the sum of its terms' absolute values, before it is rounded, which is more than the rounding
+ * where the terms cancel. */
 size_t stepq_linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int max_len);
 stepq_status stepq_linattn_prefill(const stepq_config *cfg, int layer, float *pool, int pool_slots,
                                    const int32_t *slots, const uint8_t *resume,
@@ -453,7 +456,9 @@ stepq_status stepq_stream_status(stepq_stream_t stream);
 
 /* Test support for the bounded waits (not for production use). Every wait of
  * the pipelined kernels (stepq_decode_step, the split halves, the FP32 and INT-b
- * decode steps, stepq_prefill_fp32, stepq_linattn_prefill in bf16) gives up after
+ * decode steps, stepq_prefill_fp32, and stepq_linattn_prefill in bf16 where max_len,
+ * or tokens if it is 0, is above 16 and rows of q, k and v are no nearer than their
+ * heads' channels: its other calls wait for nothing) gives up after
  * `wait_cycles` SM clock cycles (default 2e9, about one second; at least 1000;
  * stepq_linattn_prefill waits 2^31 at most), raises STEPQ_ERR_TIMEOUT and lets its
  * CTA return. withhold_item >= 0 makes every

@@ -8,7 +8,9 @@
 namespace stepq {
 namespace la {
 
-constexpr int kSms = 152;                               // a GB300's multiprocessors
+// A GB300's multiprocessors. A constant, since the bytes that a call asks for depend on it: they are the
+// same whatever device is current when they are asked for, and without one.
+constexpr int kSms = 152;
 
 // One CTA per SM takes a segment and head at a time, longest first, so the time of a call is
 // about its share W = tokens x Hv / 152 tokens a CTA, or the longest item's length L. Splitting

@@ -14,13 +14,14 @@
 // One CTA of eight warps per segment and head; warp w holds S^T of value columns 16 w .. + 15 in
 // registers, laid out as an accumulator of U^T, which is the layout of the left factor S^T too.
 // So a block's products need no exchange of the state: only P does, whose sums over the channels
-// are split over the warps. That is why these are warp-level products: for those of 64 tokens out
-// of tensor memory, the twelve tiles of one chunk's terms take 192 KB of shared memory, so that
-// no second chunk could be prepared beside it. Vectors are split into their terms once, by the thread that loads them, into swizzled rows of 256 bytes;
-// P is formed a block ahead; two barriers a block.
+// are split over the warps. That is why these are warp-level products. Out of tensor memory the
+// twelve tiles of one chunk's terms take 192 KB of shared memory for 64 tokens, with no room for a
+// second chunk beside it; for 32 tokens two would fit, which is not built. Vectors are split into
+// their terms once, by the thread that loads them, into swizzled rows of 256 bytes; P is formed a
+// block ahead; two barriers a block.
 //
-// The products' rate and latency bound it (216 of a warp a block in fp32, 140 in fp16; the pipe 69%
-// busy): 16 x 1024 tokens of 32 heads take 0.88 ms in fp32, 0.63 in fp16; 3 x 333 tokens in fp32
+// The products' rate and latency bound it (216 of a warp a block in fp32, 140 in fp16; the pipe 79%
+// busy where a CTA runs): 16 x 1024 tokens of 32 heads take 0.88 ms in fp32, 0.63 in fp16; 3 x 333 tokens in fp32
 // 76 us. In blocks of eight tokens on the FMA units the same took 1.10 and 1.10 ms, and 95 us; token by
 // token 215 us. 16-bit vectors leave room for two CTAs a multiprocessor (fp16 with one: 0.83 ms);
 // in fp32 two spill (1.00 ms).

@@ -16,7 +16,7 @@
 // chunk's whole time, 4100 cycles), so V is transposed once into tensor memory.
 // q, k and v are bf16 and enter as they are. What is fp32 enters as
 // a sum of bf16: K' as three truncated terms, exactly, since states are kept in fp32; S and P
-// as a truncated head and a rounded rest (2^-17 of each value; the result is rounded to
+// as a head and a rest, both rounded (2^-17 of each value; the result is rounded to
 // 2^-9). The state itself stays in fp32 registers and U is formed apart from it, so what is
 // added from chunk to chunk is rounded to nearest (the tensor core's own sums truncate).
 //
@@ -191,6 +191,12 @@ __device__ __forceinline__ uint32_t rounded(uint64_t p) {
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(f2hi(p)), "f"(f2lo(p)));
     return d;
+}
+// A pair's heads rounded to nearest and, rounded too, what remains of them: 2^-17 of each value is lost,
+// twice as much after truncated heads. A head does not round to infinity: finite values keep a rest.
+__device__ __forceinline__ void head_rest(uint64_t p, uint32_t &h, uint32_t &r) {
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(f2hi(p)), "f"(f2lo(p)));
+    r = rounded(fsub2(p, u2pair(h << 16, h & 0xFFFF0000u)));
 }
 __device__ __forceinline__ uint64_t pair_at(const float *p) {           // 8-byte aligned
     return *(const uint64_t *)p;
@@ -532,9 +538,7 @@ __device__ __forceinline__ void weigh_scores(const Ctx<NORM> &x, uint32_t tm, in
                 uint32_t h[8], r[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const uint64_t p = fmul2(u2pair(u[2 * i], u[2 * i + 1]), f[i]);
-                    h[i] = heads(p);
-                    r[i] = rounded(rests(p));
+                    head_rest(fmul2(u2pair(u[2 * i], u[2 * i + 1]), f[i]), h[i], r[i]);
                 }
                 const int o0 = ((2 * b) ^ (t & 7)) * 16, o1 = ((2 * b + 1) ^ (t & 7)) * 16;
                 *(uint4 *)(row + o0) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -573,10 +577,7 @@ __device__ __forceinline__ void states(const Ctx<NORM> &x, uint32_t tm) {
                 for (int i = 0; i < 4; i++) {
                     uint32_t h[8], r[8];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        h[e] = heads(s[8 * i + e]);
-                        r[e] = rounded(rests(s[8 * i + e]));
-                    }
+                    for (int e = 0; e < 8; e++) head_rest(s[8 * i + e], h[e], r[e]);
                     tc::st8(tl + kColSh + 32 * half + 8 * i, h);
                     tc::st8(tl + kColSl + 32 * half + 8 * i, r);
                 }

@@ -648,3 +648,45 @@ def test_a_wait_bound_beyond_the_clock_still_holds():
     pool.fill_(0.5)
     call()
     assert A.stepq_device_error() == 0 and torch.equal(want[0], pool) and torch.equal(want[1], y)
+
+
+# ------------------------------------------------------------------ readouts that cancel
+# 1 + r for two r's of which a rest of 8 bits after a truncated head loses 2^-16, with either sign;
+# head and rest rounded to nearest hold both exactly, and any value to 2^-17.
+UP, DOWN = 1 + 2.0 ** -7 - 2.0 ** -16, 1 + 2.0 ** -7 - 3 * 2.0 ** -16
+
+
+def check_cancelled(y, terms, dt):
+    """y against the sum of `terms` over the last axis: 2^-17 of each term's value, 64 u for the
+    sums, and half a unit."""
+    want, size = terms.sum(-1), terms.abs().sum(-1)
+    R.assert_within(y, want, R.rounded((2.0 ** -17 + 64 * R.U) * size, want, dt), "y")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("T", [9, 70])
+def test_readouts_of_a_state_that_cancel(T, dt):
+    """Half of a state's rows against the other half."""
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=1), torch.zeros(1, dtype=torch.int32, device="cuda")
+    sign = torch.ones(D, device="cuda")
+    sign[1::2] = -1
+    pool = torch.where(sign > 0, UP, DOWN).float()[:, None].expand(D, D).contiguous().view(1, 1, 1, D, D)
+    q, zero = sign.to(dt).expand(T, 1, D).contiguous(), torch.zeros((T, 1, D), dtype=dt, device="cuda")
+    y, gate = torch.empty((T, 1, D), dtype=dt, device="cuda"), torch.ones((T, 1), device="cuda")
+    A.stepq_linattn_prefill(cfg, 0, pool, slots, q, zero, zero, gate, y, max_len=T)
+    check_cancelled(y, (pool[0, 0, 0].double() * sign[:, None]).t().expand(T, 1, D, D), dt)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("T", [8, 64])
+def test_readouts_of_scores_that_cancel(T, dt):
+    """Half of a prompt's tokens against the other half."""
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=1), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.zeros((T, 1, D), dtype=dt, device="cuda") for _ in range(3))
+    q[..., :3], k[..., 0], k[..., 1] = 1, 1, 2.0 ** -7
+    k[::2, :, 2], k[1::2, :, 2] = -2.0 ** -16, -3 * 2.0 ** -16
+    v[::2], v[1::2] = 1, -1
+    pool, y = torch.zeros((1, 1, 1, D, D), device="cuda"), torch.empty((T, 1, D), dtype=dt, device="cuda")
+    A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, torch.ones((T, 1), device="cuda"), y, max_len=T)
+    scores = (q[:, 0].double() @ k[:, 0].double().t()).tril()
+    check_cancelled(y, scores[:, None, None, :] * v[:, 0].double().t()[None, None], dt)

@@ -350,7 +350,7 @@ stepq_status stepq_linattn_decode_step(const stepq_config *cfg, int layer, float
  * than `tokens` rows together, the call raises STEPQ_ERR_ARG and skips every sequence.
  * A value that is not finite may reach any output of its own sequence from the 64 tokens
  * it lies in (multiples of 64 from the start) on, and no other sequence.
- * States, and fp32 readouts, are as exact as fp32 sums. In 16 bits a readout is within 2^-15 of
+ * States, and fp32 readouts, are as exact as fp32 sums. In 16 bits a readout is within 2^-16 of
  * the sum of its terms' absolute values, before it is rounded, which is more than the rounding
  * where the terms cancel. */
 size_t stepq_linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int max_len);

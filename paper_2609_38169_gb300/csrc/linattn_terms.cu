@@ -4,11 +4,11 @@
 // With c_t = g_1 .. g_t and w_ts = g_{s+1} .. g_t inside a block of 16 tokens:
 //   Y^T = (S_0^T Q^T) diag(c_t) + V^T P^T,   P_ts = w_ts (q_t . k_s), zero for s > t
 //   S_16 = c_16 S_0 + U,   U^T = V^T K',   K'_s = w_16s k_s
-// A factor is the sum of terms, each the rest of those before rounded to bf16. fp32: three terms,
-// which leave 2^-27, and of a product the six pairs of terms of more than 2^-27 of it. fp16 and
-// bf16: q, k and v are two terms or one exactly; S and P are two (2^-18: the readout is rounded to
-// 2^-12 or 2^-9), and of their products the pairs of more than 2^-18 are taken; K' has three here
-// too, since states are kept in fp32. U is formed apart from S and added to it in fp32, smaller
+// A factor is the sum of terms, each the rest of those before rounded to bf16: an fp32 value is three
+// exactly, an fp16 value two. Of a product the pairs of terms i and j (from 0) with i + j <= 2 are
+// taken; those left out are below 2^-24 of it together. fp16 and bf16: q, k and v are two terms
+// or one; S and P are two (2^-17 of each value is lost: the readout is rounded to 2^-12 or 2^-9); K'
+// has three here too, since states are kept in fp32. U is formed apart from S and added to it in fp32, smaller
 // pairs first: what the tensor core's sums truncate does not add up from block to block.
 //
 // One CTA of eight warps per segment and head; warp w holds S^T of value columns 16 w .. + 15 in
@@ -20,8 +20,8 @@
 // their terms once, by the thread that loads them, into swizzled rows of 256 bytes; P is formed a
 // block ahead; two barriers a block.
 //
-// The products' rate and latency bound it (216 of a warp a block in fp32, 140 in fp16; the pipe 79%
-// busy where a CTA runs): 16 x 1024 tokens of 32 heads take 0.88 ms in fp32, 0.63 in fp16; 3 x 333 tokens in fp32
+// The products' rate and latency bound it (216 of a warp a block in fp32, 160 in fp16; the pipe 79%
+// busy where a CTA runs): 16 x 1024 tokens of 32 heads take 0.88 ms in fp32, 0.66 in fp16; 3 x 333 tokens in fp32
 // 76 us. In blocks of eight tokens on the FMA units the same took 1.10 and 1.10 ms, and 95 us; token by
 // token 215 us. 16-bit vectors leave room for two CTAs a multiprocessor (fp16 with one: 0.83 ms);
 // in fp32 two spill (1.00 ms).
@@ -70,12 +70,12 @@ __device__ __forceinline__ void split(uint64_t x, uint32_t (&t)[N]) {
         if (i + 1 < N) x = fsub2(x, u2pair(t[i] << 16, t[i] & 0xFFFF0000u));
     }
 }
-// d += the product of A's and B's terms i and j, i + j < MOST, smaller ones first; SETS > 1: those of
+// d += the product of A's and B's terms i and j, i + j <= 2, smaller ones first; SETS > 1: those of
 // each order i + j apart, so that fewer of the products wait for one another.
-template <int MOST, int NA, int NB, int SETS>
+template <int NA, int NB, int SETS>
 __device__ __forceinline__ void product(float (&d)[SETS][4], const uint32_t (&A)[NA][4], const uint32_t (&B0)[NB], const uint32_t (&B1)[NB]) {
 #pragma unroll
-    for (int sum = MOST - 1; sum >= 0; sum--)
+    for (int sum = 2; sum >= 0; sum--)
 #pragma unroll
         for (int i = 0; i < NA; i++)
             if (sum - i >= 0 && sum - i < NB) mma(d[sum < SETS ? sum : SETS - 1], A[i], B0[sum - i], B1[sum - i]);
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
                 b1[m] = B[m][2 * i + 1];
             }
             float p[1][4] = {};
-            product<N>(p, A, b0, b1);
+            product(p, A, b0, b1);
             *(float2 *)&sums[w * TB * TB + g * TB + 8 * i + 2 * c] = make_float2(p[0][0], p[0][1]);
             *(float2 *)&sums[w * TB * TB + (g + 8) * TB + 8 * i + 2 * c] = make_float2(p[0][2], p[0][3]);
         }
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
                         b0[m] = B[m][2 * i];
                         b1[m] = B[m][2 * i + 1];
                     }
-                    product<NS>(y[i], A, b0, b1);
+                    product(y[i], A, b0, b1);
                 }
             }
             uint32_t B[NS][4];
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
                     b1[m] = B[m][2 * i + 1];
                 }
                 float o[1][4] = {};
-                product<NS>(o, V, b0, b1);
+                product(o, V, b0, b1);
 #pragma unroll
                 for (int e = 0; e < 2; e++) {                // token 8 i + 2 c (+ 1)
                     const int tk = 8 * i + 2 * c + e;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) linattn_terms_ker
                     b1[m] = B[m][2 * i + 1];
                 }
                 float u[1][4] = {};
-                product<3>(u, V, b0, b1);
+                product(u, V, b0, b1);
 #pragma unroll
                 for (int e = 0; e < 4; e++) S[j + i][e] = fmaf(S[j + i][e], all, u[0][e]);
             }

@@ -690,3 +690,38 @@ def test_readouts_of_scores_that_cancel(T, dt):
     A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, torch.ones((T, 1), device="cuda"), y, max_len=T)
     scores = (q[:, 0].double() @ k[:, 0].double().t()).tril()
     check_cancelled(y, scores[:, None, None, :] * v[:, 0].double().t()[None, None], dt)
+
+
+# fp16 factors of two terms each, 1 and 2^-8: products of the small ones are 2^-16 of the whole.
+TWO, ABOVE, BELOW = 1 + 2.0 ** -8, 1 + 2.0 ** -8 - 2.0 ** -16, 1 + 2.0 ** -8 + 2.0 ** -16
+
+
+@pytest.mark.parametrize("T", [9, 70])
+def test_readouts_of_two_terms_and_a_state_that_cancel(T):
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=1), torch.zeros(1, dtype=torch.int32, device="cuda")
+    sign = torch.ones(D, device="cuda")
+    sign[1::2] = -1
+    pool = torch.where(sign > 0, ABOVE, BELOW).float()[:, None].expand(D, D).contiguous().view(1, 1, 1, D, D)
+    q, zero = (sign * TWO).half().expand(T, 1, D).contiguous(), torch.zeros((T, 1, D), dtype=torch.float16, device="cuda")
+    y = torch.empty_like(q)
+    A.stepq_linattn_prefill(cfg, 0, pool, slots, q, zero, zero, torch.ones((T, 1), device="cuda"), y, max_len=T)
+    check_cancelled(y, (pool[0, 0, 0].double() * q[0, 0].double()[:, None]).t().expand(T, 1, D, D), torch.float16)
+
+
+@pytest.mark.parametrize("T", [8, 64])
+@pytest.mark.parametrize("of", ["scores", "values"])
+def test_readouts_of_two_terms_and_scores_that_cancel(of, T):
+    """Scores of two terms by two, or values of two terms weighed by such scores."""
+    cfg, slots = A.Config(n_layers=1, n_key_heads=1, n_value_heads=1), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.zeros((T, 1, D), dtype=torch.float16, device="cuda") for _ in range(3))
+    if of == "scores":
+        q[:], k[::2], k[1::2] = TWO, TWO, TWO + 2.0 ** -10
+        v[::2], v[1::2] = 1, -1
+    else:
+        q[..., :3], k[..., 0], k[..., 1] = 1, 1, 2.0 ** -8
+        k[::2, :, 2], k[1::2, :, 2] = -2.0 ** -16, 2.0 ** -16
+        v[::2], v[1::2] = TWO, -TWO
+    pool, y = torch.zeros((1, 1, 1, D, D), device="cuda"), torch.empty((T, 1, D), dtype=torch.float16, device="cuda")
+    A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, torch.ones((T, 1), device="cuda"), y, max_len=T)
+    scores = (q[:, 0].double() @ k[:, 0].double().t()).tril()
+    check_cancelled(y, scores[:, None, None, :] * v[:, 0].double().t()[None, None], torch.float16)

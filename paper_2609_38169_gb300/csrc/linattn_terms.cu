@@ -60,13 +60,14 @@ __device__ __forceinline__ void load_tiles(uint32_t (&r)[4], const bf16 *row) {
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(row)) : "memory");
 }
-// The terms of two values, a pair a word.
+// The terms of two values, a pair a word. But the last of several, none rounds to infinity: the largest
+// finite values keep finite terms, and an infinite one has an infinite last.
 template <int N>
 __device__ __forceinline__ void split(uint64_t x, uint32_t (&t)[N]) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(f2lo(x), f2hi(x));
-        t[i] = *(const uint32_t *)&p;
+        if (i + 1 < N) asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(t[i]) : "f"(f2hi(x)), "f"(f2lo(x)));
+        else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(t[i]) : "f"(f2hi(x)), "f"(f2lo(x)));
         if (i + 1 < N) x = fsub2(x, u2pair(t[i] << 16, t[i] & 0xFFFF0000u));
     }
 }

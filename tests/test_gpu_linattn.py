@@ -725,3 +725,27 @@ def test_readouts_of_two_terms_and_scores_that_cancel(of, T):
     A.stepq_linattn_prefill(cfg, 0, pool, slots, q, k, v, torch.ones((T, 1), device="cuda"), y, max_len=T)
     scores = (q[:, 0].double() @ k[:, 0].double().t()).tril()
     check_cancelled(y, scores[:, None, None, :] * v[:, 0].double().t()[None, None], torch.float16)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T", [9, 150])
+def test_the_largest_finite_values_stay_where_they_are_kept_out(T, dt):
+    """The type's largest and lowest values in tokens whose key is zero, and fp32's in rows of the state
+    that no query reads and no key writes: they add nothing, neither NaN."""
+    hk, hv = 1, 2
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q, k, v, z, gate = inputs(g, T, hk, hv, dt)
+    f, lim = torch.finfo(torch.float32), torch.finfo(dt)
+    k[[3, T - 1]] = 0
+    v[3], v[T - 1] = lim.min, lim.max
+    q[:, :, [7, 90]] = 0
+    k[:, :, [7, 90]] = 0
+    pool = torch.randn((1, 1, hv, D, D), generator=g, device="cuda")
+    pool[..., 7, :], pool[..., 90, :] = f.max, f.min
+    S = pool[0, 0].double()
+    y = torch.empty((T, hv, D), dtype=dt, device="cuda")
+    cfg = A.Config(n_layers=1, n_key_heads=hk, n_value_heads=hv)
+    A.stepq_linattn_prefill(cfg, 0, pool, torch.zeros(1, dtype=torch.int32, device="cuda"), q, k, v, gate, y, max_len=T)
+    yr, ya, Sa = R.linattn(S, q, k, v, gate)
+    check_y(y, yr, ya, dt, None, None)
+    R.assert_within(pool[0, 0], S, 64 * R.U * Sa + 1e-37, "state")

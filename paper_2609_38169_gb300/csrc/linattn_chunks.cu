@@ -31,7 +31,7 @@
 // Hand-over by mbarriers, every wait bounded. Loops keep few unrolled steps: unrolled, the
 // warps' code did not fit the instruction caches (a third of the stalls of issuing warps).
 //
-// 128 prompts of 512 tokens, 16 key and 32 value heads: 441 us, 4,100 cycles a chunk and head
+// 128 prompts of 512 tokens, 16 key and 32 value heads: 445 us, 4,150 cycles a chunk and head
 // (token by token 5,490 us; the bytes alone 283). Nothing is used up: issue slots 61%, shared
 // memory 39%, the tensor pipe 34%, HBM 60%; what is left are the hand-overs between warps.
 #include "async.cuh"

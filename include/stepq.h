@@ -361,9 +361,9 @@ stepq_status stepq_linattn_prefill(const stepq_config *cfg, int layer, float *po
                                    void *workspace, size_t workspace_bytes, stepq_stream_t stream);
 
 /* The normalisation on its own: x [rows][groups * width] in dtype (rows x_stride elements
- * apart, channels contiguous) to out (the same, out_stride apart; out may be x or z with the
- * same stride, else it overlaps neither). Any width
- * from 1 on and any alignment of x, out and z that their type has; statistics in fp32. */
+ * apart, channels contiguous) to out (the same, out_stride apart). out may be x or z with the
+ * same stride (another one: STEPQ_ERR_ARG); else it overlaps neither. Any width from 1 on and
+ * any alignment of x, out and z that their type has; statistics in fp32. */
 stepq_status stepq_group_norm(int dtype, int64_t rows, int groups, int width, const void *x,
                               int64_t x_stride, void *out, int64_t out_stride,
                               const stepq_norm *norm, stepq_stream_t stream);
@@ -461,8 +461,8 @@ stepq_status stepq_stream_status(stepq_stream_t stream);
  * heads' channels: its other calls wait for nothing) gives up after
  * `wait_cycles` SM clock cycles (default 2e9, about one second; at least 1000;
  * stepq_linattn_prefill waits 2^31 at most), raises STEPQ_ERR_TIMEOUT and lets its
- * CTA return. withhold_item >= 0 makes every
- * later launch skip the copies of that item (head * B + batch entry;
+ * CTA return. withhold_item >= 0 makes every later launch skip the copies of that
+ * item (head * B + batch entry;
  * stepq_prefill_fp32: the first copies of batch entry * Hv + head;
  * stepq_linattn_prefill: of segment * Hv + head, the segments longest first), so
  * that its wait runs out and the launch reports STEPQ_ERR_TIMEOUT with its results

@@ -368,6 +368,104 @@ stepq_status stepq_group_norm(int dtype, int64_t rows, int groups, int width, co
                               int64_t x_stride, void *out, int64_t out_stride,
                               const stepq_norm *norm, stepq_stream_t stream);
 
+/* --------------------------------------------------- paged key-value cache
+ * The softmax-attention layers that hybrid models have among their recurrent ones: keys
+ * and values of every token in pages of a pool, 16 bits each or as codes of 8 or 4 bits
+ * in the manner of the INT-b states, and the attention of one new token over them. The paper has no
+ * counterpart of these calls. */
+
+/* Formats of the pages. */
+#define STEPQ_KV_BF16 0
+#define STEPQ_KV_F16 1
+#define STEPQ_KV_INT8 2
+#define STEPQ_KV_INT4 3
+
+typedef struct {
+    int n_layers;            /* attention layers that a page holds */
+    int n_heads;             /* key heads */
+    int head_dim;            /* D: 64, 128 or 256 */
+    int page_tokens;         /* 8, 16, 32, 64, 128 or 256 */
+    int format;              /* STEPQ_KV_* */
+} stepq_kv_config;
+
+/* Bytes of a page (0 if the configuration is invalid). A page holds page_tokens tokens of
+ * every layer and head, ordered (layer, head):
+ *   K rows [page_tokens] | V rows [page_tokens] | for codes: fp16 scales of K [page_tokens] | of V
+ * A row is its D channels: 2 bytes each, 1 byte (8-bit codes) or half a byte (4-bit codes,
+ * the lower channel in the lower half). Codes are offset binary u = q + 2^(b-1), and stand for
+ * (u - 2^(b-1)) s with the row's scale s. */
+size_t stepq_kv_page_bytes(const stepq_kv_config *cfg);
+
+/* The pool of pages and the sequences' page tables: token p of sequence b lies in page
+ * table[b][p / page_tokens] at place p % page_tokens. Entries that a call's tokens do not
+ * reach are not read. */
+typedef struct {
+    void *pages;             /* device, n_pages * stepq_kv_page_bytes(), 16-byte aligned */
+    int n_pages;
+    int table_width;         /* entries of a row; table_width * page_tokens <= 2^30 */
+    const int32_t *table;    /* device int32 [B][table_width] */
+    int64_t table_stride;    /* entries from one row to the next, >= 0 */
+} stepq_kv_pages;
+
+/* Packed rows of K and V: one per token, a head's D channels contiguous and the heads of a
+ * row next to each other; strides in elements from one token's row to the next (k and v may be
+ * columns of one projection's rows). 16-byte aligned, strides a multiple of 16 bytes. */
+typedef struct {
+    int dtype;               /* STEPQ_F32, STEPQ_BF16 or STEPQ_F16 */
+    void *k, *v;             /* device [tokens][n_heads][D]; only stepq_kv_read writes to them */
+    int64_t k_stride, v_stride;
+} stepq_kv_rows;
+
+/* Write the rows of B sequences into one layer of their pages: sequence b's are rows
+ * cu_seqlens[b] .. cu_seqlens[b+1] - 1 of the `tokens` packed rows (device int32 [B+1],
+ * ascending within [0, tokens]; NULL: tokens / B each, tokens a multiple of B), and become its
+ * tokens starts[b], starts[b] + 1, .. (device int32 [B]). In 16 bits a value is rounded to the
+ * format. For codes of b bits, q = 2^(b-1) - 1 and the row's absmax (over values that are not NaN),
+ *   s = fp16(clamp(absmax / q, 2^-14, 65504)),   u = clamp(rint(x / s), -q, q) + 2^(b-1)
+ * with quotients rounded to fp32 and rint to the nearest, ties to even; NaN gets the code of zero.
+ * Two tokens of a call must not share a place. A token beyond the table (or a negative start)
+ * or whose page is outside [0, n_pages) raises STEPQ_ERR_SLOT_RANGE and is skipped; a row that lies
+ * between cu_seqlens' ends and in no sequence raises STEPQ_ERR_ARG (device errors). */
+stepq_status stepq_kv_append(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
+                             const int32_t *starts, const int32_t *cu_seqlens, int B, int tokens,
+                             const stepq_kv_rows *rows, stepq_stream_t stream);
+
+/* The same tokens read back into rows: code times scale, rounded once to dtype (a value of
+ * 16 bits is only rounded). Rows of skipped tokens, and rows of no sequence, stay as they are. Rows
+ * of different tokens must not overlap (strides >= n_heads * D). */
+stepq_status stepq_kv_read(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
+                           const int32_t *starts, const int32_t *cu_seqlens, int B, int tokens,
+                           const stepq_kv_rows *rows, stepq_stream_t stream);
+
+/* One new token of each of B sequences: query row b over sequence b's cached tokens. */
+typedef struct {
+    int dtype;               /* of q and y */
+    int n_heads;             /* query heads Hq, a multiple of the key heads: head h reads key head
+                                h / (Hq / n_heads) */
+    const void *q;           /* device [B][Hq][D]; strides and alignment as in stepq_kv_rows */
+    void *y;                 /* device [B][Hq][D] out; overlaps no input but q, whose rows it may be */
+    float *lse;              /* device [B][Hq] out or NULL: ln sum_t exp(s_t) */
+    int64_t q_stride, y_stride;
+    float scale;             /* of the scores, finite */
+    int window;              /* > 0: the last `window` tokens only; 0: all */
+    int max_len;             /* the longest sequence's length (0: not known), which only chooses how
+                                the work is split, hence the last bits of the results */
+} stepq_kv_query;
+
+/* s_t = scale q . k_t over tokens t in [max(0, len_b - window), len_b) (lens: device int32 [B], the
+ * new token among them, whose rows have been appended before), y = sum_t softmax(s)_t v_t. A row
+ * without tokens, or with scores of -infinity only, gives y = 0 and lse = -infinity. Values that
+ * are not finite reach the outputs of their own sequence and key head only, and those outside
+ * the tokens none. A negative length raises STEPQ_ERR_ARG and counts as 0; one beyond the table
+ * raises STEPQ_ERR_SLOT_RANGE and ends with it; so does a page outside [0, n_pages), whose tokens
+ * are read as zeros (device errors). y and lse for equal arguments are the same in every call.
+ * workspace: device, 256-byte aligned, at least stepq_kv_workspace_bytes() for the call's q_heads, B
+ * and max_len (0: NULL is fine), clobbered. */
+size_t stepq_kv_workspace_bytes(const stepq_kv_config *cfg, int q_heads, int B, int max_len);
+stepq_status stepq_kv_attend(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
+                             const int32_t *lens, int B, const stepq_kv_query *query,
+                             void *workspace, size_t workspace_bytes, stepq_stream_t stream);
+
 /* ------------------------------------------------------------- calibration (App. A.3)
  * Accumulate sum_t g_{t,i}^2 with g_t = A_t^T q_t (Sec. 4.1, Eq.
  * kda_sensitivity) and sum_t log r_{t,u} for n calibration tokens of one layer.

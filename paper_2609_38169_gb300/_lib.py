@@ -41,8 +41,26 @@ class StepqLinattnIo(C.Structure):
                 ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("gate_stride", C.c_int64), ("y_stride", C.c_int64)]
 
 
+class StepqKvConfig(C.Structure):
+    _fields_ = [("n_layers", I), ("n_heads", I), ("head_dim", I), ("page_tokens", I), ("format", I)]
+
+
+class StepqKvPages(C.Structure):
+    _fields_ = [("pages", P), ("n_pages", I), ("table_width", I), ("table", P), ("table_stride", C.c_int64)]
+
+
+class StepqKvRows(C.Structure):
+    _fields_ = [("dtype", I), ("k", P), ("v", P), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class StepqKvQuery(C.Structure):
+    _fields_ = [("dtype", I), ("n_heads", I), ("q", P), ("y", P), ("lse", P), ("q_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("scale", C.c_float), ("window", I), ("max_len", I)]
+
+
 CFG = C.POINTER(StepqConfig)
-IO = NORM = P           # a structure by reference, or its bytes (api.py packs them: a tenth of a Structure's time)
+KV = C.POINTER(StepqKvConfig)
+IO = NORM = PAGES = ROWS = QUERY = P           # a structure by reference, or its bytes (api.py packs them: a tenth of a Structure's time)
 
 # name -> (restype, argtypes); the exported symbol set of include/stepq.h
 SIGNATURES = {
@@ -77,6 +95,11 @@ SIGNATURES = {
     "stepq_linattn_workspace_bytes": (SZ, [CFG, I, I, I]),
     "stepq_linattn_prefill": (I, [CFG, I, P, I, P, P, P, I, I, I, IO, NORM, P, SZ, P]),
     "stepq_group_norm": (I, [I, C.c_int64, I, I, P, C.c_int64, P, C.c_int64, NORM, P]),
+    "stepq_kv_page_bytes": (SZ, [KV]),
+    "stepq_kv_append": (I, [KV, I, PAGES, P, P, I, I, ROWS, P]),
+    "stepq_kv_read": (I, [KV, I, PAGES, P, P, I, I, ROWS, P]),
+    "stepq_kv_workspace_bytes": (SZ, [KV, I, I, I]),
+    "stepq_kv_attend": (I, [KV, I, PAGES, P, I, QUERY, P, SZ, P]),
     "stepq_validate_slots": (I, [P, I, I, P, P, P]),
     "stepq_validate_slots_noalloc": (I, [P, I, I, P, P]),
     "stepq_device_error": (I, [P]),

@@ -13,13 +13,14 @@ from dataclasses import dataclass, field
 import numpy as np
 
 from . import _lib
-from ._lib import StepqCalib, StepqConfig, StepqPlanInfo, check
+from ._lib import StepqCalib, StepqConfig, StepqKvConfig, StepqPlanInfo, check
 
 D = 128
 GATE_SCALAR = 0
 GATE_CHANNEL = 1
 PIVOT_BITS = 16
 ACT_NONE, ACT_SILU, ACT_SIGMOID = 0, 1, 2
+KV_BF16, KV_F16, KV_INT8, KV_INT4 = 0, 1, 2, 3
 
 
 _CONFIGS: dict = {}
@@ -584,6 +585,129 @@ def stepq_group_norm(x, groups: int, out, norm: Norm, stream=None):
     check(_lib.lib().stepq_group_norm(_dtype_code(x.dtype), rows, int(groups), channels // groups, xp, xs, op, os_,
                                       _c_norm(norm, x.dtype, rows, channels, channels // groups),
                                       _stream(stream)), "stepq_group_norm")
+
+
+# ------------------------------------------------------------------ paged key-value cache
+_KV_CONFIGS: dict = {}
+_pack_pages = struct.Struct("@PiiPq").pack            # of _lib.StepqKvPages
+_pack_rows = struct.Struct("@i4xPPqq").pack           # of _lib.StepqKvRows
+_pack_query = struct.Struct("@iiPPPqqfii4x").pack     # of _lib.StepqKvQuery
+
+
+@dataclass
+class KvConfig:
+    """stepq_kv_config: pages of page_tokens tokens for every layer and key head, as bf16 or
+    fp16 or as codes of 8 or 4 bits (KV_BF16, KV_F16, KV_INT8, KV_INT4)."""
+    n_layers: int
+    n_heads: int
+    head_dim: int = D
+    page_tokens: int = 64
+    format: int = KV_BF16
+
+    def _kept(self):
+        """The C structure by reference and the bytes of a page, kept by the fields' values."""
+        key = (self.n_layers, self.n_heads, self.head_dim, self.page_tokens, self.format)
+        kept = _KV_CONFIGS.get(key)
+        if kept is None:
+            if len(_KV_CONFIGS) >= 64:
+                _KV_CONFIGS.clear()
+            ref = C.byref(StepqKvConfig(*key))
+            kept = _KV_CONFIGS[key] = ref, int(_lib.lib().stepq_kv_page_bytes(ref))
+        return kept
+
+
+def stepq_kv_page_bytes(kv: KvConfig) -> int:
+    return kv._kept()[1]
+
+
+def alloc_pages(kv: KvConfig, n_pages: int, device="cuda"):
+    import torch
+    return torch.zeros(n_pages * stepq_kv_page_bytes(kv), dtype=torch.uint8, device=device)
+
+
+def _kv_pages(kv, pages, table, B):
+    """The configuration by reference, and the packed pages and tables of a call for B sequences."""
+    ref, nbytes = kv._kept()
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError(f"table: expected {B} rows, got shape {tuple(table.shape)}")
+    W = table.shape[1]
+    if not table.is_cuda or table.dtype is not _Torch.i32 or (W > 1 and table.stride(1) != 1):
+        raise ValueError("table: expected rows of contiguous int32 on a CUDA device")
+    if pages.get_device() != table.get_device():
+        raise ValueError("pages and table are on different devices")
+    n = pages.numel() * pages.element_size() // nbytes if nbytes else 1      # the library refuses the rest
+    return ref, _pack_pages(_dev_ptr(pages), n, W, table.data_ptr(), table.stride(0) if B > 1 else W)
+
+
+def _head_rows(t, dtype, rows, heads, dim, pages, what):
+    """Pointer and row stride of rows [rows][heads][dim] (or [rows][heads * dim]) beside `pages`."""
+    shape, st = t.shape, t.stride()
+    if t.get_device() != pages.get_device() or not t.is_cuda:
+        raise ValueError(f"{what}: expected a CUDA tensor on the pages' device")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if len(shape) == 3:
+        ok = shape[1] == heads and shape[2] == dim and st[2] == 1 and (heads == 1 or st[1] == dim)
+    else:
+        ok = len(shape) == 2 and shape[1] == heads * dim and st[1] == 1
+    if not ok or shape[0] != rows:
+        raise ValueError(f"{what}: expected {rows} contiguous rows of {heads} x {dim}, got shape {tuple(shape)}, "
+                         f"strides {tuple(st)}")
+    return t.data_ptr(), st[0] if rows > 1 else heads * dim
+
+
+def _kv_transfer(call, name, kv, layer, pages, table, starts, k, v, cu_seqlens, stream):
+    _f32()
+    B, n = starts.numel(), k.shape[0]
+    if cu_seqlens is not None and cu_seqlens.numel() != B + 1:
+        raise ValueError(f"cu_seqlens: expected {B + 1} values, got {cu_seqlens.numel()}")
+    ref, pg = _kv_pages(kv, pages, table, B)
+    kp, ks = _head_rows(k, k.dtype, n, kv.n_heads, kv.head_dim, pages, "k")
+    vp, vs = _head_rows(v, k.dtype, n, kv.n_heads, kv.head_dim, pages, "v")
+    check(call(ref, layer, pg, _dev_ptr(starts, _Torch.i32), _dev_ptr(cu_seqlens, _Torch.i32), B, n,
+               _pack_rows(_dtype_code(k.dtype), kp, vp, ks, vs), _stream(stream)), name)
+
+
+def stepq_kv_append(kv: KvConfig, layer: int, pages, table, starts, k, v, cu_seqlens=None, stream=None):
+    """Rows k, v [tokens][heads][D] (rows may be strided) into one layer of the pages: sequence
+    b's become its tokens from starts[b] (int32 [B]) on; table int32 [B][width]; cu_seqlens
+    int32 [B+1] (None: equal lengths)."""
+    _kv_transfer(_lib.lib().stepq_kv_append, "stepq_kv_append", kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+
+
+def stepq_kv_read(kv: KvConfig, layer: int, pages, table, starts, k, v, cu_seqlens=None, stream=None):
+    """The tokens that stepq_kv_append would write, read into k and v."""
+    _kv_transfer(_lib.lib().stepq_kv_read, "stepq_kv_read", kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+
+
+def stepq_kv_workspace_bytes(kv: KvConfig, q_heads: int, B: int, max_len: int = 0) -> int:
+    return int(_lib.lib().stepq_kv_workspace_bytes(kv._kept()[0], int(q_heads), int(B), int(max_len)))
+
+
+def stepq_kv_attend(kv: KvConfig, layer: int, pages, table, lens, q, y, scale=None, window: int = 0, lse=None,
+                    max_len: int = 0, workspace=None, stream=None):
+    """Attention of one token of every sequence over its lens[b] (int32 [B]) cached tokens, or the
+    last `window` of them: q, y [B][Hq][D] (rows may be strided), lse fp32 [B][Hq] or None; scale
+    1 / sqrt(D) if not given. A workspace that is needed and not given (uint8) comes from torch."""
+    f, B = _f32(), lens.numel()
+    ref, pg = _kv_pages(kv, pages, table, B)
+    Dh = kv.head_dim
+    Hq = q.shape[1] if q.dim() == 3 else q.shape[1] // Dh
+    qp, qs = _head_rows(q, q.dtype, B, Hq, Dh, pages, "q")
+    yp, ys = _head_rows(y, q.dtype, B, Hq, Dh, pages, "y")
+    if lse is not None and lse.numel() != B * Hq:
+        raise ValueError(f"lse: expected {B * Hq} values, got {lse.numel()}")
+    lib = _lib.lib()
+    if workspace is None:
+        most = table.shape[1] * kv.page_tokens
+        nbytes = lib.stepq_kv_workspace_bytes(ref, Hq, B, min(max_len, most) if max_len > 0 else most)
+        if nbytes:
+            workspace = _scratch(nbytes, q.device, stream)
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    io = _pack_query(_dtype_code(q.dtype), Hq, qp, yp, _dev_ptr(lse, f) or 0, qs, ys,
+                     Dh ** -0.5 if scale is None else scale, window, max_len)
+    check(lib.stepq_kv_attend(ref, layer, pg, _dev_ptr(lens, _Torch.i32), B, io, _dev_ptr(workspace), have,
+                              _stream(stream)), "stepq_kv_attend")
 
 
 # ------------------------------------------------------------------ calibration driver

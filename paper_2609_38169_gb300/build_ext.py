@@ -14,8 +14,10 @@ SO = os.path.join(BUILD, "libstepq.so")
 INCLUDE = os.path.join(ROOT, "include")
 SOURCES = ["plan.cpp", "api.cpp", "errors.cu", "stepq_kernels.cu", "heads.cu", "rows.cu", "baselines.cu", "intb.cu", "temporal.cu", "fp32.cu", "prefill.cu",
            "calib.cu", "calibrate.cu", "linattn.cpp", "linattn_decode.cu", "linattn_prefill.cu",
-           "linattn_plan.cu", "linattn_chunks.cu", "linattn_terms.cu", "groupnorm.cu"]
-HEADERS = ["internal.h", "device.cuh", "async.cuh", "pipeline.cuh", "tile.cuh", "tcgen05.cuh", "linattn.cuh", "linattn_prefill.cuh"]
+           "linattn_plan.cu", "linattn_chunks.cu", "linattn_terms.cu", "groupnorm.cu",
+           "kv.cpp", "kv_rows.cu", "kv_attend_bf16.cu", "kv_attend_f16.cu", "kv_attend_int8.cu", "kv_attend_int4.cu"]
+HEADERS = ["internal.h", "device.cuh", "async.cuh", "pipeline.cuh", "tile.cuh", "tcgen05.cuh", "linattn.cuh", "linattn_prefill.cuh",
+           "kv.cuh", "kv_attend.cuh", "kv_launch.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -147,6 +147,13 @@ size_t linattn_workspace_bytes(const stepq_config *cfg, int B, int tokens, int m
 // groupnorm.cu
 stepq_status launch_group_norm(int dtype, int64_t rows, int groups, int width, const void *x, int64_t x_stride,
                                void *out, int64_t out_stride, const stepq_norm *norm, cudaStream_t s);
+// kv_rows.cu, kv_attend_*.cu: the paged key-value cache (arguments checked)
+stepq_status launch_kv_rows(bool append, const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
+                            const int32_t *starts, const int32_t *cu, int B, int tokens, const stepq_kv_rows *rows,
+                            cudaStream_t s);
+size_t kv_workspace_bytes(const stepq_kv_config *cfg, int q_heads, int64_t rows, int64_t most);
+stepq_status launch_kv_attend(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages, const int32_t *lens,
+                              int B, const stepq_kv_query *q, int64_t most, void *workspace, cudaStream_t s);
 // calib.cu
 stepq_status launch_calib_observe(const stepq_config *cfg, int layers, const float *q, const float *k,
                                   const float *beta, const float *gate, int n, double *omega_sum,

@@ -1,0 +1,84 @@
+// Choice of a variant of the attention kernels, and their launch.
+#pragma once
+
+#include "kv_attend.cuh"
+
+namespace stepq {
+namespace kv {
+
+// Terms of a variant: queries and weights enter the products as sums of QT and PT terms of the
+// pages' 16-bit type.
+//  * bf16 vectors over fp16 and codes: a query of 8 bits is one term of fp16, exactly; a
+//    weight's one term has 2^-12, an eighth of the output's own rounding.
+//  * bf16 vectors over bf16: one term of a weight would have the output's own rounding again, two
+//    have 2^-17.
+//  * fp16 and fp32 vectors: two terms of fp16 (2^-23), three of bf16 (2^-25); fp16 queries need
+//    one and two of them, and take the fp32 variant.
+template <int F, int D, int NT, bool WIDE>
+using Variant = Shape<F, D, NT, F == STEPQ_KV_BF16 ? (WIDE ? 3 : 1) : (WIDE ? 2 : 1), F == STEPQ_KV_BF16 ? (WIDE ? 3 : 2) : (WIDE ? 2 : 1)>;
+
+// Runs f(Shape{}) for the variant of a call; more than 8 query heads a key head go in sixteens.
+template <int F, class Fn>
+auto by_shape(int head_dim, int groups, bool wide, Fn &&f) {
+    auto terms = [&](auto d, auto nt) {
+        constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+        return wide ? f(Variant<F, D, NT, true>{}) : f(Variant<F, D, NT, false>{});
+    };
+    auto heads = [&](auto d) {
+        return groups > 8 ? terms(d, std::integral_constant<int, 2>{}) : terms(d, std::integral_constant<int, 1>{});
+    };
+    return head_dim == 64    ? heads(std::integral_constant<int, 64>{})
+           : head_dim == 128 ? heads(std::integral_constant<int, 128>{})
+                             : heads(std::integral_constant<int, 256>{});
+}
+
+// CTAs of a call, from what the host knows: its rows and the most tokens that one has. `whole`:
+// each takes whole sequences. Fewer tokens never need more CTAs, so a workspace for `most` serves
+// every call below it.
+struct Grid { int ctas; bool whole; };
+template <class S>
+Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
+    const int64_t tiles = (most + S::TT - 1) / S::TT;
+    const int64_t heads = rows * c->n_heads * ((groups + S::HT - 1) / S::HT);
+    const int64_t resident = (int64_t)sm_count() * S::RESIDENT;
+    if (tiles <= 2 * kAttWarps) return {(int)(heads < 8 * resident ? heads : 8 * resident), true};
+    const int64_t ctas = (heads * tiles + 2 * kAttWarps - 1) / (2 * kAttWarps);
+    return {(int)(ctas < resident ? ctas : resident), false};
+}
+template <class S>
+size_t parts_bytes(const Grid &g) {
+    if (g.whole) return 0;
+    return (size_t)g.ctas * (2 * sizeof(float) * part_floats<S::HT, S::D>() + sizeof(Joined));
+}
+
+template <int F>
+size_t attend_workspace(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
+    size_t need = 0;
+    for (int wide = 0; wide < 2; wide++)
+        by_shape<F>(c->head_dim, groups, wide, [&](auto sh) {
+            using S = decltype(sh);
+            const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most));
+            if (n > need) need = n;
+        });
+    return need;
+}
+
+template <int F>
+stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int64_t most, cudaStream_t s) {
+    return by_shape<F>(c->head_dim, args.groups, args.dtype != STEPQ_BF16, [&](auto sh) {
+        using S = decltype(sh);
+        static SmemOptIn opt;
+        AttendArgs a = args;
+        if (a.window > 0 && a.window + S::TT < most) most = a.window + S::TT;      // a window ends inside a tile
+        const Grid g = grid_of<S>(c, a.groups, a.B, most);
+        a.whole = g.whole;
+        stepq_status st = opt((const void *)kv_attend_kernel<S>, S::SMEM);
+        if (st != STEPQ_OK) return st;
+        st = launch_overlapped(kv_attend_kernel<S>, g.ctas, 32 * kAttWarps, S::SMEM, s, a);
+        if (st != STEPQ_OK || g.whole) return st;
+        return launch_overlapped(kv_join_kernel<S::HT, S::D>, g.ctas, 256, 0, s, a);
+    });
+}
+
+}  // namespace kv
+}  // namespace stepq

@@ -197,10 +197,10 @@ inline stepq_status cuda_status(cudaError_t e) {
 // plain stream order 8.89 (8.16); 128 slots: 1.21 (1.11), 1.31 (0.83) and 1.24 (1.14). Both
 // parts on one stream take 9.28 and 1.38 ms, with the early start 9.27 and 1.35.
 template <class Args, class... Rest>
-inline stepq_status launch_overlapped(void (*kernel)(Args, Rest...), int grid, int block, int smem, cudaStream_t s,
+inline stepq_status launch_overlapped(void (*kernel)(Args, Rest...), dim3 grid, int block, int smem, cudaStream_t s,
                                       const Args &a, Rest... rest) {
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)grid);
+    c.gridDim = grid;
     c.blockDim = dim3((unsigned)block);
     c.dynamicSmemBytes = (size_t)smem;
     c.stream = s;

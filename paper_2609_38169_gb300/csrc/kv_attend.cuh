@@ -11,7 +11,8 @@
 // CTA's share is pieces of one or more sequences; a piece that is a whole sequence gives its
 // outputs, one that is not leaves (R, l, O) in the workspace, and a second kernel joins those.
 // Within a CTA each warp takes every fourth tile, through its own ring of shared memory filled
-// by 16-byte asynchronous copies, and waits for no other warp until the piece ends.
+// by 16-byte asynchronous copies, and waits for no other warp until the piece ends. The ring
+// runs on into the next piece's tiles, which arrive while this piece's parts are put together.
 //
 // Products by mma.sync m16n8k16 with tokens (for K) and channels (for V) as the 16 rows and
 // eight query heads as the columns, so that no part of a product is padding where eight heads
@@ -36,13 +37,20 @@ namespace stepq {
 namespace kv {
 
 constexpr int kAttWarps = 4;
+#ifndef KV_ST
+#define KV_ST 32
+#define KV_SC 3
+#define KV_S16 2
+#define KV_RC 4
+#endif
 constexpr float kLow = -3.402823466e+38f;
 
 // Workspace: for each CTA c two parts (2 c: the piece that its share begins with, 2 c + 1: one
-// that it ends with) of HT heads, [HT][D] of O and then R and l [HT] each; behind the parts an
-// int4 for each CTA that says which parts the piece begun by it and ended by others has.
+// that it ends with) of HT heads, [HT][D] of O and then R and l [HT] each. Behind them, for each
+// (sequence, virtual head) or, where those are more than the CTAs, for each CTA, which parts the
+// piece has that it begins and others end.
 struct Joined {
-    int count, first, b, vh;        // first part; the others are 2 (c + 1), 2 (c + 2), ..
+    int count, first, b, vh;        // parts; the first one's number, the others are those of the next CTAs
 };
 template <int HT, int D> __host__ __device__ constexpr int part_floats() { return HT * (D + 2); }
 
@@ -56,17 +64,21 @@ struct Shape {
     static constexpr int HT = 8 * NT;                        // heads of a CTA
     static constexpr int RB = row_bytes(F, D);
     static constexpr bool CODED = coded(F);
-    // tokens of a tile: 8 KB of K and V where that is 16 to 64 of them
-    static constexpr int TT = RB * 2 * 64 <= 8192 ? 64 : RB * 2 * 32 <= 8192 ? 32 : 16;
+    // A tile: 4 KB of codes of up to 128 head channels, else 8 or 16; 16 to 64 tokens.
+    static constexpr int WANT = CODED ? 32 * (NT * D > 128 ? NT * D : 128) : 64 * (D > 128 ? D : 128);
+    static constexpr int FIT = WANT / (2 * RB), TT = FIT > 64 ? 64 : FIT;
+    static constexpr int ST = NT * D >= 256 || TT == 16 ? 16 : KV_ST;       // taken at once
     static constexpr int TILE = 2 * TT * RB + (CODED ? 4 * TT : 0);
-    static constexpr int STAGES = 3;
-    static constexpr int RING = kAttWarps * STAGES * TILE;
-    static constexpr int MERGE = kAttWarps * HT * (D + 2) * 4;
-    static constexpr int OFF_Q = RING > MERGE ? RING : MERGE;          // [QT][NT][D / 16][32] uint2
+    static constexpr int STAGES = CODED ? KV_SC : KV_S16;
+    static constexpr int OFF_Q = kAttWarps * STAGES * TILE;            // [QT][NT][D / 16][32] uint2
     static constexpr int OFF_HEAD = OFF_Q + QT * NT * (D / 16) * 256;  // float [2][HT]: factor, offset
-    static constexpr int OFF_SCAN = OFF_HEAD + 2 * HT * 4;             // int64 [kAttWarps + 2]
+    static constexpr int OFF_SUM = OFF_HEAD + 2 * HT * 4;              // float [kAttWarps][2][HT]: R, l
+    static constexpr int OFF_SCAN = OFF_SUM + kAttWarps * 2 * HT * 4;  // int64 [kAttWarps + 2]
     static constexpr int SMEM = OFF_SCAN + 8 * (kAttWarps + 4);
-    static constexpr int RESIDENT = SMEM <= 75 * 1024 ? 3 : SMEM <= 113 * 1024 ? 2 : 1;
+    // CTAs of a multiprocessor, by shared memory and by registers
+    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED ? KV_RC : 3, BY_SMEM = 227 * 1024 / (SMEM + 1024);
+    static constexpr int RESIDENT = BY_REGS < BY_SMEM ? BY_REGS : BY_SMEM;
+    static_assert(TILE >= HT * D * 4, "a warp's part is put together in one stage of its ring");
     static constexpr int KP = RB / 4 < 16 ? RB / 4 : 16;     // bytes a lane reads of a row of K at once
     static constexpr int VP = RB / 8 < 16 ? RB / 8 : 16;     // and of V
     static constexpr int KS = D / 16;                        // steps of K's product
@@ -125,6 +137,9 @@ template <int BYTES>
 __device__ __forceinline__ Words<BYTES / 4> lds(const uint8_t *tile, uint32_t at) {
     return *(const Words<BYTES / 4> *)(tile + at);
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool valid) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
@@ -141,7 +156,7 @@ __device__ __forceinline__ uint32_t v_place(int row, int byte) {
     return (uint32_t)(row * RB + byte) ^ (RB >= 64 ? ((row >> 1) & 3) << 5 : ((row >> 2) & 1) << 5);
 }
 
-// A lane's piece of a row of K as pairs of the compute type, in the order of q_channel().
+// A lane's piece of a row of K as pairs of the compute type, in the order that Queries::put() gives the queries.
 template <int F, int N>
 __device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 / bits_of(F)]) {
 #pragma unroll
@@ -160,14 +175,6 @@ __device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 
         }
     }
 }
-// Channel of half `half` of pair j (of one piece's) as k_pairs() leaves them.
-template <int F>
-__host__ __device__ constexpr int q_channel(int j, int half) {
-    return F == STEPQ_KV_INT4 ? 8 * (j / 4) + j % 4 + 4 * half : 2 * j + half;
-}
-template <int F>
-__host__ __device__ constexpr float q_factor(int j) { return F == STEPQ_KV_INT4 && (j & 1) ? 0.0625f : 1.f; }
-
 // A lane's pieces of two tokens' rows of V as pairs of tokens, p[channel]: one 2^-24 of the code
 // without its offset, and for the odd channels of 4 bits 2^-20.
 template <int F, int N>
@@ -212,17 +219,107 @@ __device__ __forceinline__ void store4_any(void *p, int64_t i, int dtype, const 
     else la::store_vec<la::f16, 4>((la::f16 *)p + i, x);
 }
 
-// Tokens [lo, hi) of a row that count, and its tiles (one for a row without any).
-struct Span { int lo, hi, tile0, tiles; };
+// A piece: tiles from .. from + n - 1 of the `tiles` of sequence b, virtual head vh, whose tokens
+// [lo, hi) count (a row without any has one tile).
+struct Piece {
+    int b, vh, from, n, lo, hi, tile0, tiles;
+    int bad;                        // status of its length
+};
 template <int TT>
-__device__ __forceinline__ Span span_of(const AttendArgs &a, int len) {
-    Span s;
+__device__ __forceinline__ void set_span(const AttendArgs &a, int len, Piece &p) {
     const long long most = (long long)a.pg.width << a.pg.shift;
-    s.hi = len < 0 ? 0 : len > most ? (int)most : len;
-    s.lo = a.window > 0 && s.hi > a.window ? s.hi - a.window : 0;
-    s.tile0 = s.lo / TT;
-    s.tiles = max(1, (s.hi + TT - 1) / TT - s.tile0);
-    return s;
+    p.hi = len < 0 ? 0 : len > most ? (int)most : len;
+    p.bad = len < 0 ? STEPQ_ERR_ARG : len > most ? STEPQ_ERR_SLOT_RANGE : 0;
+    p.lo = a.window > 0 && p.hi > a.window ? p.hi - a.window : 0;
+    p.tile0 = p.lo / TT;
+    p.tiles = max(1, (p.hi + TT - 1) / TT - p.tile0);
+}
+template <int TT>
+__device__ __forceinline__ int tiles_of(const AttendArgs &a, int len) {
+    Piece p;
+    set_span<TT>(a, len, p);
+    return p.tiles;
+}
+
+// 2^e for e in [-126, 127].
+__device__ __forceinline__ float power2(int e) { return __int_as_float((e + 127) << 23); }
+
+// Query channels of a warp's heads w, w + kAttWarps, ..: 32 e + lane of each.
+template <class S>
+struct Queries {
+    static constexpr int H = S::HT / kAttWarps, N = S::D / 32;
+    float x[H][N];
+    __device__ __forceinline__ void load(const AttendArgs &a, int b, int h0, int nh, int w, int l) {
+#pragma unroll
+        for (int i = 0; i < H; i++)
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const int h = w + i * kAttWarps;
+                x[i][e] = h < nh ? load_any(a.q, b * a.qs + (int64_t)(h0 + h) * S::D + 32 * e + l, a.dtype) : 0.f;
+            }
+    }
+    // To shared memory as pairs in the order of K's pieces: of step ks of the product, pair (0, 1)
+    // of lane 4 head + c; with each head's factor of the scores and the offset of the codes.
+    __device__ __forceinline__ void put(const AttendArgs &a, uint8_t *smem, int w, int l) {
+        using C = typename S::C;
+        constexpr int F = S::F;
+        C *qf = (C *)(smem + S::OFF_Q);
+        float *head_k = (float *)(smem + S::OFF_HEAD), *head_off = head_k + S::HT;
+#pragma unroll
+        for (int i = 0; i < H; i++) {
+            const int h = w + i * kAttWarps;
+            float k = a.scale, off = 0.f;
+            if (std::is_same<C, la::f16>::value) {
+                // scaled by a power of two to below 2^15, where fp16 keeps 2^-39 of the largest
+                float top = 0.f;
+#pragma unroll
+                for (int e = 0; e < N; e++) top = fmaxf(top, fabsf(x[i][e]));
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const int ex = max(-126, min(126, 141 - (__float_as_int(top) >> 23)));
+#pragma unroll
+                for (int e = 0; e < N; e++) x[i][e] *= power2(ex);
+                k *= power2(-ex);
+            }
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                // channel -> piece of KP bytes, pair j in it, half; pieces 4 i + c go to lane c
+                constexpr int PC = S::KP * 8 / bits_of(F), JP = PC / 2;          // channels, pairs of a piece
+                const int ch = 32 * e + l, piece = ch / PC, in = ch % PC;
+                const int j = F == STEPQ_KV_INT4 ? 4 * (in / 8) + in % 4 : in / 2;
+                const int half = F == STEPQ_KV_INT4 ? in / 4 % 2 : in % 2;
+                const int pair = (piece / 4) * JP + j, lane = 4 * (h % 8) + piece % 4;
+                const float f = F == STEPQ_KV_INT4 && (j & 1) ? 0.0625f : 1.f;    // of a code at 2^-20
+                float rest = x[i][e] * f, used = 0.f;
+#pragma unroll
+                for (int t = 0; t < S::QT; t++) {
+                    const C v = la::from_f32<C>(rest);
+                    rest -= la::to_f32(v);
+                    used += la::to_f32(v);
+                    qf[((((t * S::NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2) * 2 + half] = v;
+                }
+                off += F == STEPQ_KV_INT4 && (j & 1) ? 16.f * used : used;
+            }
+            if (S::CODED) {
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) off += __shfl_xor_sync(0xffffffffu, off, o);
+                off *= F == STEPQ_KV_INT8 ? 128.f / 16777216.f : 8.f / 16777216.f;
+                k *= 16777216.f;
+            }
+            if (l == 0) {
+                head_k[h] = k;
+                head_off[h] = off;
+            }
+        }
+    }
+};
+
+// Channels d .. d + 3 of query head h from the sums o of weighted values and `total` of weights.
+__device__ __forceinline__ void put_output(const AttendArgs &a, int b, int h, int d, float top, float total, float (&o)[4], int D) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] / total : 0.f;
+    store4_any(a.y, b * a.ys + (int64_t)h * D + d, a.dtype, o);
+    if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = total != 0.f ? (top + log2f(total)) * 0.693147181f : -INFINITY;
 }
 
 // ------------------------------------------------------------------ the kernel
@@ -233,19 +330,22 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
     constexpr int D = S::D, TT = S::TT, RB = S::RB, NT = S::NT, HT = S::HT, F = S::F;
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, r = l >> 2, c = l & 3;
     const int chunks = (a.groups + HT - 1) / HT, VH = a.pg.n_heads * chunks;
-    float *head_k = (float *)(smem + S::OFF_HEAD), *head_off = head_k + HT;
+    const long long items = (long long)a.B * VH;
+    const float *head_k = (const float *)(smem + S::OFF_HEAD), *head_off = head_k + HT;
+    float *sums = (float *)(smem + S::OFF_SUM);
     long long *scan = (long long *)(smem + S::OFF_SCAN);
+    Joined *joined = (Joined *)(a.parts + (size_t)2 * gridDim.x * part_floats<HT, D>());
     griddep_wait();
     griddep_launch();
 
-    // The share: tiles [t, end) of all, in the order (sequence, virtual head, tile); b and the
-    // tiles of the sequences before it.
-    long long t = 0, end = 0, share = 0, before = 0;
-    int b = 0;
+    // The share: `left` tiles of all, in the order (sequence, virtual head, tile), from tile `from`
+    // of virtual head vh of sequence b on; len is lens[b].
+    long long left = 0, share = 0, item = blockIdx.x;        // item: of calls for whole sequences
+    int b = 0, vh = 0, from = 0, len = 0;
     if (!a.whole) {
         const int per = (a.B + 32 * kAttWarps - 1) / (32 * kAttWarps), i0 = min(a.B, tid * per), i1 = min(a.B, i0 + per);
         long long mine = 0;
-        for (int i = i0; i < i1; i++) mine += span_of<TT>(a, a.lens[i]).tiles;
+        for (int i = i0; i < i1; i++) mine += tiles_of<TT>(a, a.lens[i]);
         long long upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -262,115 +362,217 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
         }
         total *= VH;
         share = max((total + gridDim.x - 1) / gridDim.x, (long long)(2 * kAttWarps));
-        t = share * blockIdx.x;
-        end = min(total, t + share);
+        const long long t = share * blockIdx.x;
+        left = min(total - t, share);
         if (t < total && t >= (upto - mine) * VH && t < upto * VH) {
             long long p = upto - mine;
-            int i = i0;
+            int i = i0, n;
             for (;; i++) {
-                const int n = span_of<TT>(a, a.lens[i]).tiles;
+                n = tiles_of<TT>(a, a.lens[i]);
                 if (t < (p + n) * VH) break;
                 p += n;
             }
-            scan[kAttWarps] = p;
-            scan[kAttWarps + 1] = i;
+            const long long in = t - p * VH;
+            scan[kAttWarps] = i;
+            scan[kAttWarps + 1] = in / n;
+            scan[kAttWarps + 2] = in % n;
         }
         __syncthreads();
-        before = scan[kAttWarps];
-        b = (int)scan[kAttWarps + 1];
-        if (tid == 0)                                        // no piece goes on in other CTAs, unless one does below
-            ((Joined *)(a.parts + (size_t)2 * gridDim.x * part_floats<HT, D>()))[blockIdx.x] = Joined{0, 0, 0, 0};
-        if (t >= total) return;
-    } else {
-        t = blockIdx.x;
-        end = (long long)a.B * VH;
+        if (tid == 0 && items > gridDim.x) joined[blockIdx.x].count = 0;     // unless a piece goes on elsewhere
+        if (left <= 0) return;
+        b = (int)scan[kAttWarps];
+        vh = (int)scan[kAttWarps + 1];
+        from = (int)scan[kAttWarps + 2];
+        len = a.lens[b];
     }
 
-    const uint32_t ring = smem_addr(smem) + w * S::STAGES * S::TILE;
-    while (t < end) {
-        // The piece: virtual head vh of sequence b, its tiles from `from`, n of them.
-        int vh, from, n;
+    // The next piece of the share, n = 0 behind the last.
+    auto next_piece = [&]() {
+        Piece p{};
         if (a.whole) {
-            b = (int)(t / VH);
-            vh = (int)(t - (long long)b * VH);
-        }
-        const int len = a.lens[b];
-        const Span sp = span_of<TT>(a, len);
-        if (a.whole) {
-            from = 0;
-            n = sp.tiles;
+            if (item >= items) return p;
+            p.b = (int)(item / VH);
+            p.vh = (int)(item - (long long)p.b * VH);
+            item += gridDim.x;
+            len = a.lens[p.b];
+            set_span<TT>(a, len, p);
+            p.n = p.tiles;
         } else {
-            const long long in = t - before * VH;
-            vh = (int)(in / sp.tiles);
-            from = (int)(in - (long long)vh * sp.tiles);
-            n = (int)min((long long)(sp.tiles - from), end - t);
+            if (left <= 0) return p;
+            p.b = b;
+            p.vh = vh;
+            p.from = from;
+            set_span<TT>(a, len, p);
+            p.n = (int)min((long long)(p.tiles - from), left);
+            left -= p.n;
+            from += p.n;
+            if (from == p.tiles) {
+                from = 0;
+                if (++vh == VH) {
+                    vh = 0;
+                    if (++b < a.B) len = a.lens[b];
+                }
+            }
         }
-        if (tid == 0 && from == 0 && vh == 0) {
-            if (len < 0) raise_error(a.pg.err, STEPQ_ERR_ARG);
-            if (len > sp.hi && len > 0) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
-        }
-        const int hk = vh / chunks, g0 = (vh - hk * chunks) * HT, nh = min(HT, a.groups - g0);
-        const int h0 = hk * a.groups + g0;                   // first query head
+        return p;
+    };
+    // This warp's tiles of a piece: from + w, from + w + kAttWarps, ... below from + n.
+    auto count_of = [&](const Piece &p) { return p.n > w ? (p.n - w + kAttWarps - 1) / kAttWarps : 0; };
 
-        __syncthreads();                                     // the last piece's shared memory is free
-        // Queries, as pairs in the order of K's pieces: step ks of the product, pair (0, 1) of
-        // lane 4 head + c.
-        uint32_t *qf = (uint32_t *)(smem + S::OFF_Q);
-        for (int h = w; h < HT; h += kAttWarps) {
-            constexpr int N = D / 32;
-            float x[N], top = 0.f;
+    // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the page of
+    // octet l (eight tokens) of that tile, -1 for none.
+    struct {
+        const int32_t *table;
+        uint64_t head;
+        int tok, more, lo, hi, ids;
+    } f;
+    auto load_ids = [&]() {
+        f.ids = -1;
+        const int tok = f.tok + 8 * l;
+        if (l >= TT / 8 || f.more == 0 || tok >= f.hi || tok + 8 <= f.lo) return;
+        const int id = f.table[tok >> a.pg.shift];
+        if (id >= 0 && id < a.pg.n_pages) f.ids = id;
+        else raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+    };
+    auto fetch_from = [&](const Piece &p) {
+        f.table = a.pg.table + p.b * a.pg.table_stride;
+        f.head = (uint64_t)(p.vh / chunks) * a.pg.segment;
+        f.tok = (p.tile0 + p.from + w) * TT;
+        f.more = count_of(p);
+        f.lo = p.lo;
+        f.hi = p.hi;
+        load_ids();
+    };
+    // Stages are taken in turn: to_fill the next that copies go to, to_read the next that is read.
+    int to_fill = 0, to_read = 0, ahead = 0;                 // ahead: tiles copied and not yet read
+    // A step copies 512 bytes of rows, 16 a lane: the change of place within 128 bytes is that of the
+    // lane's part of the offset and, apart from it, that of the step's.
+    const uint32_t k_lane = k_place<RB>(16 * l / RB, 16 * l % RB), v_lane = v_place<RB>(16 * l / RB, 16 * l % RB);
+    auto copy_tile = [&]() {
+        const uint32_t dst = smem_addr(smem) + (w * S::STAGES + to_fill) * S::TILE;
+        constexpr int N = TT * RB / 512, PER = RB >= 64 ? RB / 64 : 1;       // steps, and steps of an octet
+        // this lane's octet in memory
+        const bool mine = f.ids >= 0;
+        const uint8_t *oct = a.pg.base + f.head + (mine ? (uint64_t)f.ids * a.pg.page_bytes + a.pg.slot(f.tok + 8 * l) * RB : 0);
+        const uint32_t to_v = RB << a.pg.shift;
+        if (f.tok >= f.lo && f.tok + TT <= f.hi && __all_sync(0xffffffffu, mine || l >= TT / 8)) {
 #pragma unroll
-            for (int e = 0; e < N; e++) {
-                x[e] = h < nh ? load_any(a.q, b * a.qs + (int64_t)(h0 + h) * D + 32 * e + l, a.dtype) : 0.f;
-                top = fmaxf(top, fabsf(x[e]));
-            }
-            float k = a.scale, off = 0.f;
-            if (std::is_same<C, la::f16>::value) {
-                // scaled by a power of two to at most 2^15, where fp16 keeps 2^-40 of the largest
+            for (int j0 = 0; j0 < N; j0 += PER) {
+                const uint8_t *k = (const uint8_t *)__shfl_sync(0xffffffffu, (unsigned long long)oct, (512 * j0 + 16 * l) / (8 * RB)) +
+                                   16 * l % (8 * RB);
+                const uint8_t *v = k + to_v;
 #pragma unroll
-                for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-#pragma unroll
-                for (int e = 0; e < N; e++) x[e] = ldexpf(x[e], ex);
-                k = ldexpf(k, -ex);
-            }
-#pragma unroll
-            for (int e = 0; e < N; e++) {
-                // channel -> piece of KP bytes, pair j in it, half; pieces 4 i + c go to lane c
-                constexpr int PC = S::KP * 8 / bits_of(F), JP = PC / 2;          // channels, pairs of a piece
-                const int ch = 32 * e + l, piece = ch / PC, in = ch % PC;
-                int j, half;
-                if (F == STEPQ_KV_INT4) {
-                    j = 4 * (in / 8) + in % 4;
-                    half = in / 4 % 2;
-                } else {
-                    j = in / 2;
-                    half = in % 2;
+                for (int x = 0; x < PER; x++) {
+                    const int j = j0 + x;
+                    const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
+                    copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * x);
+                    copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * x);
                 }
-                const int pair = (piece / 4) * JP + j, lane = 4 * (h % 8) + piece % 4;
-                float rest = x[e] * q_factor<F>(j);
-#pragma unroll
-                for (int i = 0; i < S::QT; i++) {
-                    const C v = la::from_f32<C>(rest);
-                    rest -= la::to_f32(v);
-                    off += la::to_f32(v) / q_factor<F>(j);
-                    ((C *)qf)[((((i * NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2) * 2 + half] = v;
-                }
             }
-            if (S::CODED) {
-#pragma unroll
-                for (int o = 1; o < 32; o *= 2) off += __shfl_xor_sync(0xffffffffu, off, o);
-                off *= F == STEPQ_KV_INT8 ? 128.f / 16777216.f : 8.f / 16777216.f;
-                k *= 16777216.f;
-            }
-            if (l == 0) {
-                head_k[h] = k;
-                head_off[h] = off;
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < N; j++) {
+                const int at = 512 * j + 16 * l, row = at / RB, byte = at % RB, tok = f.tok + row;
+                const uint8_t *src = (const uint8_t *)__shfl_sync(0xffffffffu, (unsigned long long)oct, row / 8) + at % (8 * RB);
+                const bool ok = __shfl_sync(0xffffffffu, f.ids, row / 8) >= 0 && tok >= f.lo && tok < f.hi;
+                copy16(dst + k_place<RB>(row, byte), ok ? src : a.pg.base, ok);
+                copy16(dst + TT * RB + v_place<RB>(row, byte), ok ? src + to_v : a.pg.base, ok);
             }
         }
-        __syncthreads();
+        if (S::CODED && l < TT / 8) {
+            const uint8_t *src = oct + 2 * to_v - a.pg.slot(f.tok + 8 * l) * (RB - 2);
+            copy16(dst + 2 * TT * RB + 16 * l, mine ? src : a.pg.base, mine);
+            copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, mine ? src + (2 << a.pg.shift) : a.pg.base, mine);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++to_fill == S::STAGES) to_fill = 0;
+        ahead++;
+        f.more--;
+        f.tok += kAttWarps * TT;
+    };
+
+    // What this lane reads of a tile: piece c of row r of K, piece r of rows 2 c and 2 c + 1 of V;
+    // 8 rows, and 8 pieces of V, further on lie the same.
+    const uint32_t k_at = k_place<RB>(r, c * S::KP), v_at = v_place<RB>(2 * c, r * S::VP), v_at1 = v_place<RB>(2 * c + 1, r * S::VP);
+
+    Piece p = next_piece();
+    auto first_head = [&](const Piece &x) { return x.vh / chunks * a.groups + x.vh % chunks * HT; };
+    auto heads_of = [&](const Piece &x) { return min(HT, a.groups - x.vh % chunks * HT); };
+    fetch_from(p);
+    // A warp's part of a piece goes through the stage of its ring that was read last.
+    auto stage_of = [&](int x, int stage) { return smem + (x * S::STAGES + stage) * S::TILE; };
+    struct {
+        int b, h0, nh;
+        bool all;                                            // the piece is its whole sequence
+        float *part;                                         // else where it goes
+    } out{};
+    bool first = true;
+    long long past = 0;                                      // tiles of the share's pieces before this one
+
+    for (;; first = false) {
+        const Piece q = p.n > 0 ? next_piece() : p;
+        bool rest = p.n > 0 && q.n > 0;                      // q's tiles are not looked at yet
+        // Copies up to `most` tiles ahead, on into q's.
+        auto fill = [&](int most) {
+            for (;;) {
+                if (f.more == 0) {
+                    if (!rest) return;
+                    fetch_from(q);
+                    rest = false;
+                    if (f.more == 0) return;
+                }
+                if (ahead >= most) return;
+                copy_tile();
+                if (f.more > 0) load_ids();
+            }
+        };
+        Queries<S> qs;
+        qs.load(a, p.b, first_head(p), p.n > 0 ? heads_of(p) : 0, w, l);
+        if (!first) {
+            __syncthreads();                                 // the warps' parts of the piece before
+            for (int i = tid; i < out.nh * (D / 4); i += 32 * kAttWarps) {
+                const int h = i / (D / 4), d = 4 * (i % (D / 4));
+                float top = kLow, total = 0.f, o[4] = {};
+#pragma unroll
+                for (int x = 0; x < kAttWarps; x++) top = fmaxf(top, sums[2 * x * HT + h]);
+#pragma unroll
+                for (int x = 0; x < kAttWarps; x++) {
+                    const float k = exp2_fast(sums[2 * x * HT + h] - top);
+                    const float4 v = *(const float4 *)((const float *)stage_of(x, ((const int *)scan)[x]) + h * D + d);
+                    total = fmaf(k, sums[(2 * x + 1) * HT + h], total);
+                    o[0] = fmaf(k, v.x, o[0]);
+                    o[1] = fmaf(k, v.y, o[1]);
+                    o[2] = fmaf(k, v.z, o[2]);
+                    o[3] = fmaf(k, v.w, o[3]);
+                }
+                if (out.all) {
+                    put_output(a, out.b, out.h0 + h, d, top, total, o, D);
+                } else {
+                    *(float4 *)(out.part + h * D + d) = make_float4(o[0], o[1], o[2], o[3]);
+                    if (d == 0) {
+                        out.part[HT * D + h] = top;
+                        out.part[HT * D + HT + h] = total;
+                    }
+                }
+            }
+        }
+        if (p.n == 0) break;
+        qs.put(a, smem, w, l);
+        __syncthreads();                                     // the queries are there, the parts before have been read
+        if (tid == 0 && p.bad) raise_error(a.pg.err, p.bad);
+        const int slot = 2 * (int)blockIdx.x + (first ? 0 : 1);
+        out = {p.b, first_head(p), heads_of(p), p.n == p.tiles, a.parts + (size_t)slot * part_floats<HT, D>()};
+        if (!a.whole && tid == 0 && p.from == 0) {
+            // begun here, and ended here or by one of the next CTAs
+            const Joined j{out.all ? 0 : (int)((past + p.tiles - 1) / share) + 1, slot, p.b, p.vh};
+            if (items <= gridDim.x) joined[(long long)p.b * VH + p.vh] = j;
+            else if (j.count) joined[blockIdx.x] = j;
+        }
+        past += p.n;
+        const int count = count_of(p), tok_first = (p.tile0 + p.from + w) * TT;
 
         float hf[NT][2], ho[NT][2], R[NT][2], sum[NT][2], O[NT][S::MT][4];
+        const uint2 *qf = (const uint2 *)(smem + S::OFF_Q);
         uint2 qr[S::QREG ? S::QT : 1][S::QREG ? NT : 1][S::QREG ? S::KS : 1];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -392,212 +594,188 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                    for (int ks = 0; ks < S::KS; ks++)
-                        qr[i][nt][ks] = ((const uint2 *)qf)[((i * NT + nt) * S::KS + ks) * 32 + l];
+                    for (int ks = 0; ks < S::KS; ks++) qr[i][nt][ks] = qf[((i * NT + nt) * S::KS + ks) * 32 + l];
         }
 
-        // This warp's tiles: from + w, from + w + kAttWarps, ... below from + n.
-        const int count = n > w ? (n - w + kAttWarps - 1) / kAttWarps : 0;
-        const int token0 = (sp.tile0 + from + w) * TT;       // of the warp's first tile
-        const int32_t *table = a.pg.table + b * a.pg.table_stride;
-        // page of octet l (eight tokens) of the warp's tile i, -1 for none
-        auto page_ids = [&](int i) {
-            if (l >= TT / 8 || i >= count) return -1;
-            const int tok = token0 + i * kAttWarps * TT + 8 * l;
-            if (tok >= sp.hi || tok + 8 <= sp.lo) return -1;
-            const int id = table[tok >> a.pg.shift];
-            if (id >= 0 && id < a.pg.n_pages) return id;
-            raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
-            return -1;
-        };
-        auto copy_tile = [&](int i, int ids) {
-            const uint32_t dst = ring + (i % S::STAGES) * S::TILE;
-            const int tok0 = token0 + i * kAttWarps * TT;
-            constexpr int PER = RB / 16, N = TT * PER / 32;
-#pragma unroll
-            for (int j = 0; j < N; j++) {
-                const int ch = 32 * j + l, row = ch / PER, byte = ch % PER * 16, tok = tok0 + row;
-                const int id = __shfl_sync(0xffffffffu, ids, row / 8);
-                const bool ok = id >= 0 && tok >= sp.lo && tok < sp.hi;
-                const uint8_t *src = a.pg.at(ok ? id : 0, hk) + (ok ? a.pg.slot(tok) * RB + byte : 0);
-                copy16(dst + k_place<RB>(row, byte), src, ok);
-                copy16(dst + TT * RB + v_place<RB>(row, byte), src + (ok ? RB << a.pg.shift : 0), ok);
-            }
-            if (S::CODED && l < TT / 8) {
-                const bool ok = ids >= 0;
-                const uint8_t *src = a.pg.at(ok ? ids : 0, hk) + (ok ? (2 * RB << a.pg.shift) + 2 * a.pg.slot(tok0 + 8 * l) : 0);
-                copy16(dst + 2 * TT * RB + 16 * l, src, ok);
-                copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, src + (ok ? 2 << a.pg.shift : 0), ok);
-            }
-        };
+        for (int i = 0;; i++) {
+            __syncwarp();                                    // all have read the tile before
+            fill(i < count ? S::STAGES : S::STAGES - 1);
+            if (i == count) break;
+            // the copies of this tile have landed once no more than those behind it are open
+            if (ahead == S::STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            const uint8_t *st = stage_of(w, to_read);
+            if (++to_read == S::STAGES) to_read = 0;
+            ahead--;
+            constexpr int G = S::ST / 16;
+#pragma unroll 1
+            for (int sub = 0; sub < TT; sub += S::ST) {
+                const int tok0 = tok_first + i * kAttWarps * TT + sub;
+                const bool edge = tok0 < p.lo || tok0 + S::ST > p.hi;
+                const uint8_t *rows = st + sub * RB;
 
-        int ids = page_ids(0);
+                // scores, tokens 16 g + r and + 8 by heads 2 c and 2 c + 1
+                float s[NT][G][4];
 #pragma unroll
-        for (int i = 0; i < S::STAGES - 1; i++) {
-            if (i < count) copy_tile(i, ids);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            ids = page_ids(i + 1);
-        }
-        for (int i = 0; i < count; i++) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
-            __syncwarp();                                    // all lanes' copies of tile i; all have read tile i - 1
-            if (i + S::STAGES - 1 < count) copy_tile(i + S::STAGES - 1, ids);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            ids = page_ids(i + S::STAGES);
-            const uint8_t *st = smem + (w * S::STAGES + i % S::STAGES) * S::TILE;
-            const int tok0 = token0 + i * kAttWarps * TT;
-            const bool edge = tok0 < sp.lo || tok0 + TT > sp.hi;
-
-            // scores, tokens 16 g + r and + 8 by heads 2 c and 2 c + 1
-            constexpr int G = TT / 16;
-            float s[NT][G][4];
+                for (int g = 0; g < G; g++) {
 #pragma unroll
-            for (int g = 0; g < G; g++) {
+                    for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
+                        for (int e = 0; e < 4; e++) s[nt][g][e] = 0.f;
+                    constexpr int NP = RB / (4 * S::KP), JP = S::KP * 4 / bits_of(F);    // pieces, pairs of each
 #pragma unroll
-                    for (int e = 0; e < 4; e++) s[nt][g][e] = 0.f;
-                constexpr int NP = RB / (4 * S::KP), JP = S::KP * 4 / bits_of(F);    // pieces, pairs of each
+                    for (int x = 0; x < NP; x++) {
+                        // pieces 4 x + c: an odd x differs from an even one in the bit that rows change
+                        const uint8_t *at = rows + ((x & 1) * 4 * S::KP ^ k_at) + (x >> 1) * 8 * S::KP + 16 * g * RB;
+                        uint32_t k0[JP], k8[JP];
+                        k_pairs<F>(lds<S::KP>(at, 0), k0);
+                        k_pairs<F>(lds<S::KP>(at, 8 * RB), k8);
 #pragma unroll
-                for (int p = 0; p < NP; p++) {
-                    const int byte = (4 * p + c) * S::KP;
-                    uint32_t x[JP], y[JP];
-                    k_pairs<F>(lds<S::KP>(st, k_place<RB>(16 * g + r, byte)), x);
-                    k_pairs<F>(lds<S::KP>(st, k_place<RB>(16 * g + r + 8, byte)), y);
+                        for (int j = 0; j < JP / 2; j++) {
+                            const int ks = x * (JP / 2) + j;
 #pragma unroll
-                    for (int j = 0; j < JP / 2; j++) {
-                        const int ks = p * (JP / 2) + j;
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int t = 0; t < S::QT; t++) {
+                                    uint2 v;
+                                    if constexpr (S::QREG) v = qr[t][nt][ks];
+                                    else v = qf[((t * NT + nt) * S::KS + ks) * 32 + l];
+                                    mma<C>(s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
+                                }
+                        }
+                    }
+                }
+                // base-2 exponents (x - ho) hk; masked ones are -inf
+                float sv[G][2], hk[NT][G][4];
+#pragma unroll
+                for (int g = 0; g < G; g++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        float sk = 1.f;
+                        sv[g][h] = 1.f;
+                        if (S::CODED) {
+                            const uint16_t *sc = (const uint16_t *)(st + 2 * TT * RB) + sub + 16 * g + r + 8 * h;
+                            sk = f16_val(sc[0]);
+                            sv[g][h] = fmaxf(f16_val(sc[TT]), kF16Min);      // 0 or NaN: of no token
+                        }
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                            for (int q = 0; q < S::QT; q++) {
-                                uint2 v;
-                                if constexpr (S::QREG) v = qr[q][nt][ks];
-                                else v = ((const uint2 *)qf)[((q * NT + nt) * S::KS + ks) * 32 + l];
-                                mma<C>(s[nt][g], x[2 * j], y[2 * j], x[2 * j + 1], y[2 * j + 1], v.x, v.y);
+                            for (int e = 0; e < 2; e++) {
+                                hk[nt][g][2 * h + e] = S::CODED ? hf[nt][e] * sk : hf[nt][e];
+                                if (S::CODED) s[nt][g][2 * h + e] -= ho[nt][e];
                             }
                     }
+                if (edge) {
+#pragma unroll
+                    for (int g = 0; g < G; g++)
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            const int tok = tok0 + 16 * g + r + 8 * h;
+                            if (tok >= p.lo && tok < p.hi) continue;
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int e = 0; e < 2; e++) {
+                                    s[nt][g][2 * h + e] = -INFINITY;
+                                    hk[nt][g][2 * h + e] = 1.f;
+                                }
+                        }
                 }
-            }
-            // base-2 exponents; masked ones are -inf
-            float sv[G][2];
+                // Weights 2^(s - R) sv of at most 2^15. R rises, to 7 below the largest exponent
+                // (of the weight), only when one would be above: seldom after the first tiles.
+                float wt[NT][G][4], wv[NT][G][4], most = 0.f;
 #pragma unroll
-            for (int g = 0; g < G; g++)
+                for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const int row = 16 * g + r + 8 * h;
-                    float sk = 1.f;
-                    sv[g][h] = 1.f;
-                    if (S::CODED) {
-                        const uint16_t *sc = (const uint16_t *)(st + 2 * TT * RB);
-                        sk = f16_val(sc[row]);
-                        sv[g][h] = fmaxf(f16_val(sc[TT + row]), kF16Min);    // 0 or NaN: of no token
-                    }
-                    const bool out = edge && (tok0 + row < sp.lo || tok0 + row >= sp.hi);
+                    for (int g = 0; g < G; g++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            wt[nt][g][e] = exp2_fast(fmaf(s[nt][g][e], hk[nt][g][e], -R[nt][e & 1]));
+                            wv[nt][g][e] = wt[nt][g][e] * sv[g][e >> 1];
+                            most = fmaxf(most, wv[nt][g][e]);
+                        }
+                if (__any_sync(0xffffffffu, most > 32768.f)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                         for (int e = 0; e < 2; e++) {
-                            float &x = s[nt][g][2 * h + e];
-                            x = S::CODED ? (x - ho[nt][e]) * (hf[nt][e] * sk) : x * hf[nt][e];
-                            if (out) x = -INFINITY;
+                            float top = kLow;
+#pragma unroll
+                            for (int g = 0; g < G; g++)
+#pragma unroll
+                                for (int h = 0; h < 2; h++)
+                                    top = fmaxf(top, fmaf(s[nt][g][2 * h + e], hk[nt][g][2 * h + e], S::CODED ? log2f(sv[g][h]) : 0.f));
+#pragma unroll
+                            for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                            const float up = fmaxf(R[nt][e], top - 7.f), x = exp2_fast(R[nt][e] - up);
+                            R[nt][e] = up;
+                            sum[nt][e] *= x;
+#pragma unroll
+                            for (int m = 0; m < S::MT; m++) {
+                                O[nt][m][e] *= x;
+                                O[nt][m][2 + e] *= x;
+                            }
+#pragma unroll
+                            for (int g = 0; g < G; g++)
+#pragma unroll
+                                for (int h = 0; h < 2; h++) {
+                                    wt[nt][g][2 * h + e] = exp2_fast(fmaf(s[nt][g][2 * h + e], hk[nt][g][2 * h + e], -up));
+                                    wv[nt][g][2 * h + e] = wt[nt][g][2 * h + e] * sv[g][h];
+                                }
                         }
                 }
-            // Weights 2^(s - R) sv of at most 2^15. R rises, to 7 below the largest exponent
-            // (of the weight), only when one would be above: seldom after the first tiles.
-            float wt[NT][G][4], most = 0.f;
+                // weighted v: heads' weights by tokens become the right factor by a transposition
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++)
+                for (int g = 0; g < G; g++) {
+                    uint32_t pw[NT][S::PT][2];
 #pragma unroll
-                for (int g = 0; g < G; g++)
+                    for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        wt[nt][g][e] = exp2_fast(s[nt][g][e] - R[nt][e & 1]);
-                        most = fmaxf(most, wt[nt][g][e] * sv[g][e >> 1]);
-                    }
-            if (__any_sync(0xffffffffu, most > 32768.f)) {
+                        for (int h = 0; h < 2; h++) {
+                            float x = wv[nt][g][2 * h], y = wv[nt][g][2 * h + 1];
+                            sum[nt][0] += wt[nt][g][2 * h];
+                            sum[nt][1] += wt[nt][g][2 * h + 1];
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        float top = kLow;
-#pragma unroll
-                        for (int g = 0; g < G; g++)
-#pragma unroll
-                            for (int h = 0; h < 2; h++)
-                                top = fmaxf(top, s[nt][g][2 * h + e] + (S::CODED ? log2f(sv[g][h]) : 0.f));
-#pragma unroll
-                        for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const float up = fmaxf(R[nt][e], top - 7.f), f = exp2_fast(R[nt][e] - up);
-                        R[nt][e] = up;
-                        sum[nt][e] *= f;
-#pragma unroll
-                        for (int m = 0; m < S::MT; m++) {
-                            O[nt][m][e] *= f;
-                            O[nt][m][2 + e] *= f;
-                        }
-#pragma unroll
-                        for (int g = 0; g < G; g++)
-#pragma unroll
-                            for (int h = 0; h < 2; h++) wt[nt][g][2 * h + e] = exp2_fast(s[nt][g][2 * h + e] - up);
-                    }
-            }
-            // weighted v: heads' weights by tokens become the right factor by a transposition
-#pragma unroll
-            for (int g = 0; g < G; g++) {
-                uint32_t p[NT][S::PT][2];
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                    for (int h = 0; h < 2; h++) {
-                        float x = wt[nt][g][2 * h], y = wt[nt][g][2 * h + 1];
-                        sum[nt][0] += x;
-                        sum[nt][1] += y;
-                        x *= sv[g][h];
-                        y *= sv[g][h];
-#pragma unroll
-                        for (int i = 0; i < S::PT; i++) {
-                            const uint32_t v = pack(x, y, C{});
-                            if (i + 1 < S::PT) {
-                                const float2 f = unpack(v, C{});
-                                x -= f.x;
-                                y -= f.y;
+                            for (int t = 0; t < S::PT; t++) {
+                                const uint32_t v = pack(x, y, C{});
+                                if (t + 1 < S::PT) {
+                                    const float2 u = unpack(v, C{});
+                                    x -= u.x;
+                                    y -= u.y;
+                                }
+                                pw[nt][t][h] = transpose8(v);
                             }
-                            p[nt][i][h] = transpose8(v);
                         }
+                    constexpr int NP = RB / (8 * S::VP), CH = S::VP * 8 / bits_of(F);    // pieces, channels of each
+#pragma unroll
+                    for (int z = 0; z < NP; z++) {
+                        const uint8_t *at = rows + TT * RB + 8 * z * S::VP + 16 * g * RB;
+                        uint32_t x[CH], y[CH];
+                        v_pairs<F>(lds<S::VP>(at, v_at), lds<S::VP>(at, v_at1), x);
+                        v_pairs<F>(lds<S::VP>(at, v_at + 8 * RB), lds<S::VP>(at, v_at1 + 8 * RB), y);
+#pragma unroll
+                        for (int m = 0; m < CH / 2; m++)
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int t = 0; t < S::PT; t++)
+                                    mma<C>(O[nt][z * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1], pw[nt][t][0], pw[nt][t][1]);
                     }
-                constexpr int NP = RB / (8 * S::VP), CH = S::VP * 8 / bits_of(F);    // pieces, channels of each
-#pragma unroll
-                for (int q = 0; q < NP; q++) {
-                    const int byte = (8 * q + r) * S::VP, row = 16 * g + 2 * c;
-                    const uint8_t *at = st + TT * RB;
-                    uint32_t x[CH], y[CH];
-                    v_pairs<F>(lds<S::VP>(at, v_place<RB>(row, byte)), lds<S::VP>(at, v_place<RB>(row + 1, byte)), x);
-                    v_pairs<F>(lds<S::VP>(at, v_place<RB>(row + 8, byte)), lds<S::VP>(at, v_place<RB>(row + 9, byte)), y);
-#pragma unroll
-                    for (int m = 0; m < CH / 2; m++)
-#pragma unroll
-                        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                            for (int i = 0; i < S::PT; i++)
-                                mma<C>(O[nt][q * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1], p[nt][i][0], p[nt][i][1]);
                 }
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        // The four warps' parts, through the rings' memory.
-#pragma unroll
-        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-            for (int e = 0; e < 2; e++)
-#pragma unroll
-                for (int o = 4; o < 32; o *= 2) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], o);
-        __syncthreads();
-        float *mine = (float *)smem + w * HT * (D + 2);
+
+        __syncwarp();
+        const int stage = to_read == 0 ? S::STAGES - 1 : to_read - 1;
+        float *mine = (float *)stage_of(w, stage);
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int e = 0; e < 2; e++) {
+#pragma unroll
+                for (int o = 4; o < 32; o *= 2) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], o);
                 const int h = 8 * nt + 2 * c + e;
                 constexpr int MP = S::VP * 4 / bits_of(F);    // row tiles of a piece
 #pragma unroll
@@ -605,97 +783,65 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
                     *(float2 *)(mine + h * D + (8 * (m / MP) + r) * (2 * MP) + 2 * (m % MP)) =
                         make_float2(O[nt][m][e] * v_factor<F>(0), O[nt][m][2 + e] * v_factor<F>(1));
                 if (r == 0) {
-                    mine[HT * D + h] = R[nt][e];
-                    mine[HT * D + HT + h] = sum[nt][e];
+                    sums[(w * 2) * HT + h] = R[nt][e];
+                    sums[(w * 2 + 1) * HT + h] = sum[nt][e];
                 }
             }
-        __syncthreads();
-        const bool all = n == sp.tiles;
-        // a part that is not all of its sequence: its first piece in this CTA's share or the last
-        float *part = a.parts + (size_t)(2 * blockIdx.x + (t == share * blockIdx.x ? 0 : 1)) * part_floats<HT, D>();
-        for (int i = tid; i < nh * (D / 4); i += 32 * kAttWarps) {
-            const int h = i / (D / 4), d = 4 * (i % (D / 4));
-            const float *src = (const float *)smem;
-            float top = kLow;
-#pragma unroll
-            for (int x = 0; x < kAttWarps; x++) top = fmaxf(top, src[x * HT * (D + 2) + HT * D + h]);
-            float total = 0.f, o[4] = {};
-#pragma unroll
-            for (int x = 0; x < kAttWarps; x++) {
-                const float *from_w = src + x * HT * (D + 2);
-                const float f = exp2_fast(from_w[HT * D + h] - top);
-                total = fmaf(f, from_w[HT * D + HT + h], total);
-                const float4 v = *(const float4 *)(from_w + h * D + d);
-                o[0] = fmaf(f, v.x, o[0]);
-                o[1] = fmaf(f, v.y, o[1]);
-                o[2] = fmaf(f, v.z, o[2]);
-                o[3] = fmaf(f, v.w, o[3]);
-            }
-            if (all) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] / total : 0.f;
-                store4_any(a.y, b * a.ys + (int64_t)(h0 + h) * D + d, a.dtype, o);
-                if (a.lse && d == 0)
-                    a.lse[(int64_t)b * a.hq + h0 + h] = total != 0.f ? (top + log2f(total)) * 0.693147181f : -INFINITY;
-            } else {
-                *(float4 *)(part + h * D + d) = make_float4(o[0], o[1], o[2], o[3]);
-                if (d == 0) {
-                    part[HT * D + h] = top;
-                    part[HT * D + HT + h] = total;
-                }
-            }
-        }
-        if (!a.whole && tid == 0 && from + n < sp.tiles && from == 0) {
-            // begun here, ended by CTA blockIdx.x + count - 1
-            const long long last = (t + sp.tiles - 1) / share;
-            ((Joined *)(a.parts + (size_t)2 * gridDim.x * part_floats<HT, D>()))[blockIdx.x] =
-                Joined{(int)(last - blockIdx.x) + 1, 2 * (int)blockIdx.x + (t == share * blockIdx.x ? 0 : 1), b, vh};
-        }
-        if (a.whole) {
-            t += gridDim.x;
-        } else {
-            t += n;
-            if (vh == VH - 1 && from + n == sp.tiles) {
-                before += sp.tiles;
-                b++;
-            }
-        }
+        if (l == 0) ((int *)scan)[w] = stage;
+        p = q;
     }
 }
 
-// Joins the parts of the piece that CTA blockIdx.x of the kernel above began and others ended.
+// Joins the parts of piece blockIdx.x, head blockIdx.y: a warp takes every eighth part, a lane
+// D / 32 channels.
+constexpr int kJoinWarps = 8;
 template <int HT, int D>
-__global__ void __launch_bounds__(256) kv_join_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, int ctas) {
+    __shared__ float os[kJoinWarps][D], ls[kJoinWarps], rs[kJoinWarps];
+    const int w = threadIdx.x >> 5, l = threadIdx.x & 31, h = blockIdx.y;
     griddep_wait();
     griddep_launch();
-    const Joined j = ((const Joined *)(a.parts + (size_t)2 * gridDim.x * part_floats<HT, D>()))[blockIdx.x];
+    const Joined j = ((const Joined *)(a.parts + (size_t)2 * ctas * part_floats<HT, D>()))[blockIdx.x];
     if (j.count == 0) return;
-    const int chunks = (a.groups + HT - 1) / HT, hk = j.vh / chunks, g0 = (j.vh - hk * chunks) * HT;
-    const int nh = min(HT, a.groups - g0), h0 = hk * a.groups + g0;
+    const int chunks = (a.groups + HT - 1) / HT, g0 = j.vh % chunks * HT;
+    if (h >= a.groups - g0) return;
     auto part = [&](int i) {
-        return a.parts + (size_t)(i == 0 ? j.first : 2 * (blockIdx.x + i)) * part_floats<HT, D>();
+        return a.parts + (size_t)(i == 0 ? j.first : 2 * ((j.first >> 1) + i)) * part_floats<HT, D>();
     };
-    for (int i = threadIdx.x; i < nh * (D / 4); i += 256) {
-        const int h = i / (D / 4), d = 4 * (i % (D / 4));
-        float top = kLow, total = 0.f, o[4] = {};
-#pragma unroll 8
-        for (int x = 0; x < j.count; x++) top = fmaxf(top, part(x)[HT * D + h]);
+    constexpr int N = D / 32;
+    float top = kLow, total = 0.f, o[N] = {};
 #pragma unroll 4
-        for (int x = 0; x < j.count; x++) {
-            const float *p = part(x);
-            const float f = exp2_fast(p[HT * D + h] - top);
-            total = fmaf(f, p[HT * D + HT + h], total);
-            const float4 v = *(const float4 *)(p + h * D + d);
-            o[0] = fmaf(f, v.x, o[0]);
-            o[1] = fmaf(f, v.y, o[1]);
-            o[2] = fmaf(f, v.z, o[2]);
-            o[3] = fmaf(f, v.w, o[3]);
-        }
+    for (int i = w; i < j.count; i += kJoinWarps) {
+        const float *x = part(i);
+        const float R = x[HT * D + h], sum = x[HT * D + HT + h];
+        la::Vec<float, N < 4 ? N : 4> v[N < 4 ? 1 : N / 4];
 #pragma unroll
-        for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] / total : 0.f;
-        store4_any(a.y, j.b * a.ys + (int64_t)(h0 + h) * D + d, a.dtype, o);
-        if (a.lse && d == 0)
-            a.lse[(int64_t)j.b * a.hq + h0 + h] = total != 0.f ? (top + log2f(total)) * 0.693147181f : -INFINITY;
+        for (int e = 0; e < (N < 4 ? 1 : N / 4); e++) v[e] = ((const la::Vec<float, N < 4 ? N : 4> *)(x + h * D))[32 * e + l];
+        const float up = fmaxf(top, R), k0 = exp2_fast(top - up), k1 = exp2_fast(R - up);
+        top = up;
+        total = fmaf(total, k0, sum * k1);
+#pragma unroll
+        for (int e = 0; e < N; e++) o[e] = fmaf(o[e], k0, v[e / 4].e[e % 4] * k1);
+    }
+    if (l == 0) {
+        rs[w] = top;
+        ls[w] = total;
+    }
+#pragma unroll
+    for (int e = 0; e < N; e++) os[w][(N < 4 ? N : 4) * (32 * (e / 4) + l) + e % 4] = o[e];
+    __syncthreads();
+    for (int d = 4 * threadIdx.x; d < D; d += 4 * 32 * kJoinWarps) {
+        float all = kLow, sum = 0.f, y[4] = {};
+#pragma unroll
+        for (int x = 0; x < kJoinWarps; x++) all = fmaxf(all, rs[x]);
+#pragma unroll
+        for (int x = 0; x < kJoinWarps; x++) {
+            const float k = exp2_fast(rs[x] - all);
+            sum = fmaf(k, ls[x], sum);
+#pragma unroll
+            for (int e = 0; e < 4; e++) y[e] = fmaf(k, os[x][d + e], y[e]);
+        }
+        put_output(a, j.b, j.vh / chunks * a.groups + g0 + h, d, all, sum, y, D);
     }
 }
 

@@ -76,7 +76,9 @@ stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int
         if (st != STEPQ_OK) return st;
         st = launch_overlapped(kv_attend_kernel<S>, g.ctas, 32 * kAttWarps, S::SMEM, s, a);
         if (st != STEPQ_OK || g.whole) return st;
-        return launch_overlapped(kv_join_kernel<S::HT, S::D>, g.ctas, 256, 0, s, a);
+        const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
+        return launch_overlapped(kv_join_kernel<S::HT, S::D>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
+                                 32 * kJoinWarps, 0, s, a, g.ctas);
     });
 }
 

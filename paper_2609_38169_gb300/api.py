@@ -594,7 +594,7 @@ _pack_rows = struct.Struct("@i4xPPqq").pack           # of _lib.StepqKvRows
 _pack_query = struct.Struct("@iiPPPqqfii4x").pack     # of _lib.StepqKvQuery
 
 
-@dataclass
+@dataclass(slots=True)
 class KvConfig:
     """stepq_kv_config: pages of page_tokens tokens for every layer and key head, as bf16 or
     fp16 or as codes of 8 or 4 bits (KV_BF16, KV_F16, KV_INT8, KV_INT4)."""
@@ -626,26 +626,34 @@ def alloc_pages(kv: KvConfig, n_pages: int, device="cuda"):
 
 
 def _kv_pages(kv, pages, table, B):
-    """The configuration by reference, and the packed pages and tables of a call for B sequences."""
+    """The configuration by reference, the packed pages and tables of a call for B sequences, and
+    their device."""
     ref, nbytes = kv._kept()
-    if table.dim() != 2 or table.shape[0] != B:
-        raise ValueError(f"table: expected {B} rows, got shape {tuple(table.shape)}")
-    W = table.shape[1]
-    if not table.is_cuda or table.dtype is not _Torch.i32 or (W > 1 and table.stride(1) != 1):
+    shape, dev = table.shape, table.get_device()
+    if len(shape) != 2 or shape[0] != B:
+        raise ValueError(f"table: expected {B} rows, got shape {tuple(shape)}")
+    step, W = table.stride(), shape[1]
+    if dev < 0 or table.dtype is not _Torch.i32 or (W > 1 and step[1] != 1):
         raise ValueError("table: expected rows of contiguous int32 on a CUDA device")
-    if pages.get_device() != table.get_device():
+    if pages.get_device() != dev:
         raise ValueError("pages and table are on different devices")
-    n = pages.numel() * pages.element_size() // nbytes if nbytes else 1      # the library refuses the rest
-    return ref, _pack_pages(_dev_ptr(pages), n, W, table.data_ptr(), table.stride(0) if B > 1 else W)
+    if not pages.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    # a page of 0 bytes: the library refuses the configuration
+    return ref, _pack_pages(pages.data_ptr(), pages.nbytes // nbytes if nbytes else 1, W, table.data_ptr(),
+                            step[0] if B > 1 else W), dev
 
 
-def _head_rows(t, dtype, rows, heads, dim, pages, what):
-    """Pointer and row stride of rows [rows][heads][dim] (or [rows][heads * dim]) beside `pages`."""
-    shape, st = t.shape, t.stride()
-    if t.get_device() != pages.get_device() or not t.is_cuda:
+def _head_rows(t, dtype, rows, heads, dim, dev, what):
+    """Pointer and row stride of rows [rows][heads][dim] (or [rows][heads * dim]) on the pages' device."""
+    shape = t.shape
+    if t.get_device() != dev:
         raise ValueError(f"{what}: expected a CUDA tensor on the pages' device")
     if t.dtype is not dtype:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if shape == (rows, heads, dim) and t.is_contiguous():
+        return t.data_ptr(), heads * dim
+    st = t.stride()
     if len(shape) == 3:
         ok = shape[1] == heads and shape[2] == dim and st[2] == 1 and (heads == 1 or st[1] == dim)
     else:
@@ -656,16 +664,29 @@ def _head_rows(t, dtype, rows, heads, dim, pages, what):
     return t.data_ptr(), st[0] if rows > 1 else heads * dim
 
 
+def _i32_ptr(t, n, dev, what):
+    """Pointer of n contiguous int32 on the pages' device."""
+    if t.numel() != n:
+        raise ValueError(f"{what}: expected {n} values, got {t.numel()}")
+    if t.dtype is _Torch.i32 and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{what}: expected contiguous int32 on the pages' device")
+
+
 def _kv_transfer(call, name, kv, layer, pages, table, starts, k, v, cu_seqlens, stream):
-    _f32()
-    B, n = starts.numel(), k.shape[0]
+    if _Torch.f32 is None:
+        _Torch.load()
+    B, n, dt, H, Dh = starts.numel(), k.shape[0], k.dtype, kv.n_heads, kv.head_dim
     if cu_seqlens is not None and cu_seqlens.numel() != B + 1:
         raise ValueError(f"cu_seqlens: expected {B + 1} values, got {cu_seqlens.numel()}")
-    ref, pg = _kv_pages(kv, pages, table, B)
-    kp, ks = _head_rows(k, k.dtype, n, kv.n_heads, kv.head_dim, pages, "k")
-    vp, vs = _head_rows(v, k.dtype, n, kv.n_heads, kv.head_dim, pages, "v")
-    check(call(ref, layer, pg, _dev_ptr(starts, _Torch.i32), _dev_ptr(cu_seqlens, _Torch.i32), B, n,
-               _pack_rows(_dtype_code(k.dtype), kp, vp, ks, vs), _stream(stream)), name)
+    ref, pg, dev = _kv_pages(kv, pages, table, B)
+    cu = None if cu_seqlens is None else _i32_ptr(cu_seqlens, B + 1, dev, "cu_seqlens")
+    kp, ks = _head_rows(k, dt, n, H, Dh, dev, "k")
+    vp, vs = _head_rows(v, dt, n, H, Dh, dev, "v")
+    status = call(ref, layer, pg, _i32_ptr(starts, B, dev, "starts"), cu, B, n,
+                  _pack_rows(_dtype_code(dt), kp, vp, ks, vs), _stream(stream))
+    if status:
+        check(status, name)
 
 
 def stepq_kv_append(kv: KvConfig, layer: int, pages, table, starts, k, v, cu_seqlens=None, stream=None):
@@ -689,12 +710,14 @@ def stepq_kv_attend(kv: KvConfig, layer: int, pages, table, lens, q, y, scale=No
     """Attention of one token of every sequence over its lens[b] (int32 [B]) cached tokens, or the
     last `window` of them: q, y [B][Hq][D] (rows may be strided), lse fp32 [B][Hq] or None; scale
     1 / sqrt(D) if not given. A workspace that is needed and not given (uint8) comes from torch."""
-    f, B = _f32(), lens.numel()
-    ref, pg = _kv_pages(kv, pages, table, B)
-    Dh = kv.head_dim
-    Hq = q.shape[1] if q.dim() == 3 else q.shape[1] // Dh
-    qp, qs = _head_rows(q, q.dtype, B, Hq, Dh, pages, "q")
-    yp, ys = _head_rows(y, q.dtype, B, Hq, Dh, pages, "y")
+    if _Torch.f32 is None:
+        _Torch.load()
+    B, dt, Dh = lens.numel(), q.dtype, kv.head_dim
+    ref, pg, dev = _kv_pages(kv, pages, table, B)
+    shape = q.shape
+    Hq = shape[1] if len(shape) == 3 else shape[-1] // Dh
+    qp, qs = _head_rows(q, dt, B, Hq, Dh, dev, "q")
+    yp, ys = _head_rows(y, dt, B, Hq, Dh, dev, "y")
     if lse is not None and lse.numel() != B * Hq:
         raise ValueError(f"lse: expected {B * Hq} values, got {lse.numel()}")
     lib = _lib.lib()
@@ -703,11 +726,12 @@ def stepq_kv_attend(kv: KvConfig, layer: int, pages, table, lens, q, y, scale=No
         nbytes = lib.stepq_kv_workspace_bytes(ref, Hq, B, min(max_len, most) if max_len > 0 else most)
         if nbytes:
             workspace = _scratch(nbytes, q.device, stream)
-    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    io = _pack_query(_dtype_code(q.dtype), Hq, qp, yp, _dev_ptr(lse, f) or 0, qs, ys,
-                     Dh ** -0.5 if scale is None else scale, window, max_len)
-    check(lib.stepq_kv_attend(ref, layer, pg, _dev_ptr(lens, _Torch.i32), B, io, _dev_ptr(workspace), have,
-                              _stream(stream)), "stepq_kv_attend")
+    ws, have = (None, 0) if workspace is None else (_dev_ptr(workspace), workspace.nbytes)
+    status = lib.stepq_kv_attend(ref, layer, pg, _i32_ptr(lens, B, dev, "lens"), B, _pack_query(
+        _dtype_code(dt), Hq, qp, yp, _dev_ptr(lse, _Torch.f32) or 0, qs, ys, Dh ** -0.5 if scale is None else scale,
+        window, max_len), ws, have, _stream(stream))
+    if status:
+        check(status, "stepq_kv_attend")
 
 
 # ------------------------------------------------------------------ calibration driver

@@ -14,7 +14,7 @@ int row_bits(int format) { return format == STEPQ_KV_INT4 ? 4 : format == STEPQ_
 
 stepq_status check_config(const stepq_kv_config *c) {
     if (!c || c->n_layers < 1 || c->n_heads < 1 || c->format < STEPQ_KV_BF16 || c->format > STEPQ_KV_INT4 ||
-        c->n_heads > (1 << 16) || c->n_layers > (1 << 16))
+        c->n_heads > (1 << 14) || c->n_layers > (1 << 16))
         return STEPQ_ERR_ARG;
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return STEPQ_ERR_UNSUPPORTED;
     if (c->page_tokens < 8 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1)))

@@ -5,8 +5,10 @@
 // rounded quotient: for x of 16 bits its distance from a border between two codes is zero
 // or above 2^-20 of it, so every such code is the one of the exact quotient.
 //
-// One warp per token, which finds its sequence and page once for all heads. A lane takes
-// eight channels, D / 8 lanes a row, so that a warp has 32 / (D / 8) rows at once.
+// A warp takes K or V of one token and up to kRows rows a lane: a lane has eight channels, D / 8
+// lanes a row, so that a warp holds 32 / (D / 8) heads at once. All its loads are on their way
+// before it looks at the first value (the append's before it has found the token's sequence and
+// page). HBM would bound both calls; what they have to be kept from is the issue slots.
 #include <type_traits>
 
 #include "device.cuh"
@@ -15,7 +17,7 @@
 namespace stepq {
 namespace kv {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 4, kRows = 4;
 
 struct RowsArgs {
     Pages pg;
@@ -41,25 +43,30 @@ __device__ __forceinline__ int find_sequence(const int32_t *cu, int B, int i, in
     return lo;
 }
 
-// Eight channels of a row.
-template <class T>
-__device__ __forceinline__ void load8(const T *p, float (&x)[8]) {
-    if (sizeof(T) == 4) {
-        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        const la::Vec<T, 8> v = *(const la::Vec<T, 8> *)p;
+// Eight channels of a row as they lie in memory, and as pairs of fp32.
+template <class T> struct alignas(16) Eight { T e[8]; };
+__device__ __forceinline__ void pairs(const Eight<float> &v, uint64_t (&x)[4]) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = la::to_f32(v.e[i]);
-    }
+    for (int i = 0; i < 4; i++) x[i] = f2(v.e[2 * i], v.e[2 * i + 1]);
 }
 template <class T>
-__device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
+__device__ __forceinline__ void pairs(const Eight<T> &v, uint64_t (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = f2(la::to_f32(v.e[2 * i]), la::to_f32(v.e[2 * i + 1]));
+}
+template <class T>
+__device__ __forceinline__ void store8(T *p, const uint64_t (&x)[4]) {
     if (sizeof(T) == 4) {
-        ((float4 *)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        ((float4 *)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        ((float4 *)p)[0] = make_float4(f2lo(x[0]), f2hi(x[0]), f2lo(x[1]), f2hi(x[1]));
+        ((float4 *)p)[1] = make_float4(f2lo(x[2]), f2hi(x[2]), f2lo(x[3]), f2hi(x[3]));
     } else {
-        la::store_vec<T, 8>(p, x);
+        la::Vec<T, 8> v;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            v.e[2 * i] = la::from_f32<T>(f2lo(x[i]));
+            v.e[2 * i + 1] = la::from_f32<T>(f2hi(x[i]));
+        }
+        *(la::Vec<T, 8> *)p = v;
     }
 }
 
@@ -93,88 +100,164 @@ __device__ __forceinline__ Place place_of(const RowsArgs &a, int i, int lane) {
     return {page, a.pg.slot((int)pos)};
 }
 
+// The quotient a / s, rounded, with y the rounded reciprocal of s: t = a y and then t + (a - t s) y
+// (P. Markstein, Computation of elementary functions on the IBM RISC System/6000, 1990).
+__device__ __forceinline__ float quotient(float a, float s, float y) {
+    const float t = a * y;
+    return fmaf(fmaf(-t, s, a), y, t);
+}
+
+// A lane's rows: token i, K or V (part), heads h0 + n * PER, channels 8 c on.
+template <int D>
+struct Mine {
+    static constexpr int L = D / 8, PER = 32 / L;
+    int i, lane, c, part, h0;
+    __device__ __forceinline__ Mine() {
+        i = blockIdx.x * kWarps + (threadIdx.x >> 5);
+        lane = threadIdx.x & 31;
+        c = lane % L;
+        part = blockIdx.y & 1;
+        h0 = (blockIdx.y >> 1) * PER * kRows + lane / L;
+    }
+};
+
 template <int F, int D, class T>
 __global__ void __launch_bounds__(32 * kWarps) kv_append_kernel(RowsArgs a) {
-    constexpr int RB = row_bytes(F, D), L = D / 8, PER = 32 / L;
-    const int lane = threadIdx.x & 31, i = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    constexpr int RB = row_bytes(F, D);
+    const Mine<D> m;
     griddep_wait();
     griddep_launch();
-    if (i >= a.tokens) return;
-    const Place p = place_of(a, i, lane);
+    if (m.i >= a.tokens) return;
+    const T *src = (const T *)(m.part ? a.v : a.k) + m.i * (m.part ? a.vs : a.ks) + m.h0 * D + 8 * m.c;
+    Eight<T> in[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; n++)
+        if (m.h0 + n * m.PER < a.pg.n_heads) in[n] = *(const Eight<T> *)(src + n * m.PER * D);
+    const Place p = place_of(a, m.i, m.lane);
     if (p.page < 0) return;
-    const int rows = 2 * a.pg.n_heads, c = lane % L, pt = 1 << a.pg.shift;
-    for (int r0 = 0; r0 < rows; r0 += PER) {
-        const int r = r0 + lane / L;                         // head by head, K before V
-        const bool on = r < rows;
-        const int h = r >> 1, part = r & 1;
-        float x[8] = {};
-        if (on) load8<T>((const T *)(part ? a.v : a.k) + i * (part ? a.vs : a.ks) + h * D + 8 * c, x);
-        uint8_t *seg = a.pg.at(p.page, h);
-        uint8_t *row = seg + (part * pt + p.slot) * RB;
+    uint8_t *seg = a.pg.at(p.page, m.h0);
+    const int pt = 1 << a.pg.shift, at = (m.part * pt + p.slot) * RB, at_scale = 2 * pt * RB + 2 * (m.part * pt + p.slot);
+#pragma unroll
+    for (int n = 0; n < kRows; n++, seg += m.PER * a.pg.segment) {
+        const bool on = m.h0 + n * m.PER < a.pg.n_heads;
         if (!coded(F)) {
+            if (!on) return;
             using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
-            if (on) store8<C>((C *)row + 8 * c, x);
+            uint64_t x[4];
+            pairs(in[n], x);
+            store8<C>((C *)(seg + at) + 8 * m.c, x);
             continue;
         }
-        float top = 0.f;
+        if (m.h0 - m.lane / m.L + n * m.PER >= a.pg.n_heads) return;         // no lane has a row
+        uint64_t x[4];
+        if (on) pairs(in[n], x);
+        else x[0] = x[1] = x[2] = x[3] = 0;
+        // as unsigned numbers the values' magnitudes are ordered, NaN above all
+        uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; e++) top = fmaxf(top, fabsf(x[e]));
+        for (int e = 0; e < 4; e++)
+            most = max(most, max((uint32_t)x[e] & 0x7fffffffu, (uint32_t)(x[e] >> 32) & 0x7fffffffu));
 #pragma unroll
-        for (int o = 1; o < L; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = 1; o < m.L; o *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
         constexpr float q = F == STEPQ_KV_INT8 ? 127.f : 7.f;
-        const uint16_t sb = f16_bits(fminf(fmaxf(__fdiv_rn(top, q), kF16Min), kF16Max));
-        const float s = f16_val(sb);
-        uint32_t u[8];
+        constexpr int half = F == STEPQ_KV_INT8 ? 128 : 8;
+        float top = __uint_as_float(most);
+        const bool far = !(top <= 65504.f * q);
+        if (__any_sync(0xffffffffu, far)) {
+            // a scale at its bound, or values that are not finite: NaN becomes zero, the others are clamped
+            top = 0.f;
+            float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float t = x[e] == x[e] ? fminf(fmaxf(rintf(__fdiv_rn(x[e], s)), -q), q) : 0.f;
-            u[e] = (uint32_t)(int)(t + (q + 1.f));
+            for (int e = 0; e < 8; e++) {
+                const float t = e & 1 ? f2hi(x[e / 2]) : f2lo(x[e / 2]);
+                v[e] = t == t ? t : 0.f;
+                top = fmaxf(top, fabsf(v[e]));
+            }
+#pragma unroll
+            for (int o = 1; o < m.L; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = fminf(top, 65504.f * q);
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                x[e] = f2(fminf(fmaxf(v[2 * e], -top), top), fminf(fmaxf(v[2 * e + 1], -top), top));
+        }
+        const uint16_t sb = f16_bits(fmaxf(quotient(top, q, 1.f / q), kF16Min));
+        const float s = f16_val(sb), y = __frcp_rn(s);
+        // Quotients plus 1.5 2^23 + 2^(b-1): the sum's lowest bits are the code. |x| <= top, so that
+        // no quotient is above q by more than the scale's rounding.
+        constexpr uint32_t magic = 0x4b400000u + half;
+        uint64_t u[4];
+        const uint64_t ss = f2s(-s), yy = f2s(y);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const uint64_t t = fmul2(x[e], yy);
+            u[e] = fadd2(ffma2(ffma2(t, ss, x[e]), yy, t), f2s(12582912.f + half));
         }
         if (!on) continue;
+        auto code = [&](int e) { return (uint32_t)(u[e >> 1] >> (32 * (e & 1))); };
         if (F == STEPQ_KV_INT8) {
-            const uint32_t w0 = u[0] | u[1] << 8 | u[2] << 16 | u[3] << 24, w1 = u[4] | u[5] << 8 | u[6] << 16 | u[7] << 24;
-            ((uint2 *)row)[c] = make_uint2(w0, w1);
+            uint2 w;
+            w.x = __byte_perm(__byte_perm(code(0), code(1), 0x0040), __byte_perm(code(2), code(3), 0x0040), 0x5410);
+            w.y = __byte_perm(__byte_perm(code(4), code(5), 0x0040), __byte_perm(code(6), code(7), 0x0040), 0x5410);
+            ((uint2 *)(seg + at))[m.c] = w;
         } else {
-            uint32_t w = 0;
+            // what stands above the codes adds up to a constant (mod 2^32)
+            uint32_t w = code(7);
 #pragma unroll
-            for (int e = 0; e < 8; e++) w |= u[e] << (4 * e);
-            ((uint32_t *)row)[c] = w;
+            for (int e = 6; e >= 0; e--) w = w * 16u + code(e);
+            ((uint32_t *)(seg + at))[m.c] = w - (magic - half) * 0x11111111u;
         }
-        if (c == 0) ((uint16_t *)(seg + 2 * pt * RB))[part * pt + p.slot] = sb;
+        if (m.c == 0) *(uint16_t *)(seg + at_scale) = sb;
     }
 }
 
 template <int F, int D, class T>
 __global__ void __launch_bounds__(32 * kWarps) kv_read_kernel(RowsArgs a) {
-    constexpr int RB = row_bytes(F, D), L = D / 8, PER = 32 / L;
-    const int lane = threadIdx.x & 31, i = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    constexpr int RB = row_bytes(F, D);
+    using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
+    using W = la::Vec<uint32_t, bits_of(F) / 4>;             // eight channels
+    const Mine<D> m;
     griddep_wait();
     griddep_launch();
-    if (i >= a.tokens) return;
-    const Place p = place_of(a, i, lane);
+    if (m.i >= a.tokens) return;
+    const Place p = place_of(a, m.i, m.lane);
     if (p.page < 0) return;
-    const int rows = 2 * a.pg.n_heads, c = lane % L, pt = 1 << a.pg.shift;
-    for (int r = lane / L; r < rows; r += PER) {
-        const int h = r >> 1, part = r & 1;
-        const uint8_t *seg = a.pg.at(p.page, h);
-        const uint8_t *row = seg + (part * pt + p.slot) * RB;
-        float x[8];
+    const uint8_t *seg = a.pg.at(p.page, m.h0);
+    const int pt = 1 << a.pg.shift, at = (m.part * pt + p.slot) * RB, at_scale = 2 * pt * RB + 2 * (m.part * pt + p.slot);
+    W w[kRows];
+    uint16_t sb[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; n++, seg += m.PER * a.pg.segment)
+        if (m.h0 + n * m.PER < a.pg.n_heads) {
+            w[n] = ((const W *)(seg + at))[m.c];
+            if (coded(F)) sb[n] = *(const uint16_t *)(seg + at_scale);
+        }
+    T *dst = (T *)(m.part ? a.v : a.k) + m.i * (m.part ? a.vs : a.ks) + m.h0 * D + 8 * m.c;
+#pragma unroll
+    for (int n = 0; n < kRows; n++) {
+        if (m.h0 + n * m.PER >= a.pg.n_heads) return;
+        uint64_t x[4];
         if (!coded(F)) {
-            using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
-            load8<C>((const C *)row + 8 * c, x);
+            pairs(*(const Eight<C> *)&w[n], x);
         } else {
-            const float s = f16_val(((const uint16_t *)(seg + 2 * pt * RB))[part * pt + p.slot]);
-            if (F == STEPQ_KV_INT8) {
-                const uint2 w = ((const uint2 *)row)[c];
+            // 2^23 + u 2^k less 2^23 + 2^(b-1) 2^k is exact, and so is s 2^-k
+            const float s = f16_val(sb[n]);
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = (float)((int)((e < 4 ? w.x : w.y) >> (8 * (e & 3)) & 255u) - 128) * s;
-            } else {
-                const uint32_t w = ((const uint32_t *)row)[c];
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = (float)((int)(w >> (4 * e) & 15u) - 8) * s;
+            for (int e = 0; e < 4; e++) {
+                if constexpr (F == STEPQ_KV_INT8) {
+                    const uint32_t v = w[n].e[e / 2];
+                    x[e] = u2pair(__byte_perm(v, 0x4b000000u, 0x7650 + 2 * (e & 1)), __byte_perm(v, 0x4b000000u, 0x7651 + 2 * (e & 1)));
+                    x[e] = fmul2(fadd2(x[e], f2s(-8388736.f)), f2s(s));
+                } else {
+                    const uint32_t v = e < 2 ? w[n].e[0] : w[n].e[0] >> 16;
+                    constexpr float pow16[4] = {1.f, 16.f, 256.f, 4096.f};
+                    const int k = 2 * (e & 1);
+                    x[e] = u2pair(and_or(v, 15u << (4 * k), 0x4b000000u), and_or(v, 240u << (4 * k), 0x4b000000u));
+                    x[e] = fadd2(x[e], f2(-8388608.f - 8.f * pow16[k], -8388608.f - 8.f * pow16[k + 1]));
+                    x[e] = fmul2(x[e], f2(s * (1.f / pow16[k]), s * (1.f / pow16[k + 1])));
+                }
             }
         }
-        store8<T>((T *)(part ? a.v : a.k) + i * (part ? a.vs : a.ks) + h * D + 8 * c, x);
+        store8<T>(dst + n * m.PER * D, x);
     }
 }
 
@@ -210,7 +293,8 @@ stepq_status launch_kv_rows(bool append, const stepq_kv_config *cfg, int layer, 
     a.B = B;
     a.tokens = tokens;
     a.k = rows->k; a.v = rows->v; a.ks = rows->k_stride; a.vs = rows->v_stride;
-    const int grid = (tokens + kv::kWarps - 1) / kv::kWarps;
+    const int per_warp = kv::kRows * 256 / cfg->head_dim;
+    const dim3 grid((unsigned)((tokens + kv::kWarps - 1) / kv::kWarps), 2 * ((cfg->n_heads + per_warp - 1) / per_warp));
     return kv::by_layout(cfg, [&](auto f, auto d) {
         return la::by_type(rows->dtype, [&](auto t) {
             auto *kernel = append ? kv::kv_append_kernel<decltype(f)::value, decltype(d)::value, decltype(t)>

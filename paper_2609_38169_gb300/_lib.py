@@ -2,6 +2,8 @@
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
 
 from . import build_ext
@@ -60,7 +62,8 @@ class StepqKvQuery(C.Structure):
 
 CFG = C.POINTER(StepqConfig)
 KV = C.POINTER(StepqKvConfig)
-IO = NORM = PAGES = ROWS = QUERY = P           # a structure by reference, or its bytes (api.py packs them: a tenth of a Structure's time)
+PAGES, ROWS, QUERY = C.POINTER(StepqKvPages), C.POINTER(StepqKvRows), C.POINTER(StepqKvQuery)
+IO = NORM = P           # a structure by reference, or its bytes (api.py packs them: a tenth of a Structure's time)
 
 # name -> (restype, argtypes); the exported symbol set of include/stepq.h
 SIGNATURES = {
@@ -126,6 +129,23 @@ def lib(build: bool = True):
             fn.argtypes = args
         _lib = L
     return _lib
+
+
+_bind = None
+
+
+def bind():
+    """The compiled half of the binding (csrc/bind.cpp), loaded with the first call that uses it."""
+    global _bind
+    if _bind is None:
+        import torch  # noqa: F401  (its libraries are the module's)
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("_stepq_bind", build_ext.build_bind())
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_stepq_bind", loader))
+        loader.exec_module(m)
+        m.use(*(C.cast(getattr(L, "stepq_kv_" + f), C.c_void_p).value for f in ("append", "read", "attend", "page_bytes")))
+        _bind = m
+    return _bind
 
 
 class StepqError(RuntimeError):

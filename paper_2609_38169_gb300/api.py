@@ -13,7 +13,7 @@ from dataclasses import dataclass, field
 import numpy as np
 
 from . import _lib
-from ._lib import StepqCalib, StepqConfig, StepqKvConfig, StepqPlanInfo, check
+from ._lib import StepqCalib, StepqConfig, StepqKvConfig, StepqPlanInfo, bind as _bind, check
 
 D = 128
 GATE_SCALAR = 0
@@ -588,12 +588,6 @@ def stepq_group_norm(x, groups: int, out, norm: Norm, stream=None):
 
 
 # ------------------------------------------------------------------ paged key-value cache
-_KV_CONFIGS: dict = {}
-_pack_pages = struct.Struct("@PiiPq").pack            # of _lib.StepqKvPages
-_pack_rows = struct.Struct("@i4xPPqq").pack           # of _lib.StepqKvRows
-_pack_query = struct.Struct("@iiPPPqqfii4x").pack     # of _lib.StepqKvQuery
-
-
 @dataclass(slots=True)
 class KvConfig:
     """stepq_kv_config: pages of page_tokens tokens for every layer and key head, as bf16 or
@@ -604,20 +598,12 @@ class KvConfig:
     page_tokens: int = 64
     format: int = KV_BF16
 
-    def _kept(self):
-        """The C structure by reference and the bytes of a page, kept by the fields' values."""
-        key = (self.n_layers, self.n_heads, self.head_dim, self.page_tokens, self.format)
-        kept = _KV_CONFIGS.get(key)
-        if kept is None:
-            if len(_KV_CONFIGS) >= 64:
-                _KV_CONFIGS.clear()
-            ref = C.byref(StepqKvConfig(*key))
-            kept = _KV_CONFIGS[key] = ref, int(_lib.lib().stepq_kv_page_bytes(ref))
-        return kept
+    def c(self) -> StepqKvConfig:
+        return StepqKvConfig(self.n_layers, self.n_heads, self.head_dim, self.page_tokens, self.format)
 
 
 def stepq_kv_page_bytes(kv: KvConfig) -> int:
-    return kv._kept()[1]
+    return int(_lib.lib().stepq_kv_page_bytes(C.byref(kv.c())))
 
 
 def alloc_pages(kv: KvConfig, n_pages: int, device="cuda"):
@@ -625,84 +611,24 @@ def alloc_pages(kv: KvConfig, n_pages: int, device="cuda"):
     return torch.zeros(n_pages * stepq_kv_page_bytes(kv), dtype=torch.uint8, device=device)
 
 
-def _kv_pages(kv, pages, table, B):
-    """The configuration by reference, the packed pages and tables of a call for B sequences, and
-    their device."""
-    ref, nbytes = kv._kept()
-    shape, dev = table.shape, table.get_device()
-    if len(shape) != 2 or shape[0] != B:
-        raise ValueError(f"table: expected {B} rows, got shape {tuple(shape)}")
-    step, W = table.stride(), shape[1]
-    if dev < 0 or table.dtype is not _Torch.i32 or (W > 1 and step[1] != 1):
-        raise ValueError("table: expected rows of contiguous int32 on a CUDA device")
-    if pages.get_device() != dev:
-        raise ValueError("pages and table are on different devices")
-    if not pages.is_contiguous():
-        raise ValueError("expected a contiguous tensor")
-    # a page of 0 bytes: the library refuses the configuration
-    return ref, _pack_pages(pages.data_ptr(), pages.nbytes // nbytes if nbytes else 1, W, table.data_ptr(),
-                            step[0] if B > 1 else W), dev
-
-
-def _head_rows(t, dtype, rows, heads, dim, dev, what):
-    """Pointer and row stride of rows [rows][heads][dim] (or [rows][heads * dim]) on the pages' device."""
-    shape = t.shape
-    if t.get_device() != dev:
-        raise ValueError(f"{what}: expected a CUDA tensor on the pages' device")
-    if t.dtype is not dtype:
-        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    if shape == (rows, heads, dim) and t.is_contiguous():
-        return t.data_ptr(), heads * dim
-    st = t.stride()
-    if len(shape) == 3:
-        ok = shape[1] == heads and shape[2] == dim and st[2] == 1 and (heads == 1 or st[1] == dim)
-    else:
-        ok = len(shape) == 2 and shape[1] == heads * dim and st[1] == 1
-    if not ok or shape[0] != rows:
-        raise ValueError(f"{what}: expected {rows} contiguous rows of {heads} x {dim}, got shape {tuple(shape)}, "
-                         f"strides {tuple(st)}")
-    return t.data_ptr(), st[0] if rows > 1 else heads * dim
-
-
-def _i32_ptr(t, n, dev, what):
-    """Pointer of n contiguous int32 on the pages' device."""
-    if t.numel() != n:
-        raise ValueError(f"{what}: expected {n} values, got {t.numel()}")
-    if t.dtype is _Torch.i32 and t.get_device() == dev and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{what}: expected contiguous int32 on the pages' device")
-
-
-def _kv_transfer(call, name, kv, layer, pages, table, starts, k, v, cu_seqlens, stream):
-    if _Torch.f32 is None:
-        _Torch.load()
-    B, n, dt, H, Dh = starts.numel(), k.shape[0], k.dtype, kv.n_heads, kv.head_dim
-    if cu_seqlens is not None and cu_seqlens.numel() != B + 1:
-        raise ValueError(f"cu_seqlens: expected {B + 1} values, got {cu_seqlens.numel()}")
-    ref, pg, dev = _kv_pages(kv, pages, table, B)
-    cu = None if cu_seqlens is None else _i32_ptr(cu_seqlens, B + 1, dev, "cu_seqlens")
-    kp, ks = _head_rows(k, dt, n, H, Dh, dev, "k")
-    vp, vs = _head_rows(v, dt, n, H, Dh, dev, "v")
-    status = call(ref, layer, pg, _i32_ptr(starts, B, dev, "starts"), cu, B, n,
-                  _pack_rows(_dtype_code(dt), kp, vp, ks, vs), _stream(stream))
-    if status:
-        check(status, name)
-
-
 def stepq_kv_append(kv: KvConfig, layer: int, pages, table, starts, k, v, cu_seqlens=None, stream=None):
     """Rows k, v [tokens][heads][D] (rows may be strided) into one layer of the pages: sequence
     b's become its tokens from starts[b] (int32 [B]) on; table int32 [B][width]; cu_seqlens
     int32 [B+1] (None: equal lengths)."""
-    _kv_transfer(_lib.lib().stepq_kv_append, "stepq_kv_append", kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+    status = _bind().kv_append(kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+    if status:
+        check(status, "stepq_kv_append")
 
 
 def stepq_kv_read(kv: KvConfig, layer: int, pages, table, starts, k, v, cu_seqlens=None, stream=None):
     """The tokens that stepq_kv_append would write, read into k and v."""
-    _kv_transfer(_lib.lib().stepq_kv_read, "stepq_kv_read", kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+    status = _bind().kv_read(kv, layer, pages, table, starts, k, v, cu_seqlens, stream)
+    if status:
+        check(status, "stepq_kv_read")
 
 
 def stepq_kv_workspace_bytes(kv: KvConfig, q_heads: int, B: int, max_len: int = 0) -> int:
-    return int(_lib.lib().stepq_kv_workspace_bytes(kv._kept()[0], int(q_heads), int(B), int(max_len)))
+    return int(_lib.lib().stepq_kv_workspace_bytes(C.byref(kv.c()), int(q_heads), int(B), int(max_len)))
 
 
 def stepq_kv_attend(kv: KvConfig, layer: int, pages, table, lens, q, y, scale=None, window: int = 0, lse=None,
@@ -710,26 +636,13 @@ def stepq_kv_attend(kv: KvConfig, layer: int, pages, table, lens, q, y, scale=No
     """Attention of one token of every sequence over its lens[b] (int32 [B]) cached tokens, or the
     last `window` of them: q, y [B][Hq][D] (rows may be strided), lse fp32 [B][Hq] or None; scale
     1 / sqrt(D) if not given. A workspace that is needed and not given (uint8) comes from torch."""
-    if _Torch.f32 is None:
-        _Torch.load()
-    B, dt, Dh = lens.numel(), q.dtype, kv.head_dim
-    ref, pg, dev = _kv_pages(kv, pages, table, B)
-    shape = q.shape
-    Hq = shape[1] if len(shape) == 3 else shape[-1] // Dh
-    qp, qs = _head_rows(q, dt, B, Hq, Dh, dev, "q")
-    yp, ys = _head_rows(y, dt, B, Hq, Dh, dev, "y")
-    if lse is not None and lse.numel() != B * Hq:
-        raise ValueError(f"lse: expected {B * Hq} values, got {lse.numel()}")
-    lib = _lib.lib()
-    if workspace is None:
+    if workspace is None and table.dim() == 2 and table.is_cuda:
         most = table.shape[1] * kv.page_tokens
-        nbytes = lib.stepq_kv_workspace_bytes(ref, Hq, B, min(max_len, most) if max_len > 0 else most)
+        heads = q.shape[1] if q.dim() == 3 else q.shape[-1] // kv.head_dim
+        nbytes = stepq_kv_workspace_bytes(kv, heads, lens.numel(), min(max_len, most) if max_len > 0 else most)
         if nbytes:
-            workspace = _scratch(nbytes, q.device, stream)
-    ws, have = (None, 0) if workspace is None else (_dev_ptr(workspace), workspace.nbytes)
-    status = lib.stepq_kv_attend(ref, layer, pg, _i32_ptr(lens, B, dev, "lens"), B, _pack_query(
-        _dtype_code(dt), Hq, qp, yp, _dev_ptr(lse, _Torch.f32) or 0, qs, ys, Dh ** -0.5 if scale is None else scale,
-        window, max_len), ws, have, _stream(stream))
+            workspace = _scratch(nbytes, table.device, stream)
+    status = _bind().kv_attend(kv, layer, pages, table, lens, q, y, scale, window, lse, max_len, workspace, stream)
     if status:
         check(status, "stepq_kv_attend")
 

@@ -1,10 +1,14 @@
-"""Build libstepq.so in-tree with nvcc for sm_103a (one -gencode, TUs in parallel)."""
+"""Build libstepq.so in-tree with nvcc for sm_103a (one -gencode, TUs in parallel), and beside it
+the compiled half of the Python binding, which needs the headers of the torch it is used with."""
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -21,6 +25,16 @@ HEADERS = ["internal.h", "device.cuh", "async.cuh", "pipeline.cuh", "tile.cuh", 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
+BIND_SOURCE = "bind.cpp"
+
+
+def bind_so() -> str | None:
+    """Where the binding for the installed torch is built (None: there is no torch)."""
+    if importlib.util.find_spec("torch") is None:
+        return None
+    return os.path.join(BUILD, "torch-" + importlib.metadata.version("torch"), "_stepq_bind.so")
+
+
 def nvcc() -> str:
     for cand in (shutil.which("nvcc"), "/usr/local/cuda/bin/nvcc"):
         if cand and os.path.exists(cand):
@@ -28,16 +42,50 @@ def nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libstepq.so")
 
 
-def _stale() -> bool:
-    if not os.path.exists(SO):
+def _older(so: str, sources) -> bool:
+    if not os.path.exists(so):
         return True
-    t = os.path.getmtime(SO)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(INCLUDE, "stepq.h"),
-                                                               os.path.abspath(__file__)]
+    t = os.path.getmtime(so)
+    deps = [os.path.join(CSRC, f) for f in sources] + [os.path.join(INCLUDE, "stepq.h"), os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _stale() -> bool:
+    return _older(SO, SOURCES + HEADERS)
+
+
+def build_bind(force: bool = False) -> str:
+    so = bind_so()
+    if so is None:
+        raise RuntimeError("torch not found: the device calls take its tensors")
+    if not force and not _older(so, [BIND_SOURCE]):
+        return so
+    os.makedirs(os.path.dirname(so), exist_ok=True)
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    tmp = so + f".{os.getpid()}.tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I", INCLUDE, "-I", os.path.join(torch, "include"),
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), os.path.join(CSRC, BIND_SOURCE),
+           "-o", tmp, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-lc10", "-lc10_cuda",
+           "-Wl,-rpath," + os.path.join(torch, "lib")]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on {BIND_SOURCE}:\n{r.stderr}")
+    os.replace(tmp, so)
+    return so
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Builds what is older than its sources; libstepq.so's path."""
+    with cf.ThreadPoolExecutor(max_workers=1) as ex:
+        bind = ex.submit(build_bind, force) if bind_so() else None
+        so = _build_library(force, verbose)
+        if bind:
+            bind.result()
+    return so
+
+
+def _build_library(force: bool, verbose: bool) -> str:
     if not force and not _stale():
         return SO
     os.makedirs(BUILD, exist_ok=True)

@@ -197,19 +197,27 @@ inline stepq_status cuda_status(cudaError_t e) {
 // plain stream order 8.89 (8.16); 128 slots: 1.21 (1.11), 1.31 (0.83) and 1.24 (1.14). Both
 // parts on one stream take 9.28 and 1.38 ms, with the early start 9.27 and 1.35.
 template <class Args, class... Rest>
-inline stepq_status launch_overlapped(void (*kernel)(Args, Rest...), dim3 grid, int block, int smem, cudaStream_t s,
-                                      const Args &a, Rest... rest) {
+inline stepq_status launch_clusters(void (*kernel)(Args, Rest...), dim3 grid, int cluster, int block, int smem,
+                                    cudaStream_t s, const Args &a, Rest... rest) {
     cudaLaunchConfig_t c{};
     c.gridDim = grid;
     c.blockDim = dim3((unsigned)block);
     c.dynamicSmemBytes = (size_t)smem;
     c.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     c.attrs = at;
-    c.numAttrs = 1;
+    c.numAttrs = cluster > 1 ? 2 : 1;
     return cuda_status(cudaLaunchKernelEx(&c, kernel, a, rest...));
+}
+template <class Args, class... Rest>
+inline stepq_status launch_overlapped(void (*kernel)(Args, Rest...), dim3 grid, int block, int smem, cudaStream_t s,
+                                      const Args &a, Rest... rest) {
+    return launch_clusters(kernel, grid, 1, block, smem, s, a, rest...);
 }
 
 constexpr int kSmemMax = 227 * 1024;   // dynamic shared memory one CTA can have

@@ -61,7 +61,8 @@ struct AttendArgs {
     int64_t qs, ys;
     float scale;                    // log2(e) times the call's
     int window;
-    int whole;                      // CTAs take whole sequences: no parts
+    int whole;                      // clusters take whole sequences: no parts
+    int stages;                     // of each warp's ring
     float *parts;                   // workspace: PartLayout
 };
 

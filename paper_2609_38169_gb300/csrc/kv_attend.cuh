@@ -10,6 +10,8 @@
 // dealt out in equal shares to the CTAs, which find theirs from the lengths on the device. A
 // CTA's share is pieces of one or more sequences; a piece that is a whole sequence gives its
 // outputs, one that is not leaves (R, l, O) in the workspace, and a second kernel joins those.
+// Where sequences are few and short enough, a cluster of CTAs takes each instead, whole, and
+// joins its parts through distributed shared memory: no workspace and no second kernel.
 // Within a CTA each warp takes every fourth tile, through its own ring of shared memory filled
 // by 16-byte asynchronous copies, and waits for no other warp until the piece ends. The ring
 // runs on into the next piece's tiles, which arrive while this piece's parts are put together.
@@ -69,15 +71,19 @@ struct Shape {
     static constexpr int FIT = WANT / (2 * RB), TT = FIT > 64 ? 64 : FIT;
     static constexpr int ST = NT * D >= 256 || TT == 16 ? 16 : KV_ST;       // taken at once
     static constexpr int TILE = 2 * TT * RB + (CODED ? 4 * TT : 0);
-    static constexpr int STAGES = CODED ? KV_SC : KV_S16;
-    static constexpr int OFF_Q = kAttWarps * STAGES * TILE;            // [QT][NT][D / 16][32] uint2
-    static constexpr int OFF_HEAD = OFF_Q + QT * NT * (D / 16) * 256;  // float [2][HT]: factor, offset
+    static constexpr int OFF_HEAD = QT * NT * (D / 16) * 256;          // behind the queries [QT][NT][D / 16][32] uint2:
+                                                                       // float [2][HT]: factor, offset
     static constexpr int OFF_SUM = OFF_HEAD + 2 * HT * 4;              // float [kAttWarps][2][HT]: R, l
-    static constexpr int OFF_SCAN = OFF_SUM + kAttWarps * 2 * HT * 4;  // int64 [kAttWarps + 2]
-    static constexpr int SMEM = OFF_SCAN + 8 * (kAttWarps + 4);
-    // CTAs of a multiprocessor, by shared memory and by registers
-    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED ? KV_RC : 3, BY_SMEM = 227 * 1024 / (SMEM + 1024);
-    static constexpr int RESIDENT = BY_REGS < BY_SMEM ? BY_REGS : BY_SMEM;
+    static constexpr int OFF_SCAN = OFF_SUM + kAttWarps * 2 * HT * 4;  // int64 [kAttWarps + 3]
+    static constexpr int OFF_RING = (OFF_SCAN + 8 * (kAttWarps + 3) + 127) / 128 * 128;
+    // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
+    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED ? KV_RC : 3;
+    static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
+    static constexpr int resident(int stages) {
+        const int n = 227 * 1024 / (smem(stages) + 1024);
+        return n < BY_REGS ? n : BY_REGS;
+    }
+    static constexpr int STAGES = CODED ? KV_SC : KV_S16;    // of calls that fill the GPU
     static_assert(TILE >= HT * D * 4, "a warp's part is put together in one stage of its ring");
     static constexpr int KP = RB / 4 < 16 ? RB / 4 : 16;     // bytes a lane reads of a row of K at once
     static constexpr int VP = RB / 8 < 16 ? RB / 8 : 16;     // and of V
@@ -144,6 +150,19 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool valid
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
 
+// This thread's groups of copies have landed, but for the newest n < kMostStages.
+constexpr int kMostStages = 6;
+__device__ __forceinline__ void wait_but(int n) {
+    switch (n) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 5;" ::: "memory");
+    }
+}
+
 // Place of byte `at` (row * RB + byte) of a tile's rows: 16-byte pieces change places within 128
 // bytes so that the lanes that read at once meet no bank twice. They read 64 bytes each of
 // rows r and r + 1 (K), or up to 32 of rows r, r + 2, r + 4 and r + 6 (V).
@@ -208,6 +227,28 @@ __host__ __device__ constexpr float v_factor(int odd) {
     return !coded(F) ? 1.f : F == STEPQ_KV_INT4 && odd ? 1048576.f : 16777216.f;
 }
 
+// Thread-block clusters: this CTA's place, the barrier of all their threads (which shows each other's
+// shared memory), and where CTA `rank` has what lies here at p.
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <class P>
+__device__ __forceinline__ const P *in_cluster(const P *p, uint32_t rank) {
+    uint64_t r;
+    asm("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(p), "r"(rank));
+    return (const P *)r;
+}
+
 __device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
     return dtype == STEPQ_F32 ? ((const float *)p)[i]
            : dtype == STEPQ_BF16 ? la::to_f32(((const la::bf16 *)p)[i]) : la::to_f32(((const la::f16 *)p)[i]);
@@ -263,7 +304,7 @@ struct Queries {
     __device__ __forceinline__ void put(const AttendArgs &a, uint8_t *smem, int w, int l) {
         using C = typename S::C;
         constexpr int F = S::F;
-        C *qf = (C *)(smem + S::OFF_Q);
+        C *qf = (C *)smem;
         float *head_k = (float *)(smem + S::OFF_HEAD), *head_off = head_k + S::HT;
 #pragma unroll
         for (int i = 0; i < H; i++) {
@@ -324,7 +365,7 @@ __device__ __forceinline__ void put_output(const AttendArgs &a, int b, int h, in
 
 // ------------------------------------------------------------------ the kernel
 template <class S>
-__global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(AttendArgs a) {
     extern __shared__ __align__(128) uint8_t smem[];
     using C = typename S::C;
     constexpr int D = S::D, TT = S::TT, RB = S::RB, NT = S::NT, HT = S::HT, F = S::F;
@@ -338,9 +379,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
     griddep_wait();
     griddep_launch();
 
+    // Calls for whole sequences: the CTAs of a cluster take a sequence's tiles in turn.
+    const int ctas = a.whole ? (int)cluster_size() : 1, rank = a.whole ? (int)cluster_rank() : 0;
+    const int stages = a.stages;
+    const int turn = rank * kAttWarps + w, turns = ctas * kAttWarps;
+
     // The share: `left` tiles of all, in the order (sequence, virtual head, tile), from tile `from`
     // of virtual head vh of sequence b on; len is lens[b].
-    long long left = 0, share = 0, item = blockIdx.x;        // item: of calls for whole sequences
+    long long left = 0, share = 0, item = blockIdx.x / ctas;     // item: of calls for whole sequences
     int b = 0, vh = 0, from = 0, len = 0;
     if (!a.whole) {
         const int per = (a.B + 32 * kAttWarps - 1) / (32 * kAttWarps), i0 = min(a.B, tid * per), i1 = min(a.B, i0 + per);
@@ -393,7 +439,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
             if (item >= items) return p;
             p.b = (int)(item / VH);
             p.vh = (int)(item - (long long)p.b * VH);
-            item += gridDim.x;
+            item += gridDim.x / ctas;
             len = a.lens[p.b];
             set_span<TT>(a, len, p);
             p.n = p.tiles;
@@ -416,8 +462,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
         }
         return p;
     };
-    // This warp's tiles of a piece: from + w, from + w + kAttWarps, ... below from + n.
-    auto count_of = [&](const Piece &p) { return p.n > w ? (p.n - w + kAttWarps - 1) / kAttWarps : 0; };
+    // This warp's tiles of a piece: from + turn, from + turn + turns, ... below from + n.
+    auto count_of = [&](const Piece &p) { return p.n > turn ? (p.n - turn + turns - 1) / turns : 0; };
 
     // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the page of
     // octet l (eight tokens) of that tile, -1 for none.
@@ -437,7 +483,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
     auto fetch_from = [&](const Piece &p) {
         f.table = a.pg.table + p.b * a.pg.table_stride;
         f.head = (uint64_t)(p.vh / chunks) * a.pg.segment;
-        f.tok = (p.tile0 + p.from + w) * TT;
+        f.tok = (p.tile0 + p.from + turn) * TT;
         f.more = count_of(p);
         f.lo = p.lo;
         f.hi = p.hi;
@@ -449,7 +495,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
     // lane's part of the offset and, apart from it, that of the step's.
     const uint32_t k_lane = k_place<RB>(16 * l / RB, 16 * l % RB), v_lane = v_place<RB>(16 * l / RB, 16 * l % RB);
     auto copy_tile = [&]() {
-        const uint32_t dst = smem_addr(smem) + (w * S::STAGES + to_fill) * S::TILE;
+        const uint32_t dst = smem_addr(smem) + S::OFF_RING + (w * stages + to_fill) * S::TILE;
         constexpr int N = TT * RB / 512, PER = RB >= 64 ? RB / 64 : 1;       // steps, and steps of an octet
         // this lane's octet in memory
         const bool mine = f.ids >= 0;
@@ -485,10 +531,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
             copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, mine ? src + (2 << a.pg.shift) : a.pg.base, mine);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        if (++to_fill == S::STAGES) to_fill = 0;
+        if (++to_fill == stages) to_fill = 0;
         ahead++;
         f.more--;
-        f.tok += kAttWarps * TT;
+        f.tok += turns * TT;
     };
 
     // What this lane reads of a tile: piece c of row r of K, piece r of rows 2 c and 2 c + 1 of V;
@@ -500,7 +546,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
     auto heads_of = [&](const Piece &x) { return min(HT, a.groups - x.vh % chunks * HT); };
     fetch_from(p);
     // A warp's part of a piece goes through the stage of its ring that was read last.
-    auto stage_of = [&](int x, int stage) { return smem + (x * S::STAGES + stage) * S::TILE; };
+    auto stage_of = [&](int x, int stage) { return smem + S::OFF_RING + (x * stages + stage) * S::TILE; };
     struct {
         int b, h0, nh;
         bool all;                                            // the piece is its whole sequence
@@ -529,21 +575,35 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
         Queries<S> qs;
         qs.load(a, p.b, first_head(p), p.n > 0 ? heads_of(p) : 0, w, l);
         if (!first) {
-            __syncthreads();                                 // the warps' parts of the piece before
-            for (int i = tid; i < out.nh * (D / 4); i += 32 * kAttWarps) {
+            // the warps' parts of the piece before
+            if (ctas > 1) cluster_sync();
+            else __syncthreads();
+            for (int i = tid + rank * 32 * kAttWarps; i < out.nh * (D / 4); i += 32 * turns) {
                 const int h = i / (D / 4), d = 4 * (i % (D / 4));
                 float top = kLow, total = 0.f, o[4] = {};
+#pragma unroll 2
+                for (int z = 0; z < ctas; z++) {
+                    const float *rl = ctas > 1 ? in_cluster(sums, z) : sums;
+                    const int *stage = ctas > 1 ? in_cluster((const int *)scan, z) : (const int *)scan;
+                    float up = top;
 #pragma unroll
-                for (int x = 0; x < kAttWarps; x++) top = fmaxf(top, sums[2 * x * HT + h]);
+                    for (int x = 0; x < kAttWarps; x++) up = fmaxf(up, rl[2 * x * HT + h]);
+                    const float old = exp2_fast(top - up);
+                    top = up;
+                    total *= old;
 #pragma unroll
-                for (int x = 0; x < kAttWarps; x++) {
-                    const float k = exp2_fast(sums[2 * x * HT + h] - top);
-                    const float4 v = *(const float4 *)((const float *)stage_of(x, ((const int *)scan)[x]) + h * D + d);
-                    total = fmaf(k, sums[(2 * x + 1) * HT + h], total);
-                    o[0] = fmaf(k, v.x, o[0]);
-                    o[1] = fmaf(k, v.y, o[1]);
-                    o[2] = fmaf(k, v.z, o[2]);
-                    o[3] = fmaf(k, v.w, o[3]);
+                    for (int e = 0; e < 4; e++) o[e] *= old;
+#pragma unroll
+                    for (int x = 0; x < kAttWarps; x++) {
+                        const float k = exp2_fast(rl[2 * x * HT + h] - top);
+                        const float *part = (const float *)stage_of(x, stage[x]) + h * D + d;
+                        const float4 v = *(const float4 *)(ctas > 1 ? in_cluster(part, z) : part);
+                        total = fmaf(k, rl[(2 * x + 1) * HT + h], total);
+                        o[0] = fmaf(k, v.x, o[0]);
+                        o[1] = fmaf(k, v.y, o[1]);
+                        o[2] = fmaf(k, v.z, o[2]);
+                        o[3] = fmaf(k, v.w, o[3]);
+                    }
                 }
                 if (out.all) {
                     put_output(a, out.b, out.h0 + h, d, top, total, o, D);
@@ -556,6 +616,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
                 }
             }
         }
+        if (ctas > 1 && !first) cluster_sync();              // the others have read this CTA's
         if (p.n == 0) break;
         qs.put(a, smem, w, l);
         __syncthreads();                                     // the queries are there, the parts before have been read
@@ -569,10 +630,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
             else if (j.count) joined[blockIdx.x] = j;
         }
         past += p.n;
-        const int count = count_of(p), tok_first = (p.tile0 + p.from + w) * TT;
+        const int count = count_of(p), tok_first = (p.tile0 + p.from + turn) * TT;
 
         float hf[NT][2], ho[NT][2], R[NT][2], sum[NT][2], O[NT][S::MT][4];
-        const uint2 *qf = (const uint2 *)(smem + S::OFF_Q);
+        const uint2 *qf = (const uint2 *)smem;
         uint2 qr[S::QREG ? S::QT : 1][S::QREG ? NT : 1][S::QREG ? S::KS : 1];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
@@ -599,30 +660,31 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
 
         for (int i = 0;; i++) {
             __syncwarp();                                    // all have read the tile before
-            fill(i < count ? S::STAGES : S::STAGES - 1);
+            fill(i < count ? stages : stages - 1);
             if (i == count) break;
             // the copies of this tile have landed once no more than those behind it are open
-            if (ahead == S::STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 1) : "memory");
-            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            wait_but(ahead - 1);
             __syncwarp();
             const uint8_t *st = stage_of(w, to_read);
-            if (++to_read == S::STAGES) to_read = 0;
+            if (++to_read == stages) to_read = 0;
             ahead--;
             constexpr int G = S::ST / 16;
 #pragma unroll 1
             for (int sub = 0; sub < TT; sub += S::ST) {
-                const int tok0 = tok_first + i * kAttWarps * TT + sub;
+                const int tok0 = tok_first + i * turns * TT + sub;
                 const bool edge = tok0 < p.lo || tok0 + S::ST > p.hi;
                 const uint8_t *rows = st + sub * RB;
 
                 // scores, tokens 16 g + r and + 8 by heads 2 c and 2 c + 1
+                // (sums of even and odd steps apart: a step waits for half as many)
                 float s[NT][G][4];
 #pragma unroll
                 for (int g = 0; g < G; g++) {
+                    float odd[NT][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) s[nt][g][e] = 0.f;
+                        for (int e = 0; e < 4; e++) s[nt][g][e] = odd[nt][e] = 0.f;
                     constexpr int NP = RB / (4 * S::KP), JP = S::KP * 4 / bits_of(F);    // pieces, pairs of each
 #pragma unroll
                     for (int x = 0; x < NP; x++) {
@@ -641,10 +703,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
                                     uint2 v;
                                     if constexpr (S::QREG) v = qr[t][nt][ks];
                                     else v = qf[((t * NT + nt) * S::KS + ks) * 32 + l];
-                                    mma<C>(s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
+                                    mma<C>(ks & 1 ? odd[nt] : s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
                                 }
                         }
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) s[nt][g][e] += odd[nt][e];
                 }
                 // base-2 exponents (x - ho) hk; masked ones are -inf
                 float sv[G][2], hk[NT][G][4];
@@ -768,7 +834,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::RESIDENT) kv_attend_kernel(
         }
 
         __syncwarp();
-        const int stage = to_read == 0 ? S::STAGES - 1 : to_read - 1;
+        const int stage = to_read == 0 ? stages - 1 : to_read - 1;
         float *mine = (float *)stage_of(w, stage);
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)

@@ -32,22 +32,40 @@ auto by_shape(int head_dim, int groups, bool wide, Fn &&f) {
                              : heads(std::integral_constant<int, 256>{});
 }
 
-// CTAs of a call, from what the host knows: its rows and the most tokens that one has. `whole`:
-// each takes whole sequences. Fewer tokens never need more CTAs, so a workspace for `most` serves
-// every call below it.
-struct Grid { int ctas; bool whole; };
+// CTAs of a call, from what the host knows: its rows and the most tokens that one has. cluster > 0:
+// clusters of that many take whole sequences. A warp then has up to kWholeTiles tiles, however short
+// the others' sequences are; beyond that equal shares are worth the parts and the second kernel. Shorter
+// sequences never need more CTAs for shares, so a workspace for `most` serves every call below it.
+#ifndef KV_WT
+#define KV_WT 8
+#endif
+constexpr int kWholeTiles = KV_WT;
+struct Grid { int ctas, cluster, stages; };
 template <class S>
 Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
-    const int64_t tiles = (most + S::TT - 1) / S::TT;
+    const int64_t tiles = (most + S::TT - 1) / S::TT, sms = sm_count();
     const int64_t heads = rows * c->n_heads * ((groups + S::HT - 1) / S::HT);
-    const int64_t resident = (int64_t)sm_count() * S::RESIDENT;
-    if (tiles <= 2 * kAttWarps) return {(int)(heads < 8 * resident ? heads : 8 * resident), true};
-    const int64_t ctas = (heads * tiles + 2 * kAttWarps - 1) / (2 * kAttWarps);
-    return {(int)(ctas < resident ? ctas : resident), false};
+    const int64_t resident = sms * S::resident(S::STAGES);
+    int cluster = 1;                                         // as many as find places and two tiles a warp
+    while (cluster < 8 && 2 * cluster * heads <= resident && tiles > 2 * kAttWarps * cluster) cluster *= 2;
+    const bool whole = tiles <= kWholeTiles * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
+    Grid g{0, whole ? cluster : 0, S::STAGES};
+    if (whole) {
+        g.ctas = (int)(heads < 8 * resident ? heads : 8 * resident) * cluster;
+    } else {
+        const int64_t ctas = (heads * tiles + 2 * kAttWarps - 1) / (2 * kAttWarps);
+        g.ctas = (int)(ctas < resident ? ctas : resident);
+    }
+    // Where the CTAs leave room, longer rings; where a warp has fewer tiles than stages, shorter
+    // ones that let more CTAs in.
+    const int64_t each = whole ? (tiles + kAttWarps * cluster - 1) / (kAttWarps * cluster) : kMostStages;
+    while (g.stages < kMostStages && g.stages < each && S::resident(g.stages + 1) * sms >= g.ctas) g.stages++;
+    if (g.stages > each) g.stages = (int)each;
+    return g;
 }
 template <class S>
 size_t parts_bytes(const Grid &g) {
-    if (g.whole) return 0;
+    if (g.cluster) return 0;
     return (size_t)g.ctas * (2 * sizeof(float) * part_floats<S::HT, S::D>() + sizeof(Joined));
 }
 
@@ -71,11 +89,12 @@ stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int
         AttendArgs a = args;
         if (a.window > 0 && a.window + S::TT < most) most = a.window + S::TT;      // a window ends inside a tile
         const Grid g = grid_of<S>(c, a.groups, a.B, most);
-        a.whole = g.whole;
-        stepq_status st = opt((const void *)kv_attend_kernel<S>, S::SMEM);
+        a.whole = g.cluster;
+        a.stages = g.stages;
+        stepq_status st = opt((const void *)kv_attend_kernel<S>, kSmemMax);
         if (st != STEPQ_OK) return st;
-        st = launch_overlapped(kv_attend_kernel<S>, g.ctas, 32 * kAttWarps, S::SMEM, s, a);
-        if (st != STEPQ_OK || g.whole) return st;
+        st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
+        if (st != STEPQ_OK || g.cluster) return st;
         const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
         return launch_overlapped(kv_join_kernel<S::HT, S::D>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
                                  32 * kJoinWarps, 0, s, a, g.ctas);

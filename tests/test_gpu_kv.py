@@ -518,11 +518,11 @@ def test_binding_refuses_layouts():
     attend = lambda **kw: A.stepq_kv_attend(**{**dict(kv=kv, layer=0, pages=pages, table=table, lens=n, q=q, y=q.clone()), **kw})  # noqa: E731
     append()
     attend()
-    for call, kw, say in ((append, dict(v=k.float()), "v: expected torch.bfloat16"), (append, dict(k=k.cpu()), "k: expected a CUDA"),
+    for call, kw, say in ((append, dict(v=k.float()), "v: expected BFloat16"), (append, dict(k=k.cpu()), "k: expected a CUDA"),
                           (append, dict(k=z(3, 2, 64)), "k: expected"), (append, dict(k=z(3, 2, 256)[:, :, ::2]), "k: expected"),
                           (append, dict(v=z(4, 2, 128)), "v: expected"), (append, dict(k=z(3, 2, 128, dt=torch.float64), v=z(3, 2, 128, dt=torch.float64)), "float32, bfloat16"),
                           (append, dict(table=table.long()), "table"), (append, dict(table=z(3, 4, dt=torch.int32)[:, ::2]), "table"),
-                          (append, dict(table=z(2, 2, dt=torch.int32)), "table: expected 3"), (append, dict(starts=n.long()), "starts: expected contiguous int32"),
+                          (append, dict(table=z(2, 2, dt=torch.int32)), "table: expected 3"), (append, dict(starts=n.long()), "starts: expected contiguous int32"), (attend, dict(workspace=pages[::2]), "workspace"),
                           (append, dict(pages=pages[::2]), "contiguous"), (attend, dict(y=q.float()), "y: expected"),
                           (attend, dict(y=z(3, 2, 128)), "y: expected"), (attend, dict(q=z(2, 4, 128)), "q: expected"),
                           (attend, dict(lse=z(3, 4)), "float32"), (attend, dict(lse=z(3, 2, dt=torch.float32)), "lse: expected 12")):

@@ -102,13 +102,7 @@ def test_page_bytes():
     assert all(n(**kw) == 0 for kw, _ in BAD_CONFIG)
 
 
-def test_packed_structures_are_the_declared_ones():
-    assert bytes(_lib.StepqKvPages(1, 2, 3, 4, 5)) == A._pack_pages(1, 2, 3, 4, 5)
-    assert bytes(_lib.StepqKvRows(1, 2, 3, 4, 5)) == A._pack_rows(1, 2, 3, 4, 5)
-    assert bytes(_lib.StepqKvQuery(1, 2, 3, 4, 5, 6, 7, 0.5, 9, 10)) == A._pack_query(1, 2, 3, 4, 5, 6, 7, 0.5, 9, 10)
-
-
-def test_kept_configurations_follow_the_fields():
+def test_configurations_follow_the_fields():
     kv = A.KvConfig(1, 2)
     before = A.stepq_kv_page_bytes(kv)
     kv.n_layers = 3
@@ -121,12 +115,20 @@ def test_binding_refuses_cpu_tensors_and_shapes():
     torch = pytest.importorskip("torch")
     kv, pg, t = A.KvConfig(1, 4), torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(2, 8, dtype=torch.int32)
     n, x = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 4, 128)
-    with pytest.raises(ValueError, match="table: expected rows"):
+    with pytest.raises(ValueError, match="table: expected a CUDA tensor"):
         A.stepq_kv_append(kv, 0, pg, t, n, x, x)
     with pytest.raises(ValueError, match="table: expected 3 rows"):
         A.stepq_kv_attend(kv, 0, pg, t, torch.zeros(3, dtype=torch.int32), x, x)
     with pytest.raises(ValueError, match="cu_seqlens: expected 3"):
         A.stepq_kv_read(kv, 0, pg, t, n, x, x, cu_seqlens=n)
+    with pytest.raises(ValueError, match="starts: expected a tensor"):
+        A.stepq_kv_read(kv, 0, pg, t, [0, 0], x, x)
+    with pytest.raises(ValueError, match="n_layers: .* does not fit"):
+        A.stepq_kv_read(A.KvConfig(1 << 40, 4), 0, pg, t, n, x, x)
+    with pytest.raises(TypeError):
+        A.stepq_kv_read(A.KvConfig("1", 4), 0, pg, t, n, x, x)
+    with pytest.raises(AttributeError):
+        A.stepq_kv_read(None, 0, pg, t, n, x, x)
 
 
 @pytest.fixture(scope="module")

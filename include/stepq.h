@@ -388,7 +388,7 @@ typedef struct {
     int format;              /* STEPQ_KV_* */
 } stepq_kv_config;
 
-/* Bytes of a page (0 if the configuration is invalid). A page holds page_tokens tokens of
+/* Bytes of a page, below 2^32 (0 if the configuration is invalid or its pages are larger). A page holds page_tokens tokens of
  * every layer and head, ordered (layer, head):
  *   K rows [page_tokens] | V rows [page_tokens] | for codes: fp16 scales of K [page_tokens] | of V
  * A row is its D channels: 2 bytes each, 1 byte (8-bit codes) or half a byte (4-bit codes,

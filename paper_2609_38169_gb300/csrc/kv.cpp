@@ -12,6 +12,11 @@ bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
 
 int row_bits(int format) { return format == STEPQ_KV_INT4 ? 4 : format == STEPQ_KV_INT8 ? 8 : 16; }
 
+size_t page_bytes(const stepq_kv_config *c) {
+    const size_t row = (size_t)c->head_dim * row_bits(c->format) / 8;
+    return (size_t)c->n_layers * c->n_heads * c->page_tokens * (2 * row + (row_bits(c->format) < 16 ? 4 : 0));
+}
+
 stepq_status check_config(const stepq_kv_config *c) {
     if (!c || c->n_layers < 1 || c->n_heads < 1 || c->format < STEPQ_KV_BF16 || c->format > STEPQ_KV_INT4 ||
         c->n_heads > (1 << 14) || c->n_layers > (1 << 16))
@@ -19,7 +24,7 @@ stepq_status check_config(const stepq_kv_config *c) {
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return STEPQ_ERR_UNSUPPORTED;
     if (c->page_tokens < 8 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1)))
         return STEPQ_ERR_UNSUPPORTED;
-    return STEPQ_OK;
+    return page_bytes(c) < (1ull << 32) ? STEPQ_OK : STEPQ_ERR_UNSUPPORTED;
 }
 
 stepq_status check_pages(const stepq_kv_config *c, int layer, const stepq_kv_pages *p, int B) {
@@ -60,11 +65,7 @@ bool heads_fit(const stepq_kv_config *c, int q_heads, int B) {
 
 }  // namespace
 
-extern "C" size_t stepq_kv_page_bytes(const stepq_kv_config *c) {
-    if (check_config(c) != STEPQ_OK) return 0;
-    const size_t row = (size_t)c->head_dim * row_bits(c->format) / 8;
-    return (size_t)c->n_layers * c->n_heads * c->page_tokens * (2 * row + (row_bits(c->format) < 16 ? 4 : 0));
-}
+extern "C" size_t stepq_kv_page_bytes(const stepq_kv_config *c) { return check_config(c) == STEPQ_OK ? page_bytes(c) : 0; }
 
 extern "C" stepq_status stepq_kv_append(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
                                         const int32_t *starts, const int32_t *cu_seqlens, int B, int tokens,

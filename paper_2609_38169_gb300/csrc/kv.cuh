@@ -19,7 +19,7 @@ __host__ __device__ constexpr bool coded(int format) { return bits_of(format) < 
 // One layer of the pages.
 struct Pages {
     uint8_t *base;                  // of the layer in page 0
-    uint64_t page_bytes;
+    uint32_t page_bytes;
     uint32_t segment;               // bytes of one head's part of a page
     int n_pages, shift;             // page_tokens = 1 << shift
     const int32_t *table;
@@ -30,14 +30,14 @@ struct Pages {
 
     __device__ __forceinline__ int slot(int token) const { return token & ((1 << shift) - 1); }
     __device__ __forceinline__ uint8_t *at(int page, int head) const {
-        return base + (uint64_t)page * page_bytes + (uint64_t)head * segment;
+        return base + (uint64_t)(uint32_t)page * page_bytes + (uint64_t)head * segment;
     }
 };
 
 inline Pages pages_of(const stepq_kv_config *c, int layer, const stepq_kv_pages *p) {
     Pages g{};
     g.segment = (uint32_t)c->page_tokens * (2 * row_bytes(c->format, c->head_dim) + (coded(c->format) ? 4 : 0));
-    g.page_bytes = (uint64_t)g.segment * c->n_heads * c->n_layers;
+    g.page_bytes = g.segment * (uint32_t)(c->n_heads * c->n_layers);
     g.base = (uint8_t *)p->pages + (uint64_t)g.segment * c->n_heads * layer;
     g.n_pages = p->n_pages;
     while ((1 << g.shift) < c->page_tokens) g.shift++;

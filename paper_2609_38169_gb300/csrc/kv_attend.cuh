@@ -143,25 +143,23 @@ template <int BYTES>
 __device__ __forceinline__ Words<BYTES / 4> lds(const uint8_t *tile, uint32_t at) {
     return *(const Words<BYTES / 4> *)(tile + at);
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// Pages pass through L2 once a call: what else lies there stays (measured with the usual order of
+// eviction: 200,003 tokens of 2 x 256 channels 75 us, now 71; 524,288 of 8 x 128 in 8 bits 185, 181).
+__device__ __forceinline__ uint64_t streaming() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool valid) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
 
-// This thread's groups of copies have landed, but for the newest n < kMostStages.
-constexpr int kMostStages = 6;
-__device__ __forceinline__ void wait_but(int n) {
-    switch (n) {
-    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-    case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-    default: asm volatile("cp.async.wait_group 5;" ::: "memory");
-    }
-}
+// This thread's groups of copies have landed, but for the newest N.
+template <int N>
+__device__ __forceinline__ void wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Place of byte `at` (row * RB + byte) of a tile's rows: 16-byte pieces change places within 128
 // bytes so that the lanes that read at once meet no bank twice. They read 64 bytes each of
@@ -381,7 +379,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
 
     // Calls for whole sequences: the CTAs of a cluster take a sequence's tiles in turn.
     const int ctas = a.whole ? (int)cluster_size() : 1, rank = a.whole ? (int)cluster_rank() : 0;
-    const int stages = a.stages;
+    const int stages = a.stages;                             // S::STAGES, or 1 where no warp has more tiles
     const int turn = rank * kAttWarps + w, turns = ctas * kAttWarps;
 
     // The share: `left` tiles of all, in the order (sequence, virtual head, tile), from tile `from`
@@ -465,20 +463,25 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     // This warp's tiles of a piece: from + turn, from + turn + turns, ... below from + n.
     auto count_of = [&](const Piece &p) { return p.n > turn ? (p.n - turn + turns - 1) / turns : 0; };
 
-    // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the page of
-    // octet l (eight tokens) of that tile, -1 for none.
+    // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the pages of
+    // that tile's octets (eight tokens), -1 where no token counts. A page that holds a whole
+    // tile is looked up once.
     struct {
         const int32_t *table;
         uint64_t head;
-        int tok, more, lo, hi, ids;
-    } f;
+        int tok, more, lo, hi, ids[TT / 8];
+    } f{};
+    const bool one_page = (1 << a.pg.shift) >= TT;
     auto load_ids = [&]() {
-        f.ids = -1;
-        const int tok = f.tok + 8 * l;
-        if (l >= TT / 8 || f.more == 0 || tok >= f.hi || tok + 8 <= f.lo) return;
-        const int id = f.table[tok >> a.pg.shift];
-        if (id >= 0 && id < a.pg.n_pages) f.ids = id;
-        else raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+        if (one_page) {
+            f.ids[0] = f.more > 0 && f.hi > 0 ? f.table[f.tok >> a.pg.shift] : -1;
+        } else {
+#pragma unroll
+            for (int o = 0; o < TT / 8; o++) {
+                const int tok = f.tok + 8 * o;
+                f.ids[o] = f.more > 0 && tok < f.hi && tok + 8 > f.lo ? f.table[tok >> a.pg.shift] : -1;
+            }
+        }
     };
     auto fetch_from = [&](const Piece &p) {
         f.table = a.pg.table + p.b * a.pg.table_stride;
@@ -489,46 +492,60 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         f.hi = p.hi;
         load_ids();
     };
+    const uint32_t ring = smem_addr(smem) + S::OFF_RING + w * stages * S::TILE;
+    const uint8_t *ring_at = smem + S::OFF_RING + w * stages * S::TILE;
     // Stages are taken in turn: to_fill the next that copies go to, to_read the next that is read.
     int to_fill = 0, to_read = 0, ahead = 0;                 // ahead: tiles copied and not yet read
     // A step copies 512 bytes of rows, 16 a lane: the change of place within 128 bytes is that of the
     // lane's part of the offset and, apart from it, that of the step's.
     const uint32_t k_lane = k_place<RB>(16 * l / RB, 16 * l % RB), v_lane = v_place<RB>(16 * l / RB, 16 * l % RB);
+    const uint64_t policy = streaming();
     auto copy_tile = [&]() {
-        const uint32_t dst = smem_addr(smem) + S::OFF_RING + (w * stages + to_fill) * S::TILE;
-        constexpr int N = TT * RB / 512, PER = RB >= 64 ? RB / 64 : 1;       // steps, and steps of an octet
-        // this lane's octet in memory
-        const bool mine = f.ids >= 0;
-        const uint8_t *oct = a.pg.base + f.head + (mine ? (uint64_t)f.ids * a.pg.page_bytes + a.pg.slot(f.tok + 8 * l) * RB : 0);
-        const uint32_t to_v = RB << a.pg.shift;
-        if (f.tok >= f.lo && f.tok + TT <= f.hi && __all_sync(0xffffffffu, mine || l >= TT / 8)) {
+        const uint32_t dst = ring + to_fill * S::TILE, to_v = RB << a.pg.shift;
+        constexpr int N = TT * RB / 512;                     // steps
+        const uint8_t *layer = a.pg.base + f.head;
+        const int slot = a.pg.slot(f.tok);
+        if (one_page && f.tok >= f.lo && f.tok + TT <= f.hi && (uint32_t)f.ids[0] < (uint32_t)a.pg.n_pages) {
+            const uint8_t *page = layer + (uint64_t)(uint32_t)f.ids[0] * a.pg.page_bytes;
+            const uint8_t *k = page + (slot * RB + 16 * l), *v = k + to_v;
 #pragma unroll
-            for (int j0 = 0; j0 < N; j0 += PER) {
-                const uint8_t *k = (const uint8_t *)__shfl_sync(0xffffffffu, (unsigned long long)oct, (512 * j0 + 16 * l) / (8 * RB)) +
-                                   16 * l % (8 * RB);
-                const uint8_t *v = k + to_v;
-#pragma unroll
-                for (int x = 0; x < PER; x++) {
-                    const int j = j0 + x;
-                    const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
-                    copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * x);
-                    copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * x);
-                }
+            for (int j = 0; j < N; j++) {
+                const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
+                copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * j, policy);
+                copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * j, policy);
+            }
+            if (S::CODED && l < TT / 4) {                    // K's scales, then V's
+                const bool is_v = l >= TT / 8;
+                copy16(dst + 2 * TT * RB + 16 * l, page + 2 * to_v + 2 * slot + 16 * (l & (TT / 8 - 1)) + (is_v ? 2 << a.pg.shift : 0), policy);
             }
         } else {
-#pragma unroll 1
+            // tiles of several pages; rows that are no tokens, or in no page, become zeros
+#pragma unroll
+            for (int o = 0; o < TT / 8; o++) {
+                if (one_page && o > 0) f.ids[o] = f.ids[0];
+                if ((uint32_t)f.ids[o] >= (uint32_t)a.pg.n_pages) {
+                    if (l == 0 && f.tok + 8 * o < f.hi && f.tok + 8 * o + 8 > f.lo) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+                    f.ids[o] = -1;
+                }
+            }
+#pragma unroll
             for (int j = 0; j < N; j++) {
                 const int at = 512 * j + 16 * l, row = at / RB, byte = at % RB, tok = f.tok + row;
-                const uint8_t *src = (const uint8_t *)__shfl_sync(0xffffffffu, (unsigned long long)oct, row / 8) + at % (8 * RB);
-                const bool ok = __shfl_sync(0xffffffffu, f.ids, row / 8) >= 0 && tok >= f.lo && tok < f.hi;
-                copy16(dst + k_place<RB>(row, byte), ok ? src : a.pg.base, ok);
-                copy16(dst + TT * RB + v_place<RB>(row, byte), ok ? src + to_v : a.pg.base, ok);
+                const int o = 512 * j / (8 * RB), id = RB < 64 && l >= 16 ? f.ids[o + (RB < 64)] : f.ids[o];
+                const bool ok = id >= 0 && tok >= f.lo && tok < f.hi;
+                const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + a.pg.slot(tok) * RB + byte : a.pg.base;
+                copy16(dst + k_place<RB>(row, byte), src, ok);
+                copy16(dst + TT * RB + v_place<RB>(row, byte), src + (ok ? to_v : 0), ok);
             }
-        }
-        if (S::CODED && l < TT / 8) {
-            const uint8_t *src = oct + 2 * to_v - a.pg.slot(f.tok + 8 * l) * (RB - 2);
-            copy16(dst + 2 * TT * RB + 16 * l, mine ? src : a.pg.base, mine);
-            copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, mine ? src + (2 << a.pg.shift) : a.pg.base, mine);
+            if (S::CODED && l < TT / 8) {
+                int id = f.ids[0];
+#pragma unroll
+                for (int o = 1; o < TT / 8; o++) id = l == o ? f.ids[o] : id;
+                const bool ok = id >= 0;
+                const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + 2 * to_v + 2 * a.pg.slot(f.tok + 8 * l) : a.pg.base;
+                copy16(dst + 2 * TT * RB + 16 * l, src, ok);
+                copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, src + (ok ? 2 << a.pg.shift : 0), ok);
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (++to_fill == stages) to_fill = 0;
@@ -558,20 +575,6 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     for (;; first = false) {
         const Piece q = p.n > 0 ? next_piece() : p;
         bool rest = p.n > 0 && q.n > 0;                      // q's tiles are not looked at yet
-        // Copies up to `most` tiles ahead, on into q's.
-        auto fill = [&](int most) {
-            for (;;) {
-                if (f.more == 0) {
-                    if (!rest) return;
-                    fetch_from(q);
-                    rest = false;
-                    if (f.more == 0) return;
-                }
-                if (ahead >= most) return;
-                copy_tile();
-                if (f.more > 0) load_ids();
-            }
-        };
         Queries<S> qs;
         qs.load(a, p.b, first_head(p), p.n > 0 ? heads_of(p) : 0, w, l);
         if (!first) {
@@ -658,14 +661,30 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                     for (int ks = 0; ks < S::KS; ks++) qr[i][nt][ks] = qf[((i * NT + nt) * S::KS + ks) * 32 + l];
         }
 
-        for (int i = 0;; i++) {
+        // Before the first tile is read all stages but one are on their way, those behind p's last
+        // with q's tiles; then one more a tile.
+        if (f.more == 0 && rest) {
+            fetch_from(q);
+            rest = false;
+        }
+        for (int i = min(0, ahead - (stages - 1));; i++) {
             __syncwarp();                                    // all have read the tile before
-            fill(i < count ? stages : stages - 1);
+            if (f.more > 0 && ahead < (i >= 0 && i < count ? stages : stages - 1)) {
+                copy_tile();
+                if (f.more == 0 && rest) {
+                    fetch_from(q);
+                    rest = false;
+                } else {
+                    load_ids();
+                }
+            }
+            if (i < 0) continue;
             if (i == count) break;
             // the copies of this tile have landed once no more than those behind it are open
-            wait_but(ahead - 1);
+            if (ahead == S::STAGES) wait_but<S::STAGES - 1>();
+            else wait_but<0>();
             __syncwarp();
-            const uint8_t *st = stage_of(w, to_read);
+            const uint8_t *st = ring_at + to_read * S::TILE;
             if (++to_read == stages) to_read = 0;
             ahead--;
             constexpr int G = S::ST / 16;
@@ -676,15 +695,13 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 const uint8_t *rows = st + sub * RB;
 
                 // scores, tokens 16 g + r and + 8 by heads 2 c and 2 c + 1
-                // (sums of even and odd steps apart: a step waits for half as many)
                 float s[NT][G][4];
 #pragma unroll
                 for (int g = 0; g < G; g++) {
-                    float odd[NT][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) s[nt][g][e] = odd[nt][e] = 0.f;
+                        for (int e = 0; e < 4; e++) s[nt][g][e] = 0.f;
                     constexpr int NP = RB / (4 * S::KP), JP = S::KP * 4 / bits_of(F);    // pieces, pairs of each
 #pragma unroll
                     for (int x = 0; x < NP; x++) {
@@ -703,14 +720,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                                     uint2 v;
                                     if constexpr (S::QREG) v = qr[t][nt][ks];
                                     else v = qf[((t * NT + nt) * S::KS + ks) * 32 + l];
-                                    mma<C>(ks & 1 ? odd[nt] : s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
+                                    mma<C>(s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
                                 }
                         }
                     }
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++) s[nt][g][e] += odd[nt][e];
                 }
                 // base-2 exponents (x - ho) hk; masked ones are -inf
                 float sv[G][2], hk[NT][G][4];

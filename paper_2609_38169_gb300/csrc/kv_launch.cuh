@@ -56,11 +56,8 @@ Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
         const int64_t ctas = (heads * tiles + 2 * kAttWarps - 1) / (2 * kAttWarps);
         g.ctas = (int)(ctas < resident ? ctas : resident);
     }
-    // Where the CTAs leave room, longer rings; where a warp has fewer tiles than stages, shorter
-    // ones that let more CTAs in.
-    const int64_t each = whole ? (tiles + kAttWarps * cluster - 1) / (kAttWarps * cluster) : kMostStages;
-    while (g.stages < kMostStages && g.stages < each && S::resident(g.stages + 1) * sms >= g.ctas) g.stages++;
-    if (g.stages > each) g.stages = (int)each;
+    // a warp with one tile needs one stage, which lets more CTAs in
+    if (whole && tiles <= kAttWarps * cluster) g.stages = 1;
     return g;
 }
 template <class S>

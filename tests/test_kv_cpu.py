@@ -41,7 +41,8 @@ def attend(c=None, layer=0, p=None, lens=P, B=2, q=None, ws=P, nbytes=1 << 30):
 
 BAD_CONFIG = [(dict(n_layers=0), ARG), (dict(n_heads=0), ARG), (dict(format=4), ARG), (dict(format=-1), ARG),
               (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=512), UNSUPPORTED), (dict(page_tokens=4), UNSUPPORTED),
-              (dict(page_tokens=24), UNSUPPORTED), (dict(page_tokens=512), UNSUPPORTED), (dict(n_heads=1 << 20), ARG)]
+              (dict(page_tokens=24), UNSUPPORTED), (dict(page_tokens=512), UNSUPPORTED), (dict(n_heads=1 << 20), ARG),
+              (dict(n_layers=1 << 12, n_heads=1 << 9), UNSUPPORTED)]
 BAD_PAGES = [(dict(pages=None), ARG), (dict(n_pages=0), ARG), (dict(table_width=-1), ARG), (dict(table_stride=-1), ARG),
              (dict(table=None), ARG), (dict(table_width=(1 << 26) + 1), ARG), (dict(pages=P + 8), ALIGN), (dict(table=P + 2), ALIGN)]
 

@@ -23,7 +23,9 @@
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
 // row and the queries are laid out to match. Codes u enter K's product as the fp16 subnormal
 // u 2^-24 (a mask or a byte permute), its offset 2^(b-1) sum q is subtracted from the sum; for V,
-// where that would cancel over all tokens, u - 2^(b-1) is formed first, exactly.
+// where that would cancel over all tokens, u - 2^(b-1) is formed first, exactly. (A product with the
+// offset behind each with codes saves a tenth of the instructions and no time, and costs fp32
+// outputs two bits.)
 //
 // Roundings: q enters as a sum of QT terms of the cache's 16-bit type, weights as a sum of PT,
 // everything between in fp32. One term of fp16 has 2^-12, half of bf16's eighth of a unit, two
@@ -133,11 +135,6 @@ __device__ __forceinline__ float2 unpack(uint32_t v, la::bf16) {
 __device__ __forceinline__ float2 unpack(uint32_t v, la::f16) {
     return __half22float2(*(const __half2 *)&v);
 }
-__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 template <int N> struct alignas(4 * N) Words { uint32_t w[N]; };
 template <int BYTES>
 __device__ __forceinline__ Words<BYTES / 4> lds(const uint8_t *tile, uint32_t at) {
@@ -163,14 +160,14 @@ __device__ __forceinline__ void wait_but() { asm volatile("cp.async.wait_group %
 
 // Place of byte `at` (row * RB + byte) of a tile's rows: 16-byte pieces change places within 128
 // bytes so that the lanes that read at once meet no bank twice. They read 64 bytes each of
-// rows r and r + 1 (K), or up to 32 of rows r, r + 2, r + 4 and r + 6 (V).
+// rows r and r + 1 (K), of V 16 of eight rows (16 bits) or up to 32 of rows r, r + 2, r + 4 and r + 6.
 template <int RB>
 __device__ __forceinline__ uint32_t k_place(int row, int byte) {
     return (uint32_t)(row * RB + byte) ^ (RB >= 128 ? (row & 1) << 6 : 0);
 }
-template <int RB>
+template <int F, int RB>
 __device__ __forceinline__ uint32_t v_place(int row, int byte) {
-    return (uint32_t)(row * RB + byte) ^ (RB >= 64 ? ((row >> 1) & 3) << 5 : ((row >> 2) & 1) << 5);
+    return (uint32_t)(row * RB + byte) ^ (!coded(F) ? (row & 7) << 4 : RB >= 64 ? ((row >> 1) & 3) << 5 : ((row >> 2) & 1) << 5);
 }
 
 // A lane's piece of a row of K as pairs of the compute type, in the order that Queries::put() gives the queries.
@@ -192,30 +189,38 @@ __device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 
         }
     }
 }
-// A lane's pieces of two tokens' rows of V as pairs of tokens, p[channel]: one 2^-24 of the code
+// Four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 i .. 8 i + 7 give the rows of matrix i.
+__device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
+}
+// A lane's pieces of two tokens' rows of V as pairs of tokens, p[channel]: 2^-24 of the code
 // without its offset, and for the odd channels of 4 bits 2^-20.
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 template <int F, int N>
 __device__ __forceinline__ void v_pairs(const Words<N> &a, const Words<N> &b, uint32_t (&p)[N * 32 / bits_of(F)]) {
+    constexpr uint32_t m128 = 0x80808080u, m8 = 0x80088008u;
 #pragma unroll
     for (int i = 0; i < N; i++) {
         if constexpr (F == STEPQ_KV_INT8) {
             const uint32_t lo = __byte_perm(a.w[i], b.w[i], 0x5140), hi = __byte_perm(a.w[i], b.w[i], 0x7362);
-            p[4 * i] = hadd2(__byte_perm(lo, 0u, 0x4140), 0x80808080u);
-            p[4 * i + 1] = hadd2(__byte_perm(lo, 0u, 0x4342), 0x80808080u);
-            p[4 * i + 2] = hadd2(__byte_perm(hi, 0u, 0x4140), 0x80808080u);
-            p[4 * i + 3] = hadd2(__byte_perm(hi, 0u, 0x4342), 0x80808080u);
-        } else if constexpr (F == STEPQ_KV_INT4) {
+            p[4 * i] = hadd2(__byte_perm(lo, 0u, 0x4140), m128);
+            p[4 * i + 1] = hadd2(__byte_perm(lo, 0u, 0x4342), m128);
+            p[4 * i + 2] = hadd2(__byte_perm(hi, 0u, 0x4140), m128);
+            p[4 * i + 3] = hadd2(__byte_perm(hi, 0u, 0x4342), m128);
+        } else {
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const uint32_t x = __byte_perm(a.w[i], b.w[i], h ? 0x7632 : 0x5410), y = x >> 8;
-                p[8 * i + 4 * h] = hadd2(x & 0x000f000fu, 0x80088008u);
-                p[8 * i + 4 * h + 1] = hadd2(x & 0x00f000f0u, 0x80808080u);
-                p[8 * i + 4 * h + 2] = hadd2(y & 0x000f000fu, 0x80088008u);
-                p[8 * i + 4 * h + 3] = hadd2(y & 0x00f000f0u, 0x80808080u);
+                p[8 * i + 4 * h] = hadd2(x & 0x000f000fu, m8);
+                p[8 * i + 4 * h + 1] = hadd2(x & 0x00f000f0u, m128);
+                p[8 * i + 4 * h + 2] = hadd2(y & 0x000f000fu, m8);
+                p[8 * i + 4 * h + 3] = hadd2(y & 0x00f000f0u, m128);
             }
-        } else {
-            p[2 * i] = __byte_perm(a.w[i], b.w[i], 0x5410);
-            p[2 * i + 1] = __byte_perm(a.w[i], b.w[i], 0x7632);
         }
     }
 }
@@ -498,7 +503,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     int to_fill = 0, to_read = 0, ahead = 0;                 // ahead: tiles copied and not yet read
     // A step copies 512 bytes of rows, 16 a lane: the change of place within 128 bytes is that of the
     // lane's part of the offset and, apart from it, that of the step's.
-    const uint32_t k_lane = k_place<RB>(16 * l / RB, 16 * l % RB), v_lane = v_place<RB>(16 * l / RB, 16 * l % RB);
+    const uint32_t k_lane = k_place<RB>(16 * l / RB, 16 * l % RB), v_lane = v_place<F, RB>(16 * l / RB, 16 * l % RB);
     const uint64_t policy = streaming();
     auto copy_tile = [&]() {
         const uint32_t dst = ring + to_fill * S::TILE, to_v = RB << a.pg.shift;
@@ -510,7 +515,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             const uint8_t *k = page + (slot * RB + 16 * l), *v = k + to_v;
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
+                const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<F, RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
                 copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * j, policy);
                 copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * j, policy);
             }
@@ -535,7 +540,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 const bool ok = id >= 0 && tok >= f.lo && tok < f.hi;
                 const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + a.pg.slot(tok) * RB + byte : a.pg.base;
                 copy16(dst + k_place<RB>(row, byte), src, ok);
-                copy16(dst + TT * RB + v_place<RB>(row, byte), src + (ok ? to_v : 0), ok);
+                copy16(dst + TT * RB + v_place<F, RB>(row, byte), src + (ok ? to_v : 0), ok);
             }
             if (S::CODED && l < TT / 8) {
                 int id = f.ids[0];
@@ -554,9 +559,11 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         f.tok += turns * TT;
     };
 
-    // What this lane reads of a tile: piece c of row r of K, piece r of rows 2 c and 2 c + 1 of V;
-    // 8 rows, and 8 pieces of V, further on lie the same.
-    const uint32_t k_at = k_place<RB>(r, c * S::KP), v_at = v_place<RB>(2 * c, r * S::VP), v_at1 = v_place<RB>(2 * c + 1, r * S::VP);
+    // What this lane reads of a tile: piece c of row r of K; of V in 16 bits a matrix's row of 16 bytes,
+    // of codes piece r of rows 2 c and 2 c + 1. 8 rows, and 8 pieces of V, further on lie the same.
+    const uint32_t k_at = k_place<RB>(r, c * S::KP);
+    const uint32_t v_at = S::CODED ? v_place<F, RB>(2 * c, r * S::VP) : TT * RB + v_place<F, RB>((l & 7) + (l >> 4) * 8, (l >> 3 & 1) * 16);
+    const uint32_t v_at1 = v_place<F, RB>(2 * c + 1, r * S::VP);
 
     Piece p = next_piece();
     auto first_head = [&](const Piece &x) { return x.vh / chunks * a.groups + x.vh % chunks * HT; };
@@ -635,18 +642,17 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         past += p.n;
         const int count = count_of(p), tok_first = (p.tile0 + p.from + turn) * TT;
 
-        float hf[NT][2], ho[NT][2], R[NT][2], sum[NT][2], O[NT][S::MT][4];
+        // pairs are of heads 2 c and 2 c + 1
+        uint64_t hf[NT], ho[NT], R[NT], sum[NT];
+        float O[NT][S::MT][4];
         const uint2 *qf = (const uint2 *)smem;
         uint2 qr[S::QREG ? S::QT : 1][S::QREG ? NT : 1][S::QREG ? S::KS : 1];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-#pragma unroll
-            for (int e = 0; e < 2; e++) {
-                hf[nt][e] = head_k[8 * nt + 2 * c + e];
-                ho[nt][e] = head_off[8 * nt + 2 * c + e];
-                R[nt][e] = kLow;
-                sum[nt][e] = 0.f;
-            }
+            hf[nt] = *(const uint64_t *)(head_k + 8 * nt + 2 * c);
+            ho[nt] = *(const uint64_t *)(head_off + 8 * nt + 2 * c);
+            R[nt] = f2s(kLow);
+            sum[nt] = 0;
 #pragma unroll
             for (int m = 0; m < S::MT; m++)
 #pragma unroll
@@ -725,8 +731,9 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         }
                     }
                 }
-                // base-2 exponents (x - ho) hk; masked ones are -inf
-                float sv[G][2], hk[NT][G][4];
+                // base-2 exponents x hk with x = s - ho; masked ones are -inf
+                float sv[G][2];
+                uint64_t x[NT][G][2], hk[NT][G][2];
 #pragma unroll
                 for (int g = 0; g < G; g++)
 #pragma unroll
@@ -739,12 +746,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             sv[g][h] = fmaxf(f16_val(sc[TT]), kF16Min);      // 0 or NaN: of no token
                         }
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                            for (int e = 0; e < 2; e++) {
-                                hk[nt][g][2 * h + e] = S::CODED ? hf[nt][e] * sk : hf[nt][e];
-                                if (S::CODED) s[nt][g][2 * h + e] -= ho[nt][e];
+                        for (int nt = 0; nt < NT; nt++) {
+                            x[nt][g][h] = f2(s[nt][g][2 * h], s[nt][g][2 * h + 1]);
+                            hk[nt][g][h] = hf[nt];
+                            if (S::CODED) {
+                                x[nt][g][h] = fsub2(x[nt][g][h], ho[nt]);
+                                hk[nt][g][h] = fmul2(hf[nt], f2s(sk));
                             }
+                        }
                     }
                 if (edge) {
 #pragma unroll
@@ -754,56 +763,58 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             const int tok = tok0 + 16 * g + r + 8 * h;
                             if (tok >= p.lo && tok < p.hi) continue;
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                for (int e = 0; e < 2; e++) {
-                                    s[nt][g][2 * h + e] = -INFINITY;
-                                    hk[nt][g][2 * h + e] = 1.f;
-                                }
+                            for (int nt = 0; nt < NT; nt++) {
+                                x[nt][g][h] = f2s(-INFINITY);
+                                hk[nt][g][h] = f2s(1.f);
+                            }
                         }
                 }
                 // Weights 2^(s - R) sv of at most 2^15. R rises, to 7 below the largest exponent
                 // (of the weight), only when one would be above: seldom after the first tiles.
-                float wt[NT][G][4], wv[NT][G][4], most = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < NT; nt++)
+                uint64_t wt[NT][G][2], wv[NT][G][2];
+                auto weights = [&](int nt) {
+                    const uint64_t less_r = f2(-f2lo(R[nt]), -f2hi(R[nt]));
+                    float most = 0.f;
 #pragma unroll
                     for (int g = 0; g < G; g++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            wt[nt][g][e] = exp2_fast(fmaf(s[nt][g][e], hk[nt][g][e], -R[nt][e & 1]));
-                            wv[nt][g][e] = wt[nt][g][e] * sv[g][e >> 1];
-                            most = fmaxf(most, wv[nt][g][e]);
+                        for (int h = 0; h < 2; h++) {
+                            const uint64_t t = ffma2(x[nt][g][h], hk[nt][g][h], less_r);
+                            wt[nt][g][h] = f2(exp2_fast(f2lo(t)), exp2_fast(f2hi(t)));
+                            wv[nt][g][h] = S::CODED ? fmul2(wt[nt][g][h], f2s(sv[g][h])) : wt[nt][g][h];
+                            most = fmax3(most, f2lo(wv[nt][g][h]), f2hi(wv[nt][g][h]));
                         }
+                    return most;
+                };
+                float most = weights(0);
+                if (NT > 1) most = fmaxf(most, weights(NT - 1));
                 if (__any_sync(0xffffffffu, most > 32768.f)) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
+                    for (int nt = 0; nt < NT; nt++) {
+                        float up[2], f[2];
 #pragma unroll
                         for (int e = 0; e < 2; e++) {
                             float top = kLow;
+                            auto half = [&](uint64_t v) { return e ? f2hi(v) : f2lo(v); };
 #pragma unroll
                             for (int g = 0; g < G; g++)
 #pragma unroll
                                 for (int h = 0; h < 2; h++)
-                                    top = fmaxf(top, fmaf(s[nt][g][2 * h + e], hk[nt][g][2 * h + e], S::CODED ? log2f(sv[g][h]) : 0.f));
+                                    top = fmaxf(top, fmaf(half(x[nt][g][h]), half(hk[nt][g][h]), S::CODED ? log2f(sv[g][h]) : 0.f));
 #pragma unroll
                             for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            const float up = fmaxf(R[nt][e], top - 7.f), x = exp2_fast(R[nt][e] - up);
-                            R[nt][e] = up;
-                            sum[nt][e] *= x;
+                            up[e] = fmaxf(half(R[nt]), top - 7.f);
+                            f[e] = exp2_fast(half(R[nt]) - up[e]);
 #pragma unroll
                             for (int m = 0; m < S::MT; m++) {
-                                O[nt][m][e] *= x;
-                                O[nt][m][2 + e] *= x;
+                                O[nt][m][e] *= f[e];
+                                O[nt][m][2 + e] *= f[e];
                             }
-#pragma unroll
-                            for (int g = 0; g < G; g++)
-#pragma unroll
-                                for (int h = 0; h < 2; h++) {
-                                    wt[nt][g][2 * h + e] = exp2_fast(fmaf(s[nt][g][2 * h + e], hk[nt][g][2 * h + e], -up));
-                                    wv[nt][g][2 * h + e] = wt[nt][g][2 * h + e] * sv[g][h];
-                                }
                         }
+                        R[nt] = f2(up[0], up[1]);
+                        sum[nt] = fmul2(sum[nt], f2(f[0], f[1]));
+                        weights(nt);
+                    }
                 }
                 // weighted v: heads' weights by tokens become the right factor by a transposition
 #pragma unroll
@@ -813,34 +824,46 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                         for (int h = 0; h < 2; h++) {
-                            float x = wv[nt][g][2 * h], y = wv[nt][g][2 * h + 1];
-                            sum[nt][0] += wt[nt][g][2 * h];
-                            sum[nt][1] += wt[nt][g][2 * h + 1];
+                            sum[nt] = fadd2(sum[nt], wt[nt][g][h]);
+                            uint64_t left = wv[nt][g][h];
 #pragma unroll
                             for (int t = 0; t < S::PT; t++) {
-                                const uint32_t v = pack(x, y, C{});
+                                const uint32_t v = pack(f2lo(left), f2hi(left), C{});
                                 if (t + 1 < S::PT) {
                                     const float2 u = unpack(v, C{});
-                                    x -= u.x;
-                                    y -= u.y;
+                                    left = fsub2(left, f2(u.x, u.y));
                                 }
                                 pw[nt][t][h] = transpose8(v);
                             }
                         }
-                    constexpr int NP = RB / (8 * S::VP), CH = S::VP * 8 / bits_of(F);    // pieces, channels of each
+                    if constexpr (!S::CODED) {
+                        // row tile m: channels 16 m + r and 16 m + 8 + r
 #pragma unroll
-                    for (int z = 0; z < NP; z++) {
-                        const uint8_t *at = rows + TT * RB + 8 * z * S::VP + 16 * g * RB;
-                        uint32_t x[CH], y[CH];
-                        v_pairs<F>(lds<S::VP>(at, v_at), lds<S::VP>(at, v_at1), x);
-                        v_pairs<F>(lds<S::VP>(at, v_at + 8 * RB), lds<S::VP>(at, v_at1 + 8 * RB), y);
-#pragma unroll
-                        for (int m = 0; m < CH / 2; m++)
+                        for (int m = 0; m < S::MT; m++) {
+                            uint32_t v[4];
+                            load_transposed(v, smem_addr(rows) + (v_at ^ ((m & 3) << 5)) + (m >> 2) * 128 + 16 * g * RB);
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                                 for (int t = 0; t < S::PT; t++)
-                                    mma<C>(O[nt][z * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1], pw[nt][t][0], pw[nt][t][1]);
+                                    mma<C>(O[nt][m], v[0], v[1], v[2], v[3], pw[nt][t][0], pw[nt][t][1]);
+                        }
+                    } else {
+                        constexpr int NP = RB / (8 * S::VP), CH = S::VP * 8 / bits_of(F);    // pieces, channels of each
+#pragma unroll
+                        for (int z = 0; z < NP; z++) {
+                            const uint8_t *at = rows + TT * RB + 8 * z * S::VP + 16 * g * RB;
+                            uint32_t x[CH], y[CH];
+                            v_pairs<F>(lds<S::VP>(at, v_at), lds<S::VP>(at, v_at1), x);
+                            v_pairs<F>(lds<S::VP>(at, v_at + 8 * RB), lds<S::VP>(at, v_at1 + 8 * RB), y);
+#pragma unroll
+                            for (int m = 0; m < CH / 2; m++)
+#pragma unroll
+                                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                    for (int t = 0; t < S::PT; t++)
+                                        mma<C>(O[nt][z * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1], pw[nt][t][0], pw[nt][t][1]);
+                        }
                     }
                 }
             }
@@ -853,17 +876,24 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int e = 0; e < 2; e++) {
+                float total = e ? f2hi(sum[nt]) : f2lo(sum[nt]);
 #pragma unroll
-                for (int o = 4; o < 32; o *= 2) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], o);
+                for (int o = 4; o < 32; o *= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
                 const int h = 8 * nt + 2 * c + e;
                 constexpr int MP = S::VP * 4 / bits_of(F);    // row tiles of a piece
 #pragma unroll
-                for (int m = 0; m < S::MT; m++)
-                    *(float2 *)(mine + h * D + (8 * (m / MP) + r) * (2 * MP) + 2 * (m % MP)) =
-                        make_float2(O[nt][m][e] * v_factor<F>(0), O[nt][m][2 + e] * v_factor<F>(1));
+                for (int m = 0; m < S::MT; m++) {
+                    if (S::CODED) {
+                        *(float2 *)(mine + h * D + (8 * (m / MP) + r) * (2 * MP) + 2 * (m % MP)) =
+                            make_float2(O[nt][m][e] * v_factor<F>(0), O[nt][m][2 + e] * v_factor<F>(1));
+                    } else {
+                        mine[h * D + 16 * m + r] = O[nt][m][e];
+                        mine[h * D + 16 * m + 8 + r] = O[nt][m][2 + e];
+                    }
+                }
                 if (r == 0) {
-                    sums[(w * 2) * HT + h] = R[nt][e];
-                    sums[(w * 2 + 1) * HT + h] = sum[nt][e];
+                    sums[(w * 2) * HT + h] = e ? f2hi(R[nt]) : f2lo(R[nt]);
+                    sums[(w * 2 + 1) * HT + h] = total;
                 }
             }
         if (l == 0) ((int *)scan)[w] = stage;

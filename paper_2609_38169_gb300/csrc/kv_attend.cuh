@@ -93,6 +93,7 @@ struct Shape {
     static constexpr int MT = D / 16;                        // row tiles of V's
     static constexpr bool QREG = QT * NT * KS <= 16;         // queries kept in registers
     using C = typename Compute<F>::T;
+    static constexpr bool WIDE = QT > 1;                     // fp32 and fp16 vectors; else bf16
 };
 
 // ------------------------------------------------------------------ building blocks
@@ -252,10 +253,6 @@ __device__ __forceinline__ const P *in_cluster(const P *p, uint32_t rank) {
     return (const P *)r;
 }
 
-__device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
-    return dtype == STEPQ_F32 ? ((const float *)p)[i]
-           : dtype == STEPQ_BF16 ? la::to_f32(((const la::bf16 *)p)[i]) : la::to_f32(((const la::f16 *)p)[i]);
-}
 // Four consecutive channels.
 __device__ __forceinline__ void store4_any(void *p, int64_t i, int dtype, const float (&x)[4]) {
     if (dtype == STEPQ_F32) la::store_vec<float, 4>((float *)p + i, x);
@@ -267,6 +264,7 @@ __device__ __forceinline__ void store4_any(void *p, int64_t i, int dtype, const 
 // [lo, hi) count (a row without any has one tile).
 struct Piece {
     int b, vh, from, n, lo, hi, tile0, tiles;
+    int turn;                       // of this warp: it takes tiles from + turn, and every `turns`-th after it
     int bad;                        // status of its length
 };
 template <int TT>
@@ -285,29 +283,49 @@ __device__ __forceinline__ int tiles_of(const AttendArgs &a, int len) {
     return p.tiles;
 }
 
+// a / b, mostly of numbers below 2^32 (a division of 64 bits takes some hundred instructions).
+__device__ __forceinline__ long long divided(long long a, long long b) {
+    if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
+}
 // 2^e for e in [-126, 127].
 __device__ __forceinline__ float power2(int e) { return __int_as_float((e + 127) << 23); }
 
-// Query channels of a warp's heads w, w + kAttWarps, ..: 32 e + lane of each.
+// Queries of a warp's heads w, w + kAttWarps, ..: lane l has pairs 32 k + l of each head's channels,
+// pair u the channels 2 u and 2 u + 1, of 4-bit codes 8 (u / 4) + u % 4 and the fourth after it.
 template <class S>
 struct Queries {
-    static constexpr int H = S::HT / kAttWarps, N = S::D / 32;
-    float x[H][N];
-    __device__ __forceinline__ void load(const AttendArgs &a, int b, int h0, int nh, int w, int l) {
+    static constexpr int H = S::HT / kAttWarps, N = S::D / 64;
+    static constexpr bool FOURTH = S::F == STEPQ_KV_INT4;
+    float2 x[H][N];
+    template <class T>
+    __device__ __forceinline__ void load_as(const T *q, int nh, int w, int l) {
 #pragma unroll
         for (int i = 0; i < H; i++)
 #pragma unroll
-            for (int e = 0; e < N; e++) {
-                const int h = w + i * kAttWarps;
-                x[i][e] = h < nh ? load_any(a.q, b * a.qs + (int64_t)(h0 + h) * S::D + 32 * e + l, a.dtype) : 0.f;
+            for (int k = 0; k < N; k++) {
+                const int h = w + i * kAttWarps, u = 32 * k + l;
+                const T *at = q + h * S::D + (FOURTH ? 8 * (u / 4) + u % 4 : 2 * u);
+                x[i][k] = make_float2(0.f, 0.f);
+                if (h < nh && FOURTH) x[i][k] = make_float2(la::to_f32(at[0]), la::to_f32(at[4]));
+                else if (h < nh) {
+                    const la::Vec<T, 2> v = *(const la::Vec<T, 2> *)at;
+                    x[i][k] = make_float2(la::to_f32(v.e[0]), la::to_f32(v.e[1]));
+                }
             }
+    }
+    __device__ __forceinline__ void load(const AttendArgs &a, int b, int h0, int nh, int w, int l) {
+        const int64_t at = b * a.qs + (int64_t)h0 * S::D;
+        if (!S::WIDE) load_as((const la::bf16 *)a.q + at, nh, w, l);
+        else if (a.dtype == STEPQ_F32) load_as((const float *)a.q + at, nh, w, l);
+        else load_as((const la::f16 *)a.q + at, nh, w, l);
     }
     // To shared memory as pairs in the order of K's pieces: of step ks of the product, pair (0, 1)
     // of lane 4 head + c; with each head's factor of the scores and the offset of the codes.
     __device__ __forceinline__ void put(const AttendArgs &a, uint8_t *smem, int w, int l) {
         using C = typename S::C;
         constexpr int F = S::F;
-        C *qf = (C *)smem;
+        uint32_t *qf = (uint32_t *)smem;
         float *head_k = (float *)(smem + S::OFF_HEAD), *head_off = head_k + S::HT;
 #pragma unroll
         for (int i = 0; i < H; i++) {
@@ -317,32 +335,32 @@ struct Queries {
                 // scaled by a power of two to below 2^15, where fp16 keeps 2^-39 of the largest
                 float top = 0.f;
 #pragma unroll
-                for (int e = 0; e < N; e++) top = fmaxf(top, fabsf(x[i][e]));
+                for (int e = 0; e < N; e++) top = fmax3(top, fabsf(x[i][e].x), fabsf(x[i][e].y));
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const int ex = max(-126, min(126, 141 - (__float_as_int(top) >> 23)));
 #pragma unroll
-                for (int e = 0; e < N; e++) x[i][e] *= power2(ex);
+                for (int e = 0; e < N; e++) x[i][e] = make_float2(x[i][e].x * power2(ex), x[i][e].y * power2(ex));
                 k *= power2(-ex);
             }
 #pragma unroll
             for (int e = 0; e < N; e++) {
-                // channel -> piece of KP bytes, pair j in it, half; pieces 4 i + c go to lane c
+                // pieces of KP bytes go to lanes c in turn: piece, and pair j of it
                 constexpr int PC = S::KP * 8 / bits_of(F), JP = PC / 2;          // channels, pairs of a piece
-                const int ch = 32 * e + l, piece = ch / PC, in = ch % PC;
-                const int j = F == STEPQ_KV_INT4 ? 4 * (in / 8) + in % 4 : in / 2;
-                const int half = F == STEPQ_KV_INT4 ? in / 4 % 2 : in % 2;
+                const int u = 32 * e + l, piece = u / JP, j = u % JP;
                 const int pair = (piece / 4) * JP + j, lane = 4 * (h % 8) + piece % 4;
-                const float f = F == STEPQ_KV_INT4 && (j & 1) ? 0.0625f : 1.f;    // of a code at 2^-20
-                float rest = x[i][e] * f, used = 0.f;
+                const float f = FOURTH && (j & 1) ? 0.0625f : 1.f;               // of a code at 2^-20
+                float2 rest = make_float2(x[i][e].x * f, x[i][e].y * f);
+                float used = 0.f;
 #pragma unroll
                 for (int t = 0; t < S::QT; t++) {
-                    const C v = la::from_f32<C>(rest);
-                    rest -= la::to_f32(v);
-                    used += la::to_f32(v);
-                    qf[((((t * S::NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2) * 2 + half] = v;
+                    const uint32_t v = pack(rest.x, rest.y, C{});
+                    const float2 b = unpack(v, C{});
+                    rest = make_float2(rest.x - b.x, rest.y - b.y);
+                    used += b.x + b.y;
+                    qf[(((t * S::NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2] = v;
                 }
-                off += F == STEPQ_KV_INT4 && (j & 1) ? 16.f * used : used;
+                off += FOURTH && (j & 1) ? 16.f * used : used;
             }
             if (S::CODED) {
 #pragma unroll
@@ -374,7 +392,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     constexpr int D = S::D, TT = S::TT, RB = S::RB, NT = S::NT, HT = S::HT, F = S::F;
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, r = l >> 2, c = l & 3;
     const int chunks = (a.groups + HT - 1) / HT, VH = a.pg.n_heads * chunks;
-    const long long items = (long long)a.B * VH;
+    const int items = a.B * VH;                              // far below 2^31: the host sees to it
     const float *head_k = (const float *)(smem + S::OFF_HEAD), *head_off = head_k + HT;
     float *sums = (float *)(smem + S::OFF_SUM);
     long long *scan = (long long *)(smem + S::OFF_SCAN);
@@ -385,11 +403,12 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     // Calls for whole sequences: the CTAs of a cluster take a sequence's tiles in turn.
     const int ctas = a.whole ? (int)cluster_size() : 1, rank = a.whole ? (int)cluster_rank() : 0;
     const int stages = a.stages;                             // S::STAGES, or 1 where no warp has more tiles
-    const int turn = rank * kAttWarps + w, turns = ctas * kAttWarps;
+    const int turns = ctas * kAttWarps;
 
     // The share: `left` tiles of all, in the order (sequence, virtual head, tile), from tile `from`
     // of virtual head vh of sequence b on; len is lens[b].
-    long long left = 0, share = 0, item = blockIdx.x / ctas;     // item: of calls for whole sequences
+    long long left = 0, share = 0;
+    int item = blockIdx.x / ctas;                            // of calls for whole sequences
     int b = 0, vh = 0, from = 0, len = 0;
     if (!a.whole) {
         const int per = (a.B + 32 * kAttWarps - 1) / (32 * kAttWarps), i0 = min(a.B, tid * per), i1 = min(a.B, i0 + per);
@@ -410,7 +429,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             total += scan[i];
         }
         total *= VH;
-        share = max((total + gridDim.x - 1) / gridDim.x, (long long)(2 * kAttWarps));
+        share = max(divided(total + gridDim.x - 1, gridDim.x), (long long)(2 * kAttWarps));
         const long long t = share * blockIdx.x;
         left = min(total - t, share);
         if (t < total && t >= (upto - mine) * VH && t < upto * VH) {
@@ -423,11 +442,12 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             }
             const long long in = t - p * VH;
             scan[kAttWarps] = i;
-            scan[kAttWarps + 1] = in / n;
-            scan[kAttWarps + 2] = in % n;
+            const long long head = divided(in, n);
+            scan[kAttWarps + 1] = head;
+            scan[kAttWarps + 2] = in - head * n;
         }
         __syncthreads();
-        if (tid == 0 && items > gridDim.x) joined[blockIdx.x].count = 0;     // unless a piece goes on elsewhere
+        if (tid == 0 && items > (int)gridDim.x) joined[blockIdx.x].count = 0;     // unless a piece goes on elsewhere
         if (left <= 0) return;
         b = (int)scan[kAttWarps];
         vh = (int)scan[kAttWarps + 1];
@@ -440,12 +460,13 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         Piece p{};
         if (a.whole) {
             if (item >= items) return p;
-            p.b = (int)(item / VH);
-            p.vh = (int)(item - (long long)p.b * VH);
+            p.b = item / VH;
+            p.vh = item - p.b * VH;
             item += gridDim.x / ctas;
             len = a.lens[p.b];
             set_span<TT>(a, len, p);
             p.n = p.tiles;
+            p.turn = rank * kAttWarps + w;
         } else {
             if (left <= 0) return p;
             p.b = b;
@@ -453,6 +474,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             p.from = from;
             set_span<TT>(a, len, p);
             p.n = (int)min((long long)(p.tiles - from), left);
+            p.turn = (w + (int)left) % kAttWarps;            // the share's tiles go round the warps
             left -= p.n;
             from += p.n;
             if (from == p.tiles) {
@@ -465,8 +487,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         }
         return p;
     };
-    // This warp's tiles of a piece: from + turn, from + turn + turns, ... below from + n.
-    auto count_of = [&](const Piece &p) { return p.n > turn ? (p.n - turn + turns - 1) / turns : 0; };
+    auto count_of = [&](const Piece &p) { return p.n > p.turn ? (p.n - p.turn + turns - 1) / turns : 0; };
 
     // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the pages of
     // that tile's octets (eight tokens), -1 where no token counts. A page that holds a whole
@@ -491,7 +512,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     auto fetch_from = [&](const Piece &p) {
         f.table = a.pg.table + p.b * a.pg.table_stride;
         f.head = (uint64_t)(p.vh / chunks) * a.pg.segment;
-        f.tok = (p.tile0 + p.from + turn) * TT;
+        f.tok = (p.tile0 + p.from + p.turn) * TT;
         f.more = count_of(p);
         f.lo = p.lo;
         f.hi = p.hi;
@@ -635,12 +656,12 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         out = {p.b, first_head(p), heads_of(p), p.n == p.tiles, a.parts + (size_t)slot * part_floats<HT, D>()};
         if (!a.whole && tid == 0 && p.from == 0) {
             // begun here, and ended here or by one of the next CTAs
-            const Joined j{out.all ? 0 : (int)((past + p.tiles - 1) / share) + 1, slot, p.b, p.vh};
-            if (items <= gridDim.x) joined[(long long)p.b * VH + p.vh] = j;
+            const Joined j{out.all ? 0 : (int)divided(past + p.tiles - 1, share) + 1, slot, p.b, p.vh};
+            if (items <= (int)gridDim.x) joined[p.b * VH + p.vh] = j;
             else if (j.count) joined[blockIdx.x] = j;
         }
         past += p.n;
-        const int count = count_of(p), tok_first = (p.tile0 + p.from + turn) * TT;
+        const int count = count_of(p), tok_first = (p.tile0 + p.from + p.turn) * TT;
 
         // pairs are of heads 2 c and 2 c + 1
         uint64_t hf[NT], ho[NT], R[NT], sum[NT];
@@ -902,12 +923,12 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
 }
 
 // Joins the parts of piece blockIdx.x, head blockIdx.y: a warp takes every eighth part, a lane
-// D / 32 channels.
-constexpr int kJoinWarps = 8;
+// D / 32 channels. The first parts are on their way before the weights are known.
+constexpr int kJoinWarps = 8, kJoinAhead = 6, kMostParts = 1024;
 template <int HT, int D>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, int ctas) {
-    __shared__ float os[kJoinWarps][D], ls[kJoinWarps], rs[kJoinWarps];
-    const int w = threadIdx.x >> 5, l = threadIdx.x & 31, h = blockIdx.y;
+    __shared__ float os[kJoinWarps][D], weight[kMostParts], red[2][kJoinWarps];
+    const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, h = blockIdx.y;
     griddep_wait();
     griddep_launch();
     const Joined j = ((const Joined *)(a.parts + (size_t)2 * ctas * part_floats<HT, D>()))[blockIdx.x];
@@ -917,40 +938,59 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
     auto part = [&](int i) {
         return a.parts + (size_t)(i == 0 ? j.first : 2 * ((j.first >> 1) + i)) * part_floats<HT, D>();
     };
-    constexpr int N = D / 32;
-    float top = kLow, total = 0.f, o[N] = {};
-#pragma unroll 4
-    for (int i = w; i < j.count; i += kJoinWarps) {
-        const float *x = part(i);
-        const float R = x[HT * D + h], sum = x[HT * D + HT + h];
-        la::Vec<float, N < 4 ? N : 4> v[N < 4 ? 1 : N / 4];
+    constexpr int N = D / 32, V = N < 4 ? N : 4;             // a lane's channels, of them side by side
+    struct Lane { la::Vec<float, V> v[N / V]; };
+    auto load = [&](int i) {
+        Lane x;
 #pragma unroll
-        for (int e = 0; e < (N < 4 ? 1 : N / 4); e++) v[e] = ((const la::Vec<float, N < 4 ? N : 4> *)(x + h * D))[32 * e + l];
-        const float up = fmaxf(top, R), k0 = exp2_fast(top - up), k1 = exp2_fast(R - up);
-        top = up;
-        total = fmaf(total, k0, sum * k1);
+        for (int e = 0; e < N / V; e++) x.v[e] = ((const la::Vec<float, V> *)(part(i) + h * D))[32 * e + l];
+        return x;
+    };
+    Lane ahead[kJoinAhead];
 #pragma unroll
-        for (int e = 0; e < N; e++) o[e] = fmaf(o[e], k0, v[e / 4].e[e % 4] * k1);
-    }
-    if (l == 0) {
-        rs[w] = top;
-        ls[w] = total;
+    for (int i = 0; i < kJoinAhead; i++)
+        if (w + i * kJoinWarps < j.count) ahead[i] = load(w + i * kJoinWarps);
+    float top = kLow, total = 0.f;
+    for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
+        weight[i] = part(i)[HT * D + h];
+        top = fmaxf(top, weight[i]);
     }
 #pragma unroll
-    for (int e = 0; e < N; e++) os[w][(N < 4 ? N : 4) * (32 * (e / 4) + l) + e % 4] = o[e];
+    for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (l == 0) red[0][w] = top;
     __syncthreads();
-    for (int d = 4 * threadIdx.x; d < D; d += 4 * 32 * kJoinWarps) {
-        float all = kLow, sum = 0.f, y[4] = {};
 #pragma unroll
-        for (int x = 0; x < kJoinWarps; x++) all = fmaxf(all, rs[x]);
+    for (int x = 0; x < kJoinWarps; x++) top = fmaxf(top, red[0][x]);
+    for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
+        weight[i] = exp2_fast(weight[i] - top);
+        total = fmaf(weight[i], part(i)[HT * D + HT + h], total);
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (l == 0) red[1][w] = total;
+    __syncthreads();
+    float o[N] = {};
+    auto add = [&](const Lane &x, float k) {
+#pragma unroll
+        for (int e = 0; e < N; e++) o[e] = fmaf(k, x.v[e / V].e[e % V], o[e]);
+    };
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; i++)
+        if (w + i * kJoinWarps < j.count) add(ahead[i], weight[w + i * kJoinWarps]);
+#pragma unroll 4
+    for (int i = w + kJoinAhead * kJoinWarps; i < j.count; i += kJoinWarps) add(load(i), weight[i]);
+#pragma unroll
+    for (int e = 0; e < N; e++) os[w][V * (32 * (e / V) + l) + e % V] = o[e];
+    __syncthreads();
+    for (int d = 4 * tid; d < D; d += 4 * 32 * kJoinWarps) {
+        float sum = 0.f, y[4] = {};
 #pragma unroll
         for (int x = 0; x < kJoinWarps; x++) {
-            const float k = exp2_fast(rs[x] - all);
-            sum = fmaf(k, ls[x], sum);
+            sum += red[1][x];
 #pragma unroll
-            for (int e = 0; e < 4; e++) y[e] = fmaf(k, os[x][d + e], y[e]);
+            for (int e = 0; e < 4; e++) y[e] += os[x][d + e];
         }
-        put_output(a, j.b, j.vh / chunks * a.groups + g0 + h, d, all, sum, y, D);
+        put_output(a, j.b, j.vh / chunks * a.groups + g0 + h, d, top, sum, y, D);
     }
 }
 

@@ -34,21 +34,20 @@ auto by_shape(int head_dim, int groups, bool wide, Fn &&f) {
 
 // CTAs of a call, from what the host knows: its rows and the most tokens that one has. cluster > 0:
 // clusters of that many take whole sequences. A warp then has up to kWholeTiles tiles, however short
-// the others' sequences are; beyond that equal shares are worth the parts and the second kernel. Shorter
-// sequences never need more CTAs for shares, so a workspace for `most` serves every call below it.
-#ifndef KV_WT
-#define KV_WT 8
-#endif
-constexpr int kWholeTiles = KV_WT;
+// the others' sequences are; beyond that equal shares are worth the parts and the second kernel.
+// A window makes all longer sequences equal, and twice as many tiles worth it: 33 sequences of 1,000
+// tokens' window, 10 heads of 64 (8 tiles a warp and more) 15.5 us, in shares 20.8. Without one, 7 of 14,000 in
+// 8 bits (14 tiles a warp) take 16.5 us, in shares 14.3.
+constexpr int kWholeTiles = 8;
 struct Grid { int ctas, cluster, stages; };
 template <class S>
-Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
+Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most, bool equal) {
     const int64_t tiles = (most + S::TT - 1) / S::TT, sms = sm_count();
     const int64_t heads = rows * c->n_heads * ((groups + S::HT - 1) / S::HT);
-    const int64_t resident = sms * S::resident(S::STAGES);
+    const int64_t places = sms * S::resident(S::STAGES), resident = places < kMostParts ? places : kMostParts;
     int cluster = 1;                                         // as many as find places and two tiles a warp
     while (cluster < 8 && 2 * cluster * heads <= resident && tiles > 2 * kAttWarps * cluster) cluster *= 2;
-    const bool whole = tiles <= kWholeTiles * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
+    const bool whole = tiles <= (equal ? 2 : 1) * kWholeTiles * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
     Grid g{0, whole ? cluster : 0, S::STAGES};
     if (whole) {
         g.ctas = (int)(heads < 8 * resident ? heads : 8 * resident) * cluster;
@@ -72,7 +71,7 @@ size_t attend_workspace(const stepq_kv_config *c, int groups, int64_t rows, int6
     for (int wide = 0; wide < 2; wide++)
         by_shape<F>(c->head_dim, groups, wide, [&](auto sh) {
             using S = decltype(sh);
-            const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most));
+            const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most, false));
             if (n > need) need = n;
         });
     return need;
@@ -84,8 +83,9 @@ stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int
         using S = decltype(sh);
         static SmemOptIn opt;
         AttendArgs a = args;
-        if (a.window > 0 && a.window + S::TT < most) most = a.window + S::TT;      // a window ends inside a tile
-        const Grid g = grid_of<S>(c, a.groups, a.B, most);
+        const bool equal = a.window > 0 && a.window + S::TT < most;
+        if (equal) most = a.window + S::TT;                  // a window ends inside a tile
+        const Grid g = grid_of<S>(c, a.groups, a.B, most, equal);
         a.whole = g.cluster;
         a.stages = g.stages;
         stepq_status st = opt((const void *)kv_attend_kernel<S>, kSmemMax);

@@ -398,7 +398,7 @@ size_t stepq_kv_page_bytes(const stepq_kv_config *cfg);
 
 /* The pool of pages and the sequences' page tables: token p of sequence b lies in page
  * table[b][p / page_tokens] at place p % page_tokens. Entries that a call's tokens do not
- * reach are not read. */
+ * reach may hold anything. */
 typedef struct {
     void *pages;             /* device, n_pages * stepq_kv_page_bytes(), 16-byte aligned */
     int n_pages;

@@ -40,7 +40,7 @@
 namespace stepq {
 namespace kv {
 
-constexpr int kAttWarps = 4;
+constexpr int kAttWarps = 4, kParts = 8 * kAttWarps;           // warps of a CTA, of a cluster
 #ifndef KV_ST
 #define KV_ST 32
 #define KV_SC 3
@@ -77,7 +77,9 @@ struct Shape {
                                                                        // float [2][HT]: factor, offset
     static constexpr int OFF_SUM = OFF_HEAD + 2 * HT * 4;              // float [kAttWarps][2][HT]: R, l
     static constexpr int OFF_SCAN = OFF_SUM + kAttWarps * 2 * HT * 4;  // int64 [kAttWarps + 3]
-    static constexpr int OFF_RING = (OFF_SCAN + 8 * (kAttWarps + 3) + 127) / 128 * 128;
+    // of clusters: float [HT][kParts + 2], int [kParts], float4 [kAttWarps][32]
+    static constexpr int OFF_PART = (OFF_SCAN + 8 * (kAttWarps + 3) + 15) / 16 * 16;
+    static constexpr int OFF_RING = (OFF_PART + (HT * (kParts + 2) + kParts) * 4 + kAttWarps * 512 + 127) / 128 * 128;
     // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
     static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED ? KV_RC : 3;
     static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
@@ -253,13 +255,6 @@ __device__ __forceinline__ const P *in_cluster(const P *p, uint32_t rank) {
     return (const P *)r;
 }
 
-// Four consecutive channels.
-__device__ __forceinline__ void store4_any(void *p, int64_t i, int dtype, const float (&x)[4]) {
-    if (dtype == STEPQ_F32) la::store_vec<float, 4>((float *)p + i, x);
-    else if (dtype == STEPQ_BF16) la::store_vec<la::bf16, 4>((la::bf16 *)p + i, x);
-    else la::store_vec<la::f16, 4>((la::f16 *)p + i, x);
-}
-
 // A piece: tiles from .. from + n - 1 of the `tiles` of sequence b, virtual head vh, whose tokens
 // [lo, hi) count (a row without any has one tile).
 struct Piece {
@@ -272,8 +267,11 @@ __device__ __forceinline__ void set_span(const AttendArgs &a, int len, Piece &p)
     const long long most = (long long)a.pg.width << a.pg.shift;
     p.hi = len < 0 ? 0 : len > most ? (int)most : len;
     p.bad = len < 0 ? STEPQ_ERR_ARG : len > most ? STEPQ_ERR_SLOT_RANGE : 0;
-    p.lo = a.window > 0 && p.hi > a.window ? p.hi - a.window : 0;
-    p.tile0 = p.lo / TT;
+    p.lo = p.tile0 = 0;
+    if (a.window > 0) {
+        p.lo = max(0, p.hi - a.window);
+        p.tile0 = p.lo / TT;
+    }
     p.tiles = max(1, (p.hi + TT - 1) / TT - p.tile0);
 }
 template <int TT>
@@ -377,10 +375,15 @@ struct Queries {
 };
 
 // Channels d .. d + 3 of query head h from the sums o of weighted values and `total` of weights.
+template <bool WIDE>
 __device__ __forceinline__ void put_output(const AttendArgs &a, int b, int h, int d, float top, float total, float (&o)[4], int D) {
+    const float f = total != 0.f ? 1.f / total : 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] / total : 0.f;
-    store4_any(a.y, b * a.ys + (int64_t)h * D + d, a.dtype, o);
+    for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] * f : 0.f;
+    const int64_t at = b * a.ys + (int64_t)h * D + d;
+    if (!WIDE) la::store_vec<la::bf16, 4>((la::bf16 *)a.y + at, o);
+    else if (a.dtype == STEPQ_F32) la::store_vec<float, 4>((float *)a.y + at, o);
+    else la::store_vec<la::f16, 4>((la::f16 *)a.y + at, o);
     if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = total != 0.f ? (top + log2f(total)) * 0.693147181f : -INFINITY;
 }
 
@@ -490,7 +493,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     auto count_of = [&](const Piece &p) { return p.n > p.turn ? (p.n - p.turn + turns - 1) / turns : 0; };
 
     // What is copied next: `more` tiles of a piece, the first at token `tok`; ids: the pages of
-    // that tile's octets (eight tokens), -1 where no token counts. A page that holds a whole
+    // that tile's octets (eight tokens), -1 behind the table. A page that holds a whole
     // tile is looked up once.
     struct {
         const int32_t *table;
@@ -498,15 +501,13 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         int tok, more, lo, hi, ids[TT / 8];
     } f{};
     const bool one_page = (1 << a.pg.shift) >= TT;
-    auto load_ids = [&]() {
+    const int table_end = a.pg.width << a.pg.shift;
+    auto load_ids = [&]() {                                  // nothing here waits for the sequence's length
         if (one_page) {
-            f.ids[0] = f.more > 0 && f.hi > 0 ? f.table[f.tok >> a.pg.shift] : -1;
+            f.ids[0] = f.tok < table_end ? f.table[f.tok >> a.pg.shift] : -1;
         } else {
 #pragma unroll
-            for (int o = 0; o < TT / 8; o++) {
-                const int tok = f.tok + 8 * o;
-                f.ids[o] = f.more > 0 && tok < f.hi && tok + 8 > f.lo ? f.table[tok >> a.pg.shift] : -1;
-            }
+            for (int o = 0; o < TT / 8; o++) f.ids[o] = f.tok + 8 * o < table_end ? f.table[(f.tok + 8 * o) >> a.pg.shift] : -1;
         }
     };
     auto fetch_from = [&](const Piece &p) {
@@ -607,43 +608,87 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         qs.load(a, p.b, first_head(p), p.n > 0 ? heads_of(p) : 0, w, l);
         if (!first) {
             // the warps' parts of the piece before
-            if (ctas > 1) cluster_sync();
-            else __syncthreads();
-            for (int i = tid + rank * 32 * kAttWarps; i < out.nh * (D / 4); i += 32 * turns) {
-                const int h = i / (D / 4), d = 4 * (i % (D / 4));
-                float top = kLow, total = 0.f, o[4] = {};
-#pragma unroll 2
-                for (int z = 0; z < ctas; z++) {
-                    const float *rl = ctas > 1 ? in_cluster(sums, z) : sums;
-                    const int *stage = ctas > 1 ? in_cluster((const int *)scan, z) : (const int *)scan;
-                    float up = top;
-#pragma unroll
-                    for (int x = 0; x < kAttWarps; x++) up = fmaxf(up, rl[2 * x * HT + h]);
-                    const float old = exp2_fast(top - up);
-                    top = up;
-                    total *= old;
-#pragma unroll
-                    for (int e = 0; e < 4; e++) o[e] *= old;
-#pragma unroll
-                    for (int x = 0; x < kAttWarps; x++) {
-                        const float k = exp2_fast(rl[2 * x * HT + h] - top);
-                        const float *part = (const float *)stage_of(x, stage[x]) + h * D + d;
-                        const float4 v = *(const float4 *)(ctas > 1 ? in_cluster(part, z) : part);
-                        total = fmaf(k, rl[(2 * x + 1) * HT + h], total);
-                        o[0] = fmaf(k, v.x, o[0]);
-                        o[1] = fmaf(k, v.y, o[1]);
-                        o[2] = fmaf(k, v.z, o[2]);
-                        o[3] = fmaf(k, v.w, o[3]);
-                    }
-                }
+            auto leave = [&](int h, int d, float top, float total, float(&o)[4]) {
                 if (out.all) {
-                    put_output(a, out.b, out.h0 + h, d, top, total, o, D);
+                    put_output<S::WIDE>(a, out.b, out.h0 + h, d, top, total, o, D);
                 } else {
                     *(float4 *)(out.part + h * D + d) = make_float4(o[0], o[1], o[2], o[3]);
                     if (d == 0) {
                         out.part[HT * D + h] = top;
                         out.part[HT * D + HT + h] = total;
                     }
+                }
+            };
+            auto add = [](float(&o)[4], float k, const float4 &v) {
+                o[0] = fmaf(k, v.x, o[0]);
+                o[1] = fmaf(k, v.y, o[1]);
+                o[2] = fmaf(k, v.z, o[2]);
+                o[3] = fmaf(k, v.w, o[3]);
+            };
+            if (ctas == 1) {
+                __syncthreads();
+                for (int i = tid; i < out.nh * (D / 4); i += 32 * kAttWarps) {
+                    const int h = i / (D / 4), d = 4 * (i % (D / 4));
+                    float top = kLow, total = 0.f, o[4] = {};
+#pragma unroll
+                    for (int x = 0; x < kAttWarps; x++) top = fmaxf(top, sums[2 * x * HT + h]);
+#pragma unroll
+                    for (int x = 0; x < kAttWarps; x++) {
+                        const float k = exp2_fast(sums[2 * x * HT + h] - top);
+                        total = fmaf(k, sums[(2 * x + 1) * HT + h], total);
+                        add(o, k, *(const float4 *)((const float *)stage_of(x, ((const int *)scan)[x]) + h * D + d));
+                    }
+                    leave(h, d, top, total, o);
+                }
+            } else {
+                // Weights of all warps' parts, a lane each; then each CTA a share of the channels, its
+                // warp x the parts of every CTA's warp x.
+                cluster_sync();
+                float *weight = (float *)(smem + S::OFF_PART);
+                int *stage = (int *)(weight + HT * (kParts + 2));
+                float4 *half = (float4 *)(smem + S::OFF_PART + (HT * (kParts + 2) + kParts) * 4);
+                for (int h = w; h < out.nh; h += kAttWarps) {
+                    float R = kLow, sum = 0.f;
+                    if (l < turns) {
+                        const float *rl = in_cluster((const float *)sums, l / kAttWarps) + 2 * (l % kAttWarps) * HT + h;
+                        R = rl[0];
+                        sum = rl[HT];
+                        if (h == w) stage[l] = in_cluster((const int *)scan, l / kAttWarps)[l % kAttWarps];
+                    }
+                    float top = R;
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const float k = exp2_fast(R - top);
+                    sum *= k;
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    weight[h * (kParts + 2) + l] = k;
+                    if (l == 0) {
+                        weight[h * (kParts + 2) + kParts] = top;
+                        weight[h * (kParts + 2) + kParts + 1] = sum;
+                    }
+                }
+                __syncthreads();
+                const int n = out.nh * (D / 4), each = (n + ctas - 1) / ctas, end = min(n, (rank + 1) * each);
+                for (int i0 = rank * each; i0 < end; i0 += 32) {
+                    const int i = i0 + l, h = i / (D / 4), d = 4 * (i % (D / 4));
+                    const float *k = weight + h * (kParts + 2);
+                    float o[4] = {};
+                    if (i < end) {
+#pragma unroll 8
+                        for (int z = 0; z < ctas; z++) {
+                            const float *part = (const float *)stage_of(w, stage[z * kAttWarps + w]) + h * D + d;
+                            add(o, k[z * kAttWarps + w], *(const float4 *)in_cluster(part, z));
+                        }
+                        half[w * 32 + l] = make_float4(o[0], o[1], o[2], o[3]);
+                    }
+                    __syncthreads();
+                    if (w == 0 && i < end) {
+#pragma unroll
+                        for (int x = 1; x < kAttWarps; x++) add(o, 1.f, half[x * 32 + l]);
+                        leave(h, d, k[kParts], k[kParts + 1], o);
+                    }
+                    __syncthreads();
                 }
             }
         }
@@ -925,7 +970,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
 // Joins the parts of piece blockIdx.x, head blockIdx.y: a warp takes every eighth part, a lane
 // D / 32 channels. The first parts are on their way before the weights are known.
 constexpr int kJoinWarps = 8, kJoinAhead = 6, kMostParts = 1024;
-template <int HT, int D>
+template <int HT, int D, bool WIDE>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, int ctas) {
     __shared__ float os[kJoinWarps][D], weight[kMostParts], red[2][kJoinWarps];
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, h = blockIdx.y;
@@ -990,7 +1035,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
 #pragma unroll
             for (int e = 0; e < 4; e++) y[e] += os[x][d + e];
         }
-        put_output(a, j.b, j.vh / chunks * a.groups + g0 + h, d, top, sum, y, D);
+        put_output<WIDE>(a, j.b, j.vh / chunks * a.groups + g0 + h, d, top, sum, y, D);
     }
 }
 

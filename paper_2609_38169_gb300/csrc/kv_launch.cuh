@@ -93,7 +93,7 @@ stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int
         st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
         if (st != STEPQ_OK || g.cluster) return st;
         const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
-        return launch_overlapped(kv_join_kernel<S::HT, S::D>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
+        return launch_overlapped(kv_join_kernel<S::HT, S::D, S::WIDE>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
                                  32 * kJoinWarps, 0, s, a, g.ctas);
     });
 }

@@ -45,7 +45,6 @@ constexpr int kAttWarps = 4, kParts = 8 * kAttWarps;           // warps of a CTA
 #define KV_ST 32
 #define KV_SC 3
 #define KV_S16 2
-#define KV_RC 4
 #endif
 constexpr float kLow = -3.402823466e+38f;
 
@@ -81,7 +80,7 @@ struct Shape {
     static constexpr int OFF_PART = (OFF_SCAN + 8 * (kAttWarps + 3) + 15) / 16 * 16;
     static constexpr int OFF_RING = (OFF_PART + (HT * (kParts + 2) + kParts) * 4 + kAttWarps * 512 + 127) / 128 * 128;
     // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
-    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED ? KV_RC : 3;
+    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED && QT == 1 ? 4 : 3;
     static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
     static constexpr int resident(int stages) {
         const int n = 227 * 1024 / (smem(stages) + 1024);

@@ -49,14 +49,17 @@ Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most, b
     while (cluster < 8 && 2 * cluster * heads <= resident && tiles > 2 * kAttWarps * cluster) cluster *= 2;
     const bool whole = tiles <= (equal ? 2 : 1) * kWholeTiles * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
     Grid g{0, whole ? cluster : 0, S::STAGES};
-    if (whole) {
-        g.ctas = (int)(heads < 8 * resident ? heads : 8 * resident) * cluster;
+    if (whole && tiles <= kAttWarps * cluster && heads * cluster <= sms * S::resident(1)) {
+        // a tile a warp needs one stage, which lets more CTAs in
+        g.ctas = (int)heads * cluster;
+        g.stages = 1;
+    } else if (whole) {
+        // more sequences than places: a CTA takes several, and has the next one's tiles copied meanwhile
+        g.ctas = (int)(heads < resident ? heads : resident) * cluster;
     } else {
         const int64_t ctas = (heads * tiles + 2 * kAttWarps - 1) / (2 * kAttWarps);
         g.ctas = (int)(ctas < resident ? ctas : resident);
     }
-    // a warp with one tile needs one stage, which lets more CTAs in
-    if (whole && tiles <= kAttWarps * cluster) g.stages = 1;
     return g;
 }
 template <class S>

@@ -531,46 +531,70 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         constexpr int N = TT * RB / 512;                     // steps
         const uint8_t *layer = a.pg.base + f.head;
         const int slot = a.pg.slot(f.tok);
-        if (one_page && f.tok >= f.lo && f.tok + TT <= f.hi && (uint32_t)f.ids[0] < (uint32_t)a.pg.n_pages) {
-            const uint8_t *page = layer + (uint64_t)(uint32_t)f.ids[0] * a.pg.page_bytes;
-            const uint8_t *k = page + (slot * RB + 16 * l), *v = k + to_v;
+        auto steps = [&](int j0, int n, const uint8_t *k) {  // n steps from j0 on, from k on
+            const uint8_t *v = k + to_v;
 #pragma unroll
-            for (int j = 0; j < N; j++) {
+            for (int x = 0; x < n; x++) {
+                const int j = j0 + x;
                 const uint32_t kj = k_place<RB>(512 * j / RB, 512 * j % RB) ^ (512 * j), vj = v_place<F, RB>(512 * j / RB, 512 * j % RB) ^ (512 * j);
-                copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * j, policy);
-                copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * j, policy);
+                copy16(dst + 512 * j + (k_lane ^ kj), k + 512 * x, policy);
+                copy16(dst + TT * RB + 512 * j + (v_lane ^ vj), v + 512 * x, policy);
             }
+        };
+        const bool inside = f.tok >= f.lo && f.tok + TT <= f.hi;
+        const bool one = one_page && inside && (uint32_t)f.ids[0] < (uint32_t)a.pg.n_pages;
+        bool several = inside && !one_page;
+        if (one) {
+            const uint8_t *page = layer + (uint64_t)(uint32_t)f.ids[0] * a.pg.page_bytes;
+            steps(0, N, page + (slot * RB + 16 * l));
             if (S::CODED && l < TT / 4) {                    // K's scales, then V's
                 const bool is_v = l >= TT / 8;
                 copy16(dst + 2 * TT * RB + 16 * l, page + 2 * to_v + 2 * slot + 16 * (l & (TT / 8 - 1)) + (is_v ? 2 << a.pg.shift : 0), policy);
             }
         } else {
-            // tiles of several pages; rows that are no tokens, or in no page, become zeros
+            int mine = f.ids[0];                                 // the page of octet l
 #pragma unroll
             for (int o = 0; o < TT / 8; o++) {
-                if (one_page && o > 0) f.ids[o] = f.ids[0];
-                if ((uint32_t)f.ids[o] >= (uint32_t)a.pg.n_pages) {
-                    if (l == 0 && f.tok + 8 * o < f.hi && f.tok + 8 * o + 8 > f.lo) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
-                    f.ids[o] = -1;
+                several = several && (uint32_t)f.ids[o] < (uint32_t)a.pg.n_pages;
+                if (o > 0 && !one_page) mine = l == o ? f.ids[o] : mine;
+            }
+            const uint8_t *page = layer + (uint64_t)(uint32_t)mine * a.pg.page_bytes;
+            if (several) {
+                constexpr int PER = RB >= 64 ? RB / 64 : 1;      // steps of an octet, or octets of a step in two halves
+#pragma unroll
+                for (int j0 = 0; j0 < N; j0 += PER) {
+                    constexpr int two = RB < 64;
+                    const int o = 512 * j0 / (8 * RB), id = two && l >= 16 ? f.ids[o + two] : f.ids[o];
+                    steps(j0, PER, layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + a.pg.slot(f.tok + 8 * o + (two && l >= 16 ? 8 : 0)) * RB + 16 * l % (8 * RB));
                 }
-            }
+                if (S::CODED && l < TT / 8) {
+                    const uint8_t *src = page + 2 * to_v + 2 * a.pg.slot(f.tok + 8 * l);
+                    copy16(dst + 2 * TT * RB + 16 * l, src, policy);
+                    copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, src + (2 << a.pg.shift), policy);
+                }
+            } else {
+                // rows that are no tokens, or in no page, become zeros
+                const int tok_l = f.tok + 8 * l;
+                const bool counts = l < TT / 8 && tok_l < f.hi && tok_l + 8 > f.lo;
+                if ((uint32_t)mine >= (uint32_t)a.pg.n_pages) {
+                    if (counts) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+                    mine = -1;
+                }
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const int at = 512 * j + 16 * l, row = at / RB, byte = at % RB, tok = f.tok + row;
-                const int o = 512 * j / (8 * RB), id = RB < 64 && l >= 16 ? f.ids[o + (RB < 64)] : f.ids[o];
-                const bool ok = id >= 0 && tok >= f.lo && tok < f.hi;
-                const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + a.pg.slot(tok) * RB + byte : a.pg.base;
-                copy16(dst + k_place<RB>(row, byte), src, ok);
-                copy16(dst + TT * RB + v_place<F, RB>(row, byte), src + (ok ? to_v : 0), ok);
-            }
-            if (S::CODED && l < TT / 8) {
-                int id = f.ids[0];
-#pragma unroll
-                for (int o = 1; o < TT / 8; o++) id = l == o ? f.ids[o] : id;
-                const bool ok = id >= 0;
-                const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + 2 * to_v + 2 * a.pg.slot(f.tok + 8 * l) : a.pg.base;
-                copy16(dst + 2 * TT * RB + 16 * l, src, ok);
-                copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, src + (ok ? 2 << a.pg.shift : 0), ok);
+                for (int j = 0; j < N; j++) {
+                    const int at = 512 * j + 16 * l, row = at / RB, byte = at % RB, tok = f.tok + row;
+                    const int id = __shfl_sync(0xffffffffu, mine, row / 8);
+                    const bool ok = id >= 0 && tok >= f.lo && tok < f.hi;
+                    const uint8_t *src = ok ? layer + (uint64_t)(uint32_t)id * a.pg.page_bytes + a.pg.slot(tok) * RB + byte : a.pg.base;
+                    copy16(dst + k_place<RB>(row, byte), src, ok);
+                    copy16(dst + TT * RB + v_place<F, RB>(row, byte), src + (ok ? to_v : 0), ok);
+                }
+                if (S::CODED && l < TT / 8) {
+                    const bool ok = mine >= 0 && counts;
+                    const uint8_t *src = ok ? page + 2 * to_v + 2 * a.pg.slot(tok_l) : a.pg.base;
+                    copy16(dst + 2 * TT * RB + 16 * l, src, ok);
+                    copy16(dst + 2 * TT * RB + 2 * TT + 16 * l, src + (ok ? 2 << a.pg.shift : 0), ok);
+                }
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");

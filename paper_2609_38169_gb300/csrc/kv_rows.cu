@@ -100,11 +100,45 @@ __device__ __forceinline__ Place place_of(const RowsArgs &a, int i, int lane) {
     return {page, a.pg.slot((int)pos)};
 }
 
-// The quotient a / s, rounded, with y the rounded reciprocal of s: t = a y and then t + (a - t s) y
-// (P. Markstein, Computation of elementary functions on the IBM RISC System/6000, 1990).
+// A quotient a / s by one correction: t = a y with y near 1 / s, then t + (a - t s) y, whose sum is rounded
+// once (P. Markstein, Computation of elementary functions on the IBM RISC System/6000, 1990). With y
+// within 2^-22 that sum is a / s up to 2^-44 of it. For s of 11 bits and a of 24 no quotient other than
+// a rounding border itself is so near one (a - m s is a multiple of 2^-36 of a for every border m of
+// 25 bits, and is not zero: m s has more bits than a), so the result is the rounded quotient.
 __device__ __forceinline__ float quotient(float a, float s, float y) {
     const float t = a * y;
     return fmaf(fmaf(-t, s, a), y, t);
+}
+__device__ __forceinline__ float reciprocal_near(float s) {   // 1 unit in 2^-23
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(s));
+    return y;
+}
+
+// The bits of the largest magnitude of a lane's eight values as an fp32 (NaN is above all): as
+// unsigned numbers magnitudes are ordered, two of 16 bits at a time.
+template <class T>
+__device__ __forceinline__ uint32_t magnitude(const Eight<T> &v, uint32_t most) {
+    const uint4 w = *(const uint4 *)&v;
+    const uint32_t m = 0x7fff7fffu, t = __vimax3_u16x2(w.x & m, w.y & m, w.z & m);
+    return __vimax3_u16x2(t, w.w & m, most);
+}
+__device__ __forceinline__ uint32_t magnitude(const Eight<float> &v, uint32_t most) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) most = max(most, __float_as_uint(v.e[e]) & 0x7fffffffu);
+    return most;
+}
+template <class T, int L>
+__device__ __forceinline__ float row_magnitude(const Eight<T> &v, bool on) {
+    uint32_t most = on ? magnitude(v, 0u) : 0u;
+#pragma unroll
+    for (int o = 1; o < L; o *= 2) {
+        const uint32_t x = __shfl_xor_sync(0xffffffffu, most, o);
+        most = sizeof(T) == 4 ? max(most, x) : __vmaxu2(most, x);
+    }
+    if (sizeof(T) == 4) return __uint_as_float(most);
+    const uint16_t top = (uint16_t)max(most & 0xffffu, most >> 16);
+    return la::to_f32(*(const T *)&top);
 }
 
 // A lane's rows: token i, K or V (part), heads h0 + n * PER, channels 8 c on.
@@ -152,16 +186,9 @@ __global__ void __launch_bounds__(32 * kWarps) kv_append_kernel(RowsArgs a) {
         uint64_t x[4];
         if (on) pairs(in[n], x);
         else x[0] = x[1] = x[2] = x[3] = 0;
-        // as unsigned numbers the values' magnitudes are ordered, NaN above all
-        uint32_t most = 0;
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-            most = max(most, max((uint32_t)x[e] & 0x7fffffffu, (uint32_t)(x[e] >> 32) & 0x7fffffffu));
-#pragma unroll
-        for (int o = 1; o < m.L; o *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
         constexpr float q = F == STEPQ_KV_INT8 ? 127.f : 7.f;
         constexpr int half = F == STEPQ_KV_INT8 ? 128 : 8;
-        float top = __uint_as_float(most);
+        float top = row_magnitude<T, Mine<D>::L>(in[n], on);
         const bool far = !(top <= 65504.f * q);
         if (__any_sync(0xffffffffu, far)) {
             // a scale at its bound, or values that are not finite: NaN becomes zero, the others are clamped
@@ -181,7 +208,7 @@ __global__ void __launch_bounds__(32 * kWarps) kv_append_kernel(RowsArgs a) {
                 x[e] = f2(fminf(fmaxf(v[2 * e], -top), top), fminf(fmaxf(v[2 * e + 1], -top), top));
         }
         const uint16_t sb = f16_bits(fmaxf(quotient(top, q, 1.f / q), kF16Min));
-        const float s = f16_val(sb), y = __frcp_rn(s);
+        const float s = f16_val(sb), y = reciprocal_near(s);
         // Quotients plus 1.5 2^23 + 2^(b-1): the sum's lowest bits are the code. |x| <= top, so that
         // no quotient is above q by more than the scale's rounding.
         constexpr uint32_t magic = 0x4b400000u + half;

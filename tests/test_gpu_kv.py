@@ -120,6 +120,28 @@ def test_rows_at_the_edges(fmt, dt):
     assert torch.equal(out[0], wk.float().to(dt)) and torch.equal(out[1], wv.float().to(dt))
 
 
+@pytest.mark.parametrize("fmt", [A.KV_INT8, A.KV_INT4], ids=["int8", "int4"])
+@pytest.mark.parametrize("exponent", [-13, -3, 0, 9])
+def test_borders_between_codes(fmt, exponent):
+    """fp32 values on the border of two codes, and next to it on both sides, for every scale of 11 bits."""
+    kv, q = A.KvConfig(1, 1, 128, 64, fmt), 127 if fmt == A.KV_INT8 else 7
+    g = gen(20)
+    s = (1 + torch.arange(1024, device="cuda").double() / 1024) * 2.0 ** exponent
+    k = torch.randint(-q, q, (1024, 128), generator=g, device="cuda").double() + 0.5
+    x = (k * s[:, None]).float()
+    x = torch.where(torch.arange(128, device="cuda") % 3 == 1, x.nextafter(torch.tensor(1e30, device="cuda")), x)
+    x = torch.where(torch.arange(128, device="cuda") % 3 == 2, x.nextafter(torch.tensor(-1e30, device="cuda")), x)
+    x[:, 0] = (q * s).float()                               # the row's largest: its scale is s
+    table = torch.arange(16, device="cuda", dtype=torch.int32)[None]
+    pages = torch.zeros(16 * A.stepq_kv_page_bytes(kv), dtype=torch.uint8, device="cuda")
+    want = pages.clone()
+    x = x[:, None]
+    R.append(want, kv, 0, table, [0], [1024], x, -x)
+    A.stepq_kv_append(kv, 0, pages, table, i32([0]), x, -x)
+    assert torch.equal(pages, want)
+    assert torch.equal(R.split(pages, kv)[2].reshape(-1).double(), s)
+
+
 @pytest.mark.parametrize("fmt", FORMATS, ids=fmt_ids)
 def test_equal_lengths_and_many_sequences(fmt):
     """No cu_seqlens: one token each of 1,500 sequences, then three each; 1,500 ragged ones."""

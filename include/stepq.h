@@ -417,7 +417,7 @@ typedef struct {
 } stepq_kv_rows;
 
 /* Write the rows of B sequences into one layer of their pages: sequence b's are rows
- * cu_seqlens[b] .. cu_seqlens[b+1] - 1 of the `tokens` packed rows (device int32 [B+1],
+ * cu_seqlens[b] .. cu_seqlens[b+1] - 1 of the `tokens` packed rows (at most 2^30; device int32 [B+1],
  * ascending within [0, tokens]; NULL: tokens / B each, tokens a multiple of B), and become its
  * tokens starts[b], starts[b] + 1, .. (device int32 [B]). In 16 bits a value is rounded to the
  * format. For codes of b bits, q = 2^(b-1) - 1 and the row's absmax (over values that are not NaN),

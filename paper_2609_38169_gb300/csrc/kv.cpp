@@ -31,7 +31,7 @@ stepq_status check_pages(const stepq_kv_config *c, int layer, const stepq_kv_pag
     const stepq_status st = check_config(c);
     if (st != STEPQ_OK) return st;
     if (layer < 0 || layer >= c->n_layers || !p || B < 0) return STEPQ_ERR_ARG;
-    if (!p->pages || p->n_pages < 1 || p->table_width < 0 || p->table_stride < 0 || (B > 0 && !p->table) ||
+    if (!p->pages || p->n_pages < 1 || p->table_width < 0 || p->table_stride < 0 || (B > 0 && p->table_width > 0 && !p->table) ||
         (int64_t)p->table_width * c->page_tokens > (1 << 30))
         return STEPQ_ERR_ARG;
     return aligned(p->pages, 16) && aligned(p->table, 4) ? STEPQ_OK : STEPQ_ERR_ALIGN;
@@ -47,7 +47,7 @@ stepq_status check_transfer(const stepq_kv_config *c, int layer, const stepq_kv_
                             const int32_t *cu, int B, int tokens, const stepq_kv_rows *r, bool out) {
     stepq_status st = check_pages(c, layer, p, B);
     if (st != STEPQ_OK) return st;
-    if (tokens < 0 || !r || r->dtype < STEPQ_F32 || r->dtype > STEPQ_F16) return STEPQ_ERR_ARG;
+    if (tokens < 0 || tokens > (1 << 30) || !r || r->dtype < STEPQ_F32 || r->dtype > STEPQ_F16) return STEPQ_ERR_ARG;
     if (B == 0 || tokens == 0) return STEPQ_OK;
     if (!starts || (!cu && tokens % B)) return STEPQ_ERR_ARG;
     if (!aligned(starts, 4) || !aligned(cu, 4)) return STEPQ_ERR_ALIGN;

@@ -21,11 +21,10 @@
 // share a key head. HBM bounds the call as long as these keep up; tcgen05 would want 128 rows of
 // tokens of which each is used for 8 columns, and codes would have to go back to shared memory.
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
-// row and the queries are laid out to match. Codes u enter K's product as the fp16 subnormal
-// u 2^-24 (a mask or a byte permute), its offset 2^(b-1) sum q is subtracted from the sum; for V,
-// where that would cancel over all tokens, u - 2^(b-1) is formed first, exactly. (A product with the
-// offset behind each with codes saves a tenth of the instructions and no time, and costs fp32
-// outputs two bits.)
+// row and the queries are laid out to match. Codes become fp16 exactly. Where outputs are bf16 those of
+// K enter as they are, u 2^-24 (a mask or a byte permute leaves a subnormal number), and their offset
+// 2^(b-1) sum q is subtracted from the sum; the tensor cores line products up by the exponents of normal
+// numbers, which cuts such sums off after some 17 bits (4 bits) or 21 (8 bits).
 //
 // Roundings: q enters as a sum of QT terms of the cache's 16-bit type, weights as a sum of PT,
 // everything between in fp32. One term of fp16 has 2^-12, half of bf16's eighth of a unit, two
@@ -95,6 +94,7 @@ struct Shape {
     static constexpr bool QREG = QT * NT * KS <= 16;         // queries kept in registers
     using C = typename Compute<F>::T;
     static constexpr bool WIDE = QT > 1;                     // fp32 and fp16 vectors; else bf16
+    static constexpr bool RAW = CODED && !WIDE;              // K's codes enter with their offset, at 2^-24
 };
 
 // ------------------------------------------------------------------ building blocks
@@ -137,6 +137,32 @@ __device__ __forceinline__ float2 unpack(uint32_t v, la::bf16) {
 __device__ __forceinline__ float2 unpack(uint32_t v, la::f16) {
     return __half22float2(*(const __half2 *)&v);
 }
+// d += A B for the terms B[t] of a right factor. The tensor cores' sums are cut off, not rounded, which adds up
+// over many steps: for outputs of more than 16 bits (WIDE) each product's own sum, the smallest term
+// first, is added with rounding.
+template <class C, bool WIDE, int T, class Term>
+__device__ __forceinline__ void mma_terms(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, Term &&term) {
+    if (WIDE) {
+        float sum[4] = {};
+#pragma unroll
+        for (int t = T - 1; t >= 0; t--) {
+            const uint2 b = term(t);
+            mma<C>(sum, a0, a1, a2, a3, b.x, b.y);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            const uint64_t v = fadd2(f2(d[e], d[e + 1]), f2(sum[e], sum[e + 1]));
+            d[e] = f2lo(v);
+            d[e + 1] = f2hi(v);
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < T; t++) {
+            const uint2 b = term(t);
+            mma<C>(d, a0, a1, a2, a3, b.x, b.y);
+        }
+    }
+}
 template <int N> struct alignas(4 * N) Words { uint32_t w[N]; };
 template <int BYTES>
 __device__ __forceinline__ Words<BYTES / 4> lds(const uint8_t *tile, uint32_t at) {
@@ -172,64 +198,73 @@ __device__ __forceinline__ uint32_t v_place(int row, int byte) {
     return (uint32_t)(row * RB + byte) ^ (!coded(F) ? (row & 7) << 4 : RB >= 64 ? ((row >> 1) & 3) << 5 : ((row >> 2) & 1) << 5);
 }
 
-// A lane's piece of a row of K as pairs of the compute type, in the order that Queries::put() gives the queries.
-template <int F, int N>
-__device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 / bits_of(F)]) {
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        if constexpr (F == STEPQ_KV_INT8) {
-            p[2 * i] = __byte_perm(x.w[i], 0u, 0x4140);
-            p[2 * i + 1] = __byte_perm(x.w[i], 0u, 0x4342);
-        } else if constexpr (F == STEPQ_KV_INT4) {
-            const uint32_t y = x.w[i] >> 8;
-            p[4 * i] = x.w[i] & 0x000f000fu;
-            p[4 * i + 1] = x.w[i] & 0x00f000f0u;
-            p[4 * i + 2] = y & 0x000f000fu;
-            p[4 * i + 3] = y & 0x00f000f0u;
-        } else {
-            p[i] = x.w[i];
-        }
-    }
-}
-// Four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 i .. 8 i + 7 give the rows of matrix i.
-__device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
-}
-// A lane's pieces of two tokens' rows of V as pairs of tokens, p[channel]: 2^-24 of the code
-// without its offset, and for the odd channels of 4 bits 2^-20.
 __device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// Codes without their offset as pairs of fp16, exactly: 0x6400 | u is 1024 + u, less 1024 + 2^(b-1);
+// 0x6400 | 16 u is 1024 + 16 u, of which a 16th less 64 + 8.
+__device__ __forceinline__ uint32_t codes8(uint32_t w, uint32_t bytes) { return hadd2(__byte_perm(w, 0x64646464u, bytes), 0xe480e480u); }
+__device__ __forceinline__ uint32_t codes4(uint32_t w) { return hadd2(and_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u); }
+__device__ __forceinline__ uint32_t codes4_high(uint32_t w) {
+    return hfma2(and_or(w, 0x00f000f0u, 0x64006400u), 0x2c002c00u, 0xd480d480u);
+}
+
+// A lane's piece of a row of K as pairs of the compute type, in the order that Queries::put() gives
+// the queries. RAW: codes with their offset at 2^-24, for the odd pairs of 4 bits 2^-20.
+template <int F, bool RAW, int N>
+__device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 / bits_of(F)]) {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const uint32_t w = x.w[i];
+        if constexpr (F == STEPQ_KV_INT8) {
+            p[2 * i] = RAW ? __byte_perm(w, 0u, 0x4140) : codes8(w, 0x4140);
+            p[2 * i + 1] = RAW ? __byte_perm(w, 0u, 0x4342) : codes8(w, 0x4342);
+        } else if constexpr (F == STEPQ_KV_INT4) {
+            const uint32_t y = w >> 8;
+            p[4 * i] = RAW ? w & 0x000f000fu : codes4(w);
+            p[4 * i + 1] = RAW ? w & 0x00f000f0u : codes4_high(w);
+            p[4 * i + 2] = RAW ? y & 0x000f000fu : codes4(y);
+            p[4 * i + 3] = RAW ? y & 0x00f000f0u : codes4_high(y);
+        } else {
+            p[i] = w;
+        }
+    }
+}
+
+// Four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 i .. 8 i + 7 give the rows of matrix i.
+__device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
+}
+// A lane's pieces of two tokens' rows of V as pairs of tokens, p[channel].
 template <int F, int N>
 __device__ __forceinline__ void v_pairs(const Words<N> &a, const Words<N> &b, uint32_t (&p)[N * 32 / bits_of(F)]) {
-    constexpr uint32_t m128 = 0x80808080u, m8 = 0x80088008u;
 #pragma unroll
     for (int i = 0; i < N; i++) {
         if constexpr (F == STEPQ_KV_INT8) {
             const uint32_t lo = __byte_perm(a.w[i], b.w[i], 0x5140), hi = __byte_perm(a.w[i], b.w[i], 0x7362);
-            p[4 * i] = hadd2(__byte_perm(lo, 0u, 0x4140), m128);
-            p[4 * i + 1] = hadd2(__byte_perm(lo, 0u, 0x4342), m128);
-            p[4 * i + 2] = hadd2(__byte_perm(hi, 0u, 0x4140), m128);
-            p[4 * i + 3] = hadd2(__byte_perm(hi, 0u, 0x4342), m128);
+            p[4 * i] = codes8(lo, 0x4140);
+            p[4 * i + 1] = codes8(lo, 0x4342);
+            p[4 * i + 2] = codes8(hi, 0x4140);
+            p[4 * i + 3] = codes8(hi, 0x4342);
         } else {
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const uint32_t x = __byte_perm(a.w[i], b.w[i], h ? 0x7632 : 0x5410), y = x >> 8;
-                p[8 * i + 4 * h] = hadd2(x & 0x000f000fu, m8);
-                p[8 * i + 4 * h + 1] = hadd2(x & 0x00f000f0u, m128);
-                p[8 * i + 4 * h + 2] = hadd2(y & 0x000f000fu, m8);
-                p[8 * i + 4 * h + 3] = hadd2(y & 0x00f000f0u, m128);
+                p[8 * i + 4 * h] = codes4(x);
+                p[8 * i + 4 * h + 1] = codes4_high(x);
+                p[8 * i + 4 * h + 2] = codes4(y);
+                p[8 * i + 4 * h + 3] = codes4_high(y);
             }
         }
     }
-}
-// What V's product is to be multiplied by, by the parity of the channel.
-template <int F>
-__host__ __device__ constexpr float v_factor(int odd) {
-    return !coded(F) ? 1.f : F == STEPQ_KV_INT4 && odd ? 1048576.f : 16777216.f;
 }
 
 // Thread-block clusters: this CTA's place, the barrier of all their threads (which shows each other's
@@ -346,7 +381,7 @@ struct Queries {
                 constexpr int PC = S::KP * 8 / bits_of(F), JP = PC / 2;          // channels, pairs of a piece
                 const int u = 32 * e + l, piece = u / JP, j = u % JP;
                 const int pair = (piece / 4) * JP + j, lane = 4 * (h % 8) + piece % 4;
-                const float f = FOURTH && (j & 1) ? 0.0625f : 1.f;               // of a code at 2^-20
+                const float f = S::RAW && FOURTH && (j & 1) ? 0.0625f : 1.f;     // of a code at 2^-20
                 float2 rest = make_float2(x[i][e].x * f, x[i][e].y * f);
                 float used = 0.f;
 #pragma unroll
@@ -357,9 +392,9 @@ struct Queries {
                     used += b.x + b.y;
                     qf[(((t * S::NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2] = v;
                 }
-                off += FOURTH && (j & 1) ? 16.f * used : used;
+                off += S::RAW && FOURTH && (j & 1) ? 16.f * used : used;
             }
-            if (S::CODED) {
+            if (S::RAW) {
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2) off += __shfl_xor_sync(0xffffffffu, off, o);
                 off *= F == STEPQ_KV_INT8 ? 128.f / 16777216.f : 8.f / 16777216.f;
@@ -803,20 +838,17 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         // pieces 4 x + c: an odd x differs from an even one in the bit that rows change
                         const uint8_t *at = rows + ((x & 1) * 4 * S::KP ^ k_at) + (x >> 1) * 8 * S::KP + 16 * g * RB;
                         uint32_t k0[JP], k8[JP];
-                        k_pairs<F>(lds<S::KP>(at, 0), k0);
-                        k_pairs<F>(lds<S::KP>(at, 8 * RB), k8);
+                        k_pairs<F, S::RAW>(lds<S::KP>(at, 0), k0);
+                        k_pairs<F, S::RAW>(lds<S::KP>(at, 8 * RB), k8);
 #pragma unroll
                         for (int j = 0; j < JP / 2; j++) {
                             const int ks = x * (JP / 2) + j;
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                for (int t = 0; t < S::QT; t++) {
-                                    uint2 v;
-                                    if constexpr (S::QREG) v = qr[t][nt][ks];
-                                    else v = qf[((t * NT + nt) * S::KS + ks) * 32 + l];
-                                    mma<C>(s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], v.x, v.y);
-                                }
+                                mma_terms<C, S::WIDE, S::QT>(s[nt][g], k0[2 * j], k8[2 * j], k0[2 * j + 1], k8[2 * j + 1], [&](int t) {
+                                    if constexpr (S::QREG) return qr[t][nt][ks];
+                                    else return qf[((t * NT + nt) * S::KS + ks) * 32 + l];
+                                });
                         }
                     }
                 }
@@ -838,10 +870,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         for (int nt = 0; nt < NT; nt++) {
                             x[nt][g][h] = f2(s[nt][g][2 * h], s[nt][g][2 * h + 1]);
                             hk[nt][g][h] = hf[nt];
-                            if (S::CODED) {
-                                x[nt][g][h] = fsub2(x[nt][g][h], ho[nt]);
-                                hk[nt][g][h] = fmul2(hf[nt], f2s(sk));
-                            }
+                            if (S::RAW) x[nt][g][h] = fsub2(x[nt][g][h], ho[nt]);
+                            if (S::CODED) hk[nt][g][h] = fmul2(hf[nt], f2s(sk));
                         }
                     }
                 if (edge) {
@@ -908,7 +938,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 // weighted v: heads' weights by tokens become the right factor by a transposition
 #pragma unroll
                 for (int g = 0; g < G; g++) {
-                    uint32_t pw[NT][S::PT][2];
+                    uint2 pw[NT][S::PT];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -922,7 +952,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                                     const float2 u = unpack(v, C{});
                                     left = fsub2(left, f2(u.x, u.y));
                                 }
-                                pw[nt][t][h] = transpose8(v);
+                                (h ? pw[nt][t].y : pw[nt][t].x) = transpose8(v);
                             }
                         }
                     if constexpr (!S::CODED) {
@@ -933,9 +963,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             load_transposed(v, smem_addr(rows) + (v_at ^ ((m & 3) << 5)) + (m >> 2) * 128 + 16 * g * RB);
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                for (int t = 0; t < S::PT; t++)
-                                    mma<C>(O[nt][m], v[0], v[1], v[2], v[3], pw[nt][t][0], pw[nt][t][1]);
+                                mma_terms<C, S::WIDE, S::PT>(O[nt][m], v[0], v[1], v[2], v[3], [&](int t) { return pw[nt][t]; });
                         }
                     } else {
                         constexpr int NP = RB / (8 * S::VP), CH = S::VP * 8 / bits_of(F);    // pieces, channels of each
@@ -949,9 +977,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             for (int m = 0; m < CH / 2; m++)
 #pragma unroll
                                 for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                    for (int t = 0; t < S::PT; t++)
-                                        mma<C>(O[nt][z * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1], pw[nt][t][0], pw[nt][t][1]);
+                                    mma_terms<C, S::WIDE, S::PT>(O[nt][z * (CH / 2) + m], x[2 * m], x[2 * m + 1], y[2 * m], y[2 * m + 1],
+                                                                 [&](int t) { return pw[nt][t]; });
                         }
                     }
                 }
@@ -974,7 +1001,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 for (int m = 0; m < S::MT; m++) {
                     if (S::CODED) {
                         *(float2 *)(mine + h * D + (8 * (m / MP) + r) * (2 * MP) + 2 * (m % MP)) =
-                            make_float2(O[nt][m][e] * v_factor<F>(0), O[nt][m][2 + e] * v_factor<F>(1));
+                            make_float2(O[nt][m][e], O[nt][m][2 + e]);
                     } else {
                         mine[h * D + 16 * m + r] = O[nt][m][e];
                         mine[h * D + 16 * m + 8 + r] = O[nt][m][2 + e];

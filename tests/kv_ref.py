@@ -7,7 +7,9 @@ y_d = sum_t p_t v_td with p the softmax:
  * an error e_t of a score moves y by sum_t p_t e_t (v_td - y_d). A score is a sum of D terms in
    tensor-core steps of 16 that may truncate (2 u each; D / 16 <= 16 of them, twice or three times
    for a query in terms, and a few roundings beside them): 64 u of the sum of absolute terms,
-   which for codes are those of the code with its offset. The exponent's difference from the
+   which for codes are those of the code with its offset. bf16 queries meet codes as subnormal numbers
+   u 2^-24, whose products are lined up as if u were 1024: each step may cut off 2^-23 of 1024 times
+   the head's largest |q|, in units of the code, 2^-13 |q| s. The exponent's difference from the
    reference and its exponential add 4 u of that sum (in absolute terms: |s| is below it) and 2^-21.
  * a weight enters as a sum of terms of 16 bits: eps of it, with eps = 2^-12 for one of fp16, 2^-17
    for two of bf16, 2^-23 for two of fp16, 2^-25 for three of bf16; in fp16 it also has no
@@ -114,6 +116,10 @@ def attend(pages, kv, layer, table, lens, q, scale, window=0):
         s = scale * (qb @ k.permute(1, 2, 0))                                # [heads][G][tokens]
         p = torch.softmax(s, -1)
         e = abs(scale) * (qb.abs() @ ka.permute(1, 2, 0)) * 68 * U + 2.0 ** -21
+        if BITS[kv.format] < 16 and q.dtype is torch.bfloat16:
+            s_k = split(pages, kv)[2][places(table[b:b + 1], [lo], [n - lo], kv.page_tokens)[0], layer, :,
+                                      places(table[b:b + 1], [lo], [n - lo], kv.page_tokens)[1]].double()
+            e = e + abs(scale) * D / 16 * 2.0 ** -13 * qb.abs().amax(-1, keepdim=True) * s_k.t()[:, None, :]
         vh = v.transpose(0, 1)                                               # [heads][tokens][D]
         yb = p @ vh
         steps = (n - lo) / 64 * 2 + 64

@@ -360,6 +360,50 @@ def test_values_that_are_not_finite_stay_in_their_sequence_and_head(fmt):
     assert bool(y.isfinite().all())
 
 
+def test_nothing_to_do():
+    """No sequences; sequences without tokens over a table without entries."""
+    kv = A.KvConfig(1, 2, 64, 16, A.KV_INT8)
+    pages, z = A.alloc_pages(kv, 2), lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    for B, W in ((0, 3), (0, 0), (3, 0), (3, 2)):
+        t, n, y = torch.zeros((B, W), dtype=torch.int32, device="cuda"), i32([0] * B), z(B, 4, 64) + 5
+        A.stepq_kv_attend(kv, 0, pages, t, n, z(B, 4, 64), y)
+        assert not bool(y.any())
+        A.stepq_kv_append(kv, 0, pages, t, n, z(0, 2, 64), z(0, 2, 64))
+        A.stepq_kv_read(kv, 0, pages, t, n, z(0, 2, 64), z(0, 2, 64), cu_seqlens=i32([0] * (B + 1)))
+
+
+def test_calls_stay_within_their_buffers():
+    """Nothing outside pages, rows, outputs and workspace is written."""
+    g, kv = gen(18), A.KvConfig(1, 2, 128, 16, A.KV_INT4)
+    lens = [3000, 17, 0, 900]
+    table, n = tables(g, kv, lens)
+    each, guard = A.stepq_kv_page_bytes(kv), 4096
+
+    def guarded(nbytes):
+        whole = torch.full((nbytes + 2 * guard,), 0x5A, dtype=torch.uint8, device="cuda")
+        return whole, whole[guard:guard + nbytes]
+    held = []
+    whole, pages = guarded(n * each)
+    held.append((whole, n * each))
+    pages.copy_(normal_pages(g, kv, n))
+    q = torch.randn((4, 8, 128), generator=g, device="cuda").bfloat16()
+    for max_len in (3000, 100):
+        bytes_y, bytes_l, bytes_w = 4 * 8 * 128 * 2, 4 * 8 * 4, A.stepq_kv_workspace_bytes(kv, 8, 4, 3000)
+        (wy, y), (wl, l), (ww, ws) = guarded(bytes_y), guarded(bytes_l), guarded(bytes_w)
+        held += [(wy, bytes_y), (wl, bytes_l), (ww, bytes_w)]
+        A.stepq_kv_attend(kv, 0, pages, table, i32(lens), q, y.view(torch.bfloat16).view(4, 8, 128), lse=l.view(torch.float32),
+                          max_len=max_len, workspace=ws)
+    bytes_k = sum(lens) * 2 * 128 * 2
+    rows = [guarded(bytes_k) for _ in range(2)]
+    held += [(w, bytes_k) for w, _ in rows]
+    k, v = (x.view(torch.bfloat16).view(-1, 2, 128) for _, x in rows)
+    cu = i32([sum(lens[:b]) for b in range(5)])
+    A.stepq_kv_read(kv, 0, pages, table, i32([0] * 4), k, v, cu_seqlens=cu)
+    A.stepq_kv_append(kv, 0, pages, table, i32([0] * 4), k, v, cu_seqlens=cu)
+    for whole, nbytes in held:
+        assert bool((whole[:guard] == 0x5A).all()) and bool((whole[guard + nbytes:] == 0x5A).all())
+
+
 def test_bad_lengths_and_pages_are_reported():
     g, kv = gen(13), A.KvConfig(1, 2, 64, 16, A.KV_INT8)
     lens = [40, 40, 40]

@@ -56,7 +56,7 @@ def test_refusals_in_common(call):
         assert call(p=pages(**kw)) == code, kw
     for kw in (dict(layer=-1), dict(layer=2), dict(B=-1)):
         assert call(**kw) == ARG, kw
-    assert call(B=0) == OK and call(B=0, p=pages(table=None)) == OK
+    assert call(B=0) == OK and call(B=0, p=pages(table=None)) == OK and call(B=0, p=pages(table=None, table_width=0)) == OK
 
 
 @pytest.mark.parametrize("name", ["stepq_kv_append", "stepq_kv_read"])
@@ -64,7 +64,7 @@ def test_rows_refusals(name):
     for kw, code in [(dict(dtype=3), ARG), (dict(dtype=-1), ARG), (dict(k=None), ARG), (dict(v=None), ARG), (dict(k_stride=-8), ARG),
                      (dict(k=P + 8), ALIGN), (dict(v=P + 2), ALIGN), (dict(k_stride=516), ALIGN), (dict(v_stride=514), ALIGN)]:
         assert move(name, r=rows(**kw)) == code, kw
-    assert move(name, tokens=-1) == ARG and move(name, starts=None) == ARG and move(name, tokens=5) == ARG
+    assert move(name, tokens=-1) == ARG and move(name, tokens=(1 << 30) + 2) == ARG and move(name, starts=None) == ARG and move(name, tokens=5) == ARG
     assert move(name, starts=P + 1) == ALIGN and move(name, cu=P + 2, tokens=5) == ALIGN
     assert move(name, tokens=0) == OK and move(name, tokens=0, starts=None) == OK
 

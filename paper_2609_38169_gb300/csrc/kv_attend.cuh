@@ -27,8 +27,7 @@
 // numbers, which cuts such sums off after some 17 bits (4 bits) or 21 (8 bits).
 //
 // Roundings: q enters as a sum of QT terms of the cache's 16-bit type, weights as a sum of PT,
-// everything between in fp32. One term of fp16 has 2^-12, half of bf16's eighth of a unit, two
-// of fp16 2^-23, two of bf16 2^-17, three 2^-25; see Terms.
+// everything between in fp32: see Variant.
 #pragma once
 
 #include <type_traits>
@@ -40,11 +39,6 @@ namespace stepq {
 namespace kv {
 
 constexpr int kAttWarps = 4, kParts = 8 * kAttWarps;           // warps of a CTA, of a cluster
-#ifndef KV_ST
-#define KV_ST 32
-#define KV_SC 3
-#define KV_S16 2
-#endif
 constexpr float kLow = -3.402823466e+38f;
 
 // Workspace: for each CTA c two parts (2 c: the piece that its share begins with, 2 c + 1: one
@@ -59,17 +53,22 @@ template <int HT, int D> __host__ __device__ constexpr int part_floats() { retur
 template <int F> struct Compute { using T = la::f16; };
 template <> struct Compute<STEPQ_KV_BF16> { using T = la::bf16; };
 
-// Shape of a variant.
-template <int F_, int D_, int NT_, int QT_, int PT_>
+// Shape of a variant. LARGE: of calls whose warps take many tiles (codes of up to 128 head channels).
+template <int F_, int D_, int NT_, int QT_, int PT_, bool LARGE_ = false>
 struct Shape {
+    static constexpr bool LARGE = LARGE_;
+    using Larger = Shape<F_, D_, NT_, QT_, PT_, coded(F_) && NT_ * D_ <= 128>;
     static constexpr int F = F_, D = D_, NT = NT_, QT = QT_, PT = PT_;
     static constexpr int HT = 8 * NT;                        // heads of a CTA
     static constexpr int RB = row_bytes(F, D);
     static constexpr bool CODED = coded(F);
-    // A tile: 4 KB of codes of up to 128 head channels, else 8 or 16; 16 to 64 tokens.
-    static constexpr int WANT = CODED ? 32 * (NT * D > 128 ? NT * D : 128) : 64 * (D > 128 ? D : 128);
+    // A tile: 4 KB of codes of up to 128 head channels, else 8 or 16; 16 to 64 tokens. Twice as much
+    // leaves less to do a token, and takes longer until the first output: 256 x 8,191 tokens in 4 bits
+    // 409 us, LARGE 372; 128 x 4,096 in 8 bits 189 and 178; 8 x 24 in 4 bits 5.4 and 6.4.
+    static constexpr int WANT = CODED ? (LARGE ? 64 : 32) * (NT * D > 128 ? NT * D : 128) : 64 * (D > 128 ? D : 128);
     static constexpr int FIT = WANT / (2 * RB), TT = FIT > 64 ? 64 : FIT;
-    static constexpr int ST = NT * D >= 256 || TT == 16 ? 16 : KV_ST;       // taken at once
+    static constexpr int ST = NT * D >= 256 || TT == 16 ? 16 : 32;       // taken at once
+    static_assert(TT >= 16 && TT % ST == 0, "a tile is whole parts");
     static constexpr int TILE = 2 * TT * RB + (CODED ? 4 * TT : 0);
     static constexpr int OFF_HEAD = QT * NT * (D / 16) * 256;          // behind the queries [QT][NT][D / 16][32] uint2:
                                                                        // float [2][HT]: factor, offset
@@ -79,13 +78,13 @@ struct Shape {
     static constexpr int OFF_PART = (OFF_SCAN + 8 * (kAttWarps + 3) + 15) / 16 * 16;
     static constexpr int OFF_RING = (OFF_PART + (HT * (kParts + 2) + kParts) * 4 + kAttWarps * 512 + 127) / 128 * 128;
     // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
-    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED && QT == 1 ? 4 : 3;
+    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED && QT == 1 && !LARGE ? 4 : 3;
     static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
     static constexpr int resident(int stages) {
         const int n = 227 * 1024 / (smem(stages) + 1024);
         return n < BY_REGS ? n : BY_REGS;
     }
-    static constexpr int STAGES = CODED ? KV_SC : KV_S16;    // of calls that fill the GPU
+    static constexpr int STAGES = CODED && !LARGE ? 3 : 2;   // of calls that fill the GPU
     static_assert(TILE >= HT * D * 4, "a warp's part is put together in one stage of its ring");
     static constexpr int KP = RB / 4 < 16 ? RB / 4 : 16;     // bytes a lane reads of a row of K at once
     static constexpr int VP = RB / 8 < 16 ? RB / 8 : 16;     // and of V

@@ -9,10 +9,10 @@ namespace kv {
 // Terms of a variant: queries and weights enter the products as sums of QT and PT terms of the
 // pages' 16-bit type.
 //  * bf16 vectors over fp16 and codes: a query of 8 bits is one term of fp16, exactly; a
-//    weight's one term has 2^-12, an eighth of the output's own rounding.
+//    weight's one term is within 2^-11, an eighth of the output's own rounding.
 //  * bf16 vectors over bf16: one term of a weight would have the output's own rounding again, two
-//    have 2^-17.
-//  * fp16 and fp32 vectors: two terms of fp16 (2^-23), three of bf16 (2^-25); fp16 queries need
+//    are within 2^-16.
+//  * fp16 and fp32 vectors: two terms of fp16 (2^-22), three of bf16 (2^-24); fp16 queries need
 //    one and two of them, and take the fp32 variant.
 template <int F, int D, int NT, bool WIDE>
 using Variant = Shape<F, D, NT, F == STEPQ_KV_BF16 ? (WIDE ? 3 : 1) : (WIDE ? 2 : 1), F == STEPQ_KV_BF16 ? (WIDE ? 3 : 2) : (WIDE ? 2 : 1)>;
@@ -75,29 +75,41 @@ size_t attend_workspace(const stepq_kv_config *c, int groups, int64_t rows, int6
         by_shape<F>(c->head_dim, groups, wide, [&](auto sh) {
             using S = decltype(sh);
             const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most, false));
+            const size_t m = parts_bytes<typename S::Larger>(grid_of<typename S::Larger>(c, groups, rows, most, false));
             if (n > need) need = n;
+            if (m > need) need = m;
         });
     return need;
 }
 
+template <class S>
+stepq_status launch_shape(const Grid &g, int64_t pieces, AttendArgs a, cudaStream_t s) {
+    static SmemOptIn opt;
+    a.whole = g.cluster;
+    a.stages = g.stages;
+    stepq_status st = opt((const void *)kv_attend_kernel<S>, kSmemMax);
+    if (st != STEPQ_OK) return st;
+    st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
+    if (st != STEPQ_OK || g.cluster) return st;
+    return launch_overlapped(kv_join_kernel<S::HT, S::D, S::WIDE>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
+                             32 * kJoinWarps, 0, s, a, g.ctas);
+}
+
 template <int F>
-stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &args, int64_t most, cudaStream_t s) {
-    return by_shape<F>(c->head_dim, args.groups, args.dtype != STEPQ_BF16, [&](auto sh) {
+stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &a, int64_t most, cudaStream_t s) {
+    return by_shape<F>(c->head_dim, a.groups, a.dtype != STEPQ_BF16, [&](auto sh) {
         using S = decltype(sh);
-        static SmemOptIn opt;
-        AttendArgs a = args;
+        using L = typename S::Larger;
         const bool equal = a.window > 0 && a.window + S::TT < most;
-        if (equal) most = a.window + S::TT;                  // a window ends inside a tile
+        if (equal && a.window + L::TT < most) most = a.window + L::TT;      // a window ends inside a tile
         const Grid g = grid_of<S>(c, a.groups, a.B, most, equal);
-        a.whole = g.cluster;
-        a.stages = g.stages;
-        stepq_status st = opt((const void *)kv_attend_kernel<S>, kSmemMax);
-        if (st != STEPQ_OK) return st;
-        st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
-        if (st != STEPQ_OK || g.cluster) return st;
         const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
-        return launch_overlapped(kv_join_kernel<S::HT, S::D, S::WIDE>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
-                                 32 * kJoinWarps, 0, s, a, g.ctas);
+        // large tiles from 16 small ones a warp on (15 x 19,625 tokens in 4 bits, 19 a warp: 54 us, large 49;
+        // 26 x 1,201 with fp32 vectors, 4 a warp: 18.4 and 20.3)
+        if constexpr (L::LARGE)
+            if (!g.cluster && pieces * ((most + S::TT - 1) / S::TT) >= 16ll * kAttWarps * g.ctas)
+                return launch_shape<L>(grid_of<L>(c, a.groups, a.B, most, equal), pieces, a, s);
+        return launch_shape<S>(g, pieces, a, s);
     });
 }
 

@@ -11,9 +11,9 @@ y_d = sum_t p_t v_td with p the softmax:
    u 2^-24, whose products are lined up as if u were 1024: each step may cut off 2^-23 of 1024 times
    the head's largest |q|, in units of the code, 2^-13 |q| s. The exponent's difference from the
    reference and its exponential add 4 u of that sum (in absolute terms: |s| is below it) and 2^-21.
- * a weight enters as a sum of terms of 16 bits: eps of it, with eps = 2^-12 for one of fp16, 2^-17
-   for two of bf16, 2^-23 for two of fp16, 2^-25 for three of bf16; in fp16 it also has no
-   bits below 2^-25, where the largest of a warp's is 2^7 at least: 2^-32 of the largest (of the
+ * a weight enters as a sum of terms of 16 bits, each off by half a step of its type from what the terms
+   before leave: eps of it, with eps = 2^-11 for one of fp16, (2^-8)^2 for two of bf16, (2^-11)^2 for two
+   of fp16, (2^-8)^3 for three of bf16; in fp16 it also has no bits below 2^-25, where the largest of a warp's is 2^7 at least: 2^-32 of the largest (of the
    sum of all weights at most) for each token.
  * each warp adds up a fourth of the tokens or fewer, 16 at a time: 2 u for each of the n / 64
    steps, and some 64 u for the joins.
@@ -96,8 +96,8 @@ def read(pages, kv, layer, table, starts, lens):
 
 def eps_of(fmt, dtype):
     if fmt == KV_BF16:
-        return 2.0 ** -17 if dtype is torch.bfloat16 else 2.0 ** -25
-    return 2.0 ** -12 if dtype is torch.bfloat16 else 2.0 ** -23
+        return 2.0 ** -16 if dtype is torch.bfloat16 else 2.0 ** -24
+    return 2.0 ** -11 if dtype is torch.bfloat16 else 2.0 ** -22
 
 
 def attend(pages, kv, layer, table, lens, q, scale, window=0):

@@ -253,12 +253,15 @@ def test_windows(fmt, window):
 
 
 @pytest.mark.parametrize("fmt", FORMATS, ids=fmt_ids)
-def test_many_rows_of_mixed_lengths(fmt):
+@pytest.mark.parametrize("D,heads,G,pt,dt", [(64, 4, 2, 16, torch.float16), (128, 3, 4, 8, torch.bfloat16), (128, 2, 1, 64, torch.float32),
+                                             (64, 2, 9, 32, torch.bfloat16), (128, 1, 16, 16, torch.bfloat16), (256, 2, 3, 32, torch.bfloat16)],
+                         ids=["64", "128", "128-f32", "64-9", "128-16", "256"])
+def test_many_rows_of_mixed_lengths(D, heads, G, pt, dt, fmt):
     """More (sequence, head) pairs than CTAs, shares that hold many sequences and parts of others."""
-    g, kv = gen(7), A.KvConfig(1, 4, 64, 16, fmt)
+    g, kv = gen(7), A.KvConfig(1, heads, D, pt, fmt)
     lens = (torch.rand(700, generator=g, device="cuda") ** 6 * 3000).int().tolist()
     table, n = tables(g, kv, lens)
-    q = torch.randn((700, 8, 64), generator=g, device="cuda").half()
+    q = torch.randn((700, heads * G, D), generator=g, device="cuda").to(dt)
     pages = normal_pages(g, kv, n)
     check(kv, pages, table, lens, q)
     check(kv, pages, table, lens, q, window=200)

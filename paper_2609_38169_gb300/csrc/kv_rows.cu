@@ -22,7 +22,7 @@ constexpr int kWarps = 4, kRows = 4;
 struct RowsArgs {
     Pages pg;
     const int32_t *starts, *cu;
-    int B, tokens;
+    int B, tokens, each;            // each: tokens a warp, where heads are few
     void *k, *v;                    // read only by the append
     int64_t ks, vs;
 };
@@ -70,15 +70,19 @@ __device__ __forceinline__ void store8(T *p, const uint64_t (&x)[4]) {
     }
 }
 
-// Where a token's rows go: its page and place, or page -1.
+// Where a token's rows go: its page and place, or page -1. Sequence b holds it, or one behind b.
 struct Place { int page, slot; };
-__device__ __forceinline__ Place place_of(const RowsArgs &a, int i, int lane) {
-    int b, first;
+__device__ __forceinline__ Place place_in(const RowsArgs &a, int b, int i, bool report) {
+    int first;
     if (a.cu) {
-        b = find_sequence(a.cu, a.B, i, lane);
         first = a.cu[b];
-        if (i < first || i >= a.cu[b + 1]) {
-            if (lane == 0 && (i < a.cu[a.B] && i >= a.cu[0])) raise_error(a.pg.err, STEPQ_ERR_ARG);
+        int next = a.cu[b + 1];
+        while (i >= next && b + 1 < a.B) {
+            first = next;
+            next = a.cu[++b + 1];
+        }
+        if (i < first || i >= next) {
+            if (report && i < a.cu[a.B] && i >= a.cu[0]) raise_error(a.pg.err, STEPQ_ERR_ARG);
             return {-1, 0};
         }
     } else {
@@ -89,12 +93,12 @@ __device__ __forceinline__ Place place_of(const RowsArgs &a, int i, int lane) {
     const int start = a.starts[b];
     const long long pos = (long long)start + (i - first);
     if (start < 0 || (pos >> a.pg.shift) >= a.pg.width) {
-        if (lane == 0) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+        if (report) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
         return {-1, 0};
     }
     const int page = a.pg.table[b * a.pg.table_stride + (pos >> a.pg.shift)];
     if (page < 0 || page >= a.pg.n_pages) {
-        if (lane == 0) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
+        if (report) raise_error(a.pg.err, STEPQ_ERR_SLOT_RANGE);
         return {-1, 0};
     }
     return {page, a.pg.slot((int)pos)};
@@ -141,6 +145,100 @@ __device__ __forceinline__ float row_magnitude(const Eight<T> &v, bool on) {
     return la::to_f32(*(const T *)&top);
 }
 
+// A lane's eight channels c of a row into the page: all lanes of a warp call it, those with `on` have a row.
+template <int F, int D, class T>
+__device__ __forceinline__ void put_row(const Eight<T> &in, bool on, uint8_t *row, uint8_t *scale, int c) {
+    constexpr int L = D / 8;
+    if (!coded(F)) {
+        using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
+        uint64_t x[4];
+        pairs(in, x);
+        if (on) store8<C>((C *)row + 8 * c, x);
+        return;
+    }
+    uint64_t x[4];
+    if (on) pairs(in, x);
+    else x[0] = x[1] = x[2] = x[3] = 0;
+    constexpr float q = F == STEPQ_KV_INT8 ? 127.f : 7.f;
+    constexpr int half = F == STEPQ_KV_INT8 ? 128 : 8;
+    float top = row_magnitude<T, L>(in, on);
+    const bool far = !(top <= 65504.f * q);
+    if (__any_sync(0xffffffffu, far)) {
+        // a scale at its bound, or values that are not finite: NaN becomes zero, the others are clamped
+        top = 0.f;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float t = e & 1 ? f2hi(x[e / 2]) : f2lo(x[e / 2]);
+            v[e] = t == t ? t : 0.f;
+            top = fmaxf(top, fabsf(v[e]));
+        }
+#pragma unroll
+        for (int o = 1; o < L; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = fminf(top, 65504.f * q);
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            x[e] = f2(fminf(fmaxf(v[2 * e], -top), top), fminf(fmaxf(v[2 * e + 1], -top), top));
+    }
+    const uint16_t sb = f16_bits(fmaxf(quotient(top, q, 1.f / q), kF16Min));
+    const float s = f16_val(sb), y = reciprocal_near(s);
+    // Quotients plus 1.5 2^23 + 2^(b-1): the sum's lowest bits are the code. |x| <= top, so that
+    // no quotient is above q by more than the scale's rounding.
+    constexpr uint32_t magic = 0x4b400000u + half;
+    uint64_t u[4];
+    const uint64_t ss = f2s(-s), yy = f2s(y);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const uint64_t t = fmul2(x[e], yy);
+        u[e] = fadd2(ffma2(ffma2(t, ss, x[e]), yy, t), f2s(12582912.f + half));
+    }
+    if (!on) return;
+    auto code = [&](int e) { return (uint32_t)(u[e >> 1] >> (32 * (e & 1))); };
+    if (F == STEPQ_KV_INT8) {
+        uint2 w;
+        w.x = __byte_perm(__byte_perm(code(0), code(1), 0x0040), __byte_perm(code(2), code(3), 0x0040), 0x5410);
+        w.y = __byte_perm(__byte_perm(code(4), code(5), 0x0040), __byte_perm(code(6), code(7), 0x0040), 0x5410);
+        ((uint2 *)row)[c] = w;
+    } else {
+        // what stands above the codes adds up to a constant (mod 2^32)
+        uint32_t w = code(7);
+#pragma unroll
+        for (int e = 6; e >= 0; e--) w = w * 16u + code(e);
+        ((uint32_t *)row)[c] = w - (magic - half) * 0x11111111u;
+    }
+    if (c == 0) *(uint16_t *)scale = sb;
+}
+
+// And back: eight channels as they lie in the page, to dst.
+template <int F> using Held = la::Vec<uint32_t, bits_of(F) / 4>;
+template <int F, class T>
+__device__ __forceinline__ void take_row(const Held<F> &w, uint16_t scale, T *dst) {
+    using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
+    uint64_t x[4];
+    if constexpr (!coded(F)) {
+        pairs(*(const Eight<C> *)&w, x);
+    } else {
+        // 2^23 + u 2^k less 2^23 + 2^(b-1) 2^k is exact, and so is s 2^-k
+        const float s = f16_val(scale);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            if constexpr (F == STEPQ_KV_INT8) {
+                const uint32_t v = w.e[e / 2];
+                x[e] = u2pair(__byte_perm(v, 0x4b000000u, 0x7650 + 2 * (e & 1)), __byte_perm(v, 0x4b000000u, 0x7651 + 2 * (e & 1)));
+                x[e] = fmul2(fadd2(x[e], f2s(-8388736.f)), f2s(s));
+            } else {
+                const uint32_t v = e < 2 ? w.e[0] : w.e[0] >> 16;
+                constexpr float pow16[4] = {1.f, 16.f, 256.f, 4096.f};
+                const int k = 2 * (e & 1);
+                x[e] = u2pair(and_or(v, 15u << (4 * k), 0x4b000000u), and_or(v, 240u << (4 * k), 0x4b000000u));
+                x[e] = fadd2(x[e], f2(-8388608.f - 8.f * pow16[k], -8388608.f - 8.f * pow16[k + 1]));
+                x[e] = fmul2(x[e], f2(s * (1.f / pow16[k]), s * (1.f / pow16[k + 1])));
+            }
+        }
+    }
+    store8<T>(dst, x);
+}
+
 // A lane's rows: token i, K or V (part), heads h0 + n * PER, channels 8 c on.
 template <int D>
 struct Mine {
@@ -152,6 +250,9 @@ struct Mine {
         c = lane % L;
         part = blockIdx.y & 1;
         h0 = (blockIdx.y >> 1) * PER * kRows + lane / L;
+    }
+    __device__ __forceinline__ Place place(const RowsArgs &a) const {
+        return place_in(a, a.cu ? find_sequence(a.cu, a.B, i, lane) : 0, i, lane == 0);
     }
 };
 
@@ -167,125 +268,114 @@ __global__ void __launch_bounds__(32 * kWarps) kv_append_kernel(RowsArgs a) {
 #pragma unroll
     for (int n = 0; n < kRows; n++)
         if (m.h0 + n * m.PER < a.pg.n_heads) in[n] = *(const Eight<T> *)(src + n * m.PER * D);
-    const Place p = place_of(a, m.i, m.lane);
+    const Place p = m.place(a);
     if (p.page < 0) return;
     uint8_t *seg = a.pg.at(p.page, m.h0);
     const int pt = 1 << a.pg.shift, at = (m.part * pt + p.slot) * RB, at_scale = 2 * pt * RB + 2 * (m.part * pt + p.slot);
 #pragma unroll
     for (int n = 0; n < kRows; n++, seg += m.PER * a.pg.segment) {
-        const bool on = m.h0 + n * m.PER < a.pg.n_heads;
-        if (!coded(F)) {
-            if (!on) return;
-            using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
-            uint64_t x[4];
-            pairs(in[n], x);
-            store8<C>((C *)(seg + at) + 8 * m.c, x);
-            continue;
-        }
         if (m.h0 - m.lane / m.L + n * m.PER >= a.pg.n_heads) return;         // no lane has a row
-        uint64_t x[4];
-        if (on) pairs(in[n], x);
-        else x[0] = x[1] = x[2] = x[3] = 0;
-        constexpr float q = F == STEPQ_KV_INT8 ? 127.f : 7.f;
-        constexpr int half = F == STEPQ_KV_INT8 ? 128 : 8;
-        float top = row_magnitude<T, Mine<D>::L>(in[n], on);
-        const bool far = !(top <= 65504.f * q);
-        if (__any_sync(0xffffffffu, far)) {
-            // a scale at its bound, or values that are not finite: NaN becomes zero, the others are clamped
-            top = 0.f;
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float t = e & 1 ? f2hi(x[e / 2]) : f2lo(x[e / 2]);
-                v[e] = t == t ? t : 0.f;
-                top = fmaxf(top, fabsf(v[e]));
-            }
-#pragma unroll
-            for (int o = 1; o < m.L; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            top = fminf(top, 65504.f * q);
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                x[e] = f2(fminf(fmaxf(v[2 * e], -top), top), fminf(fmaxf(v[2 * e + 1], -top), top));
-        }
-        const uint16_t sb = f16_bits(fmaxf(quotient(top, q, 1.f / q), kF16Min));
-        const float s = f16_val(sb), y = reciprocal_near(s);
-        // Quotients plus 1.5 2^23 + 2^(b-1): the sum's lowest bits are the code. |x| <= top, so that
-        // no quotient is above q by more than the scale's rounding.
-        constexpr uint32_t magic = 0x4b400000u + half;
-        uint64_t u[4];
-        const uint64_t ss = f2s(-s), yy = f2s(y);
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const uint64_t t = fmul2(x[e], yy);
-            u[e] = fadd2(ffma2(ffma2(t, ss, x[e]), yy, t), f2s(12582912.f + half));
-        }
-        if (!on) continue;
-        auto code = [&](int e) { return (uint32_t)(u[e >> 1] >> (32 * (e & 1))); };
-        if (F == STEPQ_KV_INT8) {
-            uint2 w;
-            w.x = __byte_perm(__byte_perm(code(0), code(1), 0x0040), __byte_perm(code(2), code(3), 0x0040), 0x5410);
-            w.y = __byte_perm(__byte_perm(code(4), code(5), 0x0040), __byte_perm(code(6), code(7), 0x0040), 0x5410);
-            ((uint2 *)(seg + at))[m.c] = w;
-        } else {
-            // what stands above the codes adds up to a constant (mod 2^32)
-            uint32_t w = code(7);
-#pragma unroll
-            for (int e = 6; e >= 0; e--) w = w * 16u + code(e);
-            ((uint32_t *)(seg + at))[m.c] = w - (magic - half) * 0x11111111u;
-        }
-        if (m.c == 0) *(uint16_t *)(seg + at_scale) = sb;
+        put_row<F, D, T>(in[n], m.h0 + n * m.PER < a.pg.n_heads, seg + at, seg + at_scale, m.c);
     }
 }
 
 template <int F, int D, class T>
 __global__ void __launch_bounds__(32 * kWarps) kv_read_kernel(RowsArgs a) {
     constexpr int RB = row_bytes(F, D);
-    using C = typename std::conditional<F == STEPQ_KV_BF16, la::bf16, la::f16>::type;
-    using W = la::Vec<uint32_t, bits_of(F) / 4>;             // eight channels
     const Mine<D> m;
     griddep_wait();
     griddep_launch();
     if (m.i >= a.tokens) return;
-    const Place p = place_of(a, m.i, m.lane);
+    const Place p = m.place(a);
     if (p.page < 0) return;
     const uint8_t *seg = a.pg.at(p.page, m.h0);
     const int pt = 1 << a.pg.shift, at = (m.part * pt + p.slot) * RB, at_scale = 2 * pt * RB + 2 * (m.part * pt + p.slot);
-    W w[kRows];
+    Held<F> w[kRows];
     uint16_t sb[kRows];
 #pragma unroll
     for (int n = 0; n < kRows; n++, seg += m.PER * a.pg.segment)
         if (m.h0 + n * m.PER < a.pg.n_heads) {
-            w[n] = ((const W *)(seg + at))[m.c];
+            w[n] = ((const Held<F> *)(seg + at))[m.c];
             if (coded(F)) sb[n] = *(const uint16_t *)(seg + at_scale);
         }
     T *dst = (T *)(m.part ? a.v : a.k) + m.i * (m.part ? a.vs : a.ks) + m.h0 * D + 8 * m.c;
 #pragma unroll
     for (int n = 0; n < kRows; n++) {
         if (m.h0 + n * m.PER >= a.pg.n_heads) return;
-        uint64_t x[4];
-        if (!coded(F)) {
-            pairs(*(const Eight<C> *)&w[n], x);
-        } else {
-            // 2^23 + u 2^k less 2^23 + 2^(b-1) 2^k is exact, and so is s 2^-k
-            const float s = f16_val(sb[n]);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                if constexpr (F == STEPQ_KV_INT8) {
-                    const uint32_t v = w[n].e[e / 2];
-                    x[e] = u2pair(__byte_perm(v, 0x4b000000u, 0x7650 + 2 * (e & 1)), __byte_perm(v, 0x4b000000u, 0x7651 + 2 * (e & 1)));
-                    x[e] = fmul2(fadd2(x[e], f2s(-8388736.f)), f2s(s));
-                } else {
-                    const uint32_t v = e < 2 ? w[n].e[0] : w[n].e[0] >> 16;
-                    constexpr float pow16[4] = {1.f, 16.f, 256.f, 4096.f};
-                    const int k = 2 * (e & 1);
-                    x[e] = u2pair(and_or(v, 15u << (4 * k), 0x4b000000u), and_or(v, 240u << (4 * k), 0x4b000000u));
-                    x[e] = fadd2(x[e], f2(-8388608.f - 8.f * pow16[k], -8388608.f - 8.f * pow16[k + 1]));
-                    x[e] = fmul2(x[e], f2(s * (1.f / pow16[k]), s * (1.f / pow16[k + 1])));
-                }
-            }
-        }
-        store8<T>(dst + n * m.PER * D, x);
+        take_row<F, T>(w[n], sb[n], dst + n * m.PER * D);
     }
+}
+
+// The same for prompts where heads are so few that they would leave half of a warp without a row: a
+// warp takes a.each tokens, rows n * PER + lane / L of their (token, head). 44,691 tokens of one head
+// into 4 bits and back 30 us, a token a warp 50.
+template <int D>
+struct Few {
+    static constexpr int L = D / 8, PER = 32 / L;
+    int c, part, token[kRows], head[kRows];
+    bool on[kRows];
+    Place p[kRows];
+    __device__ __forceinline__ Few(const RowsArgs &a) {
+        const int lane = threadIdx.x & 31, first = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * a.each, H = a.pg.n_heads;
+        c = lane % L;
+        part = blockIdx.y;
+        const int b = a.cu ? find_sequence(a.cu, a.B, min(first, a.tokens - 1), lane) : 0;
+#pragma unroll
+        for (int n = 0; n < kRows; n++) {
+            const int row = n * PER + lane / L;
+            token[n] = first + row / H;
+            head[n] = row % H;
+            on[n] = row < a.each * H && token[n] < a.tokens;
+            p[n] = {-1, 0};
+            if (on[n]) p[n] = place_in(a, b, token[n], c == 0);
+            on[n] = p[n].page >= 0;
+        }
+    }
+};
+
+template <int F, int D, class T>
+__global__ void __launch_bounds__(32 * kWarps) kv_append_few_kernel(RowsArgs a) {
+    constexpr int RB = row_bytes(F, D);
+    griddep_wait();
+    griddep_launch();
+    const Few<D> m(a);
+    const T *src = (const T *)(m.part ? a.v : a.k) + 8 * m.c;
+    const int64_t stride = m.part ? a.vs : a.ks;
+    Eight<T> in[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; n++)
+        if (m.on[n]) in[n] = *(const Eight<T> *)(src + m.token[n] * stride + m.head[n] * D);
+    const int pt = 1 << a.pg.shift;
+#pragma unroll
+    for (int n = 0; n < kRows; n++) {
+        uint8_t *seg = m.on[n] ? a.pg.at(m.p[n].page, m.head[n]) : a.pg.base;
+        const int at = m.part * pt + m.p[n].slot;
+        put_row<F, D, T>(in[n], m.on[n], seg + at * RB, seg + 2 * pt * RB + 2 * at, m.c);
+    }
+}
+
+template <int F, int D, class T>
+__global__ void __launch_bounds__(32 * kWarps) kv_read_few_kernel(RowsArgs a) {
+    constexpr int RB = row_bytes(F, D);
+    griddep_wait();
+    griddep_launch();
+    const Few<D> m(a);
+    const int pt = 1 << a.pg.shift;
+    Held<F> w[kRows];
+    uint16_t sb[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; n++)
+        if (m.on[n]) {
+            const uint8_t *seg = a.pg.at(m.p[n].page, m.head[n]);
+            const int at = m.part * pt + m.p[n].slot;
+            w[n] = ((const Held<F> *)(seg + at * RB))[m.c];
+            if (coded(F)) sb[n] = *(const uint16_t *)(seg + 2 * pt * RB + 2 * at);
+        }
+    T *dst = (T *)(m.part ? a.v : a.k) + 8 * m.c;
+    const int64_t stride = m.part ? a.vs : a.ks;
+#pragma unroll
+    for (int n = 0; n < kRows; n++)
+        if (m.on[n]) take_row<F, T>(w[n], sb[n], dst + m.token[n] * stride + m.head[n] * D);
 }
 
 // Runs f(format) with the pages' format as a compile-time constant.
@@ -320,12 +410,18 @@ stepq_status launch_kv_rows(bool append, const stepq_kv_config *cfg, int layer, 
     a.B = B;
     a.tokens = tokens;
     a.k = rows->k; a.v = rows->v; a.ks = rows->k_stride; a.vs = rows->v_stride;
-    const int per_warp = kv::kRows * 256 / cfg->head_dim;
-    const dim3 grid((unsigned)((tokens + kv::kWarps - 1) / kv::kWarps), 2 * ((cfg->n_heads + per_warp - 1) / per_warp));
+    const int at_once = 256 / cfg->head_dim, per_warp = kv::kRows * at_once;
+    const bool few = 2 * cfg->n_heads <= at_once && tokens >= 8192;      // enough to fill the GPU
+    a.each = few ? per_warp / cfg->n_heads : 1;
+    const dim3 grid((unsigned)((tokens + (int64_t)a.each * kv::kWarps - 1) / (a.each * kv::kWarps)),
+                    2 * ((cfg->n_heads + per_warp - 1) / per_warp));
     return kv::by_layout(cfg, [&](auto f, auto d) {
         return la::by_type(rows->dtype, [&](auto t) {
-            auto *kernel = append ? kv::kv_append_kernel<decltype(f)::value, decltype(d)::value, decltype(t)>
-                                  : kv::kv_read_kernel<decltype(f)::value, decltype(d)::value, decltype(t)>;
+            constexpr int F = decltype(f)::value, D = decltype(d)::value;
+            using T = decltype(t);
+            auto *kernel = append ? kv::kv_append_kernel<F, D, T> : kv::kv_read_kernel<F, D, T>;
+            if constexpr (D <= 128)
+                if (few) kernel = append ? kv::kv_append_few_kernel<F, D, T> : kv::kv_read_few_kernel<F, D, T>;
             return launch_overlapped(kernel, grid, 32 * kv::kWarps, 0, s, a);
         });
     });

@@ -160,6 +160,45 @@ def test_equal_lengths_and_many_sequences(fmt):
         assert torch.equal(pages, want)
 
 
+@pytest.mark.parametrize("fmt,dt", [(A.KV_BF16, torch.float32), (A.KV_INT8, torch.float16), (A.KV_INT4, torch.bfloat16)],
+                         ids=["bf16", "int8", "int4"])
+@pytest.mark.parametrize("D,heads", [(64, 1), (64, 2), (128, 1)])
+def test_long_prompts_of_few_heads(D, heads, fmt, dt):
+    """More than 8,192 tokens, several a warp: odd lengths, empty sequences in a row, bad places among them."""
+    g, kv = gen(4), A.KvConfig(1, heads, D, 8, fmt)
+    lens = [3001, 0, 0, 1, 2, 0, 4997, 3, 0, 700, 1, 1, 1, 513]
+    starts = torch.randint(0, 30, (len(lens),), generator=g, device="cuda").tolist()
+    table, n = tables(g, kv, [a + m for a, m in zip(starts, lens)])
+    pages = normal_pages(g, kv, n)
+    k, v = torch.randn((2, sum(lens) + 5, heads, D), generator=g, device="cuda").to(dt)
+    cu = i32([sum(lens[:b]) for b in range(len(lens) + 1)])
+    want = pages.clone()
+    R.append(want, kv, 0, table, starts, lens, k[:sum(lens)], v[:sum(lens)])
+    A.stepq_kv_append(kv, 0, pages, table, i32(starts), k, v, cu_seqlens=cu)
+    assert torch.equal(pages, want)
+    out = torch.full((2, len(k), heads, D), 7.0, dtype=dt, device="cuda")
+    A.stepq_kv_read(kv, 0, pages, table, i32(starts), *out, cu_seqlens=cu)
+    wk, wv, _ = R.read(pages, kv, 0, table, starts, lens)
+    for o, w in zip(out, (wk, wv)):
+        assert torch.equal(o[:sum(lens)], w.float().to(dt)) and bool((o[sum(lens):] == 7).all())
+    # a page out of range, a negative start: their tokens are skipped
+    t, s = table.clone(), list(starts)
+    t[6, 100], s[9] = n, -5
+    got = torch.full_like(out, 7.0)
+    A.stepq_kv_read(kv, 0, pages, t, i32(s), *got, cu_seqlens=cu)
+    assert A.stepq_device_error() == 2
+    skip = torch.zeros(len(k), dtype=torch.bool, device="cuda")
+    first = sum(lens[:6]) + 800 - starts[6]
+    skip[first:first + 8] = True
+    skip[sum(lens[:9]):sum(lens[:10])] = True
+    assert torch.equal(got[:, ~skip], out[:, ~skip]) and bool((got[:, skip] == 7).all())
+    # equal lengths
+    A.stepq_kv_read(kv, 0, pages, table[6:7], i32([2]), *out[:, :4990].unbind(0))
+    A.stepq_kv_read(kv, 0, pages, table[[0, 6, 6]], i32([0, 0, 3]), *(x := torch.empty((2, 9000, heads, D), dtype=dt, device="cuda")))
+    wk, wv, _ = R.read(pages, kv, 0, table[[0, 6, 6]], [0, 0, 3], [3000] * 3)
+    assert torch.equal(x[0], wk.float().to(dt)) and torch.equal(x[1], wv.float().to(dt))
+
+
 @pytest.mark.parametrize("fmt", [A.KV_BF16, A.KV_INT4], ids=["bf16", "int4"])
 def test_bad_places_are_reported_and_skipped(fmt):
     g, kv = gen(2), A.KvConfig(1, 2, 64, 16, fmt)

@@ -1016,75 +1016,113 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     }
 }
 
-// Joins the parts of piece blockIdx.x, head blockIdx.y: a warp takes every eighth part, a lane
-// D / 32 channels. The first parts are on their way before the weights are known.
+// Joins the parts of piece blockIdx.x: of head blockIdx.y, a warp every eighth part, whose first are on
+// their way before the weights are known; or where pieces are MANY (gridDim.y = 1) and have few
+// parts, a head a warp (256 x 8,191 tokens of 8 key heads in 4 bits, both kernels: 372 us with a CTA for
+// every head of every piece, 365 so).
 constexpr int kJoinWarps = 8, kJoinAhead = 6, kMostParts = 1024;
-template <int HT, int D, bool WIDE>
+template <int D>
+struct JoinLane {
+    static constexpr int N = D / 32, V = N < 4 ? N : 4;      // a lane's channels, of them side by side
+    la::Vec<float, V> v[N / V];
+    static __device__ __forceinline__ int channel(int e, int l) { return V * (32 * (e / V) + l) + e % V; }
+    __device__ __forceinline__ JoinLane(const float *p, int l) {
+#pragma unroll
+        for (int e = 0; e < N / V; e++) v[e] = ((const la::Vec<float, V> *)p)[32 * e + l];
+    }
+    __device__ __forceinline__ JoinLane() {}
+    __device__ __forceinline__ void add_to(float (&o)[N], float k) const {
+#pragma unroll
+        for (int e = 0; e < N; e++) o[e] = fmaf(k, v[e / V].e[e % V], o[e]);
+    }
+};
+template <int HT, int D, bool WIDE, bool MANY>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, int ctas) {
     __shared__ float os[kJoinWarps][D], weight[kMostParts], red[2][kJoinWarps];
-    const int tid = threadIdx.x, w = tid >> 5, l = tid & 31, h = blockIdx.y;
+    const int tid = threadIdx.x, w = tid >> 5, l = tid & 31;
     griddep_wait();
     griddep_launch();
     const Joined j = ((const Joined *)(a.parts + (size_t)2 * ctas * part_floats<HT, D>()))[blockIdx.x];
     if (j.count == 0) return;
     const int chunks = (a.groups + HT - 1) / HT, g0 = j.vh % chunks * HT;
-    if (h >= a.groups - g0) return;
+    const int nh = min(HT, a.groups - g0), h0 = j.vh / chunks * a.groups + g0;
     auto part = [&](int i) {
         return a.parts + (size_t)(i == 0 ? j.first : 2 * ((j.first >> 1) + i)) * part_floats<HT, D>();
     };
-    constexpr int N = D / 32, V = N < 4 ? N : 4;             // a lane's channels, of them side by side
-    struct Lane { la::Vec<float, V> v[N / V]; };
-    auto load = [&](int i) {
-        Lane x;
+    constexpr int N = JoinLane<D>::N;
+    if (MANY && j.count <= kJoinWarps) {
+        for (int h = w; h < nh; h += kJoinWarps) {
+            JoinLane<D> first(part(0) + h * D, l), second(part(1) + h * D, l);       // there are two at least
+            const float *x = part(min(l, j.count - 1));
+            const float R = l < j.count ? x[HT * D + h] : kLow;
+            float top = R;
 #pragma unroll
-        for (int e = 0; e < N / V; e++) x.v[e] = ((const la::Vec<float, V> *)(part(i) + h * D))[32 * e + l];
-        return x;
-    };
-    Lane ahead[kJoinAhead];
+            for (int o = 1; o < kJoinWarps; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = __shfl_sync(0xffffffffu, top, 0);
+            const float k = exp2_fast(R - top);
+            float total = l < j.count ? k * x[HT * D + HT + h] : 0.f, o[N] = {};
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; i++)
-        if (w + i * kJoinWarps < j.count) ahead[i] = load(w + i * kJoinWarps);
-    float top = kLow, total = 0.f;
-    for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
-        weight[i] = part(i)[HT * D + h];
-        top = fmaxf(top, weight[i]);
-    }
+            for (int s = 1; s < kJoinWarps; s *= 2) total += __shfl_xor_sync(0xffffffffu, total, s);
+            total = __shfl_sync(0xffffffffu, total, 0);
+            first.add_to(o, __shfl_sync(0xffffffffu, k, 0));
+            second.add_to(o, __shfl_sync(0xffffffffu, k, 1));
+            for (int i = 2; i < j.count; i++) JoinLane<D>(part(i) + h * D, l).add_to(o, __shfl_sync(0xffffffffu, k, i));
+            // a lane's channels come together through shared memory, four side by side
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (l == 0) red[0][w] = top;
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < kJoinWarps; x++) top = fmaxf(top, red[0][x]);
-    for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
-        weight[i] = exp2_fast(weight[i] - top);
-        total = fmaf(weight[i], part(i)[HT * D + HT + h], total);
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (l == 0) red[1][w] = total;
-    __syncthreads();
-    float o[N] = {};
-    auto add = [&](const Lane &x, float k) {
-#pragma unroll
-        for (int e = 0; e < N; e++) o[e] = fmaf(k, x.v[e / V].e[e % V], o[e]);
-    };
-#pragma unroll
-    for (int i = 0; i < kJoinAhead; i++)
-        if (w + i * kJoinWarps < j.count) add(ahead[i], weight[w + i * kJoinWarps]);
-#pragma unroll 4
-    for (int i = w + kJoinAhead * kJoinWarps; i < j.count; i += kJoinWarps) add(load(i), weight[i]);
-#pragma unroll
-    for (int e = 0; e < N; e++) os[w][V * (32 * (e / V) + l) + e % V] = o[e];
-    __syncthreads();
-    for (int d = 4 * tid; d < D; d += 4 * 32 * kJoinWarps) {
-        float sum = 0.f, y[4] = {};
-#pragma unroll
-        for (int x = 0; x < kJoinWarps; x++) {
-            sum += red[1][x];
-#pragma unroll
-            for (int e = 0; e < 4; e++) y[e] += os[x][d + e];
+            for (int e = 0; e < N; e++) os[w][JoinLane<D>::channel(e, l)] = o[e];
+            __syncwarp();
+            for (int d = 4 * l; d < D; d += 128) {
+                const float4 v = *(const float4 *)&os[w][d];
+                float y[4] = {v.x, v.y, v.z, v.w};
+                put_output<WIDE>(a, j.b, h0 + h, d, top, total, y, D);
+            }
+            __syncwarp();
         }
-        put_output<WIDE>(a, j.b, j.vh / chunks * a.groups + g0 + h, d, top, sum, y, D);
+        return;
+    }
+    for (int h = blockIdx.y; h < nh; h += MANY ? 1 : HT) {
+        JoinLane<D> ahead[kJoinAhead];
+#pragma unroll
+        for (int i = 0; i < kJoinAhead; i++)
+            if (w + i * kJoinWarps < j.count) ahead[i] = JoinLane<D>(part(w + i * kJoinWarps) + h * D, l);
+        float top = kLow, total = 0.f, o[N] = {};
+        for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
+            weight[i] = part(i)[HT * D + h];
+            top = fmaxf(top, weight[i]);
+        }
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        if (l == 0) red[0][w] = top;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < kJoinWarps; x++) top = fmaxf(top, red[0][x]);
+        for (int i = tid; i < j.count; i += 32 * kJoinWarps) {
+            weight[i] = exp2_fast(weight[i] - top);
+            total = fmaf(weight[i], part(i)[HT * D + HT + h], total);
+        }
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) total += __shfl_xor_sync(0xffffffffu, total, s);
+        if (l == 0) red[1][w] = total;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kJoinAhead; i++)
+            if (w + i * kJoinWarps < j.count) ahead[i].add_to(o, weight[w + i * kJoinWarps]);
+#pragma unroll 4
+        for (int i = w + kJoinAhead * kJoinWarps; i < j.count; i += kJoinWarps) JoinLane<D>(part(i) + h * D, l).add_to(o, weight[i]);
+#pragma unroll
+        for (int e = 0; e < N; e++) os[w][JoinLane<D>::channel(e, l)] = o[e];
+        __syncthreads();
+        for (int d = 4 * tid; d < D; d += 4 * 32 * kJoinWarps) {
+            float sum = 0.f, y[4] = {};
+#pragma unroll
+            for (int x = 0; x < kJoinWarps; x++) {
+                sum += red[1][x];
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] += os[x][d + e];
+            }
+            put_output<WIDE>(a, j.b, h0 + h, d, top, sum, y, D);
+        }
+        __syncthreads();                                     // before the next head's
     }
 }
 

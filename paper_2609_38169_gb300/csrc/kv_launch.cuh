@@ -91,8 +91,10 @@ stepq_status launch_shape(const Grid &g, int64_t pieces, AttendArgs a, cudaStrea
     if (st != STEPQ_OK) return st;
     st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
     if (st != STEPQ_OK || g.cluster) return st;
-    return launch_overlapped(kv_join_kernel<S::HT, S::D, S::WIDE>, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, S::HT),
-                             32 * kJoinWarps, 0, s, a, g.ctas);
+    const bool many = pieces * S::HT > 8 * sm_count();
+    auto *join = many ? kv_join_kernel<S::HT, S::D, S::WIDE, true> : kv_join_kernel<S::HT, S::D, S::WIDE, false>;
+    return launch_overlapped(join, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, many ? 1 : S::HT), 32 * kJoinWarps, 0,
+                             s, a, g.ctas);
 }
 
 template <int F>

@@ -25,13 +25,12 @@
 // rate; 128 x 4,096 in 8 bits 171 us, 6.4 TB/s; 64 ragged sequences of 131,072 in bf16 90 us, 6.0 TB/s, 4 us
 // of which pass before the first tile is asked for and 4 in the second kernel; 37 tokens 4.1 us.
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
-// row and the queries are laid out to match. Codes become fp16 exactly. Where outputs are bf16 those of
+// row and the queries are laid out to match. Codes become fp16 exactly. Where outputs have 16 bits those of
 // K enter as they are, u 2^-24 (a mask or a byte permute leaves a subnormal number), and their offset
 // 2^(b-1) sum q is subtracted from the sum; the tensor cores line products up by the exponents of normal
 // numbers, which cuts such sums off after some 17 bits (4 bits) or 21 (8 bits).
 //
-// Roundings: q enters as a sum of QT terms of the cache's 16-bit type, weights as a sum of PT,
-// everything between in fp32: see Variant.
+// Between the products (whose factors are sums of 16-bit terms, see Shape) everything is fp32.
 #pragma once
 
 #include <type_traits>
@@ -58,11 +57,22 @@ template <int F> struct Compute { using T = la::f16; };
 template <> struct Compute<STEPQ_KV_BF16> { using T = la::bf16; };
 
 // Shape of a variant. LARGE: of calls whose warps take many tiles (codes of up to 128 head channels).
-template <int F_, int D_, int NT_, int QT_, int PT_, bool LARGE_ = false>
+// Queries and weights enter the products as sums of QT and PT terms of the pages' 16-bit type (fp16 for
+// codes), as many as the vectors' type T asks for:
+//  * queries of bf16 and fp16 are one term of fp16 exactly, of bf16 one or two; of fp32 two of fp16
+//    are within 2^-22, three of bf16 within 2^-24.
+//  * outputs in bf16: a weight's one term of fp16 is within 2^-11, an eighth of the output's own rounding;
+//    of bf16 it would have that rounding again, and two are within 2^-16. Outputs in fp16 take two terms
+//    of either; in fp32 two of fp16, three of bf16.
+template <int F_, int D_, int NT_, class T_, bool LARGE_ = false>
 struct Shape {
+    using T = T_;
     static constexpr bool LARGE = LARGE_;
-    using Larger = Shape<F_, D_, NT_, QT_, PT_, coded(F_) && NT_ * D_ <= 128>;
-    static constexpr int F = F_, D = D_, NT = NT_, QT = QT_, PT = PT_;
+    using Larger = Shape<F_, D_, NT_, T_, coded(F_) && NT_ * D_ <= 128>;
+    static constexpr int F = F_, D = D_, NT = NT_;
+    static constexpr bool BF16 = std::is_same<T, la::bf16>::value, WIDE = std::is_same<T, float>::value;
+    static constexpr int QT = F == STEPQ_KV_BF16 ? (BF16 ? 1 : WIDE ? 3 : 2) : (WIDE ? 2 : 1);
+    static constexpr int PT = F == STEPQ_KV_BF16 ? (WIDE ? 3 : 2) : (BF16 ? 1 : 2);
     static constexpr int HT = 8 * NT;                        // heads of a CTA
     static constexpr int RB = row_bytes(F, D);
     static constexpr bool CODED = coded(F);
@@ -82,7 +92,7 @@ struct Shape {
     static constexpr int OFF_PART = (OFF_SCAN + 8 * (kAttWarps + 3) + 15) / 16 * 16;
     static constexpr int OFF_RING = (OFF_PART + (HT * (kParts + 2) + kParts) * 4 + kAttWarps * 512 + 127) / 128 * 128;
     // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
-    static constexpr int BY_REGS = NT * D >= 256 ? 2 : CODED && QT == 1 && !LARGE ? 4 : 3;
+    static constexpr int BY_REGS = NT * D >= 256 ? 2 : 3;
     static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
     static constexpr int resident(int stages) {
         const int n = 227 * 1024 / (smem(stages) + 1024);
@@ -96,7 +106,6 @@ struct Shape {
     static constexpr int MT = D / 16;                        // row tiles of V's
     static constexpr bool QREG = QT * NT * KS <= 16;         // queries kept in registers
     using C = typename Compute<F>::T;
-    static constexpr bool WIDE = QT > 1;                     // fp32 and fp16 vectors; else bf16
     static constexpr bool RAW = CODED && !WIDE;              // K's codes enter with their offset, at 2^-24
 };
 
@@ -141,7 +150,7 @@ __device__ __forceinline__ float2 unpack(uint32_t v, la::f16) {
     return __half22float2(*(const __half2 *)&v);
 }
 // d += A B for the terms B[t] of a right factor. The tensor cores' sums are cut off, not rounded, which adds up
-// over many steps: for outputs of more than 16 bits (WIDE) each product's own sum, the smallest term
+// over many steps: for fp32 outputs (WIDE) each product's own sum, the smallest term
 // first, is added with rounding.
 template <class C, bool WIDE, int T, class Term>
 __device__ __forceinline__ void mma_terms(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, Term &&term) {
@@ -351,9 +360,7 @@ struct Queries {
     }
     __device__ __forceinline__ void load(const AttendArgs &a, int b, int h0, int nh, int w, int l) {
         const int64_t at = b * a.qs + (int64_t)h0 * S::D;
-        if (!S::WIDE) load_as((const la::bf16 *)a.q + at, nh, w, l);
-        else if (a.dtype == STEPQ_F32) load_as((const float *)a.q + at, nh, w, l);
-        else load_as((const la::f16 *)a.q + at, nh, w, l);
+        load_as((const typename S::T *)a.q + at, nh, w, l);
     }
     // To shared memory as pairs in the order of K's pieces: of step ks of the product, pair (0, 1)
     // of lane 4 head + c; with each head's factor of the scores and the offset of the codes.
@@ -412,15 +419,13 @@ struct Queries {
 };
 
 // Channels d .. d + 3 of query head h from the sums o of weighted values and `total` of weights.
-template <bool WIDE>
+template <class T>
 __device__ __forceinline__ void put_output(const AttendArgs &a, int b, int h, int d, float top, float total, float (&o)[4], int D) {
     const float f = total != 0.f ? 1.f / total : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] = total != 0.f ? o[e] * f : 0.f;
     const int64_t at = b * a.ys + (int64_t)h * D + d;
-    if (!WIDE) la::store_vec<la::bf16, 4>((la::bf16 *)a.y + at, o);
-    else if (a.dtype == STEPQ_F32) la::store_vec<float, 4>((float *)a.y + at, o);
-    else la::store_vec<la::f16, 4>((la::f16 *)a.y + at, o);
+    la::store_vec<T, 4>((T *)a.y + at, o);
     if (a.lse && d == 0) a.lse[(int64_t)b * a.hq + h] = total != 0.f ? (top + log2f(total)) * 0.693147181f : -INFINITY;
 }
 
@@ -671,7 +676,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             // the warps' parts of the piece before
             auto leave = [&](int h, int d, float top, float total, float(&o)[4]) {
                 if (out.all) {
-                    put_output<S::WIDE>(a, out.b, out.h0 + h, d, top, total, o, D);
+                    put_output<typename S::T>(a, out.b, out.h0 + h, d, top, total, o, D);
                 } else {
                     *(float4 *)(out.part + h * D + d) = make_float4(o[0], o[1], o[2], o[3]);
                     if (d == 0) {
@@ -1040,7 +1045,7 @@ struct JoinLane {
         for (int e = 0; e < N; e++) o[e] = fmaf(k, v[e / V].e[e % V], o[e]);
     }
 };
-template <int HT, int D, bool WIDE, bool MANY>
+template <int HT, int D, class T, bool MANY>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, int ctas) {
     __shared__ float os[kJoinWarps][D], weight[kMostParts], red[2][kJoinWarps];
     const int tid = threadIdx.x, w = tid >> 5, l = tid & 31;
@@ -1078,7 +1083,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
             for (int d = 4 * l; d < D; d += 128) {
                 const float4 v = *(const float4 *)&os[w][d];
                 float y[4] = {v.x, v.y, v.z, v.w};
-                put_output<WIDE>(a, j.b, h0 + h, d, top, total, y, D);
+                put_output<T>(a, j.b, h0 + h, d, top, total, y, D);
             }
             __syncwarp();
         }
@@ -1124,7 +1129,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
 #pragma unroll
                 for (int e = 0; e < 4; e++) y[e] += os[x][d + e];
             }
-            put_output<WIDE>(a, j.b, h0 + h, d, top, sum, y, D);
+            put_output<T>(a, j.b, h0 + h, d, top, sum, y, D);
         }
         __syncthreads();                                     // before the next head's
     }

@@ -6,26 +6,17 @@
 namespace stepq {
 namespace kv {
 
-// Terms of a variant: queries and weights enter the products as sums of QT and PT terms of the
-// pages' 16-bit type.
-//  * bf16 vectors over fp16 and codes: a query of 8 bits is one term of fp16, exactly; a
-//    weight's one term is within 2^-11, an eighth of the output's own rounding.
-//  * bf16 vectors over bf16: one term of a weight would have the output's own rounding again, two
-//    are within 2^-16.
-//  * fp16 and fp32 vectors: two terms of fp16 (2^-22), three of bf16 (2^-24); fp16 queries need
-//    one and two of them, and take the fp32 variant.
-template <int F, int D, int NT, bool WIDE>
-using Variant = Shape<F, D, NT, F == STEPQ_KV_BF16 ? (WIDE ? 3 : 1) : (WIDE ? 2 : 1), F == STEPQ_KV_BF16 ? (WIDE ? 3 : 2) : (WIDE ? 2 : 1)>;
-
 // Runs f(Shape{}) for the variant of a call; more than 8 query heads a key head go in sixteens.
 template <int F, class Fn>
-auto by_shape(int head_dim, int groups, bool wide, Fn &&f) {
-    auto terms = [&](auto d, auto nt) {
+auto by_shape(int head_dim, int groups, int dtype, Fn &&f) {
+    auto types = [&](auto d, auto nt) {
         constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-        return wide ? f(Variant<F, D, NT, true>{}) : f(Variant<F, D, NT, false>{});
+        return dtype == STEPQ_F32    ? f(Shape<F, D, NT, float>{})
+               : dtype == STEPQ_BF16 ? f(Shape<F, D, NT, la::bf16>{})
+                                     : f(Shape<F, D, NT, la::f16>{});
     };
     auto heads = [&](auto d) {
-        return groups > 8 ? terms(d, std::integral_constant<int, 2>{}) : terms(d, std::integral_constant<int, 1>{});
+        return groups > 8 ? types(d, std::integral_constant<int, 2>{}) : types(d, std::integral_constant<int, 1>{});
     };
     return head_dim == 64    ? heads(std::integral_constant<int, 64>{})
            : head_dim == 128 ? heads(std::integral_constant<int, 128>{})
@@ -71,13 +62,14 @@ size_t parts_bytes(const Grid &g) {
 template <int F>
 size_t attend_workspace(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
     size_t need = 0;
-    for (int wide = 0; wide < 2; wide++)
-        by_shape<F>(c->head_dim, groups, wide, [&](auto sh) {
+    for (int dtype = STEPQ_F32; dtype <= STEPQ_F16; dtype++)
+        by_shape<F>(c->head_dim, groups, dtype, [&](auto sh) {
             using S = decltype(sh);
             const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most, false));
             const size_t m = parts_bytes<typename S::Larger>(grid_of<typename S::Larger>(c, groups, rows, most, false));
             if (n > need) need = n;
             if (m > need) need = m;
+            return 0;
         });
     return need;
 }
@@ -92,14 +84,14 @@ stepq_status launch_shape(const Grid &g, int64_t pieces, AttendArgs a, cudaStrea
     st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
     if (st != STEPQ_OK || g.cluster) return st;
     const bool many = pieces * S::HT > 8 * sm_count();
-    auto *join = many ? kv_join_kernel<S::HT, S::D, S::WIDE, true> : kv_join_kernel<S::HT, S::D, S::WIDE, false>;
+    auto *join = many ? kv_join_kernel<S::HT, S::D, typename S::T, true> : kv_join_kernel<S::HT, S::D, typename S::T, false>;
     return launch_overlapped(join, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, many ? 1 : S::HT), 32 * kJoinWarps, 0,
                              s, a, g.ctas);
 }
 
 template <int F>
 stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &a, int64_t most, cudaStream_t s) {
-    return by_shape<F>(c->head_dim, a.groups, a.dtype != STEPQ_BF16, [&](auto sh) {
+    return by_shape<F>(c->head_dim, a.groups, a.dtype, [&](auto sh) {
         using S = decltype(sh);
         using L = typename S::Larger;
         const bool equal = a.window > 0 && a.window + S::TT < most;

@@ -7,7 +7,7 @@ y_d = sum_t p_t v_td with p the softmax:
  * an error e_t of a score moves y by sum_t p_t e_t (v_td - y_d). A score is a sum of D terms in
    tensor-core steps of 16 that may truncate (2 u each; D / 16 <= 16 of them, twice or three times
    for a query in terms, and a few roundings beside them): 64 u of the sum of absolute terms,
-   which for codes are those of the code with its offset. bf16 queries meet codes as subnormal numbers
+   which for codes are those of the code with its offset. queries of 16 bits meet codes as subnormal numbers
    u 2^-24, whose products are lined up as if u were 1024: each step may cut off 2^-23 of 1024 times
    the head's largest |q|, in units of the code, 2^-13 |q| s. The exponent's difference from the
    reference and its exponential add 4 u of that sum (in absolute terms: |s| is below it) and 2^-21.
@@ -96,7 +96,7 @@ def read(pages, kv, layer, table, starts, lens):
 
 def eps_of(fmt, dtype):
     if fmt == KV_BF16:
-        return 2.0 ** -16 if dtype is torch.bfloat16 else 2.0 ** -24
+        return 2.0 ** -24 if dtype is torch.float32 else 2.0 ** -16
     return 2.0 ** -11 if dtype is torch.bfloat16 else 2.0 ** -22
 
 
@@ -116,7 +116,7 @@ def attend(pages, kv, layer, table, lens, q, scale, window=0):
         s = scale * (qb @ k.permute(1, 2, 0))                                # [heads][G][tokens]
         p = torch.softmax(s, -1)
         e = abs(scale) * (qb.abs() @ ka.permute(1, 2, 0)) * 68 * U + 2.0 ** -21
-        if BITS[kv.format] < 16 and q.dtype is torch.bfloat16:
+        if BITS[kv.format] < 16 and q.dtype is not torch.float32:
             s_k = split(pages, kv)[2][places(table[b:b + 1], [lo], [n - lo], kv.page_tokens)[0], layer, :,
                                       places(table[b:b + 1], [lo], [n - lo], kv.page_tokens)[1]].double()
             e = e + abs(scale) * D / 16 * 2.0 ** -13 * qb.abs().amax(-1, keepdim=True) * s_k.t()[:, None, :]

@@ -92,7 +92,8 @@ struct Shape {
     static constexpr int OFF_PART = (OFF_SCAN + 8 * (kAttWarps + 3) + 15) / 16 * 16;
     static constexpr int OFF_RING = (OFF_PART + (HT * (kParts + 2) + kParts) * 4 + kAttWarps * 512 + 127) / 128 * 128;
     // CTAs of a multiprocessor with rings of so many stages, by shared memory and by registers
-    static constexpr int BY_REGS = NT * D >= 256 ? 2 : 3;
+    // (16 heads of 64 channels and fp32 vectors: 64 x 4,096 tokens in 8 bits 118 us with three, 76 with two)
+    static constexpr int BY_REGS = NT * D >= 256 || (NT == 2 && WIDE) ? 2 : 3;
     static constexpr int smem(int stages) { return OFF_RING + kAttWarps * stages * TILE; }
     static constexpr int resident(int stages) {
         const int n = 227 * 1024 / (smem(stages) + 1024);
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             p.from = from;
             set_span<TT>(a, len, p);
             p.n = (int)min((long long)(p.tiles - from), left);
-            p.turn = (w + (int)left) % kAttWarps;            // the share's tiles go round the warps
+            p.turn = (w + (int)left) & (kAttWarps - 1);      // the share's tiles go round the warps
             left -= p.n;
             from += p.n;
             if (from == p.tiles) {
@@ -1026,9 +1027,9 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
 }
 
 // Joins the parts of piece blockIdx.x: of head blockIdx.y, a warp every eighth part, whose first are on
-// their way before the weights are known; or where pieces are MANY (gridDim.y = 1) and have few
-// parts, a head a warp (256 x 8,191 tokens of 8 key heads in 4 bits, both kernels: 372 us with a CTA for
-// every head of every piece, 365 so).
+// their way before the weights are known; where pieces are MANY (gridDim.y < HT) of every gridDim.y-th
+// head, or, if the piece has few parts, of a head a warp (256 x 8,191 tokens of 8 key heads in 4 bits, both
+// kernels: 372 us with a CTA for every head of every piece, 365 so).
 constexpr int kJoinWarps = 8, kJoinAhead = 6, kMostParts = 1024;
 template <int D>
 struct JoinLane {
@@ -1060,8 +1061,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
     };
     constexpr int N = JoinLane<D>::N;
     if (MANY && j.count <= kJoinWarps) {
-        for (int h = w; h < nh; h += kJoinWarps) {
-            JoinLane<D> first(part(0) + h * D, l), second(part(1) + h * D, l);       // there are two at least
+        for (int h = w + blockIdx.y * kJoinWarps; h < nh; h += gridDim.y * kJoinWarps) {
+            JoinLane<D> parts[kJoinWarps];
+#pragma unroll
+            for (int i = 0; i < kJoinWarps; i++)
+                if (i < j.count) parts[i] = JoinLane<D>(part(i) + h * D, l);
             const float *x = part(min(l, j.count - 1));
             const float R = l < j.count ? x[HT * D + h] : kLow;
             float top = R;
@@ -1073,9 +1077,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
 #pragma unroll
             for (int s = 1; s < kJoinWarps; s *= 2) total += __shfl_xor_sync(0xffffffffu, total, s);
             total = __shfl_sync(0xffffffffu, total, 0);
-            first.add_to(o, __shfl_sync(0xffffffffu, k, 0));
-            second.add_to(o, __shfl_sync(0xffffffffu, k, 1));
-            for (int i = 2; i < j.count; i++) JoinLane<D>(part(i) + h * D, l).add_to(o, __shfl_sync(0xffffffffu, k, i));
+#pragma unroll
+            for (int i = 0; i < kJoinWarps; i++)
+                if (i < j.count) parts[i].add_to(o, __shfl_sync(0xffffffffu, k, i));
             // a lane's channels come together through shared memory, four side by side
 #pragma unroll
             for (int e = 0; e < N; e++) os[w][JoinLane<D>::channel(e, l)] = o[e];
@@ -1089,7 +1093,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_join_kernel(AttendArgs a, 
         }
         return;
     }
-    for (int h = blockIdx.y; h < nh; h += MANY ? 1 : HT) {
+    for (int h = blockIdx.y; h < nh; h += MANY ? gridDim.y : HT) {
         JoinLane<D> ahead[kJoinAhead];
 #pragma unroll
         for (int i = 0; i < kJoinAhead; i++)

@@ -6,7 +6,9 @@
 namespace stepq {
 namespace kv {
 
-// Runs f(Shape{}) for the variant of a call; more than 8 query heads a key head go in sixteens.
+// Runs f(Shape{}) for the variant of a call; more than 8 query heads a key head go in sixteens, but for
+// 256 channels of codes, whose sixteens have no room (64 x 4,096 tokens of two key heads with 16 query heads
+// each, us: in 4 bits 73, in eights 64; 8 bits 80 and 86, with fp32 vectors 215 and 95; 2 x 900 tokens 21 and 10).
 template <int F, class Fn>
 auto by_shape(int head_dim, int groups, int dtype, Fn &&f) {
     auto types = [&](auto d, auto nt) {
@@ -16,12 +18,15 @@ auto by_shape(int head_dim, int groups, int dtype, Fn &&f) {
                                      : f(Shape<F, D, NT, la::f16>{});
     };
     auto heads = [&](auto d) {
-        return groups > 8 ? types(d, std::integral_constant<int, 2>{}) : types(d, std::integral_constant<int, 1>{});
+        if constexpr (!coded(F) || decltype(d)::value < 256)
+            if (groups > 8) return types(d, std::integral_constant<int, 2>{});
+        return types(d, std::integral_constant<int, 1>{});
     };
     return head_dim == 64    ? heads(std::integral_constant<int, 64>{})
            : head_dim == 128 ? heads(std::integral_constant<int, 128>{})
                              : heads(std::integral_constant<int, 256>{});
 }
+template <class S> using Half = Shape<S::F, S::D, 1, typename S::T>;
 
 // CTAs of a call, from what the host knows: its rows and the most tokens that one has. cluster > 0:
 // clusters of that many take whole sequences. A warp then has up to kWholeTiles tiles, however short
@@ -62,13 +67,20 @@ size_t parts_bytes(const Grid &g) {
 template <int F>
 size_t attend_workspace(const stepq_kv_config *c, int groups, int64_t rows, int64_t most) {
     size_t need = 0;
+    auto add = [&](auto sh) {
+        using S = decltype(sh);
+        const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most, false));
+        if (n > need) need = n;
+    };
     for (int dtype = STEPQ_F32; dtype <= STEPQ_F16; dtype++)
         by_shape<F>(c->head_dim, groups, dtype, [&](auto sh) {
             using S = decltype(sh);
-            const size_t n = parts_bytes<S>(grid_of<S>(c, groups, rows, most, false));
-            const size_t m = parts_bytes<typename S::Larger>(grid_of<typename S::Larger>(c, groups, rows, most, false));
-            if (n > need) need = n;
-            if (m > need) need = m;
+            add(sh);
+            add(typename S::Larger{});
+            if constexpr (S::NT > 1) {
+                add(Half<S>{});
+                add(typename Half<S>::Larger{});
+            }
             return 0;
         });
     return need;
@@ -83,27 +95,41 @@ stepq_status launch_shape(const Grid &g, int64_t pieces, AttendArgs a, cudaStrea
     if (st != STEPQ_OK) return st;
     st = launch_clusters(kv_attend_kernel<S>, g.ctas, g.cluster ? g.cluster : 1, 32 * kAttWarps, S::smem(g.stages), s, a);
     if (st != STEPQ_OK || g.cluster) return st;
-    const bool many = pieces * S::HT > 8 * sm_count();
-    auto *join = many ? kv_join_kernel<S::HT, S::D, typename S::T, true> : kv_join_kernel<S::HT, S::D, typename S::T, false>;
-    return launch_overlapped(join, dim3(pieces < g.ctas ? (unsigned)pieces : (unsigned)g.ctas, many ? 1 : S::HT), 32 * kJoinWarps, 0,
-                             s, a, g.ctas);
+    // CTAs for every head of a piece as far as they all run at once
+    const int joins = (int)(pieces < g.ctas ? pieces : g.ctas), at_once = 8 * sm_count() / joins;
+    const int each = at_once < 1 ? 1 : at_once < S::HT ? at_once : S::HT;
+    auto *join = each < S::HT ? kv_join_kernel<S::HT, S::D, typename S::T, true> : kv_join_kernel<S::HT, S::D, typename S::T, false>;
+    return launch_overlapped(join, dim3((unsigned)joins, (unsigned)each), 32 * kJoinWarps, 0, s, a, g.ctas);
+}
+
+template <class S>
+stepq_status launch_tiles(const stepq_kv_config *c, const AttendArgs &a, int64_t most, bool equal, cudaStream_t s) {
+    using L = typename S::Larger;
+    const Grid g = grid_of<S>(c, a.groups, a.B, most, equal);
+    const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
+    // large tiles from 16 small ones a warp on (15 x 19,625 tokens in 4 bits, 19 a warp: 54 us, large 49;
+    // 26 x 1,201 with fp32 vectors, 4 a warp: 18.4 and 20.3)
+    if constexpr (L::LARGE)
+        if (!g.cluster && pieces * ((most + S::TT - 1) / S::TT) >= 16ll * kAttWarps * g.ctas)
+            return launch_shape<L>(grid_of<L>(c, a.groups, a.B, most, equal), pieces, a, s);
+    return launch_shape<S>(g, pieces, a, s);
 }
 
 template <int F>
 stepq_status launch_attend(const stepq_kv_config *c, const AttendArgs &a, int64_t most, cudaStream_t s) {
+    constexpr int kTile = 64;                                // the largest, in which a window ends
+    const bool equal = a.window > 0 && (int64_t)a.window + kTile < most;
+    if (equal) most = a.window + kTile;
     return by_shape<F>(c->head_dim, a.groups, a.dtype, [&](auto sh) {
         using S = decltype(sh);
-        using L = typename S::Larger;
-        const bool equal = a.window > 0 && a.window + S::TT < most;
-        if (equal && a.window + L::TT < most) most = a.window + L::TT;      // a window ends inside a tile
-        const Grid g = grid_of<S>(c, a.groups, a.B, most, equal);
-        const int64_t pieces = (int64_t)a.B * c->n_heads * ((a.groups + S::HT - 1) / S::HT);
-        // large tiles from 16 small ones a warp on (15 x 19,625 tokens in 4 bits, 19 a warp: 54 us, large 49;
-        // 26 x 1,201 with fp32 vectors, 4 a warp: 18.4 and 20.3)
-        if constexpr (L::LARGE)
-            if (!g.cluster && pieces * ((most + S::TT - 1) / S::TT) >= 16ll * kAttWarps * g.ctas)
-                return launch_shape<L>(grid_of<L>(c, a.groups, a.B, most, equal), pieces, a, s);
-        return launch_shape<S>(g, pieces, a, s);
+        // in eights where sixteens would leave half of the GPU without a CTA (2 x 900 tokens of 128 channels, four
+        // key heads with 16 query heads each, us: 8 bits 12.3 in sixteens, 8.9 in eights; 4 bits 14.1 and 8.8; bf16
+        // 9.8 and 8.2. 32 ragged sequences of 500 tokens, 8 heads of 64 channels in 4 bits 18 and 33)
+        if constexpr (S::NT > 1) {
+            const Grid g = grid_of<S>(c, a.groups, a.B, most, equal);
+            if (g.cluster && 2 * g.ctas <= sm_count()) return launch_tiles<Half<S>>(c, a, most, equal, s);
+        }
+        return launch_tiles<S>(c, a, most, equal, s);
     });
 }
 

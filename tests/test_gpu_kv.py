@@ -308,6 +308,32 @@ def test_many_rows_of_mixed_lengths(D, heads, G, pt, dt, fmt):
 
 @pytest.mark.parametrize("dt", TYPES, ids=type_ids)
 @pytest.mark.parametrize("fmt", FORMATS, ids=fmt_ids)
+@pytest.mark.parametrize("D,heads,G", [(128, 4, 16), (64, 8, 12), (256, 2, 20), (128, 5, 3)])
+def test_long_rows_among_short_ones(D, heads, G, fmt, dt):
+    """Two sequences of most tokens, whose parts are many, among some of two parts and of one; and both alone."""
+    g, kv = gen(17), A.KvConfig(1, heads, D, 32, fmt)
+    lens = [20011 // heads, 9001 // heads] + [(7 * i) % 400 + 1 for i in range(38)]
+    table, n = tables(g, kv, lens)
+    pages = normal_pages(g, kv, n)
+    q = torch.randn((len(lens), heads * G, D), generator=g, device="cuda").to(dt)
+    check(kv, pages, table, lens, q)
+    check(kv, pages, table[:2], lens[:2], q[:2])
+
+
+@pytest.mark.parametrize("fmt", FORMATS, ids=fmt_ids)
+def test_a_window_beyond_every_length(fmt):
+    g, kv = gen(18), A.KvConfig(1, 2, 64, 16, fmt)
+    lens = [5000, 3, 0, 700]
+    table, n = tables(g, kv, lens)
+    pages = normal_pages(g, kv, n)
+    q = torch.randn((4, 4, 64), generator=g, device="cuda").bfloat16()
+    want = check(kv, pages, table, lens, q)
+    for window in (5000, 2 ** 30, 2 ** 31 - 64, 2 ** 31 - 1):
+        assert torch.equal(check(kv, pages, table, lens, q, window=window), want)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=type_ids)
+@pytest.mark.parametrize("fmt", FORMATS, ids=fmt_ids)
 def test_values_that_are_no_tokens(fmt, dt):
     """Every byte that is no token's set to all ones (NaN, or the largest code and a NaN scale),
     tokens before a window among them, and table entries behind the tokens out of range."""

@@ -99,6 +99,14 @@ struct Shape {
         const int n = 227 * 1024 / (smem(stages) + 1024);
         return n < BY_REGS ? n : BY_REGS;
     }
+    // What a piece costs beside its tiles, in tiles: a share of many short pieces took longer than others.
+    // 69 ragged sequences, 94,875 tokens in fp16, 5 key heads of 128 (us): none 50.8, 4 extra 45.7, 7 43.4, 10 43.0,
+    // 20 43.0; 16 query heads each 65.8, 50.5, 47.5, 44.5, 44.0. Equal lengths: no change.
+    static constexpr int EXTRA = 10;
+    // Tiles a warp up to which clusters take whole sequences: 8 light ones, 2 heavy ones. 32 ragged sequences of
+    // 500 tokens, 4 key heads of 128 with 16 query heads in 8 bits: up to 8 tiles 21.5 us, in shares 14.9;
+    // 8 x 1,500 in fp16, 8 key heads with 4: 13.1 and 14.9.
+    static constexpr int ROOM = 16384 / (TT * NT * D), WHOLE = ROOM > 8 ? 8 : ROOM < 2 ? 2 : ROOM;
     static constexpr int STAGES = CODED && !LARGE ? 3 : 2;   // of calls that fill the GPU
     static_assert(TILE >= HT * D * 4, "a warp's part is put together in one stage of its ring");
     static constexpr int KP = RB / 4 < 16 ? RB / 4 : 16;     // bytes a lane reads of a row of K at once
@@ -452,14 +460,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
     const int turns = ctas * kAttWarps;
 
     // The share: `left` tiles of all, in the order (sequence, virtual head, tile), from tile `from`
-    // of virtual head vh of sequence b on; len is lens[b].
-    long long left = 0, share = 0;
+    // of virtual head vh of sequence b on; len is lens[b]. Every piece counts EXTRA tiles more, behind its own.
+    long long left = 0, share = 0, past = 0;                 // past: of the share before the piece at hand
     int item = blockIdx.x / ctas;                            // of calls for whole sequences
     int b = 0, vh = 0, from = 0, len = 0;
     if (!a.whole) {
         const int per = (a.B + 32 * kAttWarps - 1) / (32 * kAttWarps), i0 = min(a.B, tid * per), i1 = min(a.B, i0 + per);
         long long mine = 0;
-        for (int i = i0; i < i1; i++) mine += tiles_of<TT>(a, a.lens[i]);
+        for (int i = i0; i < i1; i++) mine += tiles_of<TT>(a, a.lens[i]) + S::EXTRA;
         long long upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -482,7 +490,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             long long p = upto - mine;
             int i = i0, n;
             for (;; i++) {
-                n = tiles_of<TT>(a, a.lens[i]);
+                n = tiles_of<TT>(a, a.lens[i]) + S::EXTRA;
                 if (t < (p + n) * VH) break;
                 p += n;
             }
@@ -499,6 +507,16 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         vh = (int)scan[kAttWarps + 1];
         from = (int)scan[kAttWarps + 2];
         len = a.lens[b];
+        const int n = tiles_of<TT>(a, len);
+        if (from >= n) {                                     // in the extra ones behind a piece
+            past = n + S::EXTRA - from;
+            left -= past;
+            from = 0;
+            if (++vh == VH) {
+                vh = 0;
+                if (++b < a.B) len = a.lens[b];
+            }
+        }
     }
 
     // The next piece of the share, n = 0 behind the last.
@@ -524,6 +542,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             left -= p.n;
             from += p.n;
             if (from == p.tiles) {
+                left -= S::EXTRA;
                 from = 0;
                 if (++vh == VH) {
                     vh = 0;
@@ -666,7 +685,6 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         float *part;                                         // else where it goes
     } out{};
     bool first = true;
-    long long past = 0;                                      // tiles of the share's pieces before this one
 
     for (;; first = false) {
         const Piece q = p.n > 0 ? next_piece() : p;
@@ -772,7 +790,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
             if (items <= (int)gridDim.x) joined[p.b * VH + p.vh] = j;
             else if (j.count) joined[blockIdx.x] = j;
         }
-        past += p.n;
+        past += p.from + p.n == p.tiles ? p.n + S::EXTRA : p.n;
         const int count = count_of(p), tok_first = (p.tile0 + p.from + p.turn) * TT;
 
         // pairs are of heads 2 c and 2 c + 1

@@ -29,23 +29,25 @@ auto by_shape(int head_dim, int groups, int dtype, Fn &&f) {
 template <class S> using Half = Shape<S::F, S::D, 1, typename S::T>;
 
 // CTAs of a call, from what the host knows: its rows and the most tokens that one has. cluster > 0:
-// clusters of that many take whole sequences. A warp then has up to kWholeTiles tiles, however short
+// clusters of that many take whole sequences. A warp then has up to S::WHOLE tiles, however short
 // the others' sequences are; beyond that equal shares are worth the parts and the second kernel.
 // A window makes all longer sequences equal, and twice as many tiles worth it: 33 sequences of 1,000
 // tokens' window, 10 heads of 64 (8 tiles a warp and more) 15.5 us, in shares 20.8. Without one, 7 of 14,000 in
 // 8 bits (14 tiles a warp) take 16.5 us, in shares 14.3.
-constexpr int kWholeTiles = 8;
 struct Grid { int ctas, cluster, stages; };
 template <class S>
 Grid grid_of(const stepq_kv_config *c, int groups, int64_t rows, int64_t most, bool equal) {
     const int64_t tiles = (most + S::TT - 1) / S::TT, sms = sm_count();
     const int64_t heads = rows * c->n_heads * ((groups + S::HT - 1) / S::HT);
     const int64_t places = sms * S::resident(S::STAGES), resident = places < kMostParts ? places : kMostParts;
+    // A cluster lies within one part of the chip, where the places behind the last whole one are lost: of 152, 304
+    // and 456 places, clusters of 4 find 144, 296 and 440, of 8 find 120, 288 and 408.
+    auto lost = [](int c) { return c < 4 ? 0 : c < 8 ? 16 : 48; };
     int cluster = 1;                                         // as many as find places and two tiles a warp
-    while (cluster < 8 && 2 * cluster * heads <= resident && tiles > 2 * kAttWarps * cluster) cluster *= 2;
-    const bool whole = tiles <= (equal ? 2 : 1) * kWholeTiles * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
+    while (cluster < 8 && 2 * cluster * heads <= resident - lost(2 * cluster) && tiles > 2 * kAttWarps * cluster) cluster *= 2;
+    const bool whole = tiles <= (equal ? 2 : 1) * S::WHOLE * kAttWarps * cluster && (heads <= resident || tiles <= 2 * kAttWarps);
     Grid g{0, whole ? cluster : 0, S::STAGES};
-    if (whole && tiles <= kAttWarps * cluster && heads * cluster <= sms * S::resident(1)) {
+    if (whole && tiles <= kAttWarps * cluster && heads * cluster <= sms * S::resident(1) - lost(cluster)) {
         // a tile a warp needs one stage, which lets more CTAs in
         g.ctas = (int)heads * cluster;
         g.stages = 1;

@@ -22,7 +22,7 @@
 // tokens of which each is used for 8 columns, and codes would have to go back to shared memory.
 // Measured (both kernels; 8 key heads of 128 channels, pages of 16 or 64 tokens): 256 x 8,191 tokens in 4 bits
 // and 64 query heads 365 us, 6.1 TB/s, where the integer pipe is busy half of the time at half the issue
-// rate; 128 x 4,096 in 8 bits 171 us, 6.4 TB/s; 64 ragged sequences of 131,072 in bf16 90 us, 6.0 TB/s, 4 us
+// rate; 128 x 4,096 in 8 bits 171 us, 6.4 TB/s; 64 ragged sequences of 131,072 in bf16 84 us, 6.4 TB/s, 4 us
 // of which pass before the first tile is asked for and 4 in the second kernel; 37 tokens 4.1 us.
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
 // row and the queries are laid out to match. Codes become fp16 exactly. Where outputs have 16 bits those of
@@ -59,8 +59,8 @@ template <> struct Compute<STEPQ_KV_BF16> { using T = la::bf16; };
 // Shape of a variant. LARGE: of calls whose warps take many tiles (codes of up to 128 head channels).
 // Queries and weights enter the products as sums of QT and PT terms of the pages' 16-bit type (fp16 for
 // codes), as many as the vectors' type T asks for:
-//  * queries of bf16 and fp16 are one term of fp16 exactly, of bf16 one or two; of fp32 two of fp16
-//    are within 2^-22, three of bf16 within 2^-24.
+//  * queries of bf16 and fp16 are one term of fp16 (exactly, down to 2^-39 of their head's largest), of bf16 one
+//    or two; of fp32 two of fp16 are within 2^-22, three of bf16 within 2^-24.
 //  * outputs in bf16: a weight's one term of fp16 is within 2^-11, an eighth of the output's own rounding;
 //    of bf16 it would have that rounding again, and two are within 2^-16. Outputs in fp16 take two terms
 //    of either; in fp32 two of fp16, three of bf16.
@@ -101,7 +101,8 @@ struct Shape {
     }
     // What a piece costs beside its tiles, in tiles: a share of many short pieces took longer than others.
     // 69 ragged sequences, 94,875 tokens in fp16, 5 key heads of 128 (us): none 50.8, 4 extra 45.7, 7 43.4, 10 43.0,
-    // 20 43.0; 16 query heads each 65.8, 50.5, 47.5, 44.5, 44.0. Equal lengths: no change.
+    // 20 43.0; 16 query heads each 65.8, 50.5, 47.5, 44.5, 44.0; 100 ragged, 300,000 tokens in
+    // 4 bits 63.1, 52.5 (4 extra), 47.6 (10). Equal lengths: no change.
     static constexpr int EXTRA = 10;
     // Tiles a warp up to which clusters take whole sequences: 8 light ones, 2 heavy ones. 32 ragged sequences of
     // 500 tokens, 4 key heads of 128 with 16 query heads in 8 bits: up to 8 tiles 21.5 us, in shares 14.9;

@@ -892,7 +892,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         if (S::CODED) {
                             const uint16_t *sc = (const uint16_t *)(st + 2 * TT * RB) + sub + 16 * g + r + 8 * h;
                             sk = f16_val(sc[0]);
-                            sv[g][h] = fmaxf(f16_val(sc[TT]), kF16Min);      // 0 or NaN: of no token
+                            sv[g][h] = fmaxf(f16_val(sc[TT]), kF16Min);      // 0: of a page that nothing was written to
                         }
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) {
@@ -909,6 +909,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         for (int h = 0; h < 2; h++) {
                             const int tok = tok0 + 16 * g + r + 8 * h;
                             if (tok >= p.lo && tok < p.hi) continue;
+                            sv[g][h] = 1.f;                  // what lies there may be infinite: its weight of 0 stays 0
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++) {
                                 x[nt][g][h] = f2s(-INFINITY);

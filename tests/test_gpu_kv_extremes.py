@@ -1,0 +1,93 @@
+"""One token's attention over the paged cache at the ends of its range: what lies in places that hold no
+token, the largest values and scores, scales of zero, and scores that need more than a few bits."""
+import math
+
+import pytest
+
+from paper_2609_38169_gb300 import api as A
+
+import kv_ref as R
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+FORMATS = [A.KV_BF16, A.KV_F16, A.KV_INT8, A.KV_INT4]
+CODES = [A.KV_INT8, A.KV_INT4]
+NAMES = {A.KV_BF16: "bf16", A.KV_F16: "f16", A.KV_INT8: "int8", A.KV_INT4: "int4"}
+ids = lambda x: str(x).split(".")[1] if isinstance(x, torch.dtype) else NAMES.get(x)  # noqa: E731
+# head channels, key heads, query heads of each, tokens of a page
+SHAPES = [(64, 2, 12, 8), (128, 2, 4, 16), (256, 1, 3, 64)]
+
+
+@pytest.fixture(autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    yield
+    assert A.stepq_device_error() == 0
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def tables(g, kv, lens):
+    """A page table in random order for sequences of lens[b] tokens, and the pages' number."""
+    need = [-(-n // kv.page_tokens) for n in lens]
+    page = torch.randperm(sum(need), generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), max(need)), -7, dtype=torch.int32, device="cuda")
+    for b, n in enumerate(need):
+        table[b, :n] = page[sum(need[:b]):sum(need[:b]) + n]
+    return table, len(page)
+
+
+def attend(kv, pages, table, lens, q, scale=None, window=0, max_len=None):
+    y, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+    A.stepq_kv_attend(kv, 0, pages, table, i32(lens), q, y, scale=scale, window=window, lse=lse,
+                      max_len=max(lens) if max_len is None else max_len)
+    return y, lse
+
+
+def check(kv, pages, table, lens, q, scale=None, window=0, max_len=None):
+    y, lse = attend(kv, pages, table, lens, q, scale, window, max_len)
+    wy, wl, tol, ltol = R.attend(pages, kv, 0, table, lens, q, kv.head_dim ** -0.5 if scale is None else scale, window)
+    R.assert_within(lse, wl, ltol, "lse")
+    R.assert_within(y, wy, R.rounded(tol, wy, q.dtype), "y")
+
+
+def filled(g, kv, lens, k=None, v=None, size=1.0):
+    """Pages of rows k, v [tokens][heads][D] (or normal ones) and their table."""
+    table, n = tables(g, kv, lens)
+    pages = A.alloc_pages(kv, n)
+    shape = (sum(lens), kv.n_heads, kv.head_dim)
+    k, v = (torch.randn(shape, generator=g, device="cuda") * size if x is None else x for x in (k, v))
+    R.append(pages, kv, 0, table, [0] * len(lens), lens, k, v)
+    return pages, table
+
+
+# 16-bit words that fill what is no token: the infinities and the largest value of either type, NaN, a subnormal
+@pytest.mark.parametrize("word", [0x7C00, 0xFC00, 0x7BFF, 0x7F80, 0xFF80, 0x7FC0, 0x0001],
+                         ids=lambda w: f"{w:04x}")
+@pytest.mark.parametrize("dt", TYPES, ids=ids)
+@pytest.mark.parametrize("fmt", FORMATS, ids=ids)
+def test_what_lies_outside_the_tokens_reaches_nothing(fmt, dt, word):
+    for D, heads, G, pt in SHAPES:
+        g, kv = gen(D), A.KvConfig(1, heads, D, pt, fmt)
+        lens = [1, 5, 16, 41, 100, 333, 1500, 0]
+        full, table = filled(g, kv, lens)
+        q = torch.randn((len(lens), heads * G, D), generator=g, device="cuda").to(dt)
+        for window in (0, 21):
+            lo = [max(0, n - window) if window else 0 for n in lens]
+            page, at = R.places(table, lo, [n - a for n, a in zip(lens, lo)], pt)
+            pages = torch.full((full.numel() // 2,), word - (word >> 15 << 16), dtype=torch.int16, device="cuda").view(torch.uint8)
+            for src, dst in zip(R.split(full, kv), R.split(pages, kv)):
+                if src is not None:
+                    dst[page, 0, :, at] = src[page, 0, :, at]
+            y, lse = attend(kv, pages, table, lens, q, window=window)
+            wy, wl, tol, ltol = R.attend(full, kv, 0, table, lens, q, D ** -0.5, window)
+            R.assert_within(lse, wl, ltol, "lse")
+            R.assert_within(y, wy, R.rounded(tol, wy, dt), "y")

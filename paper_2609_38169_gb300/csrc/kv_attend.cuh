@@ -794,6 +794,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         past += p.from + p.n == p.tiles ? p.n + S::EXTRA : p.n;
         const int count = count_of(p), tok_first = (p.tile0 + p.from + p.turn) * TT;
 
+        // The largest weight. 2^15 leaves the least bits that terms in fp16 lose; in bf16 V may be as large as fp32
+        // goes, which sums of n tokens with weights of 1 / n at most do not pass, and weights have fp32's exponents.
+        const float most_wt = F == STEPQ_KV_BF16 ? power2(__clz(p.hi - p.lo) - 32) : 32768.f;
+
         // pairs are of heads 2 c and 2 c + 1
         uint64_t hf[NT], ho[NT], R[NT], sum[NT];
         float O[NT][S::MT][4];
@@ -917,8 +921,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             }
                         }
                 }
-                // Weights 2^(s - R) sv of at most 2^15. R rises, to 7 below the largest exponent
-                // (of the weight), only when one would be above: seldom after the first tiles.
+                // Weights 2^(s - R) sv of at most `most_wt`. R rises, until the largest is 8 bits below,
+                // only when one would be above: seldom after the first tiles.
                 uint64_t wt[NT][G][2], wv[NT][G][2];
                 auto weights = [&](int nt) {
                     const uint64_t less_r = f2(-f2lo(R[nt]), -f2hi(R[nt]));
@@ -936,7 +940,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 };
                 float most = weights(0);
                 if (NT > 1) most = fmaxf(most, weights(NT - 1));
-                if (__any_sync(0xffffffffu, most > 32768.f)) {
+                if (__any_sync(0xffffffffu, most > most_wt)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         float up[2], f[2];
@@ -951,7 +955,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                                     top = fmaxf(top, fmaf(half(x[nt][g][h]), half(hk[nt][g][h]), S::CODED ? log2f(sv[g][h]) : 0.f));
 #pragma unroll
                             for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            up[e] = fmaxf(half(R[nt]), top - 7.f);
+                            up[e] = fmaxf(half(R[nt]), top + (8.f - log2f(most_wt)));
                             f[e] = exp2_fast(half(R[nt]) - up[e]);
 #pragma unroll
                             for (int m = 0; m < S::MT; m++) {

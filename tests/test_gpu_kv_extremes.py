@@ -91,3 +91,37 @@ def test_what_lies_outside_the_tokens_reaches_nothing(fmt, dt, word):
             wy, wl, tol, ltol = R.attend(full, kv, 0, table, lens, q, D ** -0.5, window)
             R.assert_within(lse, wl, ltol, "lse")
             R.assert_within(y, wy, R.rounded(tol, wy, dt), "y")
+
+
+# ------------------------------------------------------------------ values
+LARGEST = torch.finfo(torch.bfloat16).max
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("D,heads,G,pt", SHAPES)
+@pytest.mark.parametrize("lens", [[1, 2, 9, 100], [3000, 700], [40001]], ids=["short", "some", "long"])
+def test_values_up_to_the_largest_of_bf16(lens, D, heads, G, pt, dt):
+    """An output lies between the values that it weighs, so it is finite where they are: all of the largest
+    magnitude, of either sign, one among small ones, and sizes whose largest scores come last."""
+    g, kv = gen(3), A.KvConfig(1, heads, D, pt, A.KV_BF16)
+    n, shape = sum(lens), (sum(lens), heads, D)
+    q = torch.randn((len(lens), heads * G, D), generator=g, device="cuda").to(dt)
+    normal = torch.randn(shape, generator=g, device="cuda")
+    rising = torch.linspace(-4, 4, n, device="cuda")[:, None, None]
+    lone = normal.clone()
+    lone[n // 2] = LARGEST
+    for v in (torch.full(shape, LARGEST, device="cuda"), LARGEST * normal.sign(), lone, normal * 2.0 ** 113, normal.clamp(-1, 1) * 2.0 ** 124):
+        for k in (None, q[:1, ::G].float() * rising):
+            pages, table = filled(g, kv, lens, k, v)
+            check(kv, pages, table, lens, q)
+            check(kv, pages, table, lens, q, window=50)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=ids)
+def test_small_values_of_bf16(dt):
+    """Values of 2^-60, whose weighted sums stay far above the least number."""
+    g, kv = gen(4), A.KvConfig(1, 2, 128, 16, A.KV_BF16)
+    lens = [1, 3000]
+    v = torch.randn((3001, 2, 128), generator=g, device="cuda") * 2.0 ** -60
+    pages, table = filled(g, kv, lens, None, v)
+    check(kv, pages, table, lens, torch.randn((2, 8, 128), generator=g, device="cuda").to(dt))

@@ -885,7 +885,11 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                     }
                 }
                 // base-2 exponents x hk with x = s - ho; masked ones are -inf
-                float sv[G][2];
+                // V's scales, for the reference at least 2^-24; the least as they are
+                float sv[G][2], least = 1.f;
+                auto v_scale = [&](int g, int h) {
+                    return f16_val(((const uint16_t *)(st + 2 * TT * RB))[TT + sub + 16 * g + r + 8 * h]);
+                };
                 uint64_t x[NT][G][2], hk[NT][G][2];
 #pragma unroll
                 for (int g = 0; g < G; g++)
@@ -894,9 +898,9 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         float sk = 1.f;
                         sv[g][h] = 1.f;
                         if (S::CODED) {
-                            const uint16_t *sc = (const uint16_t *)(st + 2 * TT * RB) + sub + 16 * g + r + 8 * h;
-                            sk = f16_val(sc[0]);
-                            sv[g][h] = fmaxf(f16_val(sc[TT]), kF16Min);      // 0: of a page that nothing was written to
+                            sk = f16_val(((const uint16_t *)(st + 2 * TT * RB))[sub + 16 * g + r + 8 * h]);
+                            sv[g][h] = fmaxf(fabsf(v_scale(g, h)), 0x1p-24f);
+                            least = fminf(least, v_scale(g, h));
                         }
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) {
@@ -940,7 +944,9 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 };
                 float most = weights(0);
                 if (NT > 1) most = fmaxf(most, weights(NT - 1));
-                if (__any_sync(0xffffffffu, most > most_wt)) {
+                // rows of zeros, of a page that nothing was written to or of none, have code 0 and scale 0
+                const bool zeros = S::CODED && least <= 0.f;
+                if (__any_sync(0xffffffffu, zeros || most > most_wt)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         float up[2], f[2];
@@ -966,6 +972,11 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         R[nt] = f2(up[0], up[1]);
                         sum[nt] = fmul2(sum[nt], f2(f[0], f[1]));
                         weights(nt);
+#pragma unroll
+                        for (int g = 0; g < G; g++)
+#pragma unroll
+                            for (int h = 0; h < 2; h++)
+                                if (zeros && sv[g][h] != 1.f) wv[nt][g][h] = fmul2(wt[nt][g][h], f2s(v_scale(g, h)));
                     }
                 }
                 // weighted v: heads' weights by tokens become the right factor by a transposition

@@ -125,3 +125,48 @@ def test_small_values_of_bf16(dt):
     v = torch.randn((3001, 2, 128), generator=g, device="cuda") * 2.0 ** -60
     pages, table = filled(g, kv, lens, None, v)
     check(kv, pages, table, lens, torch.randn((2, 8, 128), generator=g, device="cuda").to(dt))
+
+
+# ------------------------------------------------------------------ scales of codes
+@pytest.mark.parametrize("dt", TYPES, ids=ids)
+@pytest.mark.parametrize("D,heads,G,pt", SHAPES)
+@pytest.mark.parametrize("fmt", CODES, ids=ids)
+def test_scales_of_zero_stand_for_zeros(fmt, D, heads, G, pt, dt):
+    """Tokens of a page that nothing was written to count as zeros, as stepq_kv_read gives them: all of
+    a sequence, some of one; and scales below those that an append writes."""
+    g, kv = gen(5), A.KvConfig(1, heads, D, pt, fmt)
+    lens = [40, 700, 3000, 2 * pt + 3]
+    q = torch.randn((4, heads * G, D), generator=g, device="cuda").to(dt)
+    pages, table = filled(g, kv, lens)
+    blank = torch.zeros_like(pages)
+    y, _ = attend(kv, blank, table, lens, q)
+    assert not bool(y.any())
+    check(kv, blank, table, lens, q)
+    _, _, sk, sv = R.split(pages, kv)
+    some = torch.rand(sv.shape, generator=g, device="cuda")
+    sv[some < 0.3] = 0
+    sk[(some > 0.2) & (some < 0.4)] = 0
+    sv[(some > 0.5) & (some < 0.6)] = 2.0 ** -24
+    check(kv, pages, table, lens, q)
+    sv.copy_(torch.where(some < 0.5, 2.0 ** -24, 2.0 ** -20))
+    check(kv, pages, table, lens, q)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=ids)
+@pytest.mark.parametrize("fmt", FORMATS, ids=ids)
+@pytest.mark.parametrize("D,heads,G,pt", SHAPES)
+def test_pages_outside_the_pool_count_as_zeros(D, heads, G, pt, fmt, dt):
+    g, kv = gen(6), A.KvConfig(1, heads, D, pt, fmt)
+    lens = [5 * pt + 3, 700, 3000]
+    pages, table = filled(g, kv, lens)
+    n = pages.numel() // A.stepq_kv_page_bytes(kv)
+    q = torch.randn((3, heads * G, D), generator=g, device="cuda").to(dt)
+    bad, zero = table.clone(), table.clone()
+    for b, at in ((0, 0), (0, 5), (1, 3), (2, 1), (2, 3000 // pt - 1)):
+        bad[b, at], zero[b, at] = (n, -1, 1 << 30)[at % 3], n
+    y, lse = attend(kv, pages, bad, lens, q)
+    assert A.stepq_device_error() == 2
+    more = torch.cat([pages, torch.zeros(A.stepq_kv_page_bytes(kv), dtype=torch.uint8, device="cuda")])
+    wy, wl, tol, ltol = R.attend(more, kv, 0, zero, lens, q, D ** -0.5)
+    R.assert_within(lse, wl, ltol, "lse")
+    R.assert_within(y, wy, R.rounded(tol, wy, dt), "y")

@@ -417,8 +417,7 @@ struct Queries {
             if (S::RAW) {
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2) off += __shfl_xor_sync(0xffffffffu, off, o);
-                off *= F == STEPQ_KV_INT8 ? 128.f / 16777216.f : 8.f / 16777216.f;
-                k *= 16777216.f;
+                off *= F == STEPQ_KV_INT8 ? 128.f * 0x1p-24f : 8.f * 0x1p-24f;
             }
             if (l == 0) {
                 head_k[h] = k;
@@ -794,9 +793,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
         past += p.from + p.n == p.tiles ? p.n + S::EXTRA : p.n;
         const int count = count_of(p), tok_first = (p.tile0 + p.from + p.turn) * TT;
 
-        // The largest weight. 2^15 leaves the least bits that terms in fp16 lose; in bf16 V may be as large as fp32
-        // goes, which sums of n tokens with weights of 1 / n at most do not pass, and weights have fp32's exponents.
-        const float most_wt = F == STEPQ_KV_BF16 ? power2(__clz(p.hi - p.lo) - 32) : 32768.f;
+        // The largest weight, 2^-low. 2^15 leaves the least bits that terms in fp16 lose; in bf16 V may be as large as
+        // fp32 goes, which sums of n tokens with weights of 1 / n at most do not pass, and weights have fp32's exponents.
+        const int low = F == STEPQ_KV_BF16 ? 32 - __clz(p.hi - p.lo) : -15;
+        const float most_wt = power2(-low);
 
         // pairs are of heads 2 c and 2 c + 1
         uint64_t hf[NT], ho[NT], R[NT], sum[NT];
@@ -884,13 +884,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         }
                     }
                 }
-                // base-2 exponents x hk with x = s - ho; masked ones are -inf
+                // base-2 exponents x = (s - ho) sk hf, rounded before the reference is taken from them: a difference of
+                // large scores is then a difference of what the reference was found from. Masked ones are -inf.
                 // V's scales, for the reference at least 2^-24; the least as they are
                 float sv[G][2], least = 1.f;
                 auto v_scale = [&](int g, int h) {
                     return f16_val(((const uint16_t *)(st + 2 * TT * RB))[TT + sub + 16 * g + r + 8 * h]);
                 };
-                uint64_t x[NT][G][2], hk[NT][G][2];
+                uint64_t x[NT][G][2];
 #pragma unroll
                 for (int g = 0; g < G; g++)
 #pragma unroll
@@ -898,16 +899,16 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                         float sk = 1.f;
                         sv[g][h] = 1.f;
                         if (S::CODED) {
-                            sk = f16_val(((const uint16_t *)(st + 2 * TT * RB))[sub + 16 * g + r + 8 * h]);
+                            sk = f16_val(((const uint16_t *)(st + 2 * TT * RB))[sub + 16 * g + r + 8 * h]) * (S::RAW ? 0x1p24f : 1.f);
                             sv[g][h] = fmaxf(fabsf(v_scale(g, h)), 0x1p-24f);
                             least = fminf(least, v_scale(g, h));
                         }
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) {
                             x[nt][g][h] = f2(s[nt][g][2 * h], s[nt][g][2 * h + 1]);
-                            hk[nt][g][h] = hf[nt];
                             if (S::RAW) x[nt][g][h] = fsub2(x[nt][g][h], ho[nt]);
-                            if (S::CODED) hk[nt][g][h] = fmul2(hf[nt], f2s(sk));
+                            if (S::CODED) x[nt][g][h] = fmul2(x[nt][g][h], f2s(sk));
+                            x[nt][g][h] = fmul2(x[nt][g][h], hf[nt]);        // may be large, where sk makes up for it
                         }
                     }
                 if (edge) {
@@ -919,10 +920,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             if (tok >= p.lo && tok < p.hi) continue;
                             sv[g][h] = 1.f;                  // what lies there may be infinite: its weight of 0 stays 0
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) {
-                                x[nt][g][h] = f2s(-INFINITY);
-                                hk[nt][g][h] = f2s(1.f);
-                            }
+                            for (int nt = 0; nt < NT; nt++) x[nt][g][h] = f2s(-INFINITY);
                         }
                 }
                 // Weights 2^(s - R) sv of at most `most_wt`. R rises, until the largest is 8 bits below,
@@ -935,7 +933,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                     for (int g = 0; g < G; g++)
 #pragma unroll
                         for (int h = 0; h < 2; h++) {
-                            const uint64_t t = ffma2(x[nt][g][h], hk[nt][g][h], less_r);
+                            const uint64_t t = fadd2(x[nt][g][h], less_r);
                             wt[nt][g][h] = f2(exp2_fast(f2lo(t)), exp2_fast(f2hi(t)));
                             wv[nt][g][h] = S::CODED ? fmul2(wt[nt][g][h], f2s(sv[g][h])) : wt[nt][g][h];
                             most = fmax3(most, f2lo(wv[nt][g][h]), f2hi(wv[nt][g][h]));
@@ -958,10 +956,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                             for (int g = 0; g < G; g++)
 #pragma unroll
                                 for (int h = 0; h < 2; h++)
-                                    top = fmaxf(top, fmaf(half(x[nt][g][h]), half(hk[nt][g][h]), S::CODED ? log2f(sv[g][h]) : 0.f));
+                                    top = fmaxf(top, half(x[nt][g][h]) + (S::CODED ? log2f(sv[g][h]) : 0.f));
 #pragma unroll
                             for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            up[e] = fmaxf(half(R[nt]), top + (8.f - log2f(most_wt)));
+                            up[e] = fmaxf(half(R[nt]), top + (float)(low + 8));
                             f[e] = exp2_fast(half(R[nt]) - up[e]);
 #pragma unroll
                             for (int m = 0; m < S::MT; m++) {

@@ -170,3 +170,59 @@ def test_pages_outside_the_pool_count_as_zeros(D, heads, G, pt, fmt, dt):
     wy, wl, tol, ltol = R.attend(more, kv, 0, zero, lens, q, D ** -0.5)
     R.assert_within(lse, wl, ltol, "lse")
     R.assert_within(y, wy, R.rounded(tol, wy, dt), "y")
+
+
+# ------------------------------------------------------------------ scores
+def one_token(kv, fmt, dt, k, v, lens, win, q, scale, ltol):
+    """Where one token's score is so far above that the others weigh nothing (or `rest`), an output is its
+    value. Its weight comes in terms (eps) of which those in fp16 end at 2^-25, for a weight of 2^-6 at least."""
+    g = gen(7)
+    pages, table = filled(g, kv, lens, k, v)
+    wk, wv, _ = R.read(pages, kv, 0, table, [0] * len(lens), lens)
+    G = q.shape[1] // kv.n_heads
+    y, lse = attend(kv, pages, table, lens, q.to(dt), scale=scale)
+    want = wv[win].repeat_interleave(G, 1)
+    tol = want.abs() * (R.eps_of(fmt, dt) + 2.0 ** -18) + 2.0 ** -15
+    R.assert_within(y, want, R.rounded(tol, want, dt), "y")
+    score = (wk[win].repeat_interleave(G, 1) * q.double()).sum(-1) * scale
+    R.assert_within(lse, score, score.abs() * ltol + 2.0 ** -14, "lse")
+
+
+@pytest.mark.parametrize("e", [0, 10, 20, 24, 26, 28, 29, 30, 31, 32, 34, 40, 48])
+@pytest.mark.parametrize("dt", TYPES, ids=ids)
+@pytest.mark.parametrize("fmt", FORMATS, ids=ids)
+def test_one_score_far_above_the_others(fmt, dt, e):
+    """Scores of 2^6 to 2^55, of which one is above the others by a fourth of itself (the others' weights are
+    3,100 times e^-20 at most, 2^-17). Beyond 2^29 they are so far apart that no exponent lies between."""
+    for D, heads, G, pt in SHAPES:
+        g, kv = gen(D), A.KvConfig(1, heads, D, pt, fmt)
+        for lens in ([1, 3, 100], [3000, 700]):
+            n = sum(lens)
+            v = torch.randn((n, heads, D), generator=g, device="cuda").clamp(-4, 4)
+            k = torch.zeros((n, heads, D), device="cuda")
+            k[:, :, 0] = torch.randint(1, 6, (n, heads), generator=g, device="cuda").float()
+            k[:, :, 1] = 7.0                                # of every row the largest: the scales are equal
+            win = [sum(lens[:b]) + m * 3 // 4 for b, m in enumerate(lens)]
+            k[win, :, 0] = 7.0
+            q = torch.zeros((len(lens), heads * G, D), device="cuda")
+            q[:, :, 0] = 1.375 * 2.0 ** (min(e, 12) if dt is torch.float16 else e // 2)
+            # 16-bit queries over codes: each of D / 16 products cuts off 2^-13 q s, of a score of 7 q
+            ltol = 2.0 ** -20 if dt is torch.float32 or R.BITS[fmt] == 16 else 2.0 ** -11
+            one_token(kv, fmt, dt, k, v, lens, win, q, 8 * 1.375 * 2.0 ** e / float(q[0, 0, 0]), ltol)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=ids)
+@pytest.mark.parametrize("fmt", [A.KV_F16] + CODES, ids=ids)
+@pytest.mark.parametrize("e", [100, 118, 122, 126])
+def test_queries_up_to_the_largest(e, fmt, dt):
+    """Queries of up to 2^126 over keys of 7 / 1024 and less: products and scores below 2^120."""
+    g, kv, lens = gen(8), A.KvConfig(1, 1, 128, 16, fmt), [1, 40, 700]
+    k = torch.zeros((741, 1, 128), device="cuda")
+    k[:, :, 0] = torch.randint(-5, 6, (741, 1), generator=g, device="cuda").float()
+    k[:, :, 1] = 7.0
+    win = [0, 31, 541]
+    k[win, :, 0] = 7.0
+    q = torch.zeros((3, 4, 128), device="cuda")
+    q[:, :, 0] = 2.0 ** e
+    v = torch.randn((741, 1, 128), generator=g, device="cuda").clamp(-4, 4)
+    one_token(kv, fmt, dt, k / 1024, v, lens, win, q, 0.25, 2.0 ** -11)

@@ -459,6 +459,9 @@ typedef struct {
  * the tokens none. A negative length raises STEPQ_ERR_ARG and counts as 0; one beyond the table
  * raises STEPQ_ERR_SLOT_RANGE and ends with it; so does a page outside [0, n_pages), whose tokens
  * are read as zeros (device errors). y and lse for equal arguments are the same in every call.
+ * Scores, statistics and sums are held in fp32. Before y's own rounding a token's weight is within 2^-11
+ * where y is bf16 (over bf16 pages 2^-16), 2^-16 where y is fp16 over bf16 pages, else 2^-22; for bf16 q over
+ * 4-bit codes a score is within scale * max|q| * s_t * D * 2^-17, with the scale s_t of the token's row of K.
  * workspace: device, 256-byte aligned, at least stepq_kv_workspace_bytes() for the call's q_heads, B
  * and max_len (0: NULL is fine), clobbered. */
 size_t stepq_kv_workspace_bytes(const stepq_kv_config *cfg, int q_heads, int B, int max_len);

@@ -25,10 +25,14 @@
 // rate; 128 x 4,096 in 8 bits 171 us, 6.4 TB/s; 64 ragged sequences of 131,072 in bf16 84 us, 6.4 TB/s, 4 us
 // of which pass before the first tile is asked for and 4 in the second kernel; 37 tokens 4.1 us.
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
-// row and the queries are laid out to match. Codes become fp16 exactly. Where outputs have 16 bits those of
-// K enter as they are, u 2^-24 (a mask or a byte permute leaves a subnormal number), and their offset
-// 2^(b-1) sum q is subtracted from the sum; the tensor cores line products up by the exponents of normal
-// numbers, which cuts such sums off after some 17 bits (4 bits) or 21 (8 bits).
+// row and the queries are laid out to match. Codes become fp16 exactly. For bf16 vectors over 4 bits those of
+// K enter as they are, u 2^-24 (a mask leaves a subnormal number), and their offset 8 sum q is
+// subtracted from the sum. The tensor cores line products up by the exponents of normal numbers, as if u were
+// 1024, which cuts such sums off after some 17 bits: a score is within D 2^-17 of scale times its row's scale
+// times the largest |q|, 1e-4 for normal queries and keys of 128 channels, where a weight's one term is within
+// 5e-4 and the output's rounding within 4e-3. Codes without their offset take an instruction more for a pair: 256 x
+// 8,191 tokens 398 us, so 367. Elsewhere they enter so: fp16 vectors over 4 bits take 1 to 4% longer for it,
+// 8 bits nothing.
 //
 // Between the products (whose factors are sums of 16-bit terms, see Shape) everything is fp32.
 #pragma once
@@ -59,8 +63,8 @@ template <> struct Compute<STEPQ_KV_BF16> { using T = la::bf16; };
 // Shape of a variant. LARGE: of calls whose warps take many tiles (codes of up to 128 head channels).
 // Queries and weights enter the products as sums of QT and PT terms of the pages' 16-bit type (fp16 for
 // codes), as many as the vectors' type T asks for:
-//  * queries of bf16 and fp16 are one term of fp16 (exactly, down to 2^-39 of their head's largest), of bf16 one
-//    or two; of fp32 two of fp16 are within 2^-22, three of bf16 within 2^-24.
+//  * queries of bf16 and fp16 are one term of fp16 (exactly, down to 2^-39 of their head's largest; of RAW every
+//    second pair down to 2^-35), of bf16 one or two; of fp32 two of fp16 are within 2^-22, three of bf16 within 2^-24.
 //  * outputs in bf16: a weight's one term of fp16 is within 2^-11, an eighth of the output's own rounding;
 //    of bf16 it would have that rounding again, and two are within 2^-16. Outputs in fp16 take two terms
 //    of either; in fp32 two of fp16, three of bf16.
@@ -116,7 +120,7 @@ struct Shape {
     static constexpr int MT = D / 16;                        // row tiles of V's
     static constexpr bool QREG = QT * NT * KS <= 16;         // queries kept in registers
     using C = typename Compute<F>::T;
-    static constexpr bool RAW = CODED && !WIDE;              // K's codes enter with their offset, at 2^-24
+    static constexpr bool RAW = F == STEPQ_KV_INT4 && BF16;  // K's codes enter with their offset, at 2^-24
 };
 
 // ------------------------------------------------------------------ building blocks
@@ -239,15 +243,15 @@ __device__ __forceinline__ uint32_t codes4_high(uint32_t w) {
 }
 
 // A lane's piece of a row of K as pairs of the compute type, in the order that Queries::put() gives
-// the queries. RAW: codes with their offset at 2^-24, for the odd pairs of 4 bits 2^-20.
+// the queries. RAW: codes with their offset at 2^-24, for the odd pairs 2^-20.
 template <int F, bool RAW, int N>
 __device__ __forceinline__ void k_pairs(const Words<N> &x, uint32_t (&p)[N * 16 / bits_of(F)]) {
 #pragma unroll
     for (int i = 0; i < N; i++) {
         const uint32_t w = x.w[i];
         if constexpr (F == STEPQ_KV_INT8) {
-            p[2 * i] = RAW ? __byte_perm(w, 0u, 0x4140) : codes8(w, 0x4140);
-            p[2 * i + 1] = RAW ? __byte_perm(w, 0u, 0x4342) : codes8(w, 0x4342);
+            p[2 * i] = codes8(w, 0x4140);
+            p[2 * i + 1] = codes8(w, 0x4342);
         } else if constexpr (F == STEPQ_KV_INT4) {
             const uint32_t y = w >> 8;
             p[4 * i] = RAW ? w & 0x000f000fu : codes4(w);
@@ -384,7 +388,7 @@ struct Queries {
             const int h = w + i * kAttWarps;
             float k = a.scale, off = 0.f;
             if (std::is_same<C, la::f16>::value) {
-                // scaled by a power of two to below 2^15, where fp16 keeps 2^-39 of the largest
+                // scaled by a power of two to below 2^15: fp16 then keeps 2^-39 of the largest
                 float top = 0.f;
 #pragma unroll
                 for (int e = 0; e < N; e++) top = fmax3(top, fabsf(x[i][e].x), fabsf(x[i][e].y));
@@ -401,7 +405,7 @@ struct Queries {
                 constexpr int PC = S::KP * 8 / bits_of(F), JP = PC / 2;          // channels, pairs of a piece
                 const int u = 32 * e + l, piece = u / JP, j = u % JP;
                 const int pair = (piece / 4) * JP + j, lane = 4 * (h % 8) + piece % 4;
-                const float f = S::RAW && FOURTH && (j & 1) ? 0.0625f : 1.f;     // of a code at 2^-20
+                const float f = S::RAW && (j & 1) ? 0.0625f : 1.f;     // of a code at 2^-20
                 float2 rest = make_float2(x[i][e].x * f, x[i][e].y * f);
                 float used = 0.f;
 #pragma unroll
@@ -412,12 +416,12 @@ struct Queries {
                     used += b.x + b.y;
                     qf[(((t * S::NT + h / 8) * S::KS + pair / 2) * 32 + lane) * 2 + pair % 2] = v;
                 }
-                off += S::RAW && FOURTH && (j & 1) ? 16.f * used : used;
+                off += S::RAW && (j & 1) ? 16.f * used : used;
             }
             if (S::RAW) {
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2) off += __shfl_xor_sync(0xffffffffu, off, o);
-                off *= F == STEPQ_KV_INT8 ? 128.f * 0x1p-24f : 8.f * 0x1p-24f;
+                off *= 8.f * 0x1p-24f;
             }
             if (l == 0) {
                 head_k[h] = k;

@@ -226,3 +226,31 @@ def test_queries_up_to_the_largest(e, fmt, dt):
     q[:, :, 0] = 2.0 ** e
     v = torch.randn((741, 1, 128), generator=g, device="cuda").clamp(-4, 4)
     one_token(kv, fmt, dt, k / 1024, v, lens, win, q, 0.25, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("D,heads,G,pt", SHAPES)
+@pytest.mark.parametrize("fmt,dt", [(A.KV_INT8, torch.float32), (A.KV_INT4, torch.float32), (A.KV_INT8, torch.float16),
+                                    (A.KV_INT4, torch.float16), (A.KV_INT8, torch.bfloat16)], ids=ids)
+def test_small_channels_beside_a_large_one(fmt, dt, D, heads, G, pt):
+    """A query whose largest channel meets zeros of K only: a score is the sum of the small ones, held as in
+    fp32, so that it is off by 68 u of their absolute terms at most (u = 2^-24, as in kv_ref). bf16 vectors
+    over 4 bits are the exception: there the largest channel's offset takes part in the sum."""
+    g, kv, lens = gen(9), A.KvConfig(1, heads, D, pt, fmt), [40, 900]
+    k = torch.randint(-7, 8, (940, heads, D), generator=g, device="cuda").float()
+    k[:, :, 0], k[:, :, 1] = 0, 7
+    pages, table = filled(g, kv, lens, k)
+    q = torch.randint(-15, 16, (2, heads * G, D), generator=g, device="cuda") / 64
+    q[:, :, 0] = 1024
+    y, lse = attend(kv, pages, table, lens, q.to(dt), scale=0.25)
+    for b, n in enumerate(lens):
+        rk, rv, _ = R.read(pages, kv, 0, table[b:b + 1], [0], [n])
+        qb = q[b].double().view(heads, G, D)
+        s = 0.25 * (qb @ rk.permute(1, 2, 0))
+        e = 0.25 * (qb.abs() @ rk.abs().permute(1, 2, 0)) * 68 * R.U + 2.0 ** -21
+        p, steps, vh = torch.softmax(s, -1), n / 64 * 2 + 64, rv.transpose(0, 1)
+        want = torch.logsumexp(s, -1)
+        R.assert_within(lse[b].view(heads, G), want, e.amax(-1) + steps * R.U + want.abs() * 4 * R.U, "lse")
+        want = p @ vh
+        tol = (p * e) @ vh.abs() + (p * e).sum(-1, keepdim=True) * want.abs() \
+            + (R.eps_of(fmt, dt) + steps * R.U) * (p @ vh.abs()) + 2.0 ** -32 * vh.abs().sum(1, keepdim=True)
+        R.assert_within(y[b].view(heads, G, D), want, R.rounded(tol, want, dt), "y")

@@ -29,9 +29,8 @@ struct RowsArgs {
     int64_t ks, vs;
 };
 
-// The sequence of packed row i: the last whose first row is not above it. Empty sequences and
-// bounds out of order come out as the sequence that the halving ends at; the caller checks
-// that it holds the row.
+// The sequence of packed row i: the last whose first row is not above it. Bounds out of order come out as the
+// sequence that the halving ends at; the caller checks that it holds the row.
 __device__ __forceinline__ int find_sequence(const int32_t *cu, int B, int i, int lane) {
     int lo = 0, n = B;                                       // among sequences lo .. lo + n - 1
     while (n > 1) {
@@ -72,6 +71,16 @@ __device__ __forceinline__ void store8(T *p, const uint64_t (&x)[4]) {
     }
 }
 
+// Reports bounds that are not ascending within [0, tokens]: warp w of `warps` looks at the 32 sequences from 32 w
+// on, and at those 32 `warps` further on.
+__device__ __forceinline__ void check_bounds(const RowsArgs &a, int w, int warps, int lane) {
+    if (!a.cu || blockIdx.y > 0) return;
+    for (long long j = 32ll * w + lane; j < a.B; j += 32ll * warps) {
+        const int first = a.cu[j], next = a.cu[j + 1];
+        if (first < 0 || next < first || next > a.tokens) raise_error(a.pg.err, STEPQ_ERR_ARG);
+    }
+}
+
 // Where a token's rows go: its page and place, or page -1. Sequence b holds it, or one behind b.
 struct Place { int page, slot; };
 __device__ __forceinline__ Place place_in(const RowsArgs &a, int b, int i, bool report) {
@@ -83,10 +92,7 @@ __device__ __forceinline__ Place place_in(const RowsArgs &a, int b, int i, bool 
             first = next;
             next = a.cu[++b + 1];
         }
-        if (i < first || i >= next) {
-            if (report && i < a.cu[a.B] && i >= a.cu[0]) raise_error(a.pg.err, STEPQ_ERR_ARG);
-            return {-1, 0};
-        }
+        if (i < first || i >= next || first < 0 || next > a.tokens) return {-1, 0};
     } else {
         const int each = a.tokens / a.B;
         b = i / each;
@@ -254,6 +260,7 @@ struct Mine {
         h0 = (blockIdx.y >> 1) * PER * kRows + lane / L;
     }
     __device__ __forceinline__ Place place(const RowsArgs &a) const {
+        check_bounds(a, i, a.tokens, lane);
         return place_in(a, a.cu ? find_sequence(a.cu, a.B, i, lane) : 0, i, lane == 0);
     }
 };
@@ -321,6 +328,7 @@ struct Few {
         const int lane = threadIdx.x & 31, first = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * a.each, H = a.pg.n_heads;
         c = lane % L;
         part = blockIdx.y;
+        check_bounds(a, blockIdx.x * kWarps + (threadIdx.x >> 5), gridDim.x * kWarps, lane);
         const int b = a.cu ? find_sequence(a.cu, a.B, min(first, a.tokens - 1), lane) : 0;
 #pragma unroll
         for (int n = 0; n < kRows; n++) {

@@ -151,6 +151,17 @@ PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F &&f) {
     return nullptr;
 }
 
+// The library's call without Python's lock: a launch waits where the queue is full, and what is queued may be a
+// host function that takes the lock.
+template <class F>
+stepq_status unlocked(F &&call) {
+    stepq_status status;
+    Py_BEGIN_ALLOW_THREADS
+    status = call();
+    Py_END_ALLOW_THREADS
+    return status;
+}
+
 // kv, layer, pages, table, starts, k, v, cu_seqlens, stream
 template <class Fn>
 stepq_status transfer(Fn fn, PyObject *const *a) {
@@ -170,7 +181,9 @@ stepq_status transfer(Fn fn, PyObject *const *a) {
     r.v = call.rows(a[6], type, n, c.n_heads, c.head_dim, r.v_stride, "v");
     const int32_t *starts = call.int32s(a[4], B, "starts");
     const int32_t *cu = a[7] == Py_None ? nullptr : call.int32s(a[7], B + 1, "cu_seqlens");
-    return fn(&c, integer(a[1], "layer"), &p, starts, cu, (int)B, (int)n, &r, stream_of(a[8], call.device));
+    const int layer = integer(a[1], "layer");
+    const stepq_stream_t stream = stream_of(a[8], call.device);
+    return unlocked([&] { return fn(&c, layer, &p, starts, cu, (int)B, (int)n, &r, stream); });
 }
 
 PyObject *py_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -222,7 +235,9 @@ PyObject *py_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
             have = t.nbytes();
         }
         const int32_t *lens = call.int32s(a[4], B, "lens");
-        return kv_attend(&c, integer(a[1], "layer"), &p, lens, (int)B, &io, ws, have, stream_of(a[12], call.device));
+        const int layer = integer(a[1], "layer");
+        const stepq_stream_t stream = stream_of(a[12], call.device);
+        return unlocked([&] { return kv_attend(&c, layer, &p, lens, (int)B, &io, ws, have, stream); });
     });
 }
 

@@ -60,12 +60,13 @@ int dtype_code(at::ScalarType t) {
 // What a call's tensors have in common: the device that is current.
 struct Call {
     int device = -1;
-    const void *on(const at::Tensor &t, const char *what) {
+    // Where t lies; written: the call writes there, so that a tensor that still shares another's memory gets its own.
+    void *on(const at::Tensor &t, const char *what, bool written = false) {
         if (!t.is_cuda()) refuse("%s: expected a CUDA tensor", what);
         if (device < 0) device = c10::cuda::current_device();
         if (t.get_device() != device)
             refuse("%s: expected a CUDA tensor on the current device, got one on cuda:%d", what, (int)t.get_device());
-        return t.const_data_ptr();
+        return written ? t.mutable_data_ptr() : const_cast<void *>(t.const_data_ptr());
     }
     const int32_t *int32s(PyObject *o, int64_t n, const char *what) {
         const at::Tensor &t = tensor(o, what);
@@ -75,9 +76,10 @@ struct Call {
         return (const int32_t *)p;
     }
     // Rows [rows][heads][dim] or [rows][heads * dim], heads next to each other, and the stride of rows.
-    void *rows(PyObject *o, at::ScalarType type, int64_t n, int64_t heads, int64_t dim, int64_t &stride, const char *what) {
+    void *rows(PyObject *o, at::ScalarType type, int64_t n, int64_t heads, int64_t dim, int64_t &stride, const char *what,
+               bool written) {
         const at::Tensor &t = tensor(o, what);
-        const void *p = on(t, what);
+        void *p = on(t, what, written);
         if (t.scalar_type() != type) refuse("%s: expected %s, got %s", what, name_of(type), name_of(t.scalar_type()));
         const auto size = t.sizes(), step = t.strides();
         const bool ok = size.size() == 3 ? size[1] == heads && size[2] == dim && step[2] == 1 && (heads == 1 || step[1] == dim)
@@ -85,7 +87,7 @@ struct Call {
         if (!ok || size[0] != n)
             refuse("%s: expected %lld contiguous rows of %lld x %lld", what, (long long)n, (long long)heads, (long long)dim);
         stride = n > 1 ? step[0] : heads * dim;              // that of a single row is arbitrary
-        return const_cast<void *>(p);
+        return p;
     }
 };
 
@@ -106,7 +108,7 @@ stepq_kv_config config(PyObject *kv) {
     return {v[0], v[1], v[2], v[3], v[4]};
 }
 
-stepq_kv_pages pages_of(Call &call, const stepq_kv_config &c, PyObject *pages_, PyObject *table_, int64_t B) {
+stepq_kv_pages pages_of(Call &call, const stepq_kv_config &c, PyObject *pages_, PyObject *table_, int64_t B, bool written) {
     stepq_kv_pages p{};
     const at::Tensor &table = tensor(table_, "table");
     const auto size = table.sizes();
@@ -117,7 +119,7 @@ stepq_kv_pages pages_of(Call &call, const stepq_kv_config &c, PyObject *pages_, 
     p.table_width = (int)size[1];
     p.table_stride = B > 1 ? table.strides()[0] : size[1];
     const at::Tensor &pages = tensor(pages_, "pages");
-    p.pages = const_cast<void *>(call.on(pages, "pages"));
+    p.pages = call.on(pages, "pages", written);
     if (!pages.is_contiguous()) refuse("pages: expected a contiguous tensor");
     const size_t each = kv_page_bytes(&c);                   // 0: the library refuses the configuration
     const size_t n = each ? pages.nbytes() / each : 1;
@@ -163,8 +165,7 @@ stepq_status unlocked(F &&call) {
 }
 
 // kv, layer, pages, table, starts, k, v, cu_seqlens, stream
-template <class Fn>
-stepq_status transfer(Fn fn, PyObject *const *a) {
+stepq_status transfer(bool append, PyObject *const *a) {
     const stepq_kv_config c = config(a[0]);
     Call call;
     const int64_t B = tensor(a[4], "starts").numel();
@@ -174,23 +175,23 @@ stepq_status transfer(Fn fn, PyObject *const *a) {
     if (B > INT32_MAX || n > INT32_MAX) refuse("too many rows");
     if (a[7] != Py_None && tensor(a[7], "cu_seqlens").numel() != B + 1)
         refuse("cu_seqlens: expected %lld values, got %lld", (long long)(B + 1), (long long)tensor(a[7], "cu_seqlens").numel());
-    const stepq_kv_pages p = pages_of(call, c, a[2], a[3], B);
+    const stepq_kv_pages p = pages_of(call, c, a[2], a[3], B, append);
     stepq_kv_rows r{};
     r.dtype = dtype_code(type);
-    r.k = call.rows(a[5], type, n, c.n_heads, c.head_dim, r.k_stride, "k");
-    r.v = call.rows(a[6], type, n, c.n_heads, c.head_dim, r.v_stride, "v");
+    r.k = call.rows(a[5], type, n, c.n_heads, c.head_dim, r.k_stride, "k", !append);
+    r.v = call.rows(a[6], type, n, c.n_heads, c.head_dim, r.v_stride, "v", !append);
     const int32_t *starts = call.int32s(a[4], B, "starts");
     const int32_t *cu = a[7] == Py_None ? nullptr : call.int32s(a[7], B + 1, "cu_seqlens");
     const int layer = integer(a[1], "layer");
     const stepq_stream_t stream = stream_of(a[8], call.device);
-    return unlocked([&] { return fn(&c, layer, &p, starts, cu, (int)B, (int)n, &r, stream); });
+    return unlocked([&] { return (append ? kv_append : kv_read)(&c, layer, &p, starts, cu, (int)B, (int)n, &r, stream); });
 }
 
 PyObject *py_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 9, [&] { return transfer(kv_append, a); });
+    return guarded(n, 9, [&] { return transfer(true, a); });
 }
 PyObject *py_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 9, [&] { return transfer(kv_read, a); });
+    return guarded(n, 9, [&] { return transfer(false, a); });
 }
 
 // kv, layer, pages, table, lens, q, y, scale, window, lse, max_len, workspace, stream
@@ -200,7 +201,7 @@ PyObject *py_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         Call call;
         const int64_t B = tensor(a[4], "lens").numel();
         if (B > INT32_MAX) refuse("too many rows");
-        const stepq_kv_pages p = pages_of(call, c, a[2], a[3], B);
+        const stepq_kv_pages p = pages_of(call, c, a[2], a[3], B, false);
         const at::Tensor &q = tensor(a[5], "q");
         if (q.dim() != 2 && q.dim() != 3) refuse("q: expected rows of heads");
         const int64_t heads = q.dim() == 3 ? q.sizes()[1] : c.head_dim > 0 ? q.sizes()[1] / c.head_dim : 0;
@@ -209,8 +210,8 @@ PyObject *py_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         stepq_kv_query io{};
         io.dtype = dtype_code(type);
         io.n_heads = (int)heads;
-        io.q = call.rows(a[5], type, B, heads, c.head_dim, io.q_stride, "q");
-        io.y = call.rows(a[6], type, B, heads, c.head_dim, io.y_stride, "y");
+        io.y = call.rows(a[6], type, B, heads, c.head_dim, io.y_stride, "y", true);         // first: q may be the same tensor
+        io.q = call.rows(a[5], type, B, heads, c.head_dim, io.q_stride, "q", false);
         if (a[7] == Py_None) {
             io.scale = c.head_dim > 0 ? (float)(1.0 / std::sqrt((double)c.head_dim)) : 0.f;
         } else {
@@ -222,7 +223,7 @@ PyObject *py_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         io.max_len = integer(a[10], "max_len");
         if (a[9] != Py_None) {
             const at::Tensor &lse = tensor(a[9], "lse");
-            io.lse = (float *)call.on(lse, "lse");
+            io.lse = (float *)call.on(lse, "lse", true);
             if (lse.scalar_type() != at::kFloat || !lse.is_contiguous()) refuse("lse: expected contiguous float32");
             if (lse.numel() != B * heads) refuse("lse: expected %lld values, got %lld", (long long)(B * heads), (long long)lse.numel());
         }
@@ -230,7 +231,7 @@ PyObject *py_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         size_t have = 0;
         if (a[11] != Py_None) {
             const at::Tensor &t = tensor(a[11], "workspace");
-            ws = const_cast<void *>(call.on(t, "workspace"));
+            ws = call.on(t, "workspace", true);
             if (!t.is_contiguous()) refuse("workspace: expected a contiguous tensor");
             have = t.nbytes();
         }

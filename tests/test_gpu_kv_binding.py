@@ -1,4 +1,5 @@
-"""What the paged cache's compiled binding does beside the calls: it lets other Python threads run."""
+"""What the paged cache's compiled binding does beside the calls: it lets other Python threads run, and writes to no
+tensor but the ones that it is given."""
 import ctypes as C
 import subprocess
 import threading
@@ -64,3 +65,34 @@ def test_other_threads_run_while_a_call_waits(call, tmp_path):
     finally:
         _lib.bind().use(*real)
         other.join()
+
+
+def test_tensors_that_share_memory_until_one_is_written():
+    """torch's lazy clones: what a call writes reaches no other owner of the memory."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pages, table, n = A.alloc_pages(KV, 6), torch.randperm(6, generator=g, device="cuda").int().view(3, 2), torch.full((3,), 5, dtype=torch.int32, device="cuda")
+    k, v = torch.randn((2, 3, 2, 128), generator=g, device="cuda").bfloat16()
+    q = torch.randn((3, 4, 128), generator=g, device="cuda").bfloat16()
+
+    def lazy(t):
+        t = torch._lazy_clone(t)
+        assert torch._C._is_cow_tensor(t)
+        return t
+
+    A.stepq_kv_append(KV, 0, lazy(pages), table, n, k, v)
+    assert not bool(pages.any())
+    own, rows = lazy(pages), (lazy(k), lazy(v))
+    A.stepq_kv_append(KV, 0, own, table, n, *rows)              # rows are only read
+    assert torch.equal(k, rows[0]) and torch._C._is_cow_tensor(rows[0]) and bool(own.any())
+    zk = z(3, 2, 128)
+    a, b = lazy(zk), lazy(zk)
+    A.stepq_kv_read(KV, 0, own, table, n, a, b)
+    assert not bool(zk.any()) and bool(a.any()) and bool(b.any())
+    y, lse, ws = z(3, 4, 128), z(3, 4, dt=torch.float32), torch.zeros(A.stepq_kv_workspace_bytes(KV, 4, 3, 1 << 20), dtype=torch.uint8, device="cuda")
+    ly, ll, lw = lazy(y), lazy(lse), lazy(ws)
+    A.stepq_kv_attend(KV, 0, own, table, n + 1, q, ly, lse=ll, max_len=1 << 20, workspace=lw)
+    assert not bool(y.any()) and not bool(lse.any()) and not bool(ws.any()) and bool(ly.any()) and bool(ll.any())
+    both = lazy(q)                                              # outputs in place of the queries
+    A.stepq_kv_attend(KV, 0, own, table, n + 1, both, both)
+    assert torch.equal(both, ly) and not torch.equal(both, q)
+    assert A.stepq_device_error() == 0

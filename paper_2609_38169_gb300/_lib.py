@@ -119,7 +119,7 @@ def lib(build: bool = True):
     there is no fallback path."""
     global _lib
     if _lib is None:
-        path = build_ext.build() if build else build_ext.SO
+        path = build_ext.build_library() if build else build_ext.SO
         if not os.path.exists(path):
             raise RuntimeError(f"libstepq.so not built at {path}")
         L = C.CDLL(path)

@@ -1,13 +1,16 @@
 """Build libstepq.so in-tree with nvcc for sm_103a (one -gencode, TUs in parallel), and beside it
-the compiled half of the Python binding, which needs the headers of the torch it is used with."""
+the compiled half of the Python binding, which needs the headers of the torch and the Python that it is used
+with. The library needs neither."""
 from __future__ import annotations
 
 import concurrent.futures as cf
+import hashlib
 import importlib.metadata
 import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -29,10 +32,14 @@ BIND_SOURCE = "bind.cpp"
 
 
 def bind_so() -> str | None:
-    """Where the binding for the installed torch is built (None: there is no torch)."""
-    if importlib.util.find_spec("torch") is None:
+    """Where the binding for this Python and its torch is built (None: there is no torch). It is linked to the files of
+    both, so each pair has its own."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
         return None
-    return os.path.join(BUILD, "torch-" + importlib.metadata.version("torch"), "_stepq_bind.so")
+    place = hashlib.sha256(os.path.realpath(spec.origin).encode()).hexdigest()[:8]
+    name = "-".join(("torch", importlib.metadata.version("torch"), place, sysconfig.get_config_var("SOABI") or sys.implementation.cache_tag))
+    return os.path.join(BUILD, name, "_stepq_bind.so")
 
 
 def nvcc() -> str:
@@ -76,16 +83,16 @@ def build_bind(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds what is older than its sources; libstepq.so's path."""
+    """Builds what is older than its sources, the binding too if there is a torch; libstepq.so's path."""
     with cf.ThreadPoolExecutor(max_workers=1) as ex:
         bind = ex.submit(build_bind, force) if bind_so() else None
-        so = _build_library(force, verbose)
+        so = build_library(force, verbose)
         if bind:
             bind.result()
     return so
 
 
-def _build_library(force: bool, verbose: bool) -> str:
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return SO
     os.makedirs(BUILD, exist_ok=True)
@@ -119,5 +126,4 @@ def _build_library(force: bool, verbose: bool) -> str:
 
 
 if __name__ == "__main__":
-    import sys
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))

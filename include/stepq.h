@@ -426,7 +426,7 @@ typedef struct {
  * Two tokens of a call must not share a place. A token beyond the table (or a negative start)
  * or whose page is outside [0, n_pages) raises STEPQ_ERR_SLOT_RANGE and is skipped. Bounds that are not
  * ascending within [0, tokens] raise STEPQ_ERR_ARG; each row then goes to a sequence within [0, tokens]
- * that holds it, or is skipped (device errors). */
+ * that holds it, or is skipped (device errors; a call without rows launches nothing). */
 stepq_status stepq_kv_append(const stepq_kv_config *cfg, int layer, const stepq_kv_pages *pages,
                              const int32_t *starts, const int32_t *cu_seqlens, int B, int tokens,
                              const stepq_kv_rows *rows, stepq_stream_t stream);

@@ -63,7 +63,7 @@ struct AttendArgs {
     int window;
     int whole;                      // clusters take whole sequences: no parts
     int stages;                     // of each warp's ring
-    float *parts;                   // workspace: PartLayout
+    float *parts;                   // workspace, laid out as kv_attend.cuh says at Joined
 };
 
 // kv_launch.cuh, instantiated for each format in a file of its own

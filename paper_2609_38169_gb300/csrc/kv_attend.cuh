@@ -21,8 +21,8 @@
 // share a key head. HBM bounds the call as long as these keep up; tcgen05 would want 128 rows of
 // tokens of which each is used for 8 columns, and codes would have to go back to shared memory.
 // Measured (both kernels; 8 key heads of 128 channels, pages of 16 or 64 tokens): 256 x 8,191 tokens in 4 bits
-// and 64 query heads 365 us, 6.1 TB/s, where the integer pipe is busy half of the time at half the issue
-// rate; 128 x 4,096 in 8 bits 171 us, 6.4 TB/s; 64 ragged sequences of 131,072 in bf16 84 us, 6.4 TB/s, 4 us
+// and 64 query heads 367 us, 6.1 TB/s, where the integer pipe is busy half of the time at half the issue
+// rate; 128 x 4,096 in 8 bits 174 us, 6.3 TB/s; 64 ragged sequences of 131,072 in bf16 85 us, 6.3 TB/s, 4 us
 // of which pass before the first tile is asked for and 4 in the second kernel; 37 tokens 4.1 us.
 // The order of channels within a product is free, so a lane takes whole 16-byte pieces of a
 // row and the queries are laid out to match. Codes become fp16 exactly. For bf16 vectors over 4 bits those of
@@ -31,7 +31,7 @@
 // 1024, which cuts such sums off after some 17 bits: a score is within D 2^-17 of scale times its row's scale
 // times the largest |q|, 1e-4 for normal queries and keys of 128 channels, where a weight's one term is within
 // 5e-4 and the output's rounding within 4e-3. Codes without their offset take an instruction more for a pair: 256 x
-// 8,191 tokens 398 us, so 367. Elsewhere they enter so: fp16 vectors over 4 bits take 1 to 4% longer for it,
+// 8,191 tokens 397 us, so 367. Elsewhere they enter so: fp16 vectors over 4 bits take 1 to 4% longer for it,
 // 8 bits nothing.
 //
 // Between the products (whose factors are sums of 16-bit terms, see Shape) everything is fp32.
@@ -194,8 +194,8 @@ template <int BYTES>
 __device__ __forceinline__ Words<BYTES / 4> lds(const uint8_t *tile, uint32_t at) {
     return *(const Words<BYTES / 4> *)(tile + at);
 }
-// Pages pass through L2 once a call: what else lies there stays (measured with the usual order of
-// eviction: 200,003 tokens of 2 x 256 channels 75 us, now 71; 524,288 of 8 x 128 in 8 bits 185, 181).
+// Pages pass through L2 once a call: what else lies there stays (when it was added, with the usual order of
+// eviction and with this one: 200,003 tokens of 2 x 256 channels 75 and 71 us; 524,288 of 8 x 128 in 8 bits 185 and 181).
 __device__ __forceinline__ uint64_t streaming() {
     uint64_t p;
     asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -890,7 +890,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 }
                 // base-2 exponents x = (s - ho) sk hf, rounded before the reference is taken from them: a difference of
                 // large scores is then a difference of what the reference was found from. Masked ones are -inf.
-                // V's scales, for the reference at least 2^-24; the least as they are
+                // sv: V's scales, for the reference at least 2^-24 (1 where there is no token); least: the least as it is.
                 float sv[G][2], least = 1.f;
                 auto v_scale = [&](int g, int h) {
                     return f16_val(((const uint16_t *)(st + 2 * TT * RB))[TT + sub + 16 * g + r + 8 * h]);
@@ -946,7 +946,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, S::BY_REGS) kv_attend_kernel(A
                 };
                 float most = weights(0);
                 if (NT > 1) most = fmaxf(most, weights(NT - 1));
-                // rows of zeros, of a page that nothing was written to or of none, have code 0 and scale 0
+                // Rows of zeros, of a page that nothing was written to or of none, have code 0 and scale 0: their values take
+                // the scale as it is. (With a vote of their own 256 x 8,191 tokens in 4 bits took 371 us, so 368.)
                 const bool zeros = S::CODED && least <= 0.f;
                 if (__any_sync(0xffffffffu, zeros || most > most_wt)) {
 #pragma unroll

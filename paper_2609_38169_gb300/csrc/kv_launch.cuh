@@ -7,8 +7,9 @@ namespace stepq {
 namespace kv {
 
 // Runs f(Shape{}) for the variant of a call; more than 8 query heads a key head go in sixteens, but for
-// 256 channels of codes, whose sixteens have no room (64 x 4,096 tokens of two key heads with 16 query heads
-// each, us: in 4 bits 73, in eights 64; 8 bits 80 and 86, with fp32 vectors 215 and 95; 2 x 900 tokens 21 and 10).
+// 256 channels of codes, whose sixteens have little room (64 x 4,096 tokens of two key heads with 16 query heads
+// each, us: in 4 bits 73, in eights 64; 8 bits and fp32 vectors 215 and 95; 2 x 900 tokens 21 and 10. Long calls in
+// 8 bits with 16-bit vectors lose by it, 80 and 86).
 template <int F, class Fn>
 auto by_shape(int head_dim, int groups, int dtype, Fn &&f) {
     auto types = [&](auto d, auto nt) {

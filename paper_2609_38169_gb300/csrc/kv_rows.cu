@@ -9,7 +9,7 @@
 // lanes a row, so that a warp holds 32 / (D / 8) heads at once. All its loads are on their way
 // before it looks at the first value (the append's before it has found the token's sequence and
 // page). HBM bounds both calls on paper; what they have to be kept from is the issue slots (75% busy in the
-// append, 55% in reading). 20,011 tokens of 8 heads from bf16 into 8 bits 26 us, 4.7 TB/s; 32,299 back
+// append, 54 to 61% in reading). 20,011 tokens of 8 heads from bf16 into 8 bits 26 us, 4.7 TB/s; 32,299 back
 // 31 us, 6.4 TB/s; 64,000 out of 4 bits 54 us, 6.1 TB/s.
 #include <type_traits>
 
